@@ -79,7 +79,7 @@ sama_status sama_op_adapt_norm_static(const float* g, const float* m, const floa
                                       int64_t n, int64_t t, float lr, float beta1, float beta2, float eps, float alpha,
                                       float* scalars, int64_t* status, void* hip_stream);
 /* Text of the last error of an op-level call on this thread (HOST string owned by the library, "" if none); set by
- * sama_op_adapt_norm_static. */
+ * sama_op_adapt_norm_static and the calls of a token model's step below. */
 const char* sama_op_last_error(void);
 
 /* Low halves of theta +- eps v against the bf16 working copy (Eq. 5): lo_p/lo_m[k] = bf16((theta[k] +- eps v[k]) -
@@ -90,6 +90,38 @@ sama_status sama_op_perturb_lo(const float* theta, const float* vdir, const floa
 /* theta <- theta - eps v (end of Sec. 3.2), refreshing theta16 like sama_op_adam. */
 sama_status sama_op_nudge(float* theta, const float* vdir, const float* eps_ptr, void* theta16, int64_t n, int64_t n16,
                           void* hip_stream);
+
+/* ---- Operators of a token model's base step beyond the encoder's own: a scaled embedding, and clipped gradients.
+ * Types are SAMA_DTYPE_*; fp32 and bf16 may be mixed where a type is given for each side.  Strides (ld*) are in values, at least the row's length.
+ * Any length, alignment (of a value) and stride is accepted; rows whose length, start and stride are multiples of 16 bytes are moved in
+ * pieces of that size.  Sums are held in 32 bits or more, in a fixed order: the same call gives the same bits.  Workspaces need 256-byte
+ * alignment and nothing in them beforehand; calls that overlap in time need one each.  An argument that is refused gives SAMA_EINVAL,
+ * launches nothing, and sama_op_last_error() says which. */
+
+/* out[i][:] = scale * table[id_i][:] for n tokens (table [V x d]).  Ids outside [0, V) are clamped into it, as everywhere in this
+ * library; pad_id >= 0: the rows of that id (before clamping) are zero whatever the table holds there, -1: there is no such id. */
+sama_status sama_op_embedding(const void* table, int32_t table_dtype, int64_t ld_table, const int32_t* ids, int64_t n, int32_t V, int32_t d,
+                              float scale, int32_t pad_id, void* out, int32_t out_dtype, int64_t ld_out, void* hip_stream);
+
+/* Its gradient: grad[v][:] = scale * sum over the i with id_i = v of dy[i][:], in ascending i (dy [n x d], grad [V x d]).  Padding contributes
+ * nothing and its rows of dy are not read.  accumulate = 0: every row of grad is written, zeros where no token has the id; 1: the sums are
+ * added to grad (a table that is also the output matrix), and rows without a token are left alone.  n at most 2^30.  workspace: DEVICE,
+ * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for sizes that the call refuses); one that is large enough for n is for fewer tokens too
+ * only if that function says so. */
+size_t sama_op_embedding_grad_bytes(int64_t n, int32_t V, int32_t d);
+sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_dy, const int32_t* ids, int64_t n, int32_t V, int32_t d,
+                                   float scale, int32_t pad_id, int32_t accumulate, void* grad, int32_t grad_dtype, int64_t ld_grad,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The global norm of `count` gradients and their clipping:  norm = sqrt(sum of all squares) (in 64 bits),
+ * factor = min(1, max_norm / (norm + 1e-6)).  grads, counts, dtypes: HOST arrays of `count` DEVICE pointers, numbers of values and types.
+ * out: DEVICE fp32 [sum of counts], receives factor * g of all tensors one after the other (the flat gradient of sama_op_adam), or NULL: the
+ * gradients are scaled in place, and not touched where the factor is 1.  max_norm > 0; infinity gives the norm alone (out receives copies).
+ * norm_out: DEVICE fp32 [2] = {norm, factor}.  status: DEVICE, or NULL: 1 if the norm is not finite, in which case the factor is 1, else 0.
+ * workspace: DEVICE, sama_op_grad_clip_bytes() bytes.  The tensors must not overlap one another nor out. */
+size_t sama_op_grad_clip_bytes(void);
+sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* counts, const int32_t* dtypes, float max_norm, float* out,
+                              float* norm_out, int64_t* status, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Diagnostic switches, process-wide, for tests and profiling.  They take effect from the next launch and are not
  * thread-safe.

@@ -119,6 +119,12 @@ def load_library():
     L.sama_op_last_error.restype = C.c_char_p; L.sama_op_last_error.argtypes = []
     L.sama_op_perturb_lo.restype = C.c_int; L.sama_op_perturb_lo.argtypes = [vp, vp, vp, vp, vp, i64, vp]
     L.sama_op_nudge.restype = C.c_int; L.sama_op_nudge.argtypes = [vp, vp, vp, vp, i64, i64, vp]
+    L.sama_op_embedding.restype = C.c_int; L.sama_op_embedding.argtypes = [vp, i32, i64, vp, i64, i32, i32, f32, i32, vp, i32, i64, vp]
+    L.sama_op_embedding_grad_bytes.restype = C.c_size_t; L.sama_op_embedding_grad_bytes.argtypes = [i64, i32, i32]
+    L.sama_op_embedding_grad.restype = C.c_int
+    L.sama_op_embedding_grad.argtypes = [vp, i32, i64, vp, i64, i32, i32, f32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
+    L.sama_op_grad_clip_bytes.restype = C.c_size_t; L.sama_op_grad_clip_bytes.argtypes = []
+    L.sama_op_grad_clip.restype = C.c_int; L.sama_op_grad_clip.argtypes = [i64, vp, vp, vp, f32, vp, vp, vp, vp, C.c_size_t, vp]
     _lib = L
     return L
 
@@ -390,3 +396,76 @@ def op_nudge(theta, vdir, eps_t, theta16, n16):
     rc = load_library().sama_op_nudge(_p(theta), _p(vdir), _p(eps_t), _p(theta16), theta.numel(), n16, _stream())
     if rc != 0:
         raise SamaError(rc, "sama_op_nudge rejected the arguments")
+
+
+# ------------------------------------------------------------------------------------- operators of a token model's step
+def _dtype(t):
+    """SAMA_DTYPE_* of a tensor (-1, which the library refuses, for any other type)."""
+    import torch
+    return {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}.get(t.dtype, -1)
+
+
+def _rows(t, d, what):
+    """A 2-D tensor on the GPU whose rows are d neighbouring values -> its row stride."""
+    if t.dim() != 2 or t.shape[1] != d or not t.is_cuda or (d > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a [n, {d}] CUDA tensor with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(d, t.stride(0))
+
+
+def _ids(ids, n):
+    import torch
+    if ids.dtype != torch.int32 or not ids.is_cuda or not ids.is_contiguous() or ids.numel() != n:
+        raise ValueError(f"ids: expected {n} contiguous int32 values on the GPU")
+
+
+def _op(rc, name):
+    if rc != 0:
+        raise SamaError(rc, load_library().sama_op_last_error().decode() or name + " failed")
+
+
+def op_embedding(table, ids, out, *, scale=1.0, pad_id=-1):
+    """out[i] = scale * table[ids[i]] through sama_op_embedding.  table [V, d] and out [n, d]: fp32 or bf16 CUDA tensors with contiguous rows; ids: n
+    int32 values; rows of pad_id come out as zeros."""
+    V, d = table.shape
+    _ids(ids, out.shape[0])
+    _op(load_library().sama_op_embedding(_p(table), _dtype(table), _rows(table, d, "table"), _p(ids), out.shape[0], V, d, scale, pad_id, _p(out),
+                                         _dtype(out), _rows(out, d, "out"), _stream()), "sama_op_embedding")
+
+
+def embedding_grad_bytes(n, V, d):
+    return load_library().sama_op_embedding_grad_bytes(n, V, d)
+
+
+def op_embedding_grad(dy, ids, grad, workspace, *, scale=1.0, pad_id=-1, accumulate=False):
+    """grad[v] = scale * the sum of dy over the tokens with id v (added to grad with `accumulate`) through sama_op_embedding_grad.  dy [n, d], grad
+    [V, d]: fp32 or bf16; workspace: uint8, embedding_grad_bytes(n, V, d)."""
+    n, d = dy.shape
+    _ids(ids, n)
+    _op(load_library().sama_op_embedding_grad(_p(dy), _dtype(dy), _rows(dy, d, "dy"), _p(ids), n, grad.shape[0], d, scale, pad_id, int(accumulate),
+                                              _p(grad), _dtype(grad), _rows(grad, d, "grad"), _p(workspace), workspace.numel(), _stream()),
+        "sama_op_embedding_grad")
+
+
+def grad_clip_bytes():
+    return load_library().sama_op_grad_clip_bytes()
+
+
+def op_grad_clip(grads, max_norm, norm, workspace, *, out=None, status=None):
+    """Clips a list of contiguous fp32 and bf16 CUDA tensors to a global norm through sama_op_grad_clip: in place, or into the flat fp32 tensor
+    `out`.  norm: fp32 [2], receives the norm and the factor; status: int64 [1] or None; workspace: uint8, grad_clip_bytes()."""
+    import torch
+    n = len(grads)
+    total = 0
+    for g in grads:
+        if not (g.is_cuda and g.is_contiguous()):
+            raise ValueError("grads: expected contiguous CUDA tensors")
+        total += g.numel()
+    if norm.dtype != torch.float32 or norm.numel() < 2 or not norm.is_contiguous():
+        raise ValueError("norm: expected two contiguous fp32 values")
+    if out is not None and (out.dtype != torch.float32 or out.numel() != total or not out.is_contiguous()):
+        raise ValueError(f"out: expected {total} contiguous fp32 values")
+    if status is not None and (status.dtype != torch.int64 or status.numel() < 1):
+        raise ValueError("status: expected an int64 value")
+    _op(load_library().sama_op_grad_clip(n, (C.c_void_p * n)(*[g.data_ptr() for g in grads]), (C.c_int64 * n)(*[g.numel() for g in grads]),
+                                         (C.c_int32 * n)(*[_dtype(g) for g in grads]), max_norm, _p(out), _p(norm), _p(status), _p(workspace),
+                                         workspace.numel(), _stream()), "sama_op_grad_clip")

@@ -1,9 +1,12 @@
 // Op-level C entry points (include/sama_ops.h): thin argument checks around the kernel launchers.
+#include <cmath>
 #include <math.h>
 #include <mutex>
 #include <string>
+#include <vector>
 #include "../../include/sama_ops.h"
 #include "kernels.h"
+#include "token_ops.h"
 
 using namespace sama;
 
@@ -30,6 +33,31 @@ double* static_scratch() {
     g_scratch_ptr[dev] = p;
   }
   return g_scratch_ptr[dev];
+}
+
+sama_status refuse(const char* op, const char* why) { g_ops_error = std::string(op) + ": " + why; return SAMA_EINVAL; }
+sama_status launched(const char* op) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return SAMA_OK;
+  g_ops_error = std::string(op) + ": " + hipGetErrorString(e);
+  return SAMA_EHIP;
+}
+bool is_dtype(int32_t t) { return t == SAMA_DTYPE_FP32 || t == SAMA_DTYPE_BF16; }
+int value_bytes(int32_t dtype) { return dtype == SAMA_DTYPE_BF16 ? 2 : 4; }
+// aligned to a value, and rows x ld values within the address space
+bool is_rows(const void* p, int32_t dtype, int64_t rows, int64_t ld) {
+  return (uintptr_t)p % value_bytes(dtype) == 0 && ld <= ((int64_t)1 << 40) && (rows == 0 || ld <= ((int64_t)1 << 46) / rows);
+}
+constexpr int64_t MOST_TOKENS = (int64_t)1 << 30;
+// what the embedding calls have in common
+const char* check_embedding(const int32_t* ids, int64_t n, int32_t V, int32_t d, float scale, int32_t pad_id) {
+  if (n < 0 || n > MOST_TOKENS) return "n must be 0 to 2^30";
+  if (V < 1 || d < 1) return "V and d must be positive";
+  if (n > 0 && ids == nullptr) return "null ids";
+  if ((uintptr_t)ids % 4 != 0) return "ids must be aligned to 4 bytes";
+  if (!std::isfinite(scale)) return "scale must be finite";
+  if (pad_id < -1) return "pad_id must be -1 (none) or an id";
+  return nullptr;
 }
 }  // namespace
 
@@ -179,6 +207,80 @@ sama_status sama_op_nudge(float* theta, const float* vdir, const float* eps_ptr,
   (void)hipGetLastError();
   launch_nudge((hipStream_t)hip_stream, theta, vdir, eps_ptr, nullptr, (bf16_t*)theta16, nullptr, n, theta16 ? n16 : 0);
   return hipGetLastError() == hipSuccess ? SAMA_OK : SAMA_EHIP;
+}
+
+sama_status sama_op_embedding(const void* table, int32_t table_dtype, int64_t ld_table, const int32_t* ids, int64_t n, int32_t V, int32_t d,
+                              float scale, int32_t pad_id, void* out, int32_t out_dtype, int64_t ld_out, void* hip_stream) {
+  static const char* const op = "sama_op_embedding";
+  g_ops_error.clear();
+  if (!is_dtype(table_dtype) || !is_dtype(out_dtype)) return refuse(op, "types must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16");
+  if (const char* e = check_embedding(ids, n, V, d, scale, pad_id)) return refuse(op, e);
+  if (n == 0) return SAMA_OK;
+  if (!table || !out) return refuse(op, "null table or output");
+  if (ld_table < d || ld_out < d) return refuse(op, "a stride is smaller than a row");
+  if (!is_rows(table, table_dtype, V, ld_table) || !is_rows(out, out_dtype, n, ld_out)) return refuse(op, "a pointer is not aligned to its values, or a stride is too large");
+  EmbeddingArgs a{};
+  a.table = table; a.ldt = ld_table; a.table_bf16 = table_dtype == SAMA_DTYPE_BF16; a.ids = ids; a.n = n; a.V = V; a.d = d; a.scale = scale; a.pad = pad_id;
+  a.out = out; a.ldo = ld_out; a.out_bf16 = out_dtype == SAMA_DTYPE_BF16;
+  (void)hipGetLastError();
+  launch_embedding((hipStream_t)hip_stream, a);
+  return launched(op);
+}
+
+size_t sama_op_embedding_grad_bytes(int64_t n, int32_t V, int32_t d) {
+  return n < 0 || n > MOST_TOKENS || V < 1 || d < 1 ? 0 : embedding_grad_bytes(n, V, d);
+}
+
+sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_dy, const int32_t* ids, int64_t n, int32_t V, int32_t d, float scale,
+                                   int32_t pad_id, int32_t accumulate, void* grad, int32_t grad_dtype, int64_t ld_grad, void* workspace,
+                                   size_t workspace_bytes, void* hip_stream) {
+  static const char* const op = "sama_op_embedding_grad";
+  g_ops_error.clear();
+  if (!is_dtype(dy_dtype) || !is_dtype(grad_dtype)) return refuse(op, "types must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16");
+  if (const char* e = check_embedding(ids, n, V, d, scale, pad_id)) return refuse(op, e);
+  if (accumulate != 0 && accumulate != 1) return refuse(op, "accumulate must be 0 or 1");
+  if (!grad || (n > 0 && !dy)) return refuse(op, "null gradient or dy");
+  if ((n > 0 && ld_dy < d) || ld_grad < d) return refuse(op, "a stride is smaller than a row");
+  if ((n > 0 && !is_rows(dy, dy_dtype, n, ld_dy)) || !is_rows(grad, grad_dtype, V, ld_grad)) return refuse(op, "a pointer is not aligned to its values, or a stride is too large");
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < embedding_grad_bytes(n, V, d)) {
+    (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_embedding_grad_bytes()");
+    return SAMA_EWORKSPACE;
+  }
+  if (accumulate && n == 0) return SAMA_OK;
+  EmbeddingGradArgs a{};
+  a.dy = dy; a.ldy = ld_dy; a.dy_bf16 = dy_dtype == SAMA_DTYPE_BF16; a.ids = ids; a.n = n; a.V = V; a.d = d; a.scale = scale; a.pad = pad_id;
+  a.accumulate = accumulate != 0; a.grad = grad; a.ldg = ld_grad; a.grad_bf16 = grad_dtype == SAMA_DTYPE_BF16;
+  (void)hipGetLastError();
+  launch_embedding_grad((hipStream_t)hip_stream, a, workspace);
+  return launched(op);
+}
+
+size_t sama_op_grad_clip_bytes(void) { return grad_clip_bytes(); }
+
+sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* counts, const int32_t* dtypes, float max_norm, float* out,
+                              float* norm_out, int64_t* status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  static const char* const op = "sama_op_grad_clip";
+  g_ops_error.clear();
+  if (count < 0 || (count > 0 && (!grads || !counts || !dtypes))) return refuse(op, "null list, or a negative count");
+  if (!(max_norm > 0.f)) return refuse(op, "max_norm must be positive");
+  if (!norm_out || (uintptr_t)norm_out % 4 != 0 || (uintptr_t)out % 4 != 0 || (uintptr_t)status % 8 != 0) return refuse(op, "null norm_out, or a misaligned output");
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < grad_clip_bytes()) {
+    (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_grad_clip_bytes()");
+    return SAMA_EWORKSPACE;
+  }
+  std::vector<GradTensor> list((size_t)count);
+  int64_t total = 0;
+  for (int64_t k = 0; k < count; ++k) {
+    if (!is_dtype(dtypes[k])) return refuse(op, "types must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16");
+    if (counts[k] < 0 || counts[k] > ((int64_t)1 << 40) || (counts[k] > 0 && (!grads[k] || (uintptr_t)grads[k] % value_bytes(dtypes[k]) != 0)))
+      return refuse(op, "a gradient is null, misaligned or of a negative size");
+    total += counts[k];
+    if (total > ((int64_t)1 << 40)) return refuse(op, "more than 2^40 values");
+    list[k] = GradTensor{grads[k], counts[k], dtypes[k] == SAMA_DTYPE_BF16};
+  }
+  (void)hipGetLastError();
+  launch_grad_clip((hipStream_t)hip_stream, list.data(), count, max_norm, norm_out, out, status, workspace);
+  return launched(op);
 }
 
 }  // extern "C"

@@ -1,0 +1,32 @@
+// Launchers of the operators of a token model's step: embedding and its gradient, gradient clipping, the gated feed-forward block.
+// Internal; the C ABI is include/sama_ops.h, which says what each argument means and checks it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include "common.h"
+
+namespace sama {
+
+struct EmbeddingArgs {
+  const void* table; int64_t ldt; bool table_bf16;
+  const int32_t* ids; int64_t n; int V, d;
+  float scale; int pad;
+  void* out; int64_t ldo; bool out_bf16;
+};
+void launch_embedding(hipStream_t, const EmbeddingArgs&);
+
+struct EmbeddingGradArgs {
+  const void* dy; int64_t ldy; bool dy_bf16;
+  const int32_t* ids; int64_t n; int V, d;      // n < 2^31
+  float scale; int pad; bool accumulate;
+  void* grad; int64_t ldg; bool grad_bf16;
+};
+size_t embedding_grad_bytes(int64_t n, int V, int d);
+void launch_embedding_grad(hipStream_t, const EmbeddingGradArgs&, void* workspace);
+
+struct GradTensor { void* p; int64_t n; bool bf16; };
+size_t grad_clip_bytes();
+// norm[0] = ||g||, norm[1] = the factor; out: flat fp32, or null (in place); status may be null
+void launch_grad_clip(hipStream_t, const GradTensor* g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace);
+
+}  // namespace sama

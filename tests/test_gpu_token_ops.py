@@ -1,0 +1,333 @@
+"""The operators of a token model's step against plain implementations in 64 bits.
+
+Tolerances.  u = 2^-24 is the unit roundoff of fp32, 2^-8 that of bf16.  A lookup is one fp32 product and one rounding: exact.  A sum of c
+fp32 terms in any order is within c u of the sum of their sizes; the scaling and the store add one rounding each."""
+import numpy as np
+import pytest
+import torch
+from datagen import CounterRNG
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U32, U16 = 2.0 ** -24, 2.0 ** -8
+T = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def values(seed, *shape):
+    return torch.as_tensor(CounterRNG(seed).normal(1, int(np.prod(shape))).reshape(shape).astype(np.float32), device=DEV)
+
+
+def token_ids(kind, n, V, seed):
+    r = np.random.RandomState(seed)
+    if kind == "same":
+        a = np.full(n, V // 3)
+    elif kind == "zipf":
+        a = np.minimum((r.zipf(1.2, n) - 1), V - 1)
+    elif kind == "distinct":
+        a = r.permutation(max(n, V))[:n] % V
+    elif kind == "outside":
+        a = r.randint(-3, V + 3, n)
+    else:   # runs
+        a = np.repeat(r.randint(0, V, n // 7 + 1), 7)[:n]
+    return torch.as_tensor(a.astype(np.int32), device=DEV)
+
+
+def rows(shape, dtype, ld, offset):
+    """An uninitialised [n, d] view with row stride ld that begins `offset` values into its memory, over a buffer of ones."""
+    n, d = shape
+    whole = torch.ones(offset + max(n, 1) * ld, dtype=dtype, device=DEV)
+    return whole[offset:offset + n * ld].view(n, ld)[:, :d], whole
+
+
+# ------------------------------------------------------------------------------------------------------ lookup
+@pytest.mark.parametrize("table_t,out_t", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("n,V,d", [(1, 1, 1), (3, 10, 7), (128, 300, 64), (703, 1000, 100), (4097, 8192, 256), (37, 50, 1030), (2051, 600, 768), (9, 12, 2048)])
+def test_lookup(n, V, d, table_t, out_t):
+    from paper_2310_05674_amd import binding as B
+    table = values(n + d, V, d).to(T[table_t])
+    ids = token_ids("outside", n, V, n)
+    out = torch.empty(n, d, dtype=T[out_t], device=DEV)
+    B.op_embedding(table, ids, out, scale=1.7)
+    want = (table.float()[ids.clamp(0, V - 1).long()] * torch.tensor(1.7, device=DEV)).to(T[out_t])
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("ldt,ldo,offset", [(72, 64, 0), (64, 80, 8), (65, 64, 0), (64, 67, 0), (64, 64, 1), (64, 64, 4)])
+def test_lookup_strides(ldt, ldo, offset):
+    from paper_2310_05674_amd import binding as B
+    for table_t, out_t in (("fp32", "bf16"), ("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32")):
+        table, _ = rows((33, 64), T[table_t], ldt, offset)
+        table.copy_(values(3, 33, 64))
+        out, whole = rows((50, 64), T[out_t], ldo, offset)
+        ids = token_ids("zipf", 50, 33, 1)
+        B.op_embedding(table, ids, out, scale=0.5)
+        assert torch.equal(out, (table.float()[ids.long()] * 0.5).to(T[out_t]))
+        kept = torch.ones_like(whole)
+        kept[offset:offset + 50 * ldo].view(50, ldo)[:, :64] = out
+        assert torch.equal(whole, kept)                       # nothing beside the rows
+
+
+def test_lookup_padding_and_unusual_values():
+    from paper_2310_05674_amd import binding as B
+    table = values(1, 20, 96)
+    table[4] = float("nan"); table[5, 3] = float("inf"); table[6] = torch.finfo(torch.float32).tiny
+    ids = torch.tensor([4, 5, 4, 6, -1, 25, 0, 4], dtype=torch.int32, device=DEV)
+    for out_t in ("fp32", "bf16"):
+        out = torch.empty(8, 96, dtype=T[out_t], device=DEV)
+        B.op_embedding(table, ids, out, scale=2.0, pad_id=4)
+        want = (table[ids.clamp(0, 19).long()] * 2.0).to(T[out_t])
+        want[ids == 4] = 0
+        assert torch.equal(out, want)
+        B.op_embedding(table, ids, out, scale=2.0, pad_id=19)   # 25 is not the padding: padding is a token's own id, not what it is clamped to
+        assert torch.equal(out[5], (table[19] * 2.0).to(T[out_t])) and bool(torch.isnan(out[0].float()).all())
+    empty = torch.empty(0, 96, device=DEV)
+    B.op_embedding(table, ids[:0], empty)
+
+
+# ------------------------------------------------------------------------------------------------------ gradient
+def check_grad(dy, ids, V, got, scale, pad=-1, start=None):
+    i = ids.cpu().numpy()
+    real = i != pad if pad >= 0 else np.ones(len(i), bool)
+    v = np.clip(i, 0, V - 1)[real]
+    x = f64(dy)[real] * scale
+    want, size = np.zeros((V, dy.shape[1])), np.zeros((V, dy.shape[1]))
+    np.add.at(want, v, x); np.add.at(size, v, np.abs(x))
+    if start is not None:
+        want += start; size += np.abs(start)
+    count = np.bincount(v, minlength=V)[:, None].astype(np.float64)
+    tol = (count + 3) * U32 * size + (U16 * np.abs(want) * (1 + 1e-3) if got.dtype == torch.bfloat16 else 0.0)
+    g = f64(got)
+    assert np.all(np.abs(g - want) <= tol + 1e-40), float(np.max(np.abs(g - want) - tol))
+    if start is None:
+        assert np.all(g[count[:, 0] == 0] == 0.0)
+
+
+def grad_of(dy, ids, V, grad_t, **kw):
+    from paper_2310_05674_amd import binding as B
+    n, d = dy.shape
+    ws = torch.full((B.embedding_grad_bytes(n, V, d),), 0xa5, dtype=torch.uint8, device=DEV)   # nothing is expected in it
+    grad = torch.full((V, d), 7.0, dtype=T[grad_t], device=DEV)
+    B.op_embedding_grad(dy, ids, grad, ws, **kw)
+    return grad
+
+
+@pytest.mark.parametrize("dy_t,grad_t", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("kind,n,V,d", [("zipf", 1, 1, 1), ("zipf", 2, 5, 3), ("runs", 63, 7, 64), ("same", 64, 512, 72), ("zipf", 65, 513, 100), ("outside", 703, 1000, 256),
+                                        ("same", 1000, 3, 520), ("zipf", 4096, 8192, 768), ("distinct", 4096, 5000, 64), ("runs", 5000, 40, 264), ("zipf", 1500, 300000, 8)])
+def test_token_gradient(kind, n, V, d, dy_t, grad_t):
+    dy = values(n + V, n, d).to(T[dy_t])
+    ids = token_ids(kind, n, V, n + d)
+    got = grad_of(dy, ids, V, grad_t, scale=1.25)
+    check_grad(dy, ids, V, got, 1.25)
+    assert torch.equal(got, grad_of(dy, ids, V, grad_t, scale=1.25))      # a fixed order
+
+
+@pytest.mark.parametrize("kind,n,d,dy_t", [("same", 70001, 64, "bf16"), ("zipf", 70001, 136, "bf16"), ("runs", 40000, 264, "fp32"), ("same", 33000, 20, "fp32"), ("zipf", 300000, 16, "fp32")])
+def test_token_gradient_long_runs(kind, n, d, dy_t):
+    """Runs over many workgroups, and every number of sorted rows that a wave may take."""
+    dy = values(n, n, d).to(T[dy_t])
+    ids = token_ids(kind, n, 1000, 5)
+    got = grad_of(dy, ids, 1000, "fp32", scale=1.0)
+    check_grad(dy, ids, 1000, got, 1.0)
+    assert torch.equal(got, grad_of(dy, ids, 1000, "fp32", scale=1.0))
+
+
+def test_token_gradient_every_row_count():
+    """Chunk borders: 1 to 70 rows and around the sizes where a workgroup, and a wave's share, changes."""
+    for n in list(range(1, 71)) + [127, 128, 129, 255, 256, 257, 511, 513, 4095, 4097, 8191, 8193]:
+        dy = values(n, n, 24)
+        for kind in ("runs", "same"):
+            ids = token_ids(kind, n, 9, n)
+            check_grad(dy, ids, 9, grad_of(dy, ids, 9, "fp32", scale=1.0), 1.0)
+
+
+def test_token_gradient_padding():
+    n, V, d = 3000, 900, 128
+    dy, ids = values(1, n, d), token_ids("zipf", n, V, 2)
+    ids[::3] = 0
+    dy[ids == 0] = float("nan")                                        # rows of padding are not read
+    check_grad(torch.nan_to_num(dy), ids, V, grad_of(dy, ids, V, "fp32", scale=2.0, pad_id=0), 2.0, pad=0)
+    ids.fill_(5)
+    assert not grad_of(dy, ids, V, "fp32", pad_id=5).any()             # nothing but padding
+    assert not grad_of(dy[:0], ids[:0], V, "fp32").any()               # no token
+
+
+@pytest.mark.parametrize("ldy,ldg,offset", [(80, 64, 0), (64, 96, 4), (67, 64, 0), (64, 65, 0), (64, 64, 1)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_token_gradient_strides_and_accumulation(ldy, ldg, offset, accumulate):
+    from paper_2310_05674_amd import binding as B
+    n, V, d = 900, 200, 64
+    for dy_t, grad_t in (("fp32", "fp32"), ("bf16", "fp32"), ("bf16", "bf16")):
+        dy, _ = rows((n, d), T[dy_t], ldy, offset)
+        dy.copy_(values(4, n, d))
+        ids = token_ids("zipf", n, V // 2, 3)
+        grad, whole = rows((V, d), T[grad_t], ldg, offset)
+        grad.copy_(values(5, V, d))
+        before = f64(grad)
+        ws = torch.empty(B.embedding_grad_bytes(n, V, d), dtype=torch.uint8, device=DEV)
+        B.op_embedding_grad(dy, ids, grad, ws, scale=0.75, accumulate=accumulate)
+        check_grad(dy, ids, V, grad, 0.75, start=before if accumulate else None)
+        kept = torch.ones_like(whole)
+        kept[offset:offset + V * ldg].view(V, ldg)[:, :d] = grad
+        assert torch.equal(whole, kept)
+        if accumulate:
+            unseen = np.setdiff1d(np.arange(V), ids.cpu().numpy())
+            assert np.array_equal(f64(grad)[unseen], before[unseen])
+
+
+def test_token_gradient_is_the_lookups_derivative():
+    """<dy, lookup(W + e E) - lookup(W - e E)> / 2 e = <grad, E> for a lookup that is linear: only roundings differ."""
+    from paper_2310_05674_amd import binding as B
+    n, V, d, scale, e = 500, 300, 72, 1.5, 0.25
+    W, E, dy = values(1, V, d), values(2, V, d), values(3, n, d)
+    ids = token_ids("zipf", n, V, 4)
+    grad = grad_of(dy, ids, V, "fp32", scale=scale, pad_id=1)
+    up, down = torch.empty(n, d, device=DEV), torch.empty(n, d, device=DEV)
+    B.op_embedding(W + e * E, ids, up, scale=scale, pad_id=1)
+    B.op_embedding(W - e * E, ids, down, scale=scale, pad_id=1)
+    terms = f64(dy) * (f64(up) - f64(down)) / (2 * e)
+    # up and down carry three roundings each (e E, the sum, the product) of values of size |W| + |e E|
+    tol = np.sum(np.abs(f64(dy)) * 6 * U32 * (np.abs(f64(up)) + np.abs(f64(down))) / (2 * e)) + n * U32 * np.sum(np.abs(f64(grad) * f64(E)))
+    assert abs(terms.sum() - np.sum(f64(grad) * f64(E))) <= tol
+
+
+def test_token_ops_in_a_graph_and_on_another_stream():
+    from paper_2310_05674_amd import binding as B
+    n, V, d = 2500, 4000, 192
+    table, dy, ids = values(1, V, d), values(2, n, d), token_ids("zipf", n, V, 3)
+    out, grad = torch.empty(n, d, device=DEV), torch.empty(V, d, device=DEV)
+    ws = torch.empty(B.embedding_grad_bytes(n, V, d), dtype=torch.uint8, device=DEV)
+    cws, norm = torch.empty(B.grad_clip_bytes(), dtype=torch.uint8, device=DEV), torch.empty(2, device=DEV)
+    flat = torch.empty(V * d, device=DEV)
+
+    def step():
+        B.op_embedding(table, ids, out, scale=3.0)
+        B.op_embedding_grad(dy, ids, grad, ws, scale=3.0)
+        B.op_grad_clip([grad], 1.0, norm, cws, out=flat)
+
+    step()
+    want = [t.clone() for t in (out, grad, norm, flat)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for t in (out, grad, norm, flat):
+            t.fill_(9.0)
+        step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((out, grad, norm, flat), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        dy.copy_(values(20 + k, n, d)); ids.copy_(token_ids("zipf", n, V, 30 + k))
+        step()
+        want = [t.clone() for t in (out, grad, norm, flat)]
+        for t in (out, grad, norm, flat):
+            t.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out, grad, norm, flat), want)), k
+
+
+# ------------------------------------------------------------------------------------------------------ clipping
+def clip(grads, max_norm, out=None, status=None):
+    from paper_2310_05674_amd import binding as B
+    ws = torch.full((B.grad_clip_bytes(),), 0xff, dtype=torch.uint8, device=DEV)
+    norm = torch.full((2,), -1.0, device=DEV)
+    B.op_grad_clip(grads, max_norm, norm, ws, out=out, status=status)
+    return norm.cpu().numpy().astype(np.float64)
+
+
+def gradients(sizes, seed, types):
+    out = []
+    for k, n in enumerate(sizes):
+        t = T[types[k % len(types)]]
+        out.append((values(seed + k, max(n, 1))[:n] * 10.0 ** -(k % 3)).to(t))
+    return out
+
+
+@pytest.mark.parametrize("types", [("fp32",), ("bf16",), ("bf16", "fp32")])
+@pytest.mark.parametrize("sizes", [(1,), (0, 5, 0), (7, 8, 9), (8191, 8192, 8193, 8200), (100003, 1, 64), tuple(range(300)), (2 ** 21 + 5, 3)])
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+def test_clipping(sizes, types, max_norm):
+    grads = gradients(sizes, 11, types)
+    before = [f64(g) for g in grads]
+    norm = np.sqrt(sum(float(np.sum(b * b)) for b in before))
+    factor = min(1.0, max_norm / (norm + 1e-6))
+    total = sum(sizes)
+    out = torch.full((total,), 3.0, device=DEV)
+    kept = [g.clone() for g in grads]
+    status = torch.full((1,), 5, dtype=torch.int64, device=DEV)
+    # norm: one rounding to 32 bits of a sum in 64 (squares and sums: 1e-16 each, a few million of them at most)
+    for dest in (out, None):
+        got = clip(grads, max_norm, out=dest, status=status)
+        assert abs(got[0] - norm) <= 1.01 * U32 * norm and abs(got[1] - factor) <= 1.01 * U32 * factor and int(status) == 0
+        if dest is not None:
+            assert all(torch.equal(g, k) for g, k in zip(grads, kept))
+            want = np.concatenate(before) * factor
+            assert np.all(np.abs(f64(out) - want) <= 2.1 * U32 * np.abs(want))
+    for g, b, k in zip(grads, before, kept):
+        if factor == 1.0:
+            assert torch.equal(g, k)
+        else:
+            assert np.all(np.abs(f64(g) - b * factor) <= (2.1 * U32 + (U16 * 1.001 if g.dtype == torch.bfloat16 else 0)) * np.abs(b * factor))
+
+
+def test_clipping_of_views_that_begin_anywhere():
+    whole32, whole16 = values(1, 70000), values(2, 70000).to(torch.bfloat16)
+    grads, marks = [], []
+    for off, n in ((1, 20001), (20003, 9000), (30002, 8195)):
+        for w in (whole32, whole16):
+            grads.append(w[off:off + n]); marks.append((w, off, n))
+    before = [f64(g) for g in grads]
+    outside = [w.clone() for w in (whole32, whole16)]
+    norm = np.sqrt(sum(float(np.sum(b * b)) for b in before))
+    big = torch.full((sum(g.numel() for g in grads) + 3,), 4.0, device=DEV)
+    clip(grads, 2.0, out=big[1:-2])
+    want = np.concatenate(before) * (2.0 / (norm + 1e-6))
+    assert np.all(np.abs(f64(big[1:-2]) - want) <= 2.1 * U32 * np.abs(want)) and float(big[0]) == 4.0 and bool((big[-2:] == 4.0).all())
+    clip(grads, 2.0)
+    for w, old in zip((whole32, whole16), outside):
+        inside = torch.zeros(70000, dtype=torch.bool, device=DEV)
+        for ww, off, n in marks:
+            if ww is w:
+                inside[off:off + n] = True
+        assert torch.equal(w[~inside], old[~inside])
+    for g, b in zip(grads, before):
+        assert np.all(np.abs(f64(g) - b * (2.0 / (norm + 1e-6))) <= (2.1 * U32 + U16 * 1.001) * np.abs(b))
+
+
+def test_clipping_of_unusual_values():
+    huge = torch.full((5000,), 3e30, device=DEV)              # squares beyond 32 bits
+    got = clip([huge], 1.0)
+    assert abs(got[0] / (np.sqrt(5000.0) * 3e30) - 1) < 1e-6 and abs(got[1] * np.sqrt(5000.0) * 3e30 - 1) < 1e-6
+    tiny = torch.full((5000,), 1e-30, device=DEV)
+    assert abs(clip([tiny], 1e-31)[0] / (1e-30 * np.sqrt(5000.0)) - 1) < 1e-6
+    zero = torch.zeros(100, device=DEV)
+    assert tuple(clip([zero], 1.0)) == (0.0, 1.0)
+    assert tuple(clip([], 1.0)) == (0.0, 1.0)
+    for bad in (float("nan"), float("inf")):
+        g = [values(1, 1000), values(2, 500).to(torch.bfloat16)]
+        g[1][3] = bad
+        kept = [t.clone() for t in g]
+        status, out = torch.zeros(1, dtype=torch.int64, device=DEV), torch.empty(1500, device=DEV)
+        for dest in (None, out):
+            got = clip(g, 1.0, out=dest, status=status)
+            assert not np.isfinite(got[0]) and got[1] == 1.0 and int(status) == 1
+        assert all(torch.equal(a.float().nan_to_num(7.0), b.float().nan_to_num(7.0)) for a, b in zip(g, kept))
+        assert torch.equal(out.nan_to_num(7.0), torch.cat([t.float() for t in kept]).nan_to_num(7.0))
+    g = [values(3, 3000)]
+    kept = g[0].clone()
+    norm = clip(g, float("inf"))
+    assert norm[1] == 1.0 and torch.equal(g[0], kept) and abs(norm[0] / np.linalg.norm(f64(kept)) - 1) < 1e-6
+
+
+def test_clipping_gives_the_same_bits():
+    grads = gradients([70001, 5, 2 ** 20], 3, ("fp32", "bf16"))
+    a, b = torch.empty(70006 + 2 ** 20, device=DEV), torch.empty(70006 + 2 ** 20, device=DEV)
+    assert tuple(clip(grads, 0.1, out=a)) == tuple(clip(grads, 0.1, out=b)) and torch.equal(a, b)
