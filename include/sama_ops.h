@@ -91,7 +91,8 @@ sama_status sama_op_perturb_lo(const float* theta, const float* vdir, const floa
 sama_status sama_op_nudge(float* theta, const float* vdir, const float* eps_ptr, void* theta16, int64_t n, int64_t n16,
                           void* hip_stream);
 
-/* ---- Operators of a token model's base step beyond the encoder's own: a scaled embedding, and clipped gradients.
+/* ---- Operators of a token model's base step beyond the encoder's own: a scaled embedding, clipped gradients, and a gated
+ * feed-forward block.
  * Types are SAMA_DTYPE_*; fp32 and bf16 may be mixed where a type is given for each side.  Strides (ld*) are in values, at least the row's length.
  * Any length, alignment (of a value) and stride is accepted; rows whose length, start and stride are multiples of 16 bytes are moved in
  * pieces of that size.  Sums are held in 32 bits or more, in a fixed order: the same call gives the same bits.  Workspaces need 256-byte
@@ -106,8 +107,7 @@ sama_status sama_op_embedding(const void* table, int32_t table_dtype, int64_t ld
 /* Its gradient: grad[v][:] = scale * sum over the i with id_i = v of dy[i][:], in ascending i (dy [n x d], grad [V x d]).  Padding contributes
  * nothing and its rows of dy are not read.  accumulate = 0: every row of grad is written, zeros where no token has the id; 1: the sums are
  * added to grad (a table that is also the output matrix), and rows without a token are left alone.  n at most 2^30.  workspace: DEVICE,
- * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for sizes that the call refuses); one that is large enough for n is for fewer tokens too
- * only if that function says so. */
+ * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for sizes that the call refuses), which suffices for fewer tokens too. */
 size_t sama_op_embedding_grad_bytes(int64_t n, int32_t V, int32_t d);
 sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_dy, const int32_t* ids, int64_t n, int32_t V, int32_t d,
                                    float scale, int32_t pad_id, int32_t accumulate, void* grad, int32_t grad_dtype, int64_t ld_grad,
@@ -123,6 +123,31 @@ size_t sama_op_grad_clip_bytes(void);
 sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* counts, const int32_t* dtypes, float max_norm, float* out,
                               float* norm_out, int64_t* status, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* The gated feed-forward block for T tokens of width d with F hidden values:
+ *     g = x Wg^T, u = x Wu^T, h = act(g) u, y = h w_out^T
+ * x, y [T x d] with row strides ldx, ldy; w_in [2F x d], rows 0..F-1 = Wg, F..2F-1 = Wu; w_out [d x F]; hidden [T x F], receives h.  Matrices
+ * without a stride are dense.  act: SAMA_ACT_SILU (g / (1 + exp(-g))) or SAMA_ACT_GELU (with the error function).
+ * dtype SAMA_DTYPE_BF16: everything in bf16 with fp32 accumulation; h is rounded once, as y is.  d, F and the strides are multiples of 8 and
+ * pointers 16-byte aligned; strides at most 2^21, d F below 2^29.  SAMA_DTYPE_FP32: any d, F, stride and alignment of a value.  T at most 2^22, 0 does
+ * nothing.  saved: DEVICE, sama_op_glu_ffn_saved_bytes() bytes, 16-byte aligned, receives what the backward call needs besides hidden (a layout
+ * of the library's own), or NULL.  workspace: DEVICE, 256-byte aligned, sama_op_glu_ffn_bytes() bytes.  The size functions return 0 for sizes
+ * that the calls refuse; a size for T tokens suffices for fewer.  What a token gets may depend in its last bits on how many tokens it comes with; the same call gives the same bits. */
+enum { SAMA_ACT_SILU = 0, SAMA_ACT_GELU = 1 };
+size_t sama_op_glu_ffn_bytes(int64_t T, int32_t d, int32_t F, int32_t dtype);
+size_t sama_op_glu_ffn_saved_bytes(int64_t T, int32_t F, int32_t dtype);
+sama_status sama_op_glu_ffn(const void* x, int64_t ldx, const void* w_in, const void* w_out, int64_t T, int32_t d, int32_t F, int32_t act,
+                            int32_t dtype, void* y, int64_t ldy, void* hidden, void* saved, void* workspace, size_t workspace_bytes,
+                            void* hip_stream);
+
+/* Its gradients, given dy [T x d] and the x, weights, hidden and saved of the forward call:
+ *     dh = dy w_out, dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu, dw_in = [dg; du]^T x, dw_out = dy^T h
+ * dx [T x d] with row stride lddx in dtype; dw_in [2F x d] and dw_out [d x F], overwritten, in dw_dtype: dtype, or SAMA_DTYPE_FP32.  In bf16 dg and du
+ * are rounded once before the products they enter.  With T = 0 the weights' gradients are zero.  workspace: sama_op_glu_ffn_grad_bytes() bytes. */
+size_t sama_op_glu_ffn_grad_bytes(int64_t T, int32_t d, int32_t F, int32_t dtype);
+sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_in, const void* w_out, const void* hidden,
+                                 const void* saved, int64_t T, int32_t d, int32_t F, int32_t act, int32_t dtype, void* dx, int64_t lddx,
+                                 void* dw_in, void* dw_out, int32_t dw_dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Diagnostic switches, process-wide, for tests and profiling.  They take effect from the next launch and are not
  * thread-safe.
  *  - sama_dev_gemm_shape(id): every bf16 GEMM launch uses block tile `id`: 1..8 are the single-term tiles (a hi+lo
@@ -133,6 +158,8 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
  *    device, by `choice`: four bits for each sixteenth of the rows, the lowest for up to one, each 1 (256 x 192), 2 (256 x 128), 4 (128 x 96) or
  *    5 (128 x 64), anything else is SAMA_EINVAL; 0 = the heuristic (default).  No bit of a result depends on it.
  *  - sama_dev_gemm_counts(counts, 2): HOST counts since the last call: launches of that kernel for forward products and for input gradients.
+ *  - sama_dev_glu_tile(t): the products of the bf16 gated feed-forward block use the t x t tile, t = 64, 128 or 256; 0 = the heuristic (default).  Whether a
+ *    product is split over workgroups, and with it the order of its sums, goes with the tile.
  *  - sama_dev_side_stream(0): the encoder's backward passes keep every launch on the context's stream (a per-kernel profile
  *    wants one stream); 1 = default: weight gradients and optimizer slices run on the library's second stream where rows and
  *    layers are large enough for it; 2: they do for every size.  Any other value means 1.  A base step keeps its bits; a
@@ -142,6 +169,7 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
 void sama_dev_gemm_shape(int32_t id);
 sama_status sama_dev_gemm_rows(uint64_t choice);
 sama_status sama_dev_gemm_counts(int64_t* counts, int32_t n);
+void sama_dev_glu_tile(int32_t tile);
 void sama_dev_side_stream(int32_t mode);
 void sama_dev_side_sink(int32_t on);
 

@@ -125,6 +125,14 @@ def load_library():
     L.sama_op_embedding_grad.argtypes = [vp, i32, i64, vp, i64, i32, i32, f32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
     L.sama_op_grad_clip_bytes.restype = C.c_size_t; L.sama_op_grad_clip_bytes.argtypes = []
     L.sama_op_grad_clip.restype = C.c_int; L.sama_op_grad_clip.argtypes = [i64, vp, vp, vp, f32, vp, vp, vp, vp, C.c_size_t, vp]
+    sz = C.c_size_t
+    L.sama_op_glu_ffn_bytes.restype = sz; L.sama_op_glu_ffn_bytes.argtypes = [i64, i32, i32, i32]
+    L.sama_op_glu_ffn_saved_bytes.restype = sz; L.sama_op_glu_ffn_saved_bytes.argtypes = [i64, i32, i32]
+    L.sama_op_glu_ffn_grad_bytes.restype = sz; L.sama_op_glu_ffn_grad_bytes.argtypes = [i64, i32, i32, i32]
+    L.sama_op_glu_ffn.restype = C.c_int; L.sama_op_glu_ffn.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+    L.sama_op_glu_ffn_grad.restype = C.c_int
+    L.sama_op_glu_ffn_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, sz, vp]
+    L.sama_dev_glu_tile.restype = None; L.sama_dev_glu_tile.argtypes = [i32]
     _lib = L
     return L
 
@@ -407,7 +415,7 @@ def _dtype(t):
 
 def _rows(t, d, what):
     """A 2-D tensor on the GPU whose rows are d neighbouring values -> its row stride."""
-    if t.dim() != 2 or t.shape[1] != d or not t.is_cuda or (d > 1 and t.stride(1) != 1):
+    if t.dim() != 2 or t.shape[1] != d or not t.is_cuda or (d > 1 and t.shape[0] > 0 and t.stride(1) != 1):
         raise ValueError(f"{what}: expected a [n, {d}] CUDA tensor with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
     return t.stride(0) if t.shape[0] > 1 else max(d, t.stride(0))
 
@@ -469,3 +477,65 @@ def op_grad_clip(grads, max_norm, norm, workspace, *, out=None, status=None):
     _op(load_library().sama_op_grad_clip(n, (C.c_void_p * n)(*[g.data_ptr() for g in grads]), (C.c_int64 * n)(*[g.numel() for g in grads]),
                                          (C.c_int32 * n)(*[_dtype(g) for g in grads]), max_norm, _p(out), _p(norm), _p(status), _p(workspace),
                                          workspace.numel(), _stream()), "sama_op_grad_clip")
+
+
+ACT = dict(silu=0, gelu=1)
+
+
+def _glu_dtype(dtype):
+    import torch
+    return {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}.get(dtype, -1)
+
+
+def glu_ffn_bytes(T, d, F, dtype):
+    return load_library().sama_op_glu_ffn_bytes(T, d, F, _glu_dtype(dtype))
+
+
+def glu_ffn_saved_bytes(T, F, dtype):
+    return load_library().sama_op_glu_ffn_saved_bytes(T, F, _glu_dtype(dtype))
+
+
+def glu_ffn_grad_bytes(T, d, F, dtype):
+    return load_library().sama_op_glu_ffn_grad_bytes(T, d, F, _glu_dtype(dtype))
+
+
+def _dense(t, shape, dtype, what):
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {shape} CUDA tensor of {dtype}, got {tuple(t.shape)}, {t.dtype}")
+
+
+def _glu_rows(t, T, d, dtype, what):
+    if t.dtype != dtype or t.shape[0] != T:
+        raise ValueError(f"{what}: expected {T} rows of {dtype}, got {tuple(t.shape)}, {t.dtype}")
+    return _rows(t, d, what)
+
+
+def _scratch(t, need, what):
+    if t.numel() * t.element_size() < need or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {need} bytes on the GPU")
+
+
+def op_glu_ffn(x, w_in, w_out, y, hidden, workspace, *, act="silu", saved=None):
+    """y = (act(x Wg^T) * (x Wu^T)) w_out^T through sama_op_glu_ffn.  x, y [T, d] with contiguous rows; w_in [2F, d] = Wg over Wu, w_out [d, F], hidden
+    [T, F] dense; all bf16 or all fp32.  workspace: uint8, glu_ffn_bytes(T, d, F, dtype); saved: uint8, glu_ffn_saved_bytes(T, F, dtype), for
+    a backward call, or None."""
+    T, d = x.shape
+    F, t = w_out.shape[1], x.dtype
+    _dense(w_in, (2 * F, d), t, "w_in"); _dense(w_out, (d, F), t, "w_out"); _dense(hidden, (T, F), t, "hidden")
+    if saved is not None:
+        _scratch(saved, glu_ffn_saved_bytes(T, F, t), "saved")
+    _op(load_library().sama_op_glu_ffn(_p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), T, d, F, ACT[act], _glu_dtype(t), _p(y),
+                                       _glu_rows(y, T, d, t, "y"), _p(hidden), _p(saved), _p(workspace), workspace.numel(), _stream()), "sama_op_glu_ffn")
+
+
+def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, workspace, *, act="silu"):
+    """Gradients of op_glu_ffn through sama_op_glu_ffn_grad: dx [T, d] in x's type, dw_in [2F, d] and dw_out [d, F] in that or in fp32.  hidden and saved
+    are those of the forward call; workspace: uint8, glu_ffn_grad_bytes(T, d, F, dtype)."""
+    T, d = x.shape
+    F, t = w_out.shape[1], x.dtype
+    _dense(w_in, (2 * F, d), t, "w_in"); _dense(w_out, (d, F), t, "w_out"); _dense(hidden, (T, F), t, "hidden")
+    _dense(dw_in, (2 * F, d), dw_in.dtype, "dw_in"); _dense(dw_out, (d, F), dw_in.dtype, "dw_out")
+    _scratch(saved, glu_ffn_saved_bytes(T, F, t), "saved")
+    _op(load_library().sama_op_glu_ffn_grad(_p(dy), _glu_rows(dy, T, d, t, "dy"), _p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), _p(hidden),
+                                            _p(saved), T, d, F, ACT[act], _glu_dtype(t), _p(dx), _glu_rows(dx, T, d, t, "dx"), _p(dw_in), _p(dw_out),
+                                            _glu_dtype(dw_in.dtype), _p(workspace), workspace.numel(), _stream()), "sama_op_glu_ffn_grad")

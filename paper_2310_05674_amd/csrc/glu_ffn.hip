@@ -1,0 +1,719 @@
+// The gated feed-forward block in bf16 on the matrix cores, with fp32 accumulation: for T tokens of width d and F hidden values
+//   g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wo^T                                        (W_in = [Wg; Wu] [2F x d], Wo [d x F])
+//   dh = dy Wo, dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu, dW_in = [dg; du]^T x, dWo = dy^T h.
+// 6 T d F operations forward and 12 backward in four launches:
+//   k_glu_up      both projections of a tile of tokens and hidden values in one workgroup, the rows of Wg and Wu sixteen by sixteen in turn, so that
+//                 a lane has g and u of the same values and h is all that leaves it (for training also g and u, see below)
+//   k_glu_down    y
+//   k_glu_dgate   dh, and out of it [dg, du] in the epilogue; dh is never stored
+//   k_glu_grads   dx, dW_in and dWo side by side: three products that read the same [dg, du] and none of which fills the chip alone
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+#include "gelu.h"
+#include "kernels.h"
+#include "token_ops.h"
+
+namespace sama {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void lds_void;
+constexpr int LDS_MAX = 160 * 1024, BK = 64;
+
+// BM x BN outputs of a workgroup, by WGM x WGN multiplying waves; NSTAGE slabs of 64 contraction indices in LDS; PW waves that only load (0: the
+// multiplying ones do); YP: fragments of B per piece of a k-step (0: all); RD: reads of a piece lie among the first 1 / RD of the products of the piece
+// before it (0: ahead of its own products).
+template <int BM_, int BN_, int WGM_, int WGN_, int NSTAGE_, int PW_, int YP_, int RD_, int PER_CU_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, NSTAGE = NSTAGE_, PW = PW_, RD = RD_, PER_CU = PER_CU_;
+  static constexpr int WAVES = WGM * WGN, LW = PW > 0 ? PW : WAVES, THREADS = (WAVES + PW) * 64;
+  static constexpr int WM = BM / WGM, WN = BN / WGN, XT = WM / 16, YT = WN / 16;
+  static constexpr int YP = YP_ > 0 ? YP_ : YT, NP = YT / YP;
+  static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int NLA = A_BYTES / 1024 / LW, NLB = B_BYTES / 1024 / LW, NL = NLA + NLB;
+  static constexpr int LDS_BYTES = NSTAGE * STAGE_BYTES;
+  static_assert(LDS_BYTES * PER_CU <= LDS_MAX && WM % 16 == 0 && WN % 32 == 0 && YT % YP == 0, "tile");
+  static_assert(A_BYTES % (1024 * LW) == 0 && B_BYTES % (1024 * LW) == 0 && NL * (NSTAGE - 2) <= 63, "loads");
+};
+
+template <typename F, int... I>
+__device__ __forceinline__ void static_for_each(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F f) { static_for_each(std::make_integer_sequence<int, N>{}, f); }
+
+// An operand: KC, storage [rows][k] with the contraction index contiguous, staged in LDS [row][64], or KS, storage [k][rows], staged [64][rows] and fetched with
+// the transposing read.  Swizzles as in gemm_bf16.hip: of KC the 16-byte pieces of a row by (row / 2) % 8, of KS the 32-byte pieces of a k-row
+// by a function of k, so that the lanes of a fetch fill all banks.
+// PAIRS (KC): the rows of a tile are sixteen of the first half of the matrix, the same sixteen of the second half, and so on.
+enum { KC, KS, PAIRS };
+template <int R>
+__device__ __forceinline__ int chunk_swizzle(int kr) {
+  constexpr int NC = R / 16;
+  static_assert(NC % 8 == 0 || NC == 4, "tile width");
+  return NC % 8 == 0 ? (kr & 3) | ((kr >> 1) & 4) : ((kr >> 1) & 1) | ((kr >> 2) & 2);
+}
+struct Operand {
+  const bf16_t* p; uint32_t ld, rows;   // rows: of the matrix (KC) or its columns (KS); PAIRS: of a half
+};
+// Byte offset, from the slab's first element, of the 16 bytes that belong at byte `at` of its stage, and their contraction index.
+template <int S, int R>
+__device__ __forceinline__ uint32_t piece_offset(uint32_t at, const Operand& o, uint32_t& k) {
+  if constexpr (S == KS) {
+    constexpr uint32_t RB = R * 2;
+    const uint32_t kr = at / RB, q = at % RB / 16, ql = (((q >> 1) ^ (uint32_t)chunk_swizzle<R>((int)kr)) << 1) | (q & 1);
+    k = kr;
+    return kr * o.ld * 2 + ql * 16;
+  } else {
+    const uint32_t r = at / 128, c = at % 128 / 16 ^ (r / 2) % 8;
+    k = c * 8;
+    const uint32_t row = S == KC ? r : (r / 32) * 16 + r % 16 + ((r / 16) & 1) * o.rows;
+    return row * o.ld * 2 + c * 16;
+  }
+}
+template <int S, int R>
+__device__ __forceinline__ int fetch_lane_offset(int lane, int ks_or_frag) {
+  if constexpr (S == KS) {
+    const int j = lane & 15, kr = 8 * (lane >> 4) + (j >> 2);   // the swizzle is the same for kr + 4 and kr + 32
+    return kr * R * 2 + ((ks_or_frag ^ chunk_swizzle<R>(kr)) * 32) + 8 * (j & 3);
+  } else {
+    const int r = lane & 15;
+    return r * 128 + (((4 * ks_or_frag + (lane >> 4)) ^ (r / 2) % 8) * 16);
+  }
+}
+
+// Loads go through buffer descriptors: what lies behind the last value of a matrix reads as zero, so that tiles may hang over in rows and, of KS,
+// in the contraction; the pieces of a KC slab behind the end of the contraction are sent out of range.  The descriptor begins at the slab's
+// first element, so offsets stay below 2^31 whatever the size of the matrix.
+constexpr uint32_t NOWHERE = 0x80000000u, MOST = 0x7fffffffu;
+struct Window {
+  uint64_t at, left;   // address of the next slab, bytes from there to the end of the matrix
+  __device__ __forceinline__ u32x4 descriptor() const {
+    return (u32x4){(uint32_t)at, (uint32_t)(at >> 32), left > MOST ? MOST : (uint32_t)left, 0x00020000u};
+  }
+  __device__ __forceinline__ void step(uint32_t bytes) { at += bytes; left -= bytes; }
+};
+template <int S>
+__device__ __forceinline__ Window window(const Operand& o, uint32_t row0, uint32_t k0, uint32_t K) {
+  Window w;
+  const uint64_t first = S == KS ? (uint64_t)k0 * o.ld + row0 : (uint64_t)row0 * o.ld + k0;
+  const uint64_t end = S == KS ? (uint64_t)(K - 1) * o.ld + o.rows : (uint64_t)((S == PAIRS ? 2 : 1) * o.rows - 1) * o.ld + K;
+  w.at = (uint64_t)(uintptr_t)o.p + 2 * first;
+  w.left = 2 * (end - first);
+  return w;
+}
+
+template <int NL, int W>
+__device__ __forceinline__ void wait_loads(int younger) {
+  if constexpr (W == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    if (younger >= W) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NL * W) : "memory");
+    else wait_loads<NL, W - 1>(younger);
+  }
+}
+
+// acc = the products of rows i0.. of A and j0.. of B over slabs [slab0, slab0 + slabs) of the contraction K.  D = B-fragment x A-fragment: a lane has
+// four neighbouring columns 4 (lane / 16) .. + 3 of row lane % 16 of each 16 x 16 fragment.  Every wave of the workgroup calls it; those that only load
+// come back without results.  No wave may read or write the stages any more when it is called.
+template <typename T, int SA, int SB>
+__device__ __forceinline__ void contract(f32x4 (&acc)[T::XT][T::YT], unsigned char* smem, const Operand& A, const Operand& B, uint32_t i0, uint32_t j0,
+                                         uint32_t K, uint32_t slab0, int slabs) {
+  constexpr int XT = T::XT, YT = T::YT, NSTAGE = T::NSTAGE;
+  constexpr int RD = T::RD == 0 && SA != KS && SB != KS ? 9 : T::RD;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lw = T::PW > 0 ? wave - T::WAVES : wave;
+  const bool loader = T::PW == 0 || wave >= (uint32_t)T::WAVES;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)smem;
+  uint32_t offA[T::NLA], offB[T::NLB], ragged = 0;      // ragged: loads of a KC operand that are behind the contraction's end in its last slab
+  Window wa{}, wb{};
+  const uint32_t stepA = SA == KS ? BK * A.ld * 2 : BK * 2, stepB = SB == KS ? BK * B.ld * 2 : BK * 2;
+  const bool to_end = K % BK != 0 && slab0 + slabs == (K + BK - 1) / BK;
+  int next = 0;
+  uint32_t next_at = lds0 + lw * 1024;
+  auto load = [&](uint32_t to, uint32_t off, u32x4 from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+  };
+  auto issue = [&]() {
+    if (next >= slabs) return;
+    const u32x4 da = wa.descriptor(), db = wb.descriptor();
+    if (to_end && next == slabs - 1) {
+#pragma unroll
+      for (int q = 0; q < T::NLA; ++q) if (SA != KS && (ragged >> q & 1)) offA[q] = NOWHERE;
+#pragma unroll
+      for (int q = 0; q < T::NLB; ++q) if (SB != KS && (ragged >> (T::NLA + q) & 1)) offB[q] = NOWHERE;
+    }
+#pragma unroll
+    for (int q = 0; q < T::NLA; ++q) load(next_at + q * T::LW * 1024, offA[q], da);
+#pragma unroll
+    for (int q = 0; q < T::NLB; ++q) load(next_at + T::A_BYTES + q * T::LW * 1024, offB[q], db);
+    wa.step(stepA); wb.step(stepB);
+    next_at = (next + 1) % NSTAGE == 0 ? lds0 + lw * 1024 : next_at + T::STAGE_BYTES;
+    ++next;
+  };
+  auto arrive = [&](int sl) {   // slab sl is there for everybody, the stage of slab sl - 1 is free
+    if (loader) wait_loads<T::NL, NSTAGE - 2>(slabs - 1 - sl);
+    __builtin_amdgcn_s_barrier();
+    if (loader) issue();
+  };
+  if (loader) {
+    wa = window<SA>(A, i0, slab0 * BK, K); wb = window<SB>(B, j0, slab0 * BK, K);
+    const uint32_t last_k = (K - 1) % BK;
+#pragma unroll
+    for (int q = 0; q < T::NLA; ++q) { uint32_t k; offA[q] = piece_offset<SA, T::BM>((q * T::LW + lw) * 1024 + lane * 16, A, k); if (k > last_k) ragged |= 1u << q; }
+#pragma unroll
+    for (int q = 0; q < T::NLB; ++q) { uint32_t k; offB[q] = piece_offset<SB, T::BN>((q * T::LW + lw) * 1024 + lane * 16, B, k); if (k > last_k) ragged |= 1u << (T::NLA + q); }
+#pragma unroll
+    for (int s = 0; s < NSTAGE - 1; ++s) issue();
+  }
+  if (T::PW > 0 && loader) {
+    for (int i = 0; i < slabs; ++i) arrive(i);
+    return;
+  }
+
+  const int wr = (int)(wave / T::WGN) * T::WM, wc = (int)(wave % T::WGN) * T::WN;
+#pragma unroll
+  for (int x = 0; x < XT; ++x)
+#pragma unroll
+    for (int y = 0; y < YT; ++y) acc[x][y] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  constexpr int STEPS = BK / 32;
+  int fa[SA == KS ? XT : STEPS], fb[SB == KS ? YT : STEPS];
+  if (SA != KS) {
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ++ks) fa[ks] = fetch_lane_offset<SA, T::BM>(lane, ks) + wr * 128;
+  } else {
+#pragma unroll
+    for (int x = 0; x < XT; ++x) fa[x] = fetch_lane_offset<SA, T::BM>(lane, (wr >> 4) + x);
+  }
+  if (SB != KS) {
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ++ks) fb[ks] = fetch_lane_offset<SB, T::BN>(lane, ks) + wc * 128;
+  } else {
+#pragma unroll
+    for (int y = 0; y < YT; ++y) fb[y] = fetch_lane_offset<SB, T::BN>(lane, (wc >> 4) + y);
+  }
+  auto fetch = [&](const unsigned char* s, auto strided, auto r, const int* f, int frag, int ks) -> bf16x8 {
+    constexpr int R = decltype(r)::value;
+    if constexpr (!decltype(strided)::value) return *reinterpret_cast<const bf16x8*>(s + f[ks] + frag * 16 * 128);
+    const unsigned char* const p = s + f[frag] + ks * 32 * R * 2;
+    union { bf16x8 v; s16x4 h[2]; } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * R * 2));
+    return u.v;
+  };
+  auto fetchA = [&](const unsigned char* s, int x, int ks) { return fetch(s, std::bool_constant<SA == KS>{}, std::integral_constant<int, T::BM>{}, fa, x, ks); };
+  auto fetchB = [&](const unsigned char* s, int y, int ks) { return fetch(s + T::A_BYTES, std::bool_constant<SB == KS>{}, std::integral_constant<int, T::BN>{}, fb, y, ks); };
+
+  constexpr int YP = T::YP, NP = T::NP, NT = STEPS * NP, NM = XT * YP;   // pieces of a slab, products of a piece
+  static_assert(NT % 2 == 0, "operand double buffer parity");
+  bf16x8 av[2][XT], bv[2][YP];
+  auto mfma = [&](auto t, auto m) {
+    constexpr int T_ = t, ks = T_ / NP, y0 = T_ % NP * YP, x = m / YP, yy = m % YP, y = (x & 1) ? YP - 1 - yy : yy;
+    acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[T_ & 1][y], av[ks & 1][x], acc[x][y0 + y], 0, 0, 0);
+  };
+  constexpr int READS = YP + XT;
+  auto operands = [](int t) { return YP + (t % NP == 0 ? XT : 0); };
+  auto read = [&](const unsigned char* at, auto t, auto r) {
+    constexpr int T_ = t, R_ = r, ks = T_ / NP, p = T_ % NP, wa1 = p == 0 ? 1 : 0;
+    if constexpr (wa1 == 1 && R_ == 0) av[ks & 1][0] = fetchA(at, 0, ks);
+    else if constexpr (R_ - wa1 < YP) bv[T_ & 1][R_ - wa1] = fetchB(at, p * YP + R_ - wa1, ks);
+    else av[ks & 1][R_ - YP] = fetchA(at, R_ - YP, ks);
+  };
+  auto read_all = [&](const unsigned char* at, auto t) {
+    static_for<READS>([&](auto r) { if constexpr (decltype(r)::value < operands(decltype(t)::value)) read(at, t, r); });
+  };
+  auto multiply = [&](auto t) {
+    if (RD != 0) __builtin_amdgcn_sched_barrier(0);
+    static_for<NM>([&](auto m) { mfma(t, m); });
+    if (RD != 0) __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply_reading = [&](auto t, const unsigned char* at, auto tn) {
+    constexpr int nr = operands(decltype(tn)::value);
+    constexpr auto before = [](int m) { const int b = (m * nr * RD + NM - 1) / NM; return b < nr ? b : nr; };
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<NM>([&](auto m) {
+      static_for<READS>([&](auto r) { if constexpr (decltype(r)::value >= before(decltype(m)::value) && decltype(r)::value < before(decltype(m)::value + 1)) read(at, tn, r); });
+      __builtin_amdgcn_sched_barrier(0);
+      mfma(t, m);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  auto stage_of = [&](int sl) { return smem + (sl % NSTAGE) * T::STAGE_BYTES; };
+  arrive(0);
+  if constexpr (RD == 0) {
+    for (int i = 0; i < slabs; ++i) {
+      if (i > 0) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        arrive(i);
+      }
+      const unsigned char* const at = stage_of(i);
+      static_for<NT>([&](auto t) { read_all(at, t); multiply(t); });
+    }
+  } else {
+    read_all(stage_of(0), std::integral_constant<int, 0>{});
+    for (int i = 0; i + 1 < slabs; ++i) {
+      const unsigned char* const at = stage_of(i);
+      static_for<NT - 1>([&](auto t) { multiply_reading(t, at, std::integral_constant<int, decltype(t)::value + 1>{}); });
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      arrive(i + 1);
+      multiply_reading(std::integral_constant<int, NT - 1>{}, stage_of(i + 1), std::integral_constant<int, 0>{});
+    }
+    const unsigned char* const at = stage_of(slabs - 1);
+    static_for<NT - 1>([&](auto t) { multiply_reading(t, at, std::integral_constant<int, decltype(t)::value + 1>{}); });
+    multiply(std::integral_constant<int, NT - 1>{});
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- epilogues
+__device__ __forceinline__ uint2 packed(f32x4 v) { return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
+// Of two neighbouring fragments lanes 16 apart exchange halves: a lane then has eight neighbouring columns, 16 (g & 1) + 8 (g / 2) on, g = lane / 16.
+__device__ __forceinline__ uint4 side_by_side(f32x4 a, f32x4 b) {
+  uint2 v0 = packed(a), v1 = packed(b);
+  u32x2 r = __builtin_amdgcn_permlane16_swap(v0.x, v1.x, false, false); v0.x = r[0]; v1.x = r[1];
+  r = __builtin_amdgcn_permlane16_swap(v0.y, v1.y, false, false); v0.y = r[0]; v1.y = r[1];
+  return make_uint4(v0.x, v0.y, v1.x, v1.y);
+}
+__device__ __forceinline__ int pair_column(int lane) { return 16 * ((lane >> 4) & 1) + 8 * (lane >> 5); }
+
+// The gate and its derivative: silu(g) = g s, silu'(g) = s + g s (1 - s) with s = 1 / (1 + exp(-g)); gelu(g) = g P(g), gelu'(g) = P(g) + g p(g) with the
+// normal distribution P and its density p.
+template <int ACT>
+__device__ __forceinline__ float gate(float g) {
+  if constexpr (ACT == GLU_GELU) return gelu_f(g);
+  else return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
+}
+template <int ACT>
+__device__ __forceinline__ void gate_and_slope(float g, float& a, float& da) {
+  if constexpr (ACT == GLU_GELU) {
+    float e, ez;
+    erf_and_gauss(g * 0.70710678118654752f, e, ez);
+    const float cdf = 0.5f * (1.f + e);
+    a = g * cdf; da = fmaf(g * 0.39894228040143268f, ez, cdf);
+  } else {
+    const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
+    a = g * s; da = fmaf(a, 1.f - s, s);
+  }
+}
+
+// g and u as the backward pass finds them: their leading 24 bits (2^-15, where the rounding to bf16 that follows is 2^-8), four values of each in
+// three words, so that a lane's part of a 16 x 16 fragment is 16 and 8 bytes.  Blocks of 16 rows by 16 columns in row order, 1 KB and 512 bytes of
+// one block side by side: every store and load is whole lines.  Held in bf16 they would be 8 bytes of 12 and would double the error
+// of the gradients, in fp32 16.
+constexpr int SAVED_BLOCK = 1536;
+__device__ __forceinline__ void pack24(f32x4 v, uint32_t (&w)[3]) {
+  const uint32_t b[4] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  w[0] = __builtin_amdgcn_perm(b[1], b[0], 0x05030201);
+  w[1] = __builtin_amdgcn_perm(b[2], b[1], 0x06050302);
+  w[2] = __builtin_amdgcn_perm(b[3], b[2], 0x07060503);
+}
+__device__ __forceinline__ f32x4 unpack24(uint32_t w0, uint32_t w1, uint32_t w2) {
+  return (f32x4){__uint_as_float(w0 << 8), __uint_as_float(__builtin_amdgcn_perm(w1, w0, 0x0504030c)),
+                 __uint_as_float(__builtin_amdgcn_perm(w2, w1, 0x0403020c)), __uint_as_float(w2 & 0xffffff00u)};
+}
+
+struct TileOrder { uint32_t tiles, per_xcd, tm, tn; };   // tm x tn tiles
+// Workgroups are dealt to the eight XCDs in turn; each gets a run of the tiles, in groups of eight tile rows, column by column.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t& ti, uint32_t& tj) {
+  const uint32_t width = 8 * tn, grp = id / width, rest = id - grp * width, high = min(tm - grp * 8, 8u);
+  tj = rest / high; ti = grp * 8 + rest - tj * high;
+}
+
+struct UpArgs {
+  Operand x, w;          // w: PAIRS
+  uint32_t T, F, d;
+  TileOrder order;
+  bf16_t* h;             // [T x F]
+  unsigned char* saved;  // or null
+  uint32_t* tickets; int ntickets;   // of the launch behind, to be cleared
+};
+template <typename T, int ACT>
+__global__ __launch_bounds__(T::THREADS) void k_glu_up(UpArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  for (int i = blockIdx.x * T::THREADS + threadIdx.x; i < a.ntickets; i += gridDim.x * T::THREADS) a.tickets[i] = 0;
+  const uint32_t id = (blockIdx.x & 7) * a.order.per_xcd + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= a.order.per_xcd || id >= a.order.tiles) return;
+  uint32_t ti, tj;
+  tile_of(id, a.order.tm, a.order.tn, ti, tj);
+  const uint32_t i0 = ti * T::BM, j0 = tj * (T::BN / 2);
+  f32x4 acc[T::XT][T::YT];
+  contract<T, KC, PAIRS>(acc, smem, a.x, a.w, i0, j0, a.d, 0, (a.d + BK - 1) / BK);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= (uint32_t)T::WAVES) return;
+  const int lane = threadIdx.x & 63;
+  const uint32_t row0 = i0 + (wave / T::WGN) * T::WM, col0 = j0 + (wave % T::WGN) * (T::WN / 2);
+  const uint32_t blocks = (a.F + 15) / 16;
+  constexpr int GR = T::YT / 2;                     // granules of 16 hidden values
+  static_for<T::XT>([&](auto x_) {
+    constexpr int x = x_;
+    if (row0 + 16 * x >= a.T) return;
+    f32x4 h[GR];
+    static_for<GR>([&](auto q_) {
+      constexpr int q = q_;
+      const f32x4 g = acc[x][2 * q], u = acc[x][2 * q + 1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[q][e] = gate<ACT>(g[e]) * u[e];
+      if (a.saved != nullptr && col0 + 16 * q < a.F) {
+        unsigned char* const b = a.saved + ((uint64_t)((row0 >> 4) + x) * blocks + (col0 >> 4) + q) * SAVED_BLOCK;
+        uint32_t wg[3], wu[3];
+        pack24(g, wg); pack24(u, wu);
+        *reinterpret_cast<uint4*>(b + lane * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
+        *reinterpret_cast<uint2*>(b + 1024 + lane * 8) = make_uint2(wu[1], wu[2]);
+      }
+    });
+    const uint32_t row = row0 + 16 * x + (lane & 15);
+    bf16_t* const to = a.h + (uint64_t)row * a.F;
+    if constexpr (GR == 1) {
+      const uint32_t col = col0 + 4 * (lane >> 4);
+      if (row < a.T && col < a.F) *reinterpret_cast<uint2*>(to + col) = packed(h[0]);
+    } else {
+      static_for<GR / 2>([&](auto q_) {
+        constexpr int q = 2 * q_;
+        const uint4 v = side_by_side(h[q], h[q + 1]);
+        const uint32_t col = col0 + 16 * q + pair_column(lane);
+        if (row < a.T && col < a.F) *reinterpret_cast<uint4*>(to + col) = v;
+      });
+    }
+  });
+}
+
+struct DgateArgs {
+  Operand dy, w;         // w: KS
+  uint32_t T, F, d;
+  TileOrder order;
+  const unsigned char* saved;
+  bf16_t* dpre;          // [T x 2F]: dg, du
+  uint32_t* tickets; int ntickets;
+};
+template <typename T, int ACT>
+__global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  for (int i = blockIdx.x * T::THREADS + threadIdx.x; i < a.ntickets; i += gridDim.x * T::THREADS) a.tickets[i] = 0;
+  const uint32_t id = (blockIdx.x & 7) * a.order.per_xcd + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= a.order.per_xcd || id >= a.order.tiles) return;
+  uint32_t ti, tj;
+  tile_of(id, a.order.tm, a.order.tn, ti, tj);
+  const uint32_t i0 = ti * T::BM, j0 = tj * T::BN;
+  f32x4 acc[T::XT][T::YT];
+  contract<T, KC, KS>(acc, smem, a.dy, a.w, i0, j0, a.d, 0, (a.d + BK - 1) / BK);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= (uint32_t)T::WAVES) return;
+  const int lane = threadIdx.x & 63;
+  const uint32_t row0 = i0 + (wave / T::WGN) * T::WM, col0 = j0 + (wave % T::WGN) * T::WN;
+  const uint32_t blocks = (a.F + 15) / 16;
+  static_for<T::XT>([&](auto x_) {
+    constexpr int x = x_;
+    if (row0 + 16 * x >= a.T) return;
+    const uint32_t row = row0 + 16 * x + (lane & 15);
+    bf16_t* const to = a.dpre + (uint64_t)row * (2 * a.F);
+    static_for<T::YT / 2>([&](auto h_) {
+      constexpr int h = h_;
+      f32x4 dg[2], du[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t block = min((col0 >> 4) + 2 * h + k, blocks - 1);
+        const unsigned char* const b = a.saved + ((uint64_t)((row0 >> 4) + x) * blocks + block) * SAVED_BLOCK;
+        const uint4 p = *reinterpret_cast<const uint4*>(b + lane * 16);
+        const uint2 r = *reinterpret_cast<const uint2*>(b + 1024 + lane * 8);
+        const f32x4 g = unpack24(p.x, p.y, p.z), u = unpack24(p.w, r.x, r.y), dh = acc[x][2 * h + k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float s, ds;
+          gate_and_slope<ACT>(g[e], s, ds);
+          dg[k][e] = dh[e] * (u[e] * ds); du[k][e] = dh[e] * s;
+        }
+      }
+      const uint4 vg = side_by_side(dg[0], dg[1]), vu = side_by_side(du[0], du[1]);
+      const uint32_t col = col0 + 32 * h + pair_column(lane);
+      if (row < a.T && col < a.F) {
+        *reinterpret_cast<uint4*>(to + col) = vg;
+        *reinterpret_cast<uint4*>(to + a.F + col) = vu;
+      }
+    });
+  });
+}
+
+// ---------------------------------------------------------------------------------------------------- products split over the chip
+// One to three products in a launch whose tiles need not be a multiple of the chip: the slabs of all tiles, in the order of the tiles, are cut into
+// equal runs, one for each workgroup, wherever that falls (`split`); a tile that lies in several workgroups' runs is added up by the last of them to come.
+struct Product {
+  Operand A, B;
+  uint32_t M, N, K, tm, tn, slabs, first;   // first: slab of all the tiles before
+  void* C; uint32_t ldc; int strided_a, c32;
+};
+struct SplitArgs {
+  Product p[3];
+  int count, split, groups;   // groups: workgroups
+  uint64_t units;
+  float* part;                // [groups][first, last][tile]
+  uint32_t* tickets;          // [tiles], zero
+};
+template <typename T>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[T::XT][T::YT], const Product& p, uint32_t i0, uint32_t j0, uint32_t wave) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t row0 = i0 + (wave / T::WGN) * T::WM, col0 = j0 + (wave % T::WGN) * T::WN;
+  static_for<T::XT>([&](auto x_) {
+    constexpr int x = x_;
+    const uint32_t row = row0 + 16 * x + (lane & 15);
+    if (p.c32) {
+      float* const to = static_cast<float*>(p.C) + (uint64_t)row * p.ldc;
+      static_for<T::YT>([&](auto y_) {
+        const uint32_t col = col0 + 16 * decltype(y_)::value + 4 * (lane >> 4);
+        if (row < p.M && col < p.N) *reinterpret_cast<f32x4*>(to + col) = acc[x][decltype(y_)::value];
+      });
+    } else {
+      bf16_t* const to = static_cast<bf16_t*>(p.C) + (uint64_t)row * p.ldc;
+      static_for<T::YT / 2>([&](auto h_) {
+        constexpr int h = h_;
+        const uint4 v = side_by_side(acc[x][2 * h], acc[x][2 * h + 1]);
+        const uint32_t col = col0 + 32 * h + pair_column(lane);
+        if (row < p.M && col < p.N) *reinterpret_cast<uint4*>(to + col) = v;
+      });
+    }
+  });
+}
+
+// Values that one workgroup leaves for another of the same launch: written through to where every XCD sees them and read past the caches, as publish()
+// and collect() do it one value at a time.
+__device__ __forceinline__ void publish16(float* p, f32x4 v) { asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(p), "v"(v) : "memory"); }
+__device__ __forceinline__ void collect16(const float* p, f32x4 (&v)[4], int step) {
+  asm volatile("global_load_dwordx4 %0, %4, off sc1\n\tglobal_load_dwordx4 %1, %5, off sc1\n\t"
+               "global_load_dwordx4 %2, %6, off sc1\n\tglobal_load_dwordx4 %3, %7, off sc1\n\ts_waitcnt vmcnt(0)"
+               : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(p), "v"(p + step), "v"(p + 2 * step), "v"(p + 3 * step) : "memory");
+}
+
+// KINDS: 0: forward (A and B KC); 1: gradients, dx with A KC and B KS, the weights' with both KS
+template <typename T, int KIND>
+__global__ __launch_bounds__(T::THREADS) void k_glu_split(SplitArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int s_last;
+  const uint32_t groups = a.groups, per_xcd = (groups + 7) / 8, l = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per_xcd || l >= groups) return;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int FRAGS = T::XT * T::YT, TILE = T::BM * T::BN;
+  f32x4 acc[T::XT][T::YT];
+  uint64_t at = a.split ? l * a.units / groups : 0;                      // first unit of what is left
+  const uint64_t end = a.split ? (l + 1) * a.units / groups : 0;
+  bool first_piece = true;
+  do {
+    // the tile of this piece
+    int k = 0;
+    uint32_t tile = 0, tiles_before = 0, slab0 = 0;
+    if (a.split) {
+      while (k + 1 < a.count && at >= a.p[k + 1].first) { tiles_before += a.p[k].tm * a.p[k].tn; ++k; }
+      const uint32_t u = (uint32_t)(at - a.p[k].first);
+      tile = u / a.p[k].slabs; slab0 = u - tile * a.p[k].slabs;
+    } else {
+      tile = l;
+      while (k + 1 < a.count && tile >= a.p[k].tm * a.p[k].tn) { tile -= a.p[k].tm * a.p[k].tn; tiles_before += a.p[k].tm * a.p[k].tn; ++k; }
+    }
+    const Product& p = a.p[k];
+    const uint64_t tile_at = p.first + (uint64_t)tile * p.slabs;         // units of the tile
+    const int slabs = a.split ? (int)min((uint64_t)(p.slabs - slab0), end - at) : (int)p.slabs;
+    uint32_t ti, tj;
+    tile_of(tile, p.tm, p.tn, ti, tj);
+    const uint32_t i0 = ti * T::BM, j0 = tj * T::BN;
+    if (!first_piece) __syncthreads();                                   // the stages are free
+    if constexpr (KIND == 0) contract<T, KC, KC>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+    else if (p.strided_a) contract<T, KS, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+    else contract<T, KC, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+    const bool multiplies = wave < (uint32_t)T::WAVES;
+    if (slabs == (int)p.slabs) {
+      if (multiplies) store_tile<T>(acc, p, i0, j0, wave);
+    } else {
+      // the workgroups of the tile: the one that has its first unit, to the one that has its last
+      auto group_of = [&](uint64_t unit) { return (uint32_t)(((unit + 1) * groups - 1) / a.units); };
+      const uint32_t l0 = group_of(tile_at), l1 = group_of(tile_at + p.slabs - 1);
+      auto part_of = [&](uint32_t g) {   // a workgroup's last tile, if it has its beginning, else its first one
+        return a.part + ((uint64_t)2 * g + (g == l0 ? 1 : 0)) * TILE + (wave * 64 + (threadIdx.x & 63)) * 4;
+      };
+      constexpr int STEP = T::WAVES * 256;   // floats from a fragment to the next
+      if (multiplies) {
+        float* const to = part_of(l);
+        static_for<FRAGS>([&](auto f) { publish16(to + decltype(f)::value * STEP, acc[decltype(f)::value / T::YT][decltype(f)::value % T::YT]); });
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        uint32_t* const ticket = a.tickets + tiles_before + tile;
+        s_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == l1 - l0 ? 1 : 0;
+      }
+      __syncthreads();
+      if (s_last != 0 && multiplies) {       // the parts in the order of the contraction, whoever adds them
+        static_for<FRAGS / 4>([&](auto f4) {
+          constexpr int f0 = 4 * f4;
+          f32x4 sum[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] = (f32x4){0.f, 0.f, 0.f, 0.f};
+          for (uint32_t g = l0; g <= l1; ++g) {
+            f32x4 v[4];
+            if (g == l) {
+              static_for<4>([&](auto e) { v[e] = acc[(f0 + decltype(e)::value) / T::YT][(f0 + decltype(e)::value) % T::YT]; });
+            } else {
+              collect16(part_of(g) + f0 * STEP, v, STEP);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += v[e];
+          }
+          static_for<4>([&](auto e) { acc[(f0 + decltype(e)::value) / T::YT][(f0 + decltype(e)::value) % T::YT] = sum[e]; });
+        });
+        store_tile<T>(acc, p, i0, j0, wave);
+      }
+    }
+    at += slabs;
+    first_piece = false;
+  } while (a.split && at < end);
+}
+
+// ---------------------------------------------------------------------------------------------------- launches
+typedef Tile<256, 256, 2, 4, 2, 0, 2, 0, 1> T256;
+typedef Tile<128, 128, 2, 4, 4, 4, 0, 1, 1> T128;
+typedef Tile<64, 64, 2, 2, 4, 0, 0, 1, 2> T64;
+
+template <auto KERNEL, typename T, typename A>
+void launch_big(ProfScope& ps, hipStream_t st, uint32_t grid, const A& a) {
+  static bool configured = false;   // per kernel: raise the dynamic LDS limit once
+  if (!configured) {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
+    configured = true;
+  }
+  launch_kernel(ps, KERNEL, grid, T::THREADS, T::LDS_BYTES, st, a);
+}
+TileOrder order_of(uint32_t M, uint32_t N, uint32_t bm, uint32_t bn) {
+  TileOrder o{};
+  o.tm = (M + bm - 1) / bm; o.tn = (N + bn - 1) / bn; o.tiles = o.tm * o.tn; o.per_xcd = (o.tiles + 7) / 8;
+  return o;
+}
+template <typename T>
+void launch_up(ProfScope& ps, hipStream_t st, UpArgs a, int act) {
+  a.order = order_of(a.T, a.F, T::BM, T::BN / 2);
+  if (act == GLU_GELU) launch_big<k_glu_up<T, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
+  else launch_big<k_glu_up<T, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
+}
+template <typename T>
+void launch_dgate(ProfScope& ps, hipStream_t st, DgateArgs a, int act) {
+  a.order = order_of(a.T, a.F, T::BM, T::BN);
+  if (act == GLU_GELU) launch_big<k_glu_dgate<T, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
+  else launch_big<k_glu_dgate<T, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
+}
+constexpr uint64_t LEAST_RUN = 6;
+template <typename T>
+void plan_split(SplitArgs& a) {
+  uint64_t units = 0;
+  uint32_t tiles = 0;
+  for (int k = 0; k < a.count; ++k) {
+    Product& p = a.p[k];
+    p.tm = (p.M + T::BM - 1) / T::BM; p.tn = (p.N + T::BN - 1) / T::BN; p.slabs = (p.K + BK - 1) / BK; p.first = (uint32_t)units;
+    units += (uint64_t)p.tm * p.tn * p.slabs; tiles += p.tm * p.tn;
+  }
+  a.units = units;
+  const uint32_t slots = 256 * T::PER_CU;
+  // Whole tiles in rounds, or all slabs in equal runs with what it costs to add the parts up, the time of about JOIN slabs; a run has LEAST_RUN of them at least.
+  constexpr uint64_t JOIN = 6;
+  uint32_t longest = 0;
+  for (int k = 0; k < a.count; ++k) longest = std::max(longest, a.p[k].slabs);
+  const uint64_t rounds = (tiles + slots - 1) / slots, whole = rounds * longest;
+  const uint64_t groups = std::max<uint64_t>(1, std::min<uint64_t>(slots, units / LEAST_RUN)), run = (units + groups - 1) / groups + JOIN;
+  a.split = run < whole && groups > 1 ? 1 : 0;
+  a.groups = a.split ? (int)groups : (int)tiles;
+}
+template <typename T, int KIND>
+void launch_split(ProfScope& ps, hipStream_t st, SplitArgs a) {
+  plan_split<T>(a);
+  launch_big<k_glu_split<T, KIND>, T>(ps, st, 8 * ((a.groups + 7) / 8), a);
+}
+
+int g_force_tile = 0;
+int tile_for(int64_t M, int64_t N) {
+  if (g_force_tile != 0) return g_force_tile;
+  const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256), t128 = ((M + 127) / 128) * ((N + 127) / 128);
+  return t256 >= 200 ? 256 : t128 >= 100 ? 128 : 64;
+}
+// Partial sums: two tiles for each workgroup that has a run of slabs, whether they are cut or not, so that the size grows with the number of tokens and what is
+// enough for some is for fewer.
+template <typename T>
+size_t part_bytes_of(const SplitArgs& shapes) {
+  SplitArgs a = shapes;
+  plan_split<T>(a);
+  return (size_t)2 * std::max<uint64_t>(1, std::min<uint64_t>(256 * T::PER_CU, a.units / LEAST_RUN)) * T::BM * T::BN * 4;
+}
+size_t part_bytes(const SplitArgs& a) { return std::max({part_bytes_of<T256>(a), part_bytes_of<T128>(a), part_bytes_of<T64>(a)}); }
+size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+size_t most_tiles(int64_t M, int64_t N) { return (size_t)((M + 63) / 64) * ((N + 63) / 64); }
+}  // namespace
+
+void glu_ffn_force_tile(int t) { g_force_tile = t; }
+
+size_t glu_ffn_saved_bytes(int64_t T, int F) { return (size_t)((T + 15) / 16) * ((F + 15) / 16) * SAVED_BLOCK; }
+size_t glu_ffn_bytes(int64_t T, int d, int F) {
+  SplitArgs s{};
+  s.count = 1; s.p[0].M = (uint32_t)T; s.p[0].N = d; s.p[0].K = F;
+  return up256(most_tiles(T, d) * 4) + part_bytes(s);
+}
+size_t glu_ffn_grad_bytes(int64_t T, int d, int F) {
+  SplitArgs s{};
+  s.count = 3; s.p[0].M = (uint32_t)T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[1].M = 2 * F; s.p[1].N = d; s.p[1].K = (uint32_t)T; s.p[2].M = d; s.p[2].N = F; s.p[2].K = (uint32_t)T;
+  return up256((most_tiles(T, d) + most_tiles(2 * F, d) + most_tiles(d, F)) * 4) + up256((size_t)T * 2 * F * 2) + part_bytes(s);
+}
+
+void launch_glu_ffn(hipStream_t st, const GluFfnArgs& g, void* workspace) {
+  if (g.T == 0) return;
+  char* const ws = static_cast<char*>(workspace);
+  const uint32_t T = (uint32_t)g.T, d = g.d, F = g.F;
+  const size_t ntickets = most_tiles(T, d);
+  ProfScope ps(st, F_GEMM_NT, 6.0 * T * (double)d * F);
+  UpArgs u{};
+  u.x = Operand{(const bf16_t*)g.x, (uint32_t)g.ldx, T}; u.w = Operand{(const bf16_t*)g.w_in, d, F};
+  u.T = T; u.F = F; u.d = d; u.h = (bf16_t*)g.hidden; u.saved = (unsigned char*)g.saved;
+  u.tickets = (uint32_t*)ws; u.ntickets = (int)ntickets;
+  switch (tile_for(T, 2 * (int64_t)F)) {
+    case 256: launch_up<T256>(ps, st, u, g.act); break;
+    case 128: launch_up<T128>(ps, st, u, g.act); break;
+    default: launch_up<T64>(ps, st, u, g.act); break;
+  }
+  SplitArgs s{};
+  s.count = 1; s.part = (float*)(ws + up256(ntickets * 4)); s.tickets = (uint32_t*)ws;
+  Product& p = s.p[0];
+  p.A = Operand{(const bf16_t*)g.hidden, F, T}; p.B = Operand{(const bf16_t*)g.w_out, F, d};
+  p.M = T; p.N = d; p.K = F; p.C = g.y; p.ldc = (uint32_t)g.ldy;
+  switch (tile_for(T, d)) {
+    case 256: launch_split<T256, 0>(ps, st, s); break;
+    case 128: launch_split<T128, 0>(ps, st, s); break;
+    default: launch_split<T64, 0>(ps, st, s); break;
+  }
+}
+
+void launch_glu_ffn_grad(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
+  char* const ws = static_cast<char*>(workspace);
+  const uint32_t T = (uint32_t)g.T, d = g.d, F = g.F;
+  const size_t ntickets = most_tiles(T, d) + most_tiles(2 * F, d) + most_tiles(d, F);
+  bf16_t* const dpre = (bf16_t*)(ws + up256(ntickets * 4));
+  ProfScope ps(st, F_GEMM_NN, 12.0 * T * (double)d * F);
+  DgateArgs e{};
+  e.dy = Operand{(const bf16_t*)g.dy, (uint32_t)g.lddy, T}; e.w = Operand{(const bf16_t*)g.w_out, F, F};
+  e.T = T; e.F = F; e.d = d; e.saved = (const unsigned char*)g.saved; e.dpre = dpre; e.tickets = (uint32_t*)ws; e.ntickets = (int)ntickets;
+  switch (tile_for(T, F)) {
+    case 256: launch_dgate<T256>(ps, st, e, g.act); break;
+    case 128: launch_dgate<T128>(ps, st, e, g.act); break;
+    default: launch_dgate<T64>(ps, st, e, g.act); break;
+  }
+  SplitArgs s{};
+  s.count = 3; s.tickets = (uint32_t*)ws; s.part = (float*)((char*)dpre + up256((size_t)T * 2 * F * 2));
+  s.p[0].A = Operand{dpre, 2 * F, T}; s.p[0].B = Operand{(const bf16_t*)g.w_in, d, d};
+  s.p[0].M = T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[0].C = g.dx; s.p[0].ldc = (uint32_t)g.lddx;
+  s.p[1].A = Operand{dpre, 2 * F, 2 * F}; s.p[1].B = Operand{(const bf16_t*)g.x, (uint32_t)g.ldx, d};
+  s.p[1].M = 2 * F; s.p[1].N = d; s.p[1].K = T; s.p[1].C = g.dw_in; s.p[1].ldc = d; s.p[1].strided_a = 1; s.p[1].c32 = g.dw_fp32;
+  s.p[2].A = Operand{(const bf16_t*)g.dy, (uint32_t)g.lddy, d}; s.p[2].B = Operand{(const bf16_t*)g.hidden, F, F};
+  s.p[2].M = d; s.p[2].N = F; s.p[2].K = T; s.p[2].C = g.dw_out; s.p[2].ldc = F; s.p[2].strided_a = 1; s.p[2].c32 = g.dw_fp32;
+  const int64_t all = most_tiles(T, d) + most_tiles(2 * F, d) + most_tiles(d, F);
+  switch (g_force_tile != 0 ? g_force_tile : all >= 16 * 100 ? 256 : all >= 4 * 60 ? 128 : 64) {
+    case 256: launch_split<T256, 1>(ps, st, s); break;
+    case 128: launch_split<T128, 1>(ps, st, s); break;
+    default: launch_split<T64, 1>(ps, st, s); break;
+  }
+}
+
+}  // namespace sama

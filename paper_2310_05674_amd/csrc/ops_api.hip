@@ -1,4 +1,5 @@
 // Op-level C entry points (include/sama_ops.h): thin argument checks around the kernel launchers.
+#include <algorithm>
 #include <cmath>
 #include <math.h>
 #include <mutex>
@@ -59,6 +60,18 @@ const char* check_embedding(const int32_t* ids, int64_t n, int32_t V, int32_t d,
   if (pad_id < -1) return "pad_id must be -1 (none) or an id";
   return nullptr;
 }
+// what the feed-forward calls have in common
+const char* check_glu(int64_t T, int32_t d, int32_t F, int32_t dtype) {
+  if (!is_dtype(dtype)) return "dtype must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16";
+  if (T < 0 || T > ((int64_t)1 << 22)) return "T must be 0 to 2^22";
+  if (d < 1 || F < 1 || (int64_t)d * F >= ((int64_t)1 << 29)) return "d and F must be positive and d F below 2^29";
+  if (dtype == SAMA_DTYPE_BF16 && (d % 8 != 0 || F % 8 != 0)) return "d and F must be multiples of 8 in bf16";
+  return nullptr;
+}
+bool is_glu_rows(const void* p, int64_t ld, int32_t d, int32_t dtype) {
+  return p != nullptr && ld >= d && ld <= ((int64_t)1 << 21) && (dtype == SAMA_DTYPE_BF16 ? ((uintptr_t)p & 15) == 0 && ld % 8 == 0 : ((uintptr_t)p & 3) == 0);
+}
+bool is_glu_dense(const void* p, int32_t dtype) { return p != nullptr && ((uintptr_t)p & (dtype == SAMA_DTYPE_BF16 ? 15 : 3)) == 0; }
 }  // namespace
 
 extern "C" {
@@ -282,5 +295,75 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
   launch_grad_clip((hipStream_t)hip_stream, list.data(), count, max_norm, norm_out, out, status, workspace);
   return launched(op);
 }
+
+size_t sama_op_glu_ffn_bytes(int64_t T, int32_t d, int32_t F, int32_t dtype) {
+  if (check_glu(T, d, F, dtype) != nullptr) return 0;
+  return std::max<size_t>(256, dtype == SAMA_DTYPE_BF16 ? glu_ffn_bytes(T, d, F) : glu_ffn_f32_bytes(T, d, F));
+}
+size_t sama_op_glu_ffn_saved_bytes(int64_t T, int32_t F, int32_t dtype) {
+  if (check_glu(T, 8, F, dtype) != nullptr) return 0;
+  return std::max<size_t>(256, dtype == SAMA_DTYPE_BF16 ? glu_ffn_saved_bytes(T, F) : glu_ffn_f32_saved_bytes(T, F));
+}
+size_t sama_op_glu_ffn_grad_bytes(int64_t T, int32_t d, int32_t F, int32_t dtype) {
+  if (check_glu(T, d, F, dtype) != nullptr) return 0;
+  return std::max<size_t>(256, dtype == SAMA_DTYPE_BF16 ? glu_ffn_grad_bytes(T, d, F) : glu_ffn_f32_grad_bytes(T, d, F));
+}
+
+sama_status sama_op_glu_ffn(const void* x, int64_t ldx, const void* w_in, const void* w_out, int64_t T, int32_t d, int32_t F, int32_t act, int32_t dtype,
+                            void* y, int64_t ldy, void* hidden, void* saved, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  static const char* const op = "sama_op_glu_ffn";
+  g_ops_error.clear();
+  if (const char* e = check_glu(T, d, F, dtype)) return refuse(op, e);
+  if (act != SAMA_ACT_SILU && act != SAMA_ACT_GELU) return refuse(op, "act must be SAMA_ACT_SILU or SAMA_ACT_GELU");
+  if (T == 0) return SAMA_OK;
+  if (!is_glu_rows(x, ldx, d, dtype) || !is_glu_rows(y, ldy, d, dtype)) return refuse(op, "x or y is null or misaligned, or its stride is too small, too large or (bf16) no multiple of 8");
+  if (!is_glu_dense(w_in, dtype) || !is_glu_dense(w_out, dtype) || !is_glu_dense(hidden, dtype)) return refuse(op, "a weight or hidden is null or misaligned");
+  if (((uintptr_t)saved & 15) != 0) return refuse(op, "saved must be 16-byte aligned");
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < sama_op_glu_ffn_bytes(T, d, F, dtype)) {
+    (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_glu_ffn_bytes()");
+    return SAMA_EWORKSPACE;
+  }
+  GluFfnArgs a{};
+  a.x = x; a.ldx = ldx; a.w_in = w_in; a.w_out = w_out; a.T = T; a.d = d; a.F = F; a.act = act; a.y = y; a.ldy = ldy; a.hidden = hidden; a.saved = saved;
+  (void)hipGetLastError();
+  if (dtype == SAMA_DTYPE_BF16) launch_glu_ffn((hipStream_t)hip_stream, a, workspace);
+  else launch_glu_ffn_f32((hipStream_t)hip_stream, a, workspace);
+  return launched(op);
+}
+
+sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_in, const void* w_out, const void* hidden,
+                                 const void* saved, int64_t T, int32_t d, int32_t F, int32_t act, int32_t dtype, void* dx, int64_t lddx, void* dw_in,
+                                 void* dw_out, int32_t dw_dtype, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  static const char* const op = "sama_op_glu_ffn_grad";
+  g_ops_error.clear();
+  if (const char* e = check_glu(T, d, F, dtype)) return refuse(op, e);
+  if (act != SAMA_ACT_SILU && act != SAMA_ACT_GELU) return refuse(op, "act must be SAMA_ACT_SILU or SAMA_ACT_GELU");
+  if (dw_dtype != dtype && dw_dtype != SAMA_DTYPE_FP32) return refuse(op, "dw_dtype must be dtype or SAMA_DTYPE_FP32");
+  if (!is_glu_dense(dw_in, dtype) || !is_glu_dense(dw_out, dtype)) return refuse(op, "a weight's gradient is null or misaligned");
+  if (T > 0) {
+    if (!is_glu_rows(x, ldx, d, dtype) || !is_glu_rows(dy, lddy, d, dtype) || !is_glu_rows(dx, lddx, d, dtype))
+      return refuse(op, "x, dy or dx is null or misaligned, or its stride is too small, too large or (bf16) no multiple of 8");
+    if (!is_glu_dense(w_in, dtype) || !is_glu_dense(w_out, dtype) || !is_glu_dense(hidden, dtype)) return refuse(op, "a weight or hidden is null or misaligned");
+    if (saved == nullptr || ((uintptr_t)saved & 15) != 0) return refuse(op, "saved must be what the forward call wrote, 16-byte aligned");
+  }
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < sama_op_glu_ffn_grad_bytes(T, d, F, dtype)) {
+    (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_glu_ffn_grad_bytes()");
+    return SAMA_EWORKSPACE;
+  }
+  (void)hipGetLastError();
+  if (T == 0) {
+    const int64_t words = dw_dtype == SAMA_DTYPE_FP32 ? (int64_t)d * F : (int64_t)d * F / 2;   // bf16: d F is even
+    launch_fill_f32((hipStream_t)hip_stream, (float*)dw_in, 0.f, 2 * words);
+    launch_fill_f32((hipStream_t)hip_stream, (float*)dw_out, 0.f, words);
+    return launched(op);
+  }
+  GluFfnGradArgs a{};
+  a.dy = dy; a.lddy = lddy; a.x = x; a.ldx = ldx; a.w_in = w_in; a.w_out = w_out; a.hidden = hidden; a.saved = saved; a.T = T; a.d = d; a.F = F; a.act = act;
+  a.dx = dx; a.lddx = lddx; a.dw_in = dw_in; a.dw_out = dw_out; a.dw_fp32 = dw_dtype == SAMA_DTYPE_FP32;
+  if (dtype == SAMA_DTYPE_BF16) launch_glu_ffn_grad((hipStream_t)hip_stream, a, workspace);
+  else launch_glu_ffn_grad_f32((hipStream_t)hip_stream, a, workspace);
+  return launched(op);
+}
+void sama_dev_glu_tile(int32_t tile) { glu_ffn_force_tile(tile); }
 
 }  // extern "C"

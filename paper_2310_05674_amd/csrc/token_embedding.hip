@@ -453,8 +453,10 @@ GradPlan plan_grad(int64_t n, int V, int d, int vec) {
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
   g.order = take((size_t)n * 4); g.sorted = take((size_t)n * 4); g.start = take(((size_t)V + 1) * 4);
-  g.tickets = take((size_t)g.chunks * g.slices * 4);
-  g.part = take((size_t)g.chunks * 2 * g.slices * 64 * vec * 4);
+  // room for the most chunks that n or fewer tokens may be cut into (sum_rows)
+  const int64_t most = std::max((n + SUM_WAVES * 16 - 1) / (SUM_WAVES * 16), std::min<int64_t>((n + SUM_WAVES - 1) / SUM_WAVES, 512 / g.slices + 2));
+  g.tickets = take((size_t)most * g.slices * 4);
+  g.part = take((size_t)most * 2 * g.slices * 64 * vec * 4);
   g.bytes = at;
   return g;
 }

@@ -29,4 +29,28 @@ size_t grad_clip_bytes();
 // norm[0] = ||g||, norm[1] = the factor; out: flat fp32, or null (in place); status may be null
 void launch_grad_clip(hipStream_t, const GradTensor* g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace);
 
+// The gated feed-forward block (bf16: glu_ffn.hip, fp32: glu_ffn_f32.hip), shapes as in include/sama_ops.h.
+enum { GLU_SILU = 0, GLU_GELU = 1 };
+struct GluFfnArgs {
+  const void* x; int64_t ldx; const void *w_in, *w_out;
+  int64_t T; int d, F, act;
+  void* y; int64_t ldy; void *hidden, *saved;
+};
+struct GluFfnGradArgs {
+  const void* dy; int64_t lddy; const void* x; int64_t ldx; const void *w_in, *w_out, *hidden, *saved;
+  int64_t T; int d, F, act;
+  void* dx; int64_t lddx; void *dw_in, *dw_out; bool dw_fp32;
+};
+size_t glu_ffn_saved_bytes(int64_t T, int F);
+size_t glu_ffn_bytes(int64_t T, int d, int F);
+size_t glu_ffn_grad_bytes(int64_t T, int d, int F);
+void launch_glu_ffn(hipStream_t, const GluFfnArgs&, void* workspace);
+void launch_glu_ffn_grad(hipStream_t, const GluFfnGradArgs&, void* workspace);
+size_t glu_ffn_f32_saved_bytes(int64_t T, int F);
+size_t glu_ffn_f32_bytes(int64_t T, int d, int F);
+size_t glu_ffn_f32_grad_bytes(int64_t T, int d, int F);
+void launch_glu_ffn_f32(hipStream_t, const GluFfnArgs&, void* workspace);
+void launch_glu_ffn_grad_f32(hipStream_t, const GluFfnGradArgs&, void* workspace);
+void glu_ffn_force_tile(int tile);   // tuning hook: 0 = heuristic
+
 }  // namespace sama

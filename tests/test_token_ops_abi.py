@@ -48,7 +48,8 @@ def test_embedding_gradient_refusals(lib):
     assert lib.sama_op_embedding_grad(*dict(good, n=0, acc=1, dy=None, ids=None).values()) == 0
     for bad in ((-1, 10, 64), (2 ** 30 + 1, 10, 64), (3, 0, 64), (3, 10, 0)):
         assert lib.sama_op_embedding_grad_bytes(*bad) == 0
-    # what suffices for many tokens suffices for the tables of a small model; sizes stay far from overflow
+    sizes = [lib.sama_op_embedding_grad_bytes(n, 5000, 768) for n in list(range(0, 9000, 37)) + [20000, 65536, 10 ** 6]]
+    assert sizes == sorted(sizes)                     # what suffices for many tokens suffices for fewer
     assert lib.sama_op_embedding_grad_bytes(2 ** 30, 2 ** 31 - 1, 1024) > 2 ** 33
 
 
@@ -67,3 +68,32 @@ def test_clipping_refusals(lib):
     for bad in (dict(ws=None), dict(ws=P + 64), dict(wb=lib.sama_op_grad_clip_bytes() - 1)):
         rc, text = call(**bad)
         assert rc == 3 and text.startswith("sama_op_grad_clip: "), (bad, rc, text)
+
+
+def test_feed_forward_refusals(lib):
+    T, d, F = 5, 64, 72
+    for dtype in (BF16, F32):
+        size, saved = lib.sama_op_glu_ffn_bytes(T, d, F, dtype), lib.sama_op_glu_ffn_saved_bytes(T, F, dtype)
+        assert size > 0 and saved > 0
+        good = dict(x=P, ldx=64, wi=P, wo=P, T=T, d=d, F=F, act=0, dtype=dtype, y=P, ldy=64, hidden=P, saved=None, ws=P, wb=size, st=None)
+        bad = [dict(T=-1), dict(T=2 ** 22 + 1), dict(d=0), dict(F=-8), dict(d=2 ** 15, F=2 ** 14), dict(act=2), dict(act=-1), dict(dtype=2), dict(x=None), dict(y=None),
+               dict(wi=None), dict(wo=None), dict(hidden=None), dict(ldx=63), dict(ldy=56), dict(ldx=2 ** 22), dict(x=P + 1), dict(saved=P + 4)]
+        if dtype == BF16:
+            bad += [dict(d=60), dict(F=70), dict(ldx=68), dict(ldy=66), dict(x=P + 8), dict(wi=P + 8), dict(wo=P + 4), dict(hidden=P + 2), dict(y=P + 8)]
+        refused(lib, "sama_op_glu_ffn", good, bad)
+        refused(lib, "sama_op_glu_ffn", good, [dict(ws=None), dict(ws=P + 16), dict(wb=size - 1)], code=3)
+        assert lib.sama_op_glu_ffn(*dict(good, T=0, x=None, y=None, hidden=None).values()) == 0
+        size = lib.sama_op_glu_ffn_grad_bytes(T, d, F, dtype)
+        good = dict(dy=P, lddy=64, x=P, ldx=64, wi=P, wo=P, hidden=P, saved=P, T=T, d=d, F=F, act=1, dtype=dtype, dx=P, lddx=64, dwi=P, dwo=P, dwt=dtype, ws=P, wb=size,
+                    st=None)
+        bad = [dict(T=-1), dict(d=-64), dict(act=9), dict(dtype=-1), dict(dy=None), dict(x=None), dict(dx=None), dict(wi=None), dict(wo=None), dict(hidden=None), dict(saved=None),
+               dict(saved=P + 8), dict(dwi=None), dict(dwo=None), dict(lddy=10), dict(lddx=63), dict(dwt=3), dict(dwt=-1)]
+        bad += [dict(dwt=BF16)] if dtype == F32 else [dict(dx=P + 8), dict(lddy=68), dict(dwi=P + 8), dict(F=4)]
+        refused(lib, "sama_op_glu_ffn_grad", good, bad)
+        refused(lib, "sama_op_glu_ffn_grad", good, [dict(ws=None), dict(ws=P + 16), dict(wb=size - 1)], code=3)
+    for f in (lib.sama_op_glu_ffn_bytes, lib.sama_op_glu_ffn_grad_bytes):
+        assert f(-1, 64, 72, BF16) == f(5, 60, 72, BF16) == f(5, 64, 72, 2) == f(5, 2 ** 15, 2 ** 14, F32) == 0
+        for dtype in (BF16, F32):
+            sizes = [f(T, 520, 1368, dtype) for T in list(range(0, 3000, 23)) + [8192, 65536, 2 ** 22]]
+            assert sizes == sorted(sizes)             # what suffices for many tokens suffices for fewer
+            assert f(2 ** 22, 4096, 16384, dtype) > 0
