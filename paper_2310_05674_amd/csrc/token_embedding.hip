@@ -4,15 +4,18 @@
 //
 // The gradient sorts the tokens by id, which gives every id's rows one after the other in ascending i, and sums each run in a fixed
 // order in 32 bits: the same bits from call to call, without an atomic on a sum.  Two launches.
-//   k_token_sort   A workgroup owns a range of ids (V / 512 of them or so) and looks through all tokens twice, 16 waves a section of
-//                  them each: it counts its ids and those below its range, turns the counts into places, and puts its tokens there, a
-//                  wave 64 at a time in order (ranks among equal ids by ballots).  No workgroup waits for another.  The rows of the
-//                  gradient without a token are zeroed here, while others still sort: for a vocabulary of 30522 and 4096 tokens that
-//                  is most of all bytes.
-//   k_token_sum    16 waves of `P` sorted rows each and a slice of the columns.  Runs inside a wave go out directly, runs over waves
+//   k_token_sort   A workgroup owns every 256th id and looks through all tokens, 16 waves a section of them each: it counts its ids and
+//                  those of the workgroups before it, turns the counts into places, and puts its tokens there, a wave 64 at a time in order
+//                  (ranks among equal ids by ballots).  Every 256th and not 256th parts of the table: the low ids are the frequent ones of
+//                  most vocabularies, and one workgroup had half of the tokens.  No workgroup waits for another.
+//                  Beside each a second one zeroes a share of the gradient: for a vocabulary of 30522 and 4096 tokens that is most of all
+//                  bytes, and sorting hides behind it.  Zeroing only the rows that stay so, in the launch behind this one, moves a fifth
+//                  less and takes longer.
+//   k_token_sum    8 waves of `P` sorted rows each and a slice of the columns.  Runs inside a wave go out directly, runs over waves
 //                  are joined through LDS, runs over workgroups through partial sums that the last of them to finish adds in order.
 //                  A fixed number of rows to a workgroup and not of ids: texts have one token in ten the same, and padding more.
 #include <algorithm>
+#include <type_traits>
 #include "kernels.h"
 #include "token_ops.h"
 
@@ -68,6 +71,38 @@ __device__ __forceinline__ void put(float* p, const float (&f)[8]) {
 }
 __device__ __forceinline__ void put(bf16_t* p, const float (&f)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+// What passes through the caches once: rows of dy, each read by one workgroup, and the rows that are summed, which go out among the zeroed rows still on their
+// way.  us for 65521 tokens of 1024 into 50304 rows, 4096 of 768 into 30522: kept 88.0, 27.2, these stores 83.3, 25.5, the loads as well 78.0, 25.7,
+// the zeroing as well 77.0, 27.8.
+template <typename T, int VEC>
+__device__ __forceinline__ Values<T, VEC> load_once(const T* p) {
+  Values<T, VEC> v;
+  if constexpr (VEC * sizeof(T) == 16) {
+    typedef decltype(v.v) V;
+    v.v = __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p)));
+  } else {
+    v.load(p);
+  }
+  return v;
+}
+template <int VEC>
+__device__ __forceinline__ void put_once(bf16_t* p, const float (&f)[VEC]) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  if constexpr (VEC == 8) __builtin_nontemporal_store((u4){pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])}, reinterpret_cast<u4*>(p));
+  else if constexpr (VEC == 4) __builtin_nontemporal_store((u2){pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])}, reinterpret_cast<u2*>(p));
+  else put(p, f);
+}
+template <int VEC>
+__device__ __forceinline__ void put_once(float* p, const float (&f)[VEC]) {
+  if constexpr (VEC >= 4) {
+#pragma unroll
+    for (int k = 0; k < VEC; k += 4) __builtin_nontemporal_store((f32x4){f[k], f[k + 1], f[k + 2], f[k + 3]}, reinterpret_cast<f32x4*>(p + k));
+  } else {
+    put(p, f);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------- lookup
@@ -137,41 +172,174 @@ void launch_lookup(hipStream_t st, ProfScope& ps, const LookupArgs& a) {
 
 // ---------------------------------------------------------------------------------------------------- gradient: the sort
 constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, SORT_RANGE = 512;   // ids of a workgroup at most
-constexpr int SUM_WAVES = 16;
+constexpr int SUM_WAVES = 8;
+// The order of the ids: id mod 2^lg, then id / 2^lg, of which there are up to `range`.
+struct IdOrder {
+  int lg, range;
+  __host__ __device__ __forceinline__ int groups() const { return 1 << lg; }
+  __host__ __device__ __forceinline__ int64_t places() const { return (int64_t)groups() * range; }
+  __host__ __device__ __forceinline__ int64_t place(int id) const { return (int64_t)(id & (groups() - 1)) * range + (id >> lg); }
+};
+IdOrder order_of(int V) {
+  IdOrder o{8, 0};   // a workgroup to a CU
+  while (((V - 1) >> o.lg) + 1 > SORT_RANGE) ++o.lg;
+  o.range = ((V - 1) >> o.lg) + 1;
+  return o;
+}
 
 struct SortArgs {
-  const int32_t* ids; int n, V, pad, range;
-  int32_t *order, *sorted, *start;   // [n] token of each place, [n] its id, [V + 1] first place of each id
+  const int32_t* ids; int n, V, pad;
+  IdOrder o;
+  int32_t *order, *sorted, *start;   // [n] token of each place, [n] its id, [groups range + 1] first place of each id in the order of the ids
   uint32_t* tickets; int ntickets;
-  void* grad; int64_t ldg; int d, elem;   // rows to zero (null: none), bytes of a value
+  char* grad; int64_t row, ld, rows; int fills;   // bytes of a row of the gradient and from one to the next; workgroups that zero them
 };
 
+// Zeroes a share of the gradient's rows, all of them: which have no token is not known yet.
+__device__ __forceinline__ void zero_share(const SortArgs& a, int share) {
+  const int tid = threadIdx.x;
+  const bool dense = a.row == a.ld, wide = (((uintptr_t)a.grad | (uintptr_t)a.ld | (uintptr_t)a.row) & 15) == 0;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  if (dense && wide) {
+    const int64_t pieces = a.rows * (a.row / 16), each = (pieces + a.fills - 1) / a.fills;
+    const int64_t from = share * each, to = min(from + each, pieces);
+    for (int64_t i = from + tid; i < to; i += SORT_THREADS) *reinterpret_cast<f32x4*>(a.grad + i * 16) = zero;
+    return;
+  }
+  for (int64_t r = (int64_t)share * SORT_WAVES + (tid >> 6); r < a.rows; r += (int64_t)a.fills * SORT_WAVES) {
+    char* const row = a.grad + r * a.ld;
+    if (wide) {
+      for (int64_t b = (tid & 63) * 16; b < a.row; b += 1024) *reinterpret_cast<f32x4*>(row + b) = zero;
+    } else {
+      for (int64_t b = (tid & 63) * 2; b < a.row; b += 128) *reinterpret_cast<uint16_t*>(row + b) = 0;
+    }
+  }
+}
+
+// A wave's tokens are read once: those of the workgroup's ids go, in order, into a list in LDS of LIST places.  A wave that has more of them (of an id
+// that half a batch consists of) reads its tokens again instead.  Looking through the ids is bound by instructions, each of the 256 workgroups
+// looks at all of them: six vector instructions for 64, the rest is on masks in scalar registers.
+constexpr int LIST = 1024, GROUP = 256, LIST_BITS = 23;   // tokens a wave takes at a time, four neighbours a lane; bits of a token's number in its section
+static_assert(SORT_RANGE <= 1 << (32 - LIST_BITS), "the list has the id above them");
 __global__ __launch_bounds__(SORT_THREADS) void k_token_sort(SortArgs a) {
-  extern __shared__ int32_t place[];         // [waves][range]: counts, then the next place of each id for each wave's tokens
+  extern __shared__ __attribute__((aligned(16))) uint32_t s_list[];   // [waves][LIST]: token of the section, id
+  int32_t* const place = reinterpret_cast<int32_t*>(s_list + SORT_WAVES * LIST);   // [waves][range]: counts, then the next place of each id for each wave's tokens
   __shared__ int32_t s_wave[SORT_WAVES], s_below[SORT_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lo = blockIdx.x * a.range, range = min(a.range, a.V - lo);
-  for (int i = blockIdx.x * SORT_THREADS + tid; i < a.ntickets; i += gridDim.x * SORT_THREADS) a.tickets[i] = 0;
-  for (int i = tid; i < SORT_WAVES * range; i += SORT_THREADS) place[i] = 0;
-  __syncthreads();
-  const int section = ((a.n + SORT_WAVES - 1) / SORT_WAVES + 63) / 64 * 64;
-  const int first = min(wave * section, a.n), last = min(first + section, a.n);   // (wave * section <= n + 15 * 64)
+  if (blockIdx.x >= (uint32_t)a.o.groups()) return zero_share(a, blockIdx.x - a.o.groups());
+  const int own = blockIdx.x, range = a.o.range, mask = a.o.groups() - 1, lg = a.o.lg, most = a.V - 1, n = a.n;
+  const int pad = a.pad >= 0 ? a.pad : INT32_MIN;                  // (ids below zero are taken as -1: none is that)
+  for (int i = blockIdx.x * SORT_THREADS + tid; i < a.ntickets; i += a.o.groups() * SORT_THREADS) a.tickets[i] = 0;
   int32_t* const mine = place + wave * range;
-  // which of its range's ids a token has; `below`: it has a smaller one
-  auto of = [&](int id, bool& below) {
-    const bool real = a.pad < 0 || id != a.pad;
-    id = min(max(id, 0), a.V - 1) - lo;
-    below = real && id < 0;
-    return real && id >= 0 && id < range ? id : -1;
+  for (int i = lane; i < range; i += 64) mine[i] = 0;
+  // an odd number of KB: sections 16 KB apart would begin in one channel of the L2, and all workgroups read the same at the same time
+  const int section = (((n + SORT_WAVES - 1) / SORT_WAVES + GROUP - 1) / GROUP | 1) * GROUP;
+  const int first = (int)min((int64_t)wave * section, (int64_t)n), last = (int)min((int64_t)first + section, (int64_t)n);
+  const int bits = range > 1 ? 32 - __builtin_clz(range - 1) : 0;
+  auto clamped = [&](int id) { return min(max(id, 0), most); };
+  auto rank_in = [&](uint64_t lanes, int from) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, from)); };
+  // the lanes of `among` that have this lane's id: of the first few ids that there are one by one, then by a ballot for each bit
+  auto equals = [&](int id, uint64_t among) {
+    uint64_t same = 0, left = among;
+#pragma unroll 1
+    for (int k = 0; k < 4 && left != 0; ++k) {
+      const int v = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+      const uint64_t with = __ballot(id == v) & left;
+      if (id == v) same = with;
+      left &= ~with;
+    }
+    if (left == 0) return same;
+    uint64_t rest = left;
+    for (int k = 0; k < bits; ++k) {
+      const bool set = (id >> k) & 1;
+      const uint64_t with = __ballot(set);
+      rest &= set ? with : ~with;
+    }
+    return left >> lane & 1 ? rest : same;
   };
-  int below = 0;
-#pragma unroll 8
-  for (int i = first + lane; i < last; i += 64) {
-    bool b;
-    const int id = of(a.ids[i], b);
-    below += b ? 1 : 0;
-    if (id >= 0) atomicAdd(mine + id, 1);
+  typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));   // a load of 16 bytes wants no more than a word's alignment
+  const int room = section <= 1 << LIST_BITS ? LIST : 0;
+  int below = 0, listed = 0;                 // tokens of workgroups before this one, of this one: the same in every lane
+  auto look = [&](int i0, i4 now, auto whole) {
+    const int t[4] = {max(now[0], -1), max(now[1], -1), max(now[2], -1), max(now[3], -1)};
+    bool here[4];
+    uint64_t have[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int g = clamped(t[e]) & mask;
+      const bool counts = t[e] != pad && (decltype(whole)::value || i0 + 4 * lane + e < last);
+      here[e] = counts && g == own;
+      have[e] = __ballot(here[e]);
+      below += __popcll(__ballot(counts && g < own));
+    }
+    if ((have[0] | have[1] | have[2] | have[3]) == 0) return;
+    int at = listed;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) at = rank_in(have[e], at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (here[e]) {   // (a list that is too short is not used)
+        s_list[wave * LIST + min(at, LIST - 1)] = (uint32_t)(i0 - first + 4 * lane + e) | (uint32_t)(clamped(t[e]) >> lg) << LIST_BITS;
+        ++at;
+      }
+      listed += __popcll(have[e]);
+    }
+  };
+  constexpr int AHEAD = 4;
+  const int groups = (last - first) / GROUP;   // whole ones
+  const int32_t* const ids = a.ids + first + 4 * lane;
+  i4 next[AHEAD] = {};
+  auto fetch = [&](int g) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) if (g + u < groups) next[u] = *reinterpret_cast<const i4*>(ids + (int64_t)(g + u) * GROUP);
+  };
+  fetch(0);
+  for (int g = 0; g < groups; g += AHEAD) {
+    i4 now[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
+    fetch(g + AHEAD);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) if (g + u < groups) look(first + (g + u) * GROUP, now[u], std::true_type{});
   }
+  if (first + groups * GROUP < last) {
+    const int i = first + groups * GROUP + 4 * lane;
+    look(first + groups * GROUP, (i4){a.ids[min(i, n - 1)], a.ids[min(i + 1, n - 1)], a.ids[min(i + 2, n - 1)], a.ids[min(i + 3, n - 1)]}, std::false_type{});
+  }
+  // f(id or -1, token) for this wave's tokens of the workgroup's ids, 64 in order at a time
+  auto each = [&](auto f) {
+    if (listed <= room) {
+      for (int k0 = 0; k0 < listed; k0 += 64) {
+        const uint32_t v = s_list[wave * LIST + min(k0 + lane, LIST - 1)];
+        f(k0 + lane < listed ? (int)(v >> LIST_BITS) : -1, first + (int)(v & ((1u << LIST_BITS) - 1)));
+      }
+      return;
+    }
+    constexpr int DEEP = 8;
+    int32_t ahead[DEEP];
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int u = 0; u < DEEP; ++u) ahead[u] = a.ids[min(i0 + 64 * u + lane, n - 1)];
+    };
+    load(first);
+    for (int i0 = first; i0 < last; i0 += 64 * DEEP) {
+      int32_t ids[DEEP];
+#pragma unroll
+      for (int u = 0; u < DEEP; ++u) ids[u] = ahead[u];
+      if (i0 + 64 * DEEP < last) load(i0 + 64 * DEEP);
+#pragma unroll
+      for (int u = 0; u < DEEP; ++u) {
+        const int i = i0 + 64 * u + lane, id = clamped(ids[u]);
+        f(i < last && (id & mask) == own && max(ids[u], -1) != pad ? id >> lg : -1, i);
+      }
+    }
+  };
+  each([&](int id, int) {
+    uint64_t some = __ballot(id >= 0);
+    if (some == 0) return;
+    some = equals(id, some);
+    if (id >= 0 && rank_in(some, 0) == 0) mine[id] += __popcll(some);   // the first of each id: no two lanes at one place
+  });
   __syncthreads();
   // places: ids in order, of an id the waves in order
   int total = 0;
@@ -183,79 +351,42 @@ __global__ __launch_bounds__(SORT_THREADS) void k_token_sort(SortArgs a) {
     const int t = __shfl_up(upto, s, 64);
     if (lane >= s) upto += t;
   }
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) below += __shfl_xor(below, s, 64);
   if (lane == 63) s_wave[wave] = upto;
   if (lane == 0) s_below[wave] = below;
   __syncthreads();
   int at = upto - total;
   for (int w = 0; w < SORT_WAVES; ++w) at += s_below[w] + (w < wave ? s_wave[w] : 0);
   if (tid < range) {
-    a.start[lo + tid] = at;
-    if (lo + tid == a.V - 1) a.start[a.V] = at + total;
+    a.start[(int64_t)own * range + tid] = at;
+    if (own == mask && tid == range - 1) a.start[a.o.places()] = at + total;
     for (int w = 0; w < SORT_WAVES; ++w) {
       const int c = place[w * range + tid];
-      place[w * range + tid] = total > 0 ? at : -1;
+      place[w * range + tid] = at;
       at += c;
     }
   }
   __syncthreads();
-  // the rows nobody has: a wave a row, before it sorts, so that the stores drain meanwhile
-  if (a.grad != nullptr) {
-    const int64_t bytes = (int64_t)a.d * a.elem, ld = a.ldg * a.elem;
-    const bool wide = (((uintptr_t)a.grad | (uintptr_t)ld | (uintptr_t)bytes) & 15) == 0;
-    for (int r = wave; r < range; r += SORT_WAVES) {
-      if (mine[r] >= 0) continue;
-      char* const row = static_cast<char*>(a.grad) + (lo + r) * ld;
-      if (wide) {
-        for (int64_t b = lane * 16; b < bytes; b += 1024) *reinterpret_cast<uint4*>(row + b) = make_uint4(0, 0, 0, 0);
-      } else {
-        for (int64_t b = lane * 2; b < bytes; b += 128) *reinterpret_cast<uint16_t*>(row + b) = 0;
-      }
+  each([&](int id, int token) {   // (each wave reads and changes its own places)
+    uint64_t peers = __ballot(id >= 0);
+    if (peers == 0) return;
+    peers = equals(id, peers);
+    if (id >= 0) {
+      const int rank = rank_in(peers, 0), to = mine[id];
+      a.order[to + rank] = token;
+      a.sorted[to + rank] = (id << lg) + own;
+      if (rank == 0) mine[id] = to + __popcll(peers);
     }
-  }
-  // (each wave reads and changes its own places from here on)
-  const int bits = range > 1 ? 32 - __builtin_clz(range - 1) : 0;
-  constexpr int AHEAD = 4;   // groups of 64 tokens whose ids are loaded before the ones at hand are placed
-  int32_t next_ids[AHEAD];
-  auto fetch = [&](int i0) {
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) next_ids[u] = a.ids[min(i0 + 64 * u + lane, a.n - 1)];
-  };
-  if (first < last) fetch(first);
-  for (int i0 = first; i0 < last; i0 += 64 * AHEAD) {
-    int32_t ids[AHEAD];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) ids[u] = next_ids[u];
-    if (i0 + 64 * AHEAD < last) fetch(i0 + 64 * AHEAD);
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int i = i0 + 64 * u + lane;
-      bool b;
-      const int id = i < last ? of(ids[u], b) : -1;
-      uint64_t peers = __ballot(id >= 0);
-      if (peers == 0) continue;
-      for (int k = 0; k < bits; ++k) {
-        const bool set = (id >> k) & 1;
-        const uint64_t with = __ballot(set);
-        peers &= set ? with : ~with;
-      }
-      if (id >= 0) {
-        const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(peers >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)peers, 0)), next = mine[id];
-        a.order[next + rank] = i;
-        a.sorted[next + rank] = lo + id;
-        if (rank == 0) mine[id] = next + __popcll(peers);
-      }
-    }
-  }
+  });
 }
 
 // ---------------------------------------------------------------------------------------------------- gradient: the sums
 struct SumArgs {
   const void* dy; int64_t ldy;
-  const int32_t *order, *sorted, *start; int V, d;
+  const int32_t *order, *sorted, *start; int n, d;
+  IdOrder o;
   float scale; int accumulate;
   void* grad; int64_t ldg;
+  int slices;                       // of the columns
   float* part; uint32_t* tickets;   // [chunks][head, tail][d rounded up to whole slices]; [chunks][slices]
 };
 __device__ __forceinline__ void publish_pair(float* p, float x, float y) {
@@ -285,11 +416,18 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   __shared__ float s_head[SUM_WAVES][SLICE];   // a wave's part of a run that began before it
   __shared__ int s_last[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int chunk = blockIdx.x, slice = blockIdx.y, slices = gridDim.y;
-  const int m = a.start[a.V], c0 = chunk * CHUNK;                   // tokens that count
+  const int slices = a.slices, chunk = blockIdx.x / slices, slice = blockIdx.x - chunk * slices;
+  // what is read first does not wait for the number of tokens that count (what lies behind them is not used)
+  const int c0 = chunk * CHUNK, q = c0 + wave * P;
+  const int my_id = a.sorted[min(q + lane, a.n - 1)], my_row = a.order[min(q + lane, a.n - 1)];
+  const int around = a.sorted[lane == 0 ? max(min(q, a.n) - 1, 0) : min(q + P, a.n - 1)], head_id = a.sorted[c0];
+  const int m = a.start[a.o.places()];
   if (c0 >= m) return;
   const int c1 = min(c0 + CHUNK, m);
-  const int q0 = min(c0 + wave * P, c1), nq = min(P, c1 - q0);
+  const int q0 = min(q, c1), nq = min(P, c1 - q0);
+  const int last_id = a.sorted[c1 - 1];
+  const int *const head_at = a.start + a.o.place(head_id), *const tail_at = a.start + a.o.place(last_id);
+  const int head_from = head_at[0], head_to = head_at[1], tail_from = tail_at[0], tail_to = tail_at[1];
   const int col = slice * SLICE + lane * VEC;
   const bool have = col < a.d;                                      // (d is a multiple of VEC)
   const TI* const dy = static_cast<const TI*>(a.dy) + (have ? col : 0);
@@ -317,7 +455,7 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
         for (int k = 0; k < VEC; ++k) f[k] += o[k];
       }
     }
-    put(p, f);
+    put_once(p, f);
   };
   auto head_out = [&](const float (&s)[VEC]) {
 #pragma unroll
@@ -333,16 +471,14 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   bool own_run = false;      // the run at the wave's end began here and goes on behind it
   int tail_id = -1;
   if (nq > 0) {
-    const int my = min(q0 + lane, c1 - 1);
-    const int my_id = a.sorted[my], my_row = a.order[my];
-    const int before = q0 > 0 ? a.sorted[q0 - 1] : -1, behind = q0 + nq < m ? a.sorted[q0 + nq] : -1;
+    const int before = q0 > 0 ? __builtin_amdgcn_readlane(around, 0) : -1, behind = q0 + nq < m ? __builtin_amdgcn_readlane(around, 1) : -1;
     constexpr int B = P < 8 ? P : 8;
     int run = before;
     bool began = false;
     for (int j0 = 0; j0 < nq; j0 += B) {
       Values<TI, VEC> v[B];
 #pragma unroll
-      for (int j = 0; j < B; ++j) v[j].load(dy + (int64_t)__builtin_amdgcn_readlane(my_row, min(j0 + j, nq - 1)) * a.ldy);
+      for (int j = 0; j < B; ++j) v[j] = load_once<TI, VEC>(dy + (int64_t)__builtin_amdgcn_readlane(my_row, min(j0 + j, nq - 1)) * a.ldy);
 #pragma unroll
       for (int j = 0; j < B; ++j) {
         if (j0 + j >= nq) break;
@@ -372,10 +508,7 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   // ---- runs over waves; those over workgroups leave their part
   const int64_t width = (int64_t)slices * SLICE;
   float* const parts = a.part + slice * SLICE + lane * VEC;   // of chunk c: + (2 c + which) width
-  const int head_id = a.sorted[c0], last_id = a.sorted[c1 - 1];
-  const int head_from = a.start[head_id], head_to = a.start[head_id + 1];
   const bool head_over = head_from < c0;                                   // the first run began in an earlier workgroup
-  const int tail_from = a.start[last_id], tail_to = a.start[last_id + 1];
   const bool tail_over = tail_to > c1 && tail_from >= c0;                  // the last one begins here and goes on
   auto upto_wave = [&](int to) { return (min(to, c1) - 1 - c0) / P; };     // the wave of a run's last row here
   if (wave == 0 && head_over) {
@@ -384,7 +517,7 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
     publish_values<VEC>(parts + (2 * (int64_t)chunk) * width, s);
   }
   if (own_run) {
-    const int to = a.start[tail_id + 1];
+    const int to = a.start[a.o.place(tail_id) + 1];
     for (int w = wave + 1; w <= upto_wave(to); ++w) head_add(w, acc);
     if (to > c1) publish_values<VEC>(parts + (2 * (int64_t)chunk + 1) * width, acc);
     else finish(tail_id, acc);
@@ -435,10 +568,10 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   }
 }
 
-// Sorted rows of a wave: the most of 16 to 1 that leave the chip 256 workgroups.
+// Sorted rows of a wave: the most of 16 to 1 that leave the chip 512 workgroups.
 int sum_rows(int64_t n, int slices) {
   int p = 16;
-  while (p > 1 && (n + SUM_WAVES * p - 1) / (SUM_WAVES * p) * slices < 256) p /= 2;
+  while (p > 1 && (n + SUM_WAVES * p - 1) / (SUM_WAVES * p) * slices < 512) p /= 2;
   return p;
 }
 // What a call needs for the widest slices, and for the narrowest: pointers and strides that a call comes with decide between them.
@@ -452,9 +585,9 @@ GradPlan plan_grad(int64_t n, int V, int d, int vec) {
   g.chunks = (n + SUM_WAVES * g.P - 1) / (SUM_WAVES * g.P);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-  g.order = take((size_t)n * 4); g.sorted = take((size_t)n * 4); g.start = take(((size_t)V + 1) * 4);
+  g.order = take((size_t)n * 4); g.sorted = take((size_t)n * 4); g.start = take(((size_t)order_of(V).places() + 1) * 4);
   // room for the most chunks that n or fewer tokens may be cut into (sum_rows)
-  const int64_t most = std::max((n + SUM_WAVES * 16 - 1) / (SUM_WAVES * 16), std::min<int64_t>((n + SUM_WAVES - 1) / SUM_WAVES, 512 / g.slices + 2));
+  const int64_t most = std::max((n + SUM_WAVES * 16 - 1) / (SUM_WAVES * 16), std::min<int64_t>((n + SUM_WAVES - 1) / SUM_WAVES, 1024 / g.slices + 2));
   g.tickets = take((size_t)most * g.slices * 4);
   g.part = take((size_t)most * 2 * g.slices * 64 * vec * 4);
   g.bytes = at;
@@ -463,7 +596,7 @@ GradPlan plan_grad(int64_t n, int V, int d, int vec) {
 
 template <typename TI, typename TO, int VEC>
 void launch_sum(hipStream_t st, ProfScope& ps, const SumArgs& s, const GradPlan& g) {
-  const dim3 grid((uint32_t)g.chunks, g.slices);
+  const uint32_t grid = (uint32_t)(g.chunks * g.slices);
   switch (g.P) {
     case 16: return launch_kernel(ps, k_token_sum<TI, TO, VEC, 16>, grid, SUM_WAVES * 64, 0, st, s);
     case 8: return launch_kernel(ps, k_token_sum<TI, TO, VEC, 8>, grid, SUM_WAVES * 64, 0, st, s);
@@ -503,15 +636,21 @@ void launch_embedding_grad(hipStream_t st, const EmbeddingGradArgs& e, void* wor
   ProfScope ps(st, F_OTHER, 0.0);
   SortArgs s{};
   s.ids = e.ids; s.n = (int)e.n; s.V = e.V; s.pad = e.pad;
-  // two workgroups to a CU, which sort and zero by turns
-  s.range = std::min(SORT_RANGE, std::max(1, (e.V + 511) / 512));
+  s.o = order_of(e.V);
+  s.grad = (char*)e.grad; s.row = (int64_t)e.d * (e.grad_bf16 ? 2 : 4); s.ld = e.ldg * (e.grad_bf16 ? 2 : 4); s.rows = e.V;
+  s.fills = e.accumulate ? 0 : 256;
   s.order = (int32_t*)(ws + g.order); s.sorted = (int32_t*)(ws + g.sorted); s.start = (int32_t*)(ws + g.start);
   s.tickets = (uint32_t*)(ws + g.tickets); s.ntickets = (int)(g.chunks * g.slices);
-  s.grad = e.accumulate ? nullptr : e.grad; s.ldg = e.ldg; s.d = e.d; s.elem = e.grad_bf16 ? 2 : 4;
-  launch_kernel(ps, k_token_sort, (e.V + s.range - 1) / s.range, SORT_THREADS, SORT_WAVES * s.range * 4, st, s);
+  static bool configured = false;   // more than 64 KB of LDS with the largest ranges
+  if (!configured) {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_token_sort), hipFuncAttributeMaxDynamicSharedMemorySize, SORT_WAVES * (SORT_RANGE + LIST) * 4);
+    configured = true;
+  }
+  launch_kernel(ps, k_token_sort, s.o.groups() + s.fills, SORT_THREADS, SORT_WAVES * (s.o.range + LIST) * 4, st, s);
   if (e.n == 0) return;
   SumArgs a{};
-  a.dy = e.dy; a.ldy = e.ldy; a.order = s.order; a.sorted = s.sorted; a.start = s.start; a.V = e.V; a.d = e.d; a.scale = e.scale;
+  a.slices = g.slices;
+  a.dy = e.dy; a.ldy = e.ldy; a.order = s.order; a.sorted = s.sorted; a.start = s.start; a.n = s.n; a.o = s.o; a.d = e.d; a.scale = e.scale;
   a.accumulate = e.accumulate; a.grad = e.grad; a.ldg = e.ldg; a.part = (float*)(ws + g.part); a.tickets = s.tickets;
   auto go = [&](auto ti, auto to, auto wide) {
     typedef decltype(ti) TI;
