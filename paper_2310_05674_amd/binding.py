@@ -3,6 +3,7 @@ supplies device memory and the current HIP stream, every step runs in the librar
 fallback: without libsama.so (or without a GPU) construction fails."""
 import ctypes as C
 import os
+from array import array
 
 MODEL_MLP, MODEL_ENCODER = 0, 1
 DTYPE_FP32, DTYPE_BF16 = 0, 1
@@ -407,22 +408,45 @@ def op_nudge(theta, vdir, eps_t, theta16, n16):
 
 
 # ------------------------------------------------------------------------------------- operators of a token model's step
+# A call of the smallest sizes takes the GPU a few microseconds, and what the marshalling takes is added to them where calls do not queue up: types are
+# looked up in one table, the stream is asked for without making an object of it.
+_DTYPES = {}
+
+
+def _torch():
+    """torch, imported at the first call, and the table of types filled."""
+    import torch
+    if not _DTYPES:
+        _DTYPES.update({torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16})
+        _DTYPES["int32"] = torch.int32
+    return torch
+
+
 def _dtype(t):
     """SAMA_DTYPE_* of a tensor (-1, which the library refuses, for any other type)."""
-    import torch
-    return {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}.get(t.dtype, -1)
+    if not _DTYPES:
+        _torch()
+    return _DTYPES.get(t.dtype, -1)
+
+
+def _raw_stream():
+    """The current stream of the current device, as a number."""
+    c = _torch()._C
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def _rows(t, d, what):
     """A 2-D tensor on the GPU whose rows are d neighbouring values -> its row stride."""
-    if t.dim() != 2 or t.shape[1] != d or not t.is_cuda or (d > 1 and t.shape[0] > 0 and t.stride(1) != 1):
-        raise ValueError(f"{what}: expected a [n, {d}] CUDA tensor with contiguous rows, got {tuple(t.shape)}, strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(d, t.stride(0))
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == d and t.is_cuda:
+        ld, step = t.stride()
+        if step == 1 or d == 1 or shape[0] == 0:
+            return ld if shape[0] > 1 else max(d, ld)
+    raise ValueError(f"{what}: expected a [n, {d}] CUDA tensor with contiguous rows, got {tuple(shape)}, strides {t.stride()}")
 
 
 def _ids(ids, n):
-    import torch
-    if ids.dtype != torch.int32 or not ids.is_cuda or not ids.is_contiguous() or ids.numel() != n:
+    if ids.dtype is not _DTYPES["int32"] or not ids.is_cuda or ids.numel() != n or not ids.is_contiguous():
         raise ValueError(f"ids: expected {n} contiguous int32 values on the GPU")
 
 
@@ -435,9 +459,13 @@ def op_embedding(table, ids, out, *, scale=1.0, pad_id=-1):
     """out[i] = scale * table[ids[i]] through sama_op_embedding.  table [V, d] and out [n, d]: fp32 or bf16 CUDA tensors with contiguous rows; ids: n
     int32 values; rows of pad_id come out as zeros."""
     V, d = table.shape
-    _ids(ids, out.shape[0])
-    _op(load_library().sama_op_embedding(_p(table), _dtype(table), _rows(table, d, "table"), _p(ids), out.shape[0], V, d, scale, pad_id, _p(out),
-                                         _dtype(out), _rows(out, d, "out"), _stream()), "sama_op_embedding")
+    n = out.shape[0]
+    stream = _raw_stream()
+    _ids(ids, n)
+    rc = load_library().sama_op_embedding(table.data_ptr(), _dtype(table), _rows(table, d, "table"), ids.data_ptr(), n, V, d, scale, pad_id,
+                                          out.data_ptr(), _dtype(out), _rows(out, d, "out"), stream)
+    if rc != 0:
+        _op(rc, "sama_op_embedding")
 
 
 def embedding_grad_bytes(n, V, d):
@@ -448,10 +476,13 @@ def op_embedding_grad(dy, ids, grad, workspace, *, scale=1.0, pad_id=-1, accumul
     """grad[v] = scale * the sum of dy over the tokens with id v (added to grad with `accumulate`) through sama_op_embedding_grad.  dy [n, d], grad
     [V, d]: fp32 or bf16; workspace: uint8, embedding_grad_bytes(n, V, d)."""
     n, d = dy.shape
+    stream = _raw_stream()
     _ids(ids, n)
-    _op(load_library().sama_op_embedding_grad(_p(dy), _dtype(dy), _rows(dy, d, "dy"), _p(ids), n, grad.shape[0], d, scale, pad_id, int(accumulate),
-                                              _p(grad), _dtype(grad), _rows(grad, d, "grad"), _p(workspace), workspace.numel(), _stream()),
-        "sama_op_embedding_grad")
+    rc = load_library().sama_op_embedding_grad(dy.data_ptr(), _dtype(dy), _rows(dy, d, "dy"), ids.data_ptr(), n, grad.shape[0], d, scale, pad_id,
+                                               1 if accumulate else 0, grad.data_ptr(), _dtype(grad), _rows(grad, d, "grad"), workspace.data_ptr(),
+                                               workspace.numel(), stream)
+    if rc != 0:
+        _op(rc, "sama_op_embedding_grad")
 
 
 def grad_clip_bytes():
@@ -461,30 +492,33 @@ def grad_clip_bytes():
 def op_grad_clip(grads, max_norm, norm, workspace, *, out=None, status=None):
     """Clips a list of contiguous fp32 and bf16 CUDA tensors to a global norm through sama_op_grad_clip: in place, or into the flat fp32 tensor
     `out`.  norm: fp32 [2], receives the norm and the factor; status: int64 [1] or None; workspace: uint8, grad_clip_bytes()."""
-    import torch
+    torch = _torch()
     n = len(grads)
-    total = 0
+    # three passes over the list, each of one method, and flat arrays of machine words: a list of a hundred tensors takes the time of the kernels otherwise
+    pointers = array("Q", [g.data_ptr() for g in grads])
+    counts = array("q", [g.numel() for g in grads])
+    dtypes = array("i", [_DTYPES.get(g.dtype, -1) for g in grads])
     for g in grads:
-        if not (g.is_cuda and g.is_contiguous()):
+        if not (g.is_contiguous() and g.is_cuda):
             raise ValueError("grads: expected contiguous CUDA tensors")
-        total += g.numel()
     if norm.dtype != torch.float32 or norm.numel() < 2 or not norm.is_contiguous():
         raise ValueError("norm: expected two contiguous fp32 values")
-    if out is not None and (out.dtype != torch.float32 or out.numel() != total or not out.is_contiguous()):
-        raise ValueError(f"out: expected {total} contiguous fp32 values")
+    if out is not None and (out.dtype != torch.float32 or out.numel() != sum(counts) or not out.is_contiguous()):
+        raise ValueError(f"out: expected {sum(counts)} contiguous fp32 values")
     if status is not None and (status.dtype != torch.int64 or status.numel() < 1):
         raise ValueError("status: expected an int64 value")
-    _op(load_library().sama_op_grad_clip(n, (C.c_void_p * n)(*[g.data_ptr() for g in grads]), (C.c_int64 * n)(*[g.numel() for g in grads]),
-                                         (C.c_int32 * n)(*[_dtype(g) for g in grads]), max_norm, _p(out), _p(norm), _p(status), _p(workspace),
-                                         workspace.numel(), _stream()), "sama_op_grad_clip")
+    rc = load_library().sama_op_grad_clip(n, pointers.buffer_info()[0], counts.buffer_info()[0], dtypes.buffer_info()[0], max_norm, _p(out), _p(norm),
+                                          _p(status), _p(workspace), workspace.numel(), _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_grad_clip")
 
 
 ACT = dict(silu=0, gelu=1)
 
 
 def _glu_dtype(dtype):
-    import torch
-    return {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}.get(dtype, -1)
+    _torch()
+    return _DTYPES.get(dtype, -1)
 
 
 def glu_ffn_bytes(T, d, F, dtype):
@@ -500,7 +534,7 @@ def glu_ffn_grad_bytes(T, d, F, dtype):
 
 
 def _dense(t, shape, dtype, what):
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {shape} CUDA tensor of {dtype}, got {tuple(t.shape)}, {t.dtype}")
 
 
@@ -525,7 +559,7 @@ def op_glu_ffn(x, w_in, w_out, y, hidden, workspace, *, act="silu", saved=None):
     if saved is not None:
         _scratch(saved, glu_ffn_saved_bytes(T, F, t), "saved")
     _op(load_library().sama_op_glu_ffn(_p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), T, d, F, ACT[act], _glu_dtype(t), _p(y),
-                                       _glu_rows(y, T, d, t, "y"), _p(hidden), _p(saved), _p(workspace), workspace.numel(), _stream()), "sama_op_glu_ffn")
+                                       _glu_rows(y, T, d, t, "y"), _p(hidden), _p(saved), _p(workspace), workspace.numel(), _raw_stream()), "sama_op_glu_ffn")
 
 
 def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, workspace, *, act="silu"):
@@ -538,4 +572,4 @@ def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, worksp
     _scratch(saved, glu_ffn_saved_bytes(T, F, t), "saved")
     _op(load_library().sama_op_glu_ffn_grad(_p(dy), _glu_rows(dy, T, d, t, "dy"), _p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), _p(hidden),
                                             _p(saved), T, d, F, ACT[act], _glu_dtype(t), _p(dx), _glu_rows(dx, T, d, t, "dx"), _p(dw_in), _p(dw_out),
-                                            _glu_dtype(dw_in.dtype), _p(workspace), workspace.numel(), _stream()), "sama_op_glu_ffn_grad")
+                                            _glu_dtype(dw_in.dtype), _p(workspace), workspace.numel(), _raw_stream()), "sama_op_glu_ffn_grad")

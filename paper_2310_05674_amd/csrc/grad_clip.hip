@@ -5,9 +5,9 @@
 // arrive from memory, far fewer than its 64-bit units take), in a fixed order.
 //
 // The tensors' pointers and sizes travel in the kernel's arguments, up to TENSORS a launch: nothing is copied to the device first, so a call
-// may be captured.  A tensor is cut into units, a block takes every so many-th unit of all of them.  One launch of each kernel for
-// models of up to TENSORS tensors: the blocks of the second add the partial sums up for themselves instead of waiting for a last block.
-// The second kernel walks the units backwards: the end of the gradients is what the last-level cache still holds.
+// may be captured.  A tensor is cut into units of 32 KB, a block takes a run of them.  One launch of each kernel for
+// models of up to TENSORS tensors: the blocks of the second add the partial sums up for themselves instead of waiting for a last block, while
+// their first unit is on its way.  The second kernel walks the units backwards: the end of the gradients is what the last-level cache still holds.
 #include <algorithm>
 #include <cmath>
 #include "kernels.h"
@@ -17,7 +17,7 @@ namespace sama {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-constexpr int TENSORS = 112, UNIT = 8192, THREADS = 256, PARTIALS = 2048;
+constexpr int TENSORS = 112, THREADS = 256, PER = 8, UNIT_BYTES = THREADS * PER * 16, PARTIALS = 2048;
 
 struct ClipTable {
   int count, units;
@@ -33,6 +33,26 @@ struct ClipTable {
 };
 static_assert(sizeof(ClipTable) <= 4000, "kernel arguments");
 
+// A tensor's values before its first 16-byte boundary, fewer than eight, belong to its unit 0 beside that unit's 32 KB.
+struct Unit {
+  int k;             // tensor
+  int64_t n, at;     // values behind those, of them the unit begins with number `at`
+  const char* p;     // the tensor
+  int head, half;
+  __device__ __forceinline__ int size() const { return half ? 2 : 4; }
+  __device__ __forceinline__ int values() const { return UNIT_BYTES >> (half ? 1 : 2); }
+  __device__ __forceinline__ bool whole() const { return at + values() <= n; }
+};
+__device__ __forceinline__ Unit unit_at(const ClipTable& t, int k, int unit) {
+  Unit u;
+  u.k = k;
+  u.half = (t.bf16[k >> 5] >> (k & 31)) & 1;
+  u.p = static_cast<const char*>(t.p[k]);
+  u.head = (int)min((int64_t)((16 - ((uintptr_t)u.p & 15)) & 15) / u.size(), t.n[k]);
+  u.n = t.n[k] - u.head;
+  u.at = (int64_t)(unit - t.first[k]) * u.values();
+  return u;
+}
 // the tensor that a unit belongs to, found by a wave at once
 __device__ __forceinline__ int tensor_of(const ClipTable& t, int unit) {
   const int lane = threadIdx.x & 63;
@@ -41,36 +61,25 @@ __device__ __forceinline__ int tensor_of(const ClipTable& t, int unit) {
   for (int c = 0; c < TENSORS; c += 64) k += __popcll(__ballot(c + lane < t.count && t.first[min(c + lane, TENSORS)] <= unit));
   return __builtin_amdgcn_readfirstlane(k);
 }
-// values before the first 16-byte boundary
-__device__ __forceinline__ int ahead(const void* p, int size) { return (int)((16 - ((uintptr_t)p & 15)) & 15) / size; }
-
-template <typename T>
-__device__ __forceinline__ double square_sum(const T* p, int64_t n, int64_t at) {
-  constexpr int V = 16 / sizeof(T), PER = UNIT / THREADS / V;
-  auto sq = [](float x) { return (double)x * (double)x; };
-  auto val = [](T x) { if constexpr (sizeof(T) == 2) return bf16_to_f32(x); else return x; };
-  double s = 0.0;
-  const int head = (int)min((int64_t)ahead(p, sizeof(T)), n);
-  if (at == 0 && (int)threadIdx.x < head) s += sq(val(p[threadIdx.x]));
-  p += head; n -= head;
-  if (at + UNIT <= n) {
-    uint4 v[PER];
+// `halves`: a thread's eight bf16 values of a piece are two times four, 2 KB apart, so that the fp32 values they become are stored in whole lines
+__device__ __forceinline__ void load_whole(const Unit& u, bool halves, uint4 (&v)[PER]) {
+  const char* const p = u.p + ((u.head + u.at) << (u.half ? 1 : 2));
+  if (halves) {
 #pragma unroll
-    for (int u = 0; u < PER; ++u) v[u] = *reinterpret_cast<const uint4*>(p + at + (int64_t)(u * THREADS + threadIdx.x) * V);
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if constexpr (sizeof(T) == 4) s += sq(__uint_as_float(w[k]));
-        else s += sq(__uint_as_float(w[k] << 16)) + sq(__uint_as_float(w[k] & 0xffff0000u));
-      }
+    for (int i = 0; i < PER; ++i) {
+      const uint2 a = *reinterpret_cast<const uint2*>(p + (2 * i * THREADS + threadIdx.x) * 8), b = *reinterpret_cast<const uint2*>(p + ((2 * i + 1) * THREADS + threadIdx.x) * 8);
+      v[i] = make_uint4(a.x, a.y, b.x, b.y);
     }
-  } else {
-    for (int64_t i = at + threadIdx.x; i < n; i += THREADS) s += sq(val(p[i]));
+    return;
   }
-  return s;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = *reinterpret_cast<const uint4*>(p + (i * THREADS + threadIdx.x) * 16);
 }
+__device__ __forceinline__ float value_at(const Unit& u, int64_t i) {   // i: of the tensor
+  return u.half ? bf16_to_f32(reinterpret_cast<const bf16_t*>(u.p)[i]) : reinterpret_cast<const float*>(u.p)[i];
+}
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 __device__ __forceinline__ double block_sum64(double s, double* red) {
   s = wave_sum(s);
@@ -81,64 +90,97 @@ __device__ __forceinline__ double block_sum64(double s, double* red) {
   for (int w = 0; w < THREADS / 64; ++w) s += red[w];
   return s;
 }
+// a block's run of the units
+__device__ __forceinline__ void run_of(int units, int& from, int& to) {
+  from = (int)((int64_t)units * blockIdx.x / gridDim.x);
+  to = (int)((int64_t)units * (blockIdx.x + 1) / gridDim.x);
+}
 
 __global__ __launch_bounds__(THREADS) void k_square_sums(ClipTable t) {
   __shared__ double red[THREADS / 64];
-  double s = 0.0;
-  for (int unit = blockIdx.x; unit < t.units; unit += gridDim.x) {
-    const int k = tensor_of(t, unit);
-    const int64_t at = (int64_t)(unit - t.first[k]) * UNIT;
-    s += (t.bf16[k >> 5] >> (k & 31)) & 1 ? square_sum(static_cast<const bf16_t*>(t.p[k]), t.n[k], at)
-                                           : square_sum(static_cast<const float*>(t.p[k]), t.n[k], at);
+  double s[4] = {};
+  auto add = [&](int i, float x) { s[i & 3] += (double)x * (double)x; };
+  int from, to;
+  run_of(t.units, from, to);
+  if (from < to) {
+    int k = tensor_of(t, from);
+    for (int unit = from; unit < to; ++unit) {
+      while (unit >= t.first[k + 1]) ++k;
+      const Unit u = unit_at(t, k, unit);
+      if (u.at == 0 && (int)threadIdx.x < u.head) add(0, value_at(u, threadIdx.x));
+      if (u.whole()) {
+        uint4 v[PER];
+        load_whole(u, false, v);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (u.half) { add(e, low(w[e])); add(e + 2, high(w[e])); }
+            else add(e, __uint_as_float(w[e]));
+          }
+        }
+      } else {
+        for (int64_t i = u.at + threadIdx.x; i < u.n; i += THREADS) add(0, value_at(u, u.head + i));
+      }
+    }
   }
-  s = block_sum64(s, red);
-  if (threadIdx.x == 0) t.partial[blockIdx.x] = t.add ? t.partial[blockIdx.x] + s : s;
+  const double sum = block_sum64((s[0] + s[1]) + (s[2] + s[3]), red);
+  if (threadIdx.x == 0) t.partial[blockIdx.x] = t.add ? t.partial[blockIdx.x] + sum : sum;
 }
 
-template <typename T, typename O>
-__device__ __forceinline__ void scale_unit(const T* p, O* to, int64_t n, int64_t at, float f) {
-  constexpr int V = 16 / sizeof(T), PER = UNIT / THREADS / V;
+// Results go past the caches, which keep the gradients for the second reading instead, and the next norm does not wait for them to be written back.
+__device__ __forceinline__ void store_once(char* p, f32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(p)); }
+// One unit, whose values are in v if it is a whole one, times f to `dest` (the tensor's place): bf16 in place, else fp32.
+__device__ __forceinline__ void scale_unit(const Unit& u, const uint4 (&v)[PER], void* dest, bool to_bf16, float f) {
   auto one = [&](int64_t i) {
-    if constexpr (sizeof(T) == 4) to[i] = p[i] * f;
-    else if constexpr (sizeof(O) == 2) to[i] = f32_to_bf16(bf16_to_f32(p[i]) * f);
-    else to[i] = bf16_to_f32(p[i]) * f;
+    const float x = value_at(u, i) * f;
+    if (to_bf16) static_cast<bf16_t*>(dest)[i] = f32_to_bf16(x);
+    else static_cast<float*>(dest)[i] = x;
   };
-  const int head = (int)min((int64_t)ahead(p, sizeof(T)), n);
-  if (at == 0 && (int)threadIdx.x < head) one(threadIdx.x);
-  p += head; to += head; n -= head;
-  if (at + UNIT <= n && ((uintptr_t)to & 15) == 0) {
-    uint4 v[PER];
+  if (u.at == 0 && (int)threadIdx.x < u.head) one(threadIdx.x);
+  char* const at = static_cast<char*>(dest) + ((u.head + u.at) << (to_bf16 ? 1 : 2));
+  if (u.whole() && ((uintptr_t)at & 15) == 0) {
 #pragma unroll
-    for (int u = 0; u < PER; ++u) v[u] = *reinterpret_cast<const uint4*>(p + at + (int64_t)(u * THREADS + threadIdx.x) * V);
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      O* const o = to + at + (int64_t)(u * THREADS + threadIdx.x) * V;
-      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-      if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<f32x4*>(o) = (f32x4){__uint_as_float(w[0]) * f, __uint_as_float(w[1]) * f, __uint_as_float(w[2]) * f, __uint_as_float(w[3]) * f};
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+      const int piece = i * THREADS + threadIdx.x;
+      if (!u.half) {
+        store_once(at + piece * 16, (f32x4){__uint_as_float(w[0]) * f, __uint_as_float(w[1]) * f, __uint_as_float(w[2]) * f, __uint_as_float(w[3]) * f});
+      } else if (to_bf16) {
+        *reinterpret_cast<uint4*>(at + piece * 16) = make_uint4(pack_bf16x2(low(w[0]) * f, high(w[0]) * f), pack_bf16x2(low(w[1]) * f, high(w[1]) * f),
+                                                                pack_bf16x2(low(w[2]) * f, high(w[2]) * f), pack_bf16x2(low(w[3]) * f, high(w[3]) * f));
       } else {
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16) * f; x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u) * f; }
-        if constexpr (sizeof(O) == 2) {
-          *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-        } else {
-          *reinterpret_cast<f32x4*>(o) = (f32x4){x[0], x[1], x[2], x[3]};
-          *reinterpret_cast<f32x4*>(o + 4) = (f32x4){x[4], x[5], x[6], x[7]};
-        }
+        const int first = 2 * i * THREADS + threadIdx.x;
+        store_once(at + first * 16, (f32x4){low(w[0]) * f, high(w[0]) * f, low(w[1]) * f, high(w[1]) * f});
+        store_once(at + (first + THREADS) * 16, (f32x4){low(w[2]) * f, high(w[2]) * f, low(w[3]) * f, high(w[3]) * f});
       }
     }
   } else {
-    const int64_t end = min(at + UNIT, n);
-    for (int64_t i = at + threadIdx.x; i < end; i += THREADS) one(i);
+    const int64_t end = min(u.at + u.values(), u.n);
+    for (int64_t i = u.at + threadIdx.x; i < end; i += THREADS) one(u.head + i);
   }
 }
 
 __global__ __launch_bounds__(THREADS) void k_clip(ClipTable t) {
   __shared__ double red[THREADS / 64];
   double s = 0.0;
+  double part[PARTIALS / THREADS];
 #pragma unroll
-  for (int i = 0; i < PARTIALS; i += THREADS) s += i + (int)threadIdx.x < t.partials ? t.partial[i + threadIdx.x] : 0.0;
+  for (int i = 0; i < PARTIALS / THREADS; ++i) part[i] = i * THREADS + (int)threadIdx.x < t.partials ? t.partial[i * THREADS + threadIdx.x] : 0.0;
+  int from, to;
+  run_of(t.units, from, to);
+  { const int f = t.units - to; to = t.units - from; from = f; }
+  int k = 0;
+  Unit u{};
+  uint4 v[PER] = {};
+  if (from < to) {
+    k = tensor_of(t, to - 1);
+    u = unit_at(t, k, to - 1);
+    if (u.whole()) load_whole(u, t.out != nullptr && u.half, v);
+  }
+#pragma unroll
+  for (int i = 0; i < PARTIALS / THREADS; ++i) s += part[i];
   const double norm = sqrt(block_sum64(s, red));
   const bool finite = norm <= 1.7976931348623157e308;
   const float factor = finite ? (float)fmin(1.0, t.max_norm / (norm + 1e-6)) : 1.f;
@@ -147,17 +189,14 @@ __global__ __launch_bounds__(THREADS) void k_clip(ClipTable t) {
     if (t.status != nullptr) *t.status = finite ? 0 : 1;
   }
   if (t.out == nullptr && factor == 1.f) return;
-  for (int unit = t.units - 1 - (int)blockIdx.x; unit >= 0; unit -= gridDim.x) {
-    const int k = tensor_of(t, unit);
-    const int64_t at = (int64_t)(unit - t.first[k]) * UNIT;
-    const bool half = (t.bf16[k >> 5] >> (k & 31)) & 1;
-    if (t.out != nullptr) {
-      if (half) scale_unit(static_cast<const bf16_t*>(t.p[k]), t.out + t.to[k], t.n[k], at, factor);
-      else scale_unit(static_cast<const float*>(t.p[k]), t.out + t.to[k], t.n[k], at, factor);
-    } else {
-      if (half) scale_unit(static_cast<const bf16_t*>(t.p[k]), static_cast<bf16_t*>(t.p[k]), t.n[k], at, factor);
-      else scale_unit(static_cast<const float*>(t.p[k]), static_cast<float*>(t.p[k]), t.n[k], at, factor);
+  for (int unit = to - 1; unit >= from; --unit) {
+    if (unit < to - 1) {
+      while (unit < t.first[k]) --k;
+      u = unit_at(t, k, unit);
+      if (u.whole()) load_whole(u, t.out != nullptr && u.half, v);
     }
+    if (t.out != nullptr) scale_unit(u, v, t.out + t.to[k], false, factor);
+    else scale_unit(u, v, t.p[k], u.half != 0, factor);
   }
 }
 }  // namespace
@@ -171,7 +210,7 @@ void launch_grad_clip(hipStream_t st, const GradTensor* g, int64_t count, double
     for (uint32_t& w : t.bf16) w = 0;
     for (; k < count && t.count < TENSORS; ++k) {
       if (g[k].n == 0) continue;
-      const int64_t units = (g[k].n + UNIT - 1) / UNIT;
+      const int64_t each = g[k].bf16 ? UNIT_BYTES / 2 : UNIT_BYTES / 4, units = (g[k].n + each - 1) / each;
       if (t.count > 0 && t.units + units > (1 << 30)) break;
       t.p[t.count] = g[k].p; t.n[t.count] = g[k].n; t.to[t.count] = flat; t.first[t.count] = t.units;
       if (g[k].bf16) t.bf16[t.count >> 5] |= 1u << (t.count & 31);
@@ -181,10 +220,11 @@ void launch_grad_clip(hipStream_t st, const GradTensor* g, int64_t count, double
   };
   ClipTable t{};
   int most = 0;
-  for (int64_t k = 0, flat = 0; k < count;) { next(k, flat, t); most = std::max(most, t.units); }
+  int64_t total = 0;
+  for (int64_t k = 0, flat = 0; k < count;) { next(k, flat, t); most = std::max(most, t.units); total = flat; }
   const int blocks = std::max(1, std::min(most, PARTIALS));
   t.max_norm = max_norm; t.partial = static_cast<double*>(workspace); t.partials = blocks; t.out = out;
-  ProfScope ps(st, F_OTHER, 0.0);
+  ProfScope ps(st, F_OTHER, 12.0 * total);
   int64_t k = 0, flat = 0;
   t.add = 0;
   do {
