@@ -568,6 +568,172 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_split(SplitArgs a) {
   } while (a.split && at < end);
 }
 
+// ---------------------------------------------------------------------------------------------------- a few tokens
+// With up to 16 NT tokens reading the weights is the work, 6 d F bytes, and a product over slabs in LDS is mostly waiting: loads, barrier, loads.  Here a wave
+// takes 16 rows of weights and a share of the contraction, in the operand layout straight from memory (lane r + 16 q: eight values of row r), AHEAD
+// steps of 32 at once, so that nearly all of a workgroup's weights are asked for before the first arrives; the tokens are the other operand, and
+// come from the caches.  The waves' shares meet in LDS, in order.  What it measures stands at launch_glu_ffn().
+template <int NA, int NT>
+__device__ __forceinline__ void contract_few(f32x4 (&acc)[NA][NT], const bf16_t* w, uint64_t next_w, const bf16_t* x, uint32_t ldx, uint32_t T, uint32_t K, uint32_t step0,
+                                             uint32_t step1) {
+  const int lane = threadIdx.x & 63, q = lane >> 4;
+  constexpr int AHEAD = NA * NT == 1 ? 8 : 4;
+#pragma unroll
+  for (int n = 0; n < NA; ++n)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  const bf16_t* xr[NT];   // (tokens that are not there: the last one's results again, which nobody stores)
+#pragma unroll
+  for (int t = 0; t < NT; ++t) xr[t] = x + (uint64_t)min(16 * t + (lane & 15), T - 1) * ldx;
+  for (uint32_t s0 = step0; s0 < step1; s0 += AHEAD) {
+    bf16x8 a[AHEAD][NA], b[AHEAD][NT];
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const uint32_t k = min(32 * min(s0 + s, step1 - 1) + 8 * q, K - 8);   // K is a multiple of 8
+#pragma unroll
+      for (int n = 0; n < NA; ++n) a[s][n] = *reinterpret_cast<const bf16x8*>(w + n * next_w + k);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) b[s][t] = *reinterpret_cast<const bf16x8*>(xr[t] + k);
+    }
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      if (s0 + s >= step1) break;
+      if (32 * (s0 + s) + 8 * q >= K) {                                     // behind the end: zeros on both sides
+#pragma unroll
+        for (int n = 0; n < NA; ++n) a[s][n] = bf16x8{};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) b[s][t] = bf16x8{};
+      }
+#pragma unroll
+      for (int n = 0; n < NA; ++n)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][n], b[s][t], acc[n][t], 0, 0, 0);
+    }
+  }
+}
+__device__ __forceinline__ uint32_t share_of(uint32_t steps, uint32_t share, uint32_t of) { return steps * share / of; }
+
+// h (and what the backward pass wants) of 16 hidden values: a wave an eighth of the contraction
+template <int NT, int ACT>
+__global__ __launch_bounds__(512) void k_glu_up_few(UpArgs a) {
+  __shared__ f32x4 part[8][2][NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t f0 = blockIdx.x * 16, steps = (a.d + 31) / 32;
+  f32x4 acc[2][NT];
+  const bf16_t* const w = a.w.p + (uint64_t)min(f0 + (lane & 15), a.F - 1) * a.d;
+  contract_few<2, NT>(acc, w, (uint64_t)a.F * a.d, a.x.p, a.x.ld, a.T, a.d, share_of(steps, wave, 8), share_of(steps, wave + 1, 8));
+#pragma unroll
+  for (int t = 0; t < NT; ++t) { part[wave][0][t][lane] = acc[0][t]; part[wave][1][t][lane] = acc[1][t]; }
+  __syncthreads();
+  if (wave >= NT || 16 * wave >= (int)a.T) return;
+  const int t = wave;
+  f32x4 g = part[0][0][t][lane], u = part[0][1][t][lane], h;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) { g += part[k][0][t][lane]; u += part[k][1][t][lane]; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = gate<ACT>(g[e]) * u[e];
+  if (a.saved != nullptr) {
+    unsigned char* const b = a.saved + ((uint64_t)t * ((a.F + 15) / 16) + blockIdx.x) * SAVED_BLOCK;
+    uint32_t wg[3], wu[3];
+    pack24(g, wg); pack24(u, wu);
+    *reinterpret_cast<uint4*>(b + lane * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
+    *reinterpret_cast<uint2*>(b + 1024 + lane * 8) = make_uint2(wu[1], wu[2]);
+  }
+  const uint32_t row = 16 * t + (lane & 15), col = f0 + 4 * (lane >> 4);
+  if (row < a.T && col < a.F) *reinterpret_cast<uint2*>(a.h + (uint64_t)row * a.F + col) = packed(h);
+}
+
+struct DownFewArgs { const bf16_t *h, *w; uint32_t T, F, d; bf16_t* y; uint32_t ldy; };
+constexpr int DOWN_WAVES = 16;
+template <int NT>
+__global__ __launch_bounds__(DOWN_WAVES * 64) void k_glu_down_few(DownFewArgs a) {
+  __shared__ f32x4 part[DOWN_WAVES][NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t r0 = blockIdx.x * 16, steps = (a.F + 31) / 32;
+  f32x4 acc[1][NT];
+  contract_few<1, NT>(acc, a.w + (uint64_t)min(r0 + (lane & 15), a.d - 1) * a.F, 0, a.h, a.F, a.T, a.F, share_of(steps, wave, DOWN_WAVES), share_of(steps, wave + 1, DOWN_WAVES));
+#pragma unroll
+  for (int t = 0; t < NT; ++t) part[wave][t][lane] = acc[0][t];
+  __syncthreads();
+  if (wave >= NT || 16 * wave >= (int)a.T) return;
+  f32x4 s = part[0][wave][lane];
+  for (int k = 1; k < DOWN_WAVES; ++k) s += part[k][wave][lane];
+  const uint32_t row = 16 * wave + (lane & 15), col = r0 + 4 * (lane >> 4);
+  if (row < a.T && col < a.d) *reinterpret_cast<uint2*>(a.y + (uint64_t)row * a.ldy + col) = packed(s);
+}
+
+// Up to four tokens: four rows of weights to a workgroup, 256 bytes of each a load (in the 4 x 4 x 4 product of sixteen blocks a block is the next
+// eight values of the contraction), so that four times as many workgroups ask for weights.  Lane 4 b + i: row, and token, i of block b.  One token, us: 1024 x 4096
+// 5.2 + 4.1 (25 MB: 2.7 TB/s with the launches, of which there is nothing to hide them behind), 16 rows at a time 5.6 + 7.3; 2048 x 5504 10.5 + 5.4 (68 MB:
+// 4.3 TB/s), 14.1 + 10.8.
+__device__ __forceinline__ f32x4 contract_rows(const bf16_t* w, const bf16_t* x, uint32_t K, uint32_t step0, uint32_t step1) {
+  const uint32_t b = (threadIdx.x & 63) >> 2;
+  constexpr int AHEAD = 4;
+  union Piece { bf16x8 v; s16x4 h[2]; };
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (uint32_t s0 = step0; s0 < step1; s0 += AHEAD) {
+    Piece p[AHEAD], t[AHEAD];
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const uint32_t k = min(128 * min(s0 + s, step1 - 1) + 8 * b, K - 8);
+      p[s].v = *reinterpret_cast<const bf16x8*>(w + k);
+      t[s].v = *reinterpret_cast<const bf16x8*>(x + k);
+    }
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      if (s0 + s >= step1) break;
+      if (128 * (s0 + s) + 8 * b >= K) { p[s].v = bf16x8{}; t[s].v = bf16x8{}; }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) acc = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(p[s].h[e], t[s].h[e], acc, 0, 0, 0);
+    }
+  }
+  const auto add = [](float x, float y) { return x + y; };
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {   // over the blocks: lanes 32, 16, 8 and 4 apart
+    acc[e] = join16(join32(acc[e], add), add);
+    acc[e] += rot16<8>(acc[e]);
+    acc[e] += rot16<4>(acc[e]);
+  }
+  return acc;                     // in every block's lane j: the four rows' products with token j
+}
+template <int ACT>
+__global__ __launch_bounds__(256) void k_glu_up_rows(UpArgs a) {
+  __shared__ f32x4 part[4][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 3;
+  const uint32_t f0 = blockIdx.x * 4, steps = (a.d + 127) / 128;
+  const f32x4 acc = contract_rows(a.w.p + (uint64_t)(f0 + i + (wave & 1) * a.F) * a.d, a.x.p + (uint64_t)min((uint32_t)i, a.T - 1) * a.x.ld, a.d,
+                                  share_of(steps, wave >> 1, 2), share_of(steps, (wave >> 1) + 1, 2));
+  if (lane < 4) part[wave][lane] = acc;
+  __syncthreads();
+  if (threadIdx.x >= a.T) return;
+  const f32x4 g = part[0][i] + part[2][i], u = part[1][i] + part[3][i];
+  f32x4 h;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = gate<ACT>(g[e]) * u[e];
+  if (a.saved != nullptr) {
+    unsigned char* const b = a.saved + (uint64_t)(f0 >> 4) * SAVED_BLOCK;
+    const int at = 16 * ((f0 >> 2) & 3) + i;      // the lane of a fragment that has these four columns
+    uint32_t wg[3], wu[3];
+    pack24(g, wg); pack24(u, wu);
+    *reinterpret_cast<uint4*>(b + at * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
+    *reinterpret_cast<uint2*>(b + 1024 + at * 8) = make_uint2(wu[1], wu[2]);
+  }
+  *reinterpret_cast<uint2*>(a.h + (uint64_t)i * a.F + f0) = packed(h);
+}
+__global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
+  __shared__ f32x4 part[8][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 3;
+  const uint32_t r0 = blockIdx.x * 4, steps = (a.F + 127) / 128;
+  const f32x4 acc = contract_rows(a.w + (uint64_t)(r0 + i) * a.F, a.h + (uint64_t)min((uint32_t)i, a.T - 1) * a.F, a.F, share_of(steps, wave, 8), share_of(steps, wave + 1, 8));
+  if (lane < 4) part[wave][lane] = acc;
+  __syncthreads();
+  if (threadIdx.x >= a.T) return;
+  f32x4 s = part[0][i];
+#pragma unroll
+  for (int k = 1; k < 8; ++k) s += part[k][i];
+  *reinterpret_cast<uint2*>(a.y + (uint64_t)i * a.ldy + r0) = packed(s);
+}
+
 // ---------------------------------------------------------------------------------------------------- launches
 typedef Tile<256, 256, 2, 4, 2, 0, 2, 0, 1> T256;
 typedef Tile<128, 128, 2, 4, 4, 4, 0, 1, 1> T128;
@@ -586,6 +752,18 @@ TileOrder order_of(uint32_t M, uint32_t N, uint32_t bm, uint32_t bn) {
   TileOrder o{};
   o.tm = (M + bm - 1) / bm; o.tn = (N + bn - 1) / bn; o.tiles = o.tm * o.tn; o.per_xcd = (o.tiles + 7) / 8;
   return o;
+}
+template <int NT>
+void launch_few(ProfScope& ps, hipStream_t st, const UpArgs& u, const DownFewArgs& w, int act) {
+  const uint32_t up = (u.F + 15) / 16, down = (w.d + 15) / 16;
+  if (act == GLU_GELU) launch_kernel(ps, k_glu_up_few<NT, GLU_GELU>, up, 512, 0, st, u);
+  else launch_kernel(ps, k_glu_up_few<NT, GLU_SILU>, up, 512, 0, st, u);
+  launch_kernel(ps, k_glu_down_few<NT>, down, DOWN_WAVES * 64, 0, st, w);
+}
+void launch_rows(ProfScope& ps, hipStream_t st, const UpArgs& u, const DownFewArgs& w, int act) {
+  if (act == GLU_GELU) launch_kernel(ps, k_glu_up_rows<GLU_GELU>, u.F / 4, 256, 0, st, u);
+  else launch_kernel(ps, k_glu_up_rows<GLU_SILU>, u.F / 4, 256, 0, st, u);
+  launch_kernel(ps, k_glu_down_rows, w.d / 4, 512, 0, st, w);
 }
 template <typename T>
 void launch_up(ProfScope& ps, hipStream_t st, UpArgs a, int act) {
@@ -668,6 +846,15 @@ void launch_glu_ffn(hipStream_t st, const GluFfnArgs& g, void* workspace) {
   UpArgs u{};
   u.x = Operand{(const bf16_t*)g.x, (uint32_t)g.ldx, T}; u.w = Operand{(const bf16_t*)g.w_in, d, F};
   u.T = T; u.F = F; u.d = d; u.h = (bf16_t*)g.hidden; u.saved = (unsigned char*)g.saved;
+  // Few tokens without tiles.  us a call, this way / by tiles: 512 x 1368 1 token 10.2 / 13.7, 16 11.4 / 14.0, 32 12.2 / 14.3, 48 14.7 / 14.5; 1024 x 4096 1
+  // 9.5 / 19.5, 5 13.1 / 19.6, 16 15.4 / 19.7, 32 20.1 / 20.2, 48 25.6 / 20.2; 2048 x 5504 1 15.0 / 27.2, 4 19.6 / 27.3, 5 27.7 / 27.3, 16 33.5 / 27.6.
+  if (g_force_tile == 0 && (T <= 4 || (T <= 32 && (uint64_t)d * F <= (1u << 22)))) {
+    const DownFewArgs w{(const bf16_t*)g.hidden, (const bf16_t*)g.w_out, T, F, d, (bf16_t*)g.y, (uint32_t)g.ldy};
+    if (T <= 4) launch_rows(ps, st, u, w, g.act);
+    else if (T <= 16) launch_few<1>(ps, st, u, w, g.act);
+    else launch_few<2>(ps, st, u, w, g.act);
+    return;
+  }
   u.tickets = (uint32_t*)ws; u.ntickets = (int)ntickets;
   switch (tile_for(T, 2 * (int64_t)F)) {
     case 256: launch_up<T256>(ps, st, u, g.act); break;
