@@ -1,4 +1,4 @@
-// The gated feed-forward block in bf16 on the matrix cores, with fp32 accumulation: for T tokens of width d and F hidden values
+// The gated feed-forward block on the matrix cores, in bf16 with fp32 accumulation or in fp32: for T tokens of width d and F hidden values
 //   g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wo^T                                        (W_in = [Wg; Wu] [2F x d], Wo [d x F])
 //   dh = dy Wo, dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu, dW_in = [dg; du]^T x, dWo = dy^T h.
 // 6 T d F operations forward and 12 backward in four launches:
@@ -23,9 +23,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
-constexpr int LDS_MAX = 160 * 1024, BK = 64;
+constexpr int LDS_MAX = 160 * 1024;
+// Elements E: bf16_t or float.  A slab is 128 bytes of the contraction, 64 or 32 indices, two k-steps of 64 bytes; a lane's operand of a k-step is 16 bytes,
+// for one 16x16x32 product in bf16 or four of 16x16x4 in fp32.
+constexpr int SLAB = 128;
+template <typename E> constexpr uint32_t DEPTH = SLAB / sizeof(E);
 
-// BM x BN outputs of a workgroup, by WGM x WGN multiplying waves; NSTAGE slabs of 64 contraction indices in LDS; PW waves that only load (0: the
+// BM x BN outputs of a workgroup, by WGM x WGN multiplying waves; NSTAGE slabs of the contraction in LDS; PW waves that only load (0: the
 // multiplying ones do); YP: fragments of B per piece of a k-step (0: all); RD: reads of a piece lie among the first 1 / RD of the products of the piece
 // before it (0: ahead of its own products).
 template <int BM_, int BN_, int WGM_, int WGN_, int NSTAGE_, int PW_, int YP_, int RD_, int PER_CU_>
@@ -34,7 +38,7 @@ struct Tile {
   static constexpr int WAVES = WGM * WGN, LW = PW > 0 ? PW : WAVES, THREADS = (WAVES + PW) * 64;
   static constexpr int WM = BM / WGM, WN = BN / WGN, XT = WM / 16, YT = WN / 16;
   static constexpr int YP = YP_ > 0 ? YP_ : YT, NP = YT / YP;
-  static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int A_BYTES = BM * SLAB, B_BYTES = BN * SLAB, STAGE_BYTES = A_BYTES + B_BYTES;
   static constexpr int NLA = A_BYTES / 1024 / LW, NLB = B_BYTES / 1024 / LW, NL = NLA + NLB;
   static constexpr int LDS_BYTES = NSTAGE * STAGE_BYTES;
   static_assert(LDS_BYTES * PER_CU <= LDS_MAX && WM % 16 == 0 && WN % 32 == 0 && YT % YP == 0, "tile");
@@ -46,40 +50,45 @@ __device__ __forceinline__ void static_for_each(std::integer_sequence<int, I...>
 template <int N, typename F>
 __device__ __forceinline__ void static_for(F f) { static_for_each(std::make_integer_sequence<int, N>{}, f); }
 
-// An operand: KC, storage [rows][k] with the contraction index contiguous, staged in LDS [row][64], or KS, storage [k][rows], staged [64][rows] and fetched with
-// the transposing read.  Swizzles as in gemm_bf16.hip: of KC the 16-byte pieces of a row by (row / 2) % 8, of KS the 32-byte pieces of a k-row
-// by a function of k, so that the lanes of a fetch fill all banks.
+// An operand: KC, storage [rows][k] with the contraction index contiguous, staged in LDS [row][slab], or KS, storage [k][rows], staged [slab][rows] and fetched with
+// the transposing read (bf16) or a word at a time (fp32).  Swizzles as in gemm_bf16.hip: of KC the 16-byte pieces of a row by (row / 2) % 8, of KS
+// pieces of 16 rows of a k-row by a function of k, so that the lanes of a fetch fill all banks.
 // PAIRS (KC): the rows of a tile are sixteen of the first half of the matrix, the same sixteen of the second half, and so on.
 enum { KC, KS, PAIRS };
-template <int R>
+template <typename E, int R>
 __device__ __forceinline__ int chunk_swizzle(int kr) {
   constexpr int NC = R / 16;
   static_assert(NC % 8 == 0 || NC == 4, "tile width");
-  return NC % 8 == 0 ? (kr & 3) | ((kr >> 1) & 4) : ((kr >> 1) & 1) | ((kr >> 2) & 2);
+  if constexpr (sizeof(E) == 4) return (kr >> 2) & 3;   // the four k-rows that a fetch of a word reads, four apart
+  else return NC % 8 == 0 ? (kr & 3) | ((kr >> 1) & 4) : ((kr >> 1) & 1) | ((kr >> 2) & 2);
 }
 struct Operand {
-  const bf16_t* p; uint32_t ld, rows;   // rows: of the matrix (KC) or its columns (KS); PAIRS: of a half
+  const void* p; uint32_t ld, rows;   // rows: of the matrix (KC) or its columns (KS); PAIRS: of a half
 };
 // Byte offset, from the slab's first element, of the 16 bytes that belong at byte `at` of its stage, and their contraction index.
-template <int S, int R>
+template <typename E, int S, int R>
 __device__ __forceinline__ uint32_t piece_offset(uint32_t at, const Operand& o, uint32_t& k) {
+  constexpr uint32_t Z = sizeof(E);
   if constexpr (S == KS) {
-    constexpr uint32_t RB = R * 2;
-    const uint32_t kr = at / RB, q = at % RB / 16, ql = (((q >> 1) ^ (uint32_t)chunk_swizzle<R>((int)kr)) << 1) | (q & 1);
+    constexpr uint32_t RB = R * Z, PP = Z;   // pieces of 16 bytes in 16 rows
+    const uint32_t kr = at / RB, q = at % RB / 16, ql = ((q / PP) ^ (uint32_t)chunk_swizzle<E, R>((int)kr)) * PP + q % PP;
     k = kr;
-    return kr * o.ld * 2 + ql * 16;
+    return kr * o.ld * Z + ql * 16;
   } else {
-    const uint32_t r = at / 128, c = at % 128 / 16 ^ (r / 2) % 8;
-    k = c * 8;
+    const uint32_t r = at / SLAB, c = at % SLAB / 16 ^ (r / 2) % 8;
+    k = c * (16 / Z);
     const uint32_t row = S == KC ? r : (r / 32) * 16 + r % 16 + ((r / 16) & 1) * o.rows;
-    return row * o.ld * 2 + c * 16;
+    return row * o.ld * Z + c * 16;
   }
 }
-template <int S, int R>
+template <typename E, int S, int R>
 __device__ __forceinline__ int fetch_lane_offset(int lane, int ks_or_frag) {
-  if constexpr (S == KS) {
+  if constexpr (S == KS && sizeof(E) == 4) {
+    const int kr = 4 * (lane >> 4);                             // and the three behind it; the same swizzle for kr + 16
+    return kr * R * 4 + ((ks_or_frag ^ chunk_swizzle<E, R>(kr)) * 64) + 4 * (lane & 15);
+  } else if constexpr (S == KS) {
     const int j = lane & 15, kr = 8 * (lane >> 4) + (j >> 2);   // the swizzle is the same for kr + 4 and kr + 32
-    return kr * R * 2 + ((ks_or_frag ^ chunk_swizzle<R>(kr)) * 32) + 8 * (j & 3);
+    return kr * R * 2 + ((ks_or_frag ^ chunk_swizzle<E, R>(kr)) * 32) + 8 * (j & 3);
   } else {
     const int r = lane & 15;
     return r * 128 + (((4 * ks_or_frag + (lane >> 4)) ^ (r / 2) % 8) * 16);
@@ -97,13 +106,13 @@ struct Window {
   }
   __device__ __forceinline__ void step(uint32_t bytes) { at += bytes; left -= bytes; }
 };
-template <int S>
+template <typename E, int S>
 __device__ __forceinline__ Window window(const Operand& o, uint32_t row0, uint32_t k0, uint32_t K) {
   Window w;
   const uint64_t first = S == KS ? (uint64_t)k0 * o.ld + row0 : (uint64_t)row0 * o.ld + k0;
   const uint64_t end = S == KS ? (uint64_t)(K - 1) * o.ld + o.rows : (uint64_t)((S == PAIRS ? 2 : 1) * o.rows - 1) * o.ld + K;
-  w.at = (uint64_t)(uintptr_t)o.p + 2 * first;
-  w.left = 2 * (end - first);
+  w.at = (uint64_t)(uintptr_t)o.p + sizeof(E) * first;
+  w.left = sizeof(E) * (end - first);
   return w;
 }
 
@@ -120,7 +129,7 @@ __device__ __forceinline__ void wait_loads(int younger) {
 // acc = the products of rows i0.. of A and j0.. of B over slabs [slab0, slab0 + slabs) of the contraction K.  D = B-fragment x A-fragment: a lane has
 // four neighbouring columns 4 (lane / 16) .. + 3 of row lane % 16 of each 16 x 16 fragment.  Every wave of the workgroup calls it; those that only load
 // come back without results.  No wave may read or write the stages any more when it is called.
-template <typename T, int SA, int SB>
+template <typename T, typename E, int SA, int SB>
 __device__ __forceinline__ void contract(f32x4 (&acc)[T::XT][T::YT], unsigned char* smem, const Operand& A, const Operand& B, uint32_t i0, uint32_t j0,
                                          uint32_t K, uint32_t slab0, int slabs) {
   constexpr int XT = T::XT, YT = T::YT, NSTAGE = T::NSTAGE;
@@ -131,7 +140,8 @@ __device__ __forceinline__ void contract(f32x4 (&acc)[T::XT][T::YT], unsigned ch
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)smem;
   uint32_t offA[T::NLA], offB[T::NLB], ragged = 0;      // ragged: loads of a KC operand that are behind the contraction's end in its last slab
   Window wa{}, wb{};
-  const uint32_t stepA = SA == KS ? BK * A.ld * 2 : BK * 2, stepB = SB == KS ? BK * B.ld * 2 : BK * 2;
+  constexpr uint32_t BK = DEPTH<E>;
+  const uint32_t stepA = SA == KS ? SLAB * A.ld : SLAB, stepB = SB == KS ? SLAB * B.ld : SLAB;
   const bool to_end = K % BK != 0 && slab0 + slabs == (K + BK - 1) / BK;
   int next = 0;
   uint32_t next_at = lds0 + lw * 1024;
@@ -161,12 +171,12 @@ __device__ __forceinline__ void contract(f32x4 (&acc)[T::XT][T::YT], unsigned ch
     if (loader) issue();
   };
   if (loader) {
-    wa = window<SA>(A, i0, slab0 * BK, K); wb = window<SB>(B, j0, slab0 * BK, K);
+    wa = window<E, SA>(A, i0, slab0 * BK, K); wb = window<E, SB>(B, j0, slab0 * BK, K);
     const uint32_t last_k = (K - 1) % BK;
 #pragma unroll
-    for (int q = 0; q < T::NLA; ++q) { uint32_t k; offA[q] = piece_offset<SA, T::BM>((q * T::LW + lw) * 1024 + lane * 16, A, k); if (k > last_k) ragged |= 1u << q; }
+    for (int q = 0; q < T::NLA; ++q) { uint32_t k; offA[q] = piece_offset<E, SA, T::BM>((q * T::LW + lw) * 1024 + lane * 16, A, k); if (k > last_k) ragged |= 1u << q; }
 #pragma unroll
-    for (int q = 0; q < T::NLB; ++q) { uint32_t k; offB[q] = piece_offset<SB, T::BN>((q * T::LW + lw) * 1024 + lane * 16, B, k); if (k > last_k) ragged |= 1u << (T::NLA + q); }
+    for (int q = 0; q < T::NLB; ++q) { uint32_t k; offB[q] = piece_offset<E, SB, T::BN>((q * T::LW + lw) * 1024 + lane * 16, B, k); if (k > last_k) ragged |= 1u << (T::NLA + q); }
 #pragma unroll
     for (int s = 0; s < NSTAGE - 1; ++s) issue();
   }
@@ -180,40 +190,51 @@ __device__ __forceinline__ void contract(f32x4 (&acc)[T::XT][T::YT], unsigned ch
   for (int x = 0; x < XT; ++x)
 #pragma unroll
     for (int y = 0; y < YT; ++y) acc[x][y] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  constexpr int STEPS = BK / 32;
+  constexpr int STEPS = 2;
   int fa[SA == KS ? XT : STEPS], fb[SB == KS ? YT : STEPS];
   if (SA != KS) {
 #pragma unroll
-    for (int ks = 0; ks < STEPS; ++ks) fa[ks] = fetch_lane_offset<SA, T::BM>(lane, ks) + wr * 128;
+    for (int ks = 0; ks < STEPS; ++ks) fa[ks] = fetch_lane_offset<E, SA, T::BM>(lane, ks) + wr * SLAB;
   } else {
 #pragma unroll
-    for (int x = 0; x < XT; ++x) fa[x] = fetch_lane_offset<SA, T::BM>(lane, (wr >> 4) + x);
+    for (int x = 0; x < XT; ++x) fa[x] = fetch_lane_offset<E, SA, T::BM>(lane, (wr >> 4) + x);
   }
   if (SB != KS) {
 #pragma unroll
-    for (int ks = 0; ks < STEPS; ++ks) fb[ks] = fetch_lane_offset<SB, T::BN>(lane, ks) + wc * 128;
+    for (int ks = 0; ks < STEPS; ++ks) fb[ks] = fetch_lane_offset<E, SB, T::BN>(lane, ks) + wc * SLAB;
   } else {
 #pragma unroll
-    for (int y = 0; y < YT; ++y) fb[y] = fetch_lane_offset<SB, T::BN>(lane, (wc >> 4) + y);
+    for (int y = 0; y < YT; ++y) fb[y] = fetch_lane_offset<E, SB, T::BN>(lane, (wc >> 4) + y);
   }
-  auto fetch = [&](const unsigned char* s, auto strided, auto r, const int* f, int frag, int ks) -> bf16x8 {
+  typedef std::conditional_t<sizeof(E) == 4, f32x4, bf16x8> Frag;
+  auto fetch = [&](const unsigned char* s, auto strided, auto r, const int* f, int frag, int ks) -> Frag {
     constexpr int R = decltype(r)::value;
-    if constexpr (!decltype(strided)::value) return *reinterpret_cast<const bf16x8*>(s + f[ks] + frag * 16 * 128);
-    const unsigned char* const p = s + f[frag] + ks * 32 * R * 2;
-    union { bf16x8 v; s16x4 h[2]; } u;
-    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * R * 2));
-    return u.v;
+    if constexpr (!decltype(strided)::value) {
+      return *reinterpret_cast<const Frag*>(s + f[ks] + frag * 16 * SLAB);
+    } else if constexpr (sizeof(E) == 4) {
+      const float* const p = reinterpret_cast<const float*>(s + f[frag] + ks * 16 * R * 4);
+      return (f32x4){p[0], p[R], p[2 * R], p[3 * R]};
+    } else {
+      const unsigned char* const p = s + f[frag] + ks * 32 * R * 2;
+      union { bf16x8 v; s16x4 h[2]; } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * R * 2));
+      return u.v;
+    }
   };
   auto fetchA = [&](const unsigned char* s, int x, int ks) { return fetch(s, std::bool_constant<SA == KS>{}, std::integral_constant<int, T::BM>{}, fa, x, ks); };
   auto fetchB = [&](const unsigned char* s, int y, int ks) { return fetch(s + T::A_BYTES, std::bool_constant<SB == KS>{}, std::integral_constant<int, T::BN>{}, fb, y, ks); };
 
   constexpr int YP = T::YP, NP = T::NP, NT = STEPS * NP, NM = XT * YP;   // pieces of a slab, products of a piece
   static_assert(NT % 2 == 0, "operand double buffer parity");
-  bf16x8 av[2][XT], bv[2][YP];
+  Frag av[2][XT], bv[2][YP];
   auto mfma = [&](auto t, auto m) {
     constexpr int T_ = t, ks = T_ / NP, y0 = T_ % NP * YP, x = m / YP, yy = m % YP, y = (x & 1) ? YP - 1 - yy : yy;
-    acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[T_ & 1][y], av[ks & 1][x], acc[x][y0 + y], 0, 0, 0);
+    if constexpr (sizeof(E) == 4) {
+      static_for<4>([&](auto e) { acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[T_ & 1][y][decltype(e)::value], av[ks & 1][x][decltype(e)::value], acc[x][y0 + y], 0, 0, 0); });
+    } else {
+      acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[T_ & 1][y], av[ks & 1][x], acc[x][y0 + y], 0, 0, 0);
+    }
   };
   constexpr int READS = YP + XT;
   auto operands = [](int t) { return YP + (t % NP == 0 ? XT : 0); };
@@ -281,22 +302,27 @@ __device__ __forceinline__ int pair_column(int lane) { return 16 * ((lane >> 4) 
 
 // The gate and its derivative: silu(g) = g s, silu'(g) = s + g s (1 - s) with s = 1 / (1 + exp(-g)); gelu(g) = g P(g), gelu'(g) = P(g) + g p(g) with the
 // normal distribution P and its density p.
-template <int ACT>
-__device__ __forceinline__ float gate(float g) {
-  if constexpr (ACT == GLU_GELU) return gelu_f(g);
-  else return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
-}
-template <int ACT>
+// In fp32 with the full-precision exp and erf, in bf16 with the fast ones, whose error is 1e-6.
+template <typename E, int ACT>
 __device__ __forceinline__ void gate_and_slope(float g, float& a, float& da) {
   if constexpr (ACT == GLU_GELU) {
-    float e, ez;
-    erf_and_gauss(g * 0.70710678118654752f, e, ez);
-    const float cdf = 0.5f * (1.f + e);
+    float erfz, ez;
+    if constexpr (sizeof(E) == 4) { erfz = erff(g * 0.70710678118654752f); ez = expf(-0.5f * g * g); }
+    else erf_and_gauss(g * 0.70710678118654752f, erfz, ez);
+    const float cdf = 0.5f * (1.f + erfz);
     a = g * cdf; da = fmaf(g * 0.39894228040143268f, ez, cdf);
   } else {
-    const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
+    float s;
+    if constexpr (sizeof(E) == 4) s = 1.f / (1.f + expf(-g));
+    else s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
     a = g * s; da = fmaf(a, 1.f - s, s);
   }
+}
+template <typename E, int ACT>
+__device__ __forceinline__ float gate(float g) {
+  float a, da;
+  gate_and_slope<E, ACT>(g, a, da);
+  return a;
 }
 
 // g and u as the backward pass finds them: their leading 24 bits (2^-15, where the rounding to bf16 that follows is 2^-8), four values of each in
@@ -326,11 +352,11 @@ struct UpArgs {
   Operand x, w;          // w: PAIRS
   uint32_t T, F, d;
   TileOrder order;
-  bf16_t* h;             // [T x F]
-  unsigned char* saved;  // or null
+  void* h;               // [T x F]
+  void* saved;           // or null
   uint32_t* tickets; int ntickets;   // of the launch behind, to be cleared
 };
-template <typename T, int ACT>
+template <typename T, typename E, int ACT>
 __global__ __launch_bounds__(T::THREADS) void k_glu_up(UpArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   for (int i = blockIdx.x * T::THREADS + threadIdx.x; i < a.ntickets; i += gridDim.x * T::THREADS) a.tickets[i] = 0;
@@ -340,7 +366,7 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_up(UpArgs a) {
   tile_of(id, a.order.tm, a.order.tn, ti, tj);
   const uint32_t i0 = ti * T::BM, j0 = tj * (T::BN / 2);
   f32x4 acc[T::XT][T::YT];
-  contract<T, KC, PAIRS>(acc, smem, a.x, a.w, i0, j0, a.d, 0, (a.d + BK - 1) / BK);
+  contract<T, E, KC, PAIRS>(acc, smem, a.x, a.w, i0, j0, a.d, 0, (a.d + DEPTH<E> - 1) / DEPTH<E>);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (wave >= (uint32_t)T::WAVES) return;
   const int lane = threadIdx.x & 63;
@@ -350,26 +376,36 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_up(UpArgs a) {
   static_for<T::XT>([&](auto x_) {
     constexpr int x = x_;
     if (row0 + 16 * x >= a.T) return;
+    const uint32_t row = row0 + 16 * x + (lane & 15);
+    E* const to = static_cast<E*>(a.h) + (uint64_t)row * a.F;
     f32x4 h[GR];
     static_for<GR>([&](auto q_) {
       constexpr int q = q_;
       const f32x4 g = acc[x][2 * q], u = acc[x][2 * q + 1];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[q][e] = gate<ACT>(g[e]) * u[e];
-      if (a.saved != nullptr && col0 + 16 * q < a.F) {
-        unsigned char* const b = a.saved + ((uint64_t)((row0 >> 4) + x) * blocks + (col0 >> 4) + q) * SAVED_BLOCK;
+      for (int e = 0; e < 4; ++e) h[q][e] = gate<E, ACT>(g[e]) * u[e];
+      const uint32_t col = col0 + 16 * q + 4 * (lane >> 4);
+      if constexpr (sizeof(E) == 4) {
+        if (row < a.T && col < a.F) {
+          *reinterpret_cast<f32x4*>(to + col) = h[q];
+          if (a.saved != nullptr) {
+            float* const b = static_cast<float*>(a.saved) + (uint64_t)row * (2 * a.F) + col;
+            *reinterpret_cast<f32x4*>(b) = g;
+            *reinterpret_cast<f32x4*>(b + a.F) = u;
+          }
+        }
+      } else if (a.saved != nullptr && col0 + 16 * q < a.F) {
+        unsigned char* const b = static_cast<unsigned char*>(a.saved) + ((uint64_t)((row0 >> 4) + x) * blocks + (col0 >> 4) + q) * SAVED_BLOCK;
         uint32_t wg[3], wu[3];
         pack24(g, wg); pack24(u, wu);
         *reinterpret_cast<uint4*>(b + lane * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
         *reinterpret_cast<uint2*>(b + 1024 + lane * 8) = make_uint2(wu[1], wu[2]);
       }
     });
-    const uint32_t row = row0 + 16 * x + (lane & 15);
-    bf16_t* const to = a.h + (uint64_t)row * a.F;
-    if constexpr (GR == 1) {
+    if constexpr (sizeof(E) == 2 && GR == 1) {
       const uint32_t col = col0 + 4 * (lane >> 4);
       if (row < a.T && col < a.F) *reinterpret_cast<uint2*>(to + col) = packed(h[0]);
-    } else {
+    } else if constexpr (sizeof(E) == 2) {
       static_for<GR / 2>([&](auto q_) {
         constexpr int q = 2 * q_;
         const uint4 v = side_by_side(h[q], h[q + 1]);
@@ -384,11 +420,11 @@ struct DgateArgs {
   Operand dy, w;         // w: KS
   uint32_t T, F, d;
   TileOrder order;
-  const unsigned char* saved;
-  bf16_t* dpre;          // [T x 2F]: dg, du
+  const void* saved;
+  void* dpre;            // [T x 2F]: dg, du
   uint32_t* tickets; int ntickets;
 };
-template <typename T, int ACT>
+template <typename T, typename E, int ACT>
 __global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   for (int i = blockIdx.x * T::THREADS + threadIdx.x; i < a.ntickets; i += gridDim.x * T::THREADS) a.tickets[i] = 0;
@@ -398,41 +434,55 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
   tile_of(id, a.order.tm, a.order.tn, ti, tj);
   const uint32_t i0 = ti * T::BM, j0 = tj * T::BN;
   f32x4 acc[T::XT][T::YT];
-  contract<T, KC, KS>(acc, smem, a.dy, a.w, i0, j0, a.d, 0, (a.d + BK - 1) / BK);
+  contract<T, E, KC, KS>(acc, smem, a.dy, a.w, i0, j0, a.d, 0, (a.d + DEPTH<E> - 1) / DEPTH<E>);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (wave >= (uint32_t)T::WAVES) return;
   const int lane = threadIdx.x & 63;
   const uint32_t row0 = i0 + (wave / T::WGN) * T::WM, col0 = j0 + (wave % T::WGN) * T::WN;
   const uint32_t blocks = (a.F + 15) / 16;
+  auto backward = [&](f32x4 g, f32x4 u, f32x4 dh, f32x4& dg, f32x4& du) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float s, ds;
+      gate_and_slope<E, ACT>(g[e], s, ds);
+      dg[e] = dh[e] * (u[e] * ds); du[e] = dh[e] * s;
+    }
+  };
   static_for<T::XT>([&](auto x_) {
     constexpr int x = x_;
     if (row0 + 16 * x >= a.T) return;
     const uint32_t row = row0 + 16 * x + (lane & 15);
-    bf16_t* const to = a.dpre + (uint64_t)row * (2 * a.F);
-    static_for<T::YT / 2>([&](auto h_) {
-      constexpr int h = h_;
-      f32x4 dg[2], du[2];
+    E* const to = static_cast<E*>(a.dpre) + (uint64_t)row * (2 * a.F);
+    if constexpr (sizeof(E) == 4) {
+      static_for<T::YT>([&](auto y_) {
+        const uint32_t col = col0 + 16 * decltype(y_)::value + 4 * (lane >> 4);
+        if (row >= a.T || col >= a.F) return;
+        const float* const b = static_cast<const float*>(a.saved) + (uint64_t)row * (2 * a.F) + col;
+        f32x4 dg, du;
+        backward(*reinterpret_cast<const f32x4*>(b), *reinterpret_cast<const f32x4*>(b + a.F), acc[x][decltype(y_)::value], dg, du);
+        *reinterpret_cast<f32x4*>(to + col) = dg;
+        *reinterpret_cast<f32x4*>(to + a.F + col) = du;
+      });
+    } else {
+      static_for<T::YT / 2>([&](auto h_) {
+        constexpr int h = h_;
+        f32x4 dg[2], du[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t block = min((col0 >> 4) + 2 * h + k, blocks - 1);
-        const unsigned char* const b = a.saved + ((uint64_t)((row0 >> 4) + x) * blocks + block) * SAVED_BLOCK;
-        const uint4 p = *reinterpret_cast<const uint4*>(b + lane * 16);
-        const uint2 r = *reinterpret_cast<const uint2*>(b + 1024 + lane * 8);
-        const f32x4 g = unpack24(p.x, p.y, p.z), u = unpack24(p.w, r.x, r.y), dh = acc[x][2 * h + k];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float s, ds;
-          gate_and_slope<ACT>(g[e], s, ds);
-          dg[k][e] = dh[e] * (u[e] * ds); du[k][e] = dh[e] * s;
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t block = min((col0 >> 4) + 2 * h + k, blocks - 1);
+          const unsigned char* const b = static_cast<const unsigned char*>(a.saved) + ((uint64_t)((row0 >> 4) + x) * blocks + block) * SAVED_BLOCK;
+          const uint4 p = *reinterpret_cast<const uint4*>(b + lane * 16);
+          const uint2 r = *reinterpret_cast<const uint2*>(b + 1024 + lane * 8);
+          backward(unpack24(p.x, p.y, p.z), unpack24(p.w, r.x, r.y), acc[x][2 * h + k], dg[k], du[k]);
         }
-      }
-      const uint4 vg = side_by_side(dg[0], dg[1]), vu = side_by_side(du[0], du[1]);
-      const uint32_t col = col0 + 32 * h + pair_column(lane);
-      if (row < a.T && col < a.F) {
-        *reinterpret_cast<uint4*>(to + col) = vg;
-        *reinterpret_cast<uint4*>(to + a.F + col) = vu;
-      }
-    });
+        const uint4 vg = side_by_side(dg[0], dg[1]), vu = side_by_side(du[0], du[1]);
+        const uint32_t col = col0 + 32 * h + pair_column(lane);
+        if (row < a.T && col < a.F) {
+          *reinterpret_cast<uint4*>(to + col) = vg;
+          *reinterpret_cast<uint4*>(to + a.F + col) = vu;
+        }
+      });
+    }
   });
 }
 
@@ -485,8 +535,8 @@ __device__ __forceinline__ void collect16(const float* p, f32x4 (&v)[4], int ste
                : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(p), "v"(p + step), "v"(p + 2 * step), "v"(p + 3 * step) : "memory");
 }
 
-// KINDS: 0: forward (A and B KC); 1: gradients, dx with A KC and B KS, the weights' with both KS
-template <typename T, int KIND>
+// KIND 0: forward (A and B KC); 1: gradients, dx with A KC and B KS, the weights' with both KS
+template <typename T, typename E, int KIND>
 __global__ __launch_bounds__(T::THREADS) void k_glu_split(SplitArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   __shared__ int s_last;
@@ -517,9 +567,9 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_split(SplitArgs a) {
     tile_of(tile, p.tm, p.tn, ti, tj);
     const uint32_t i0 = ti * T::BM, j0 = tj * T::BN;
     if (!first_piece) __syncthreads();                                   // the stages are free
-    if constexpr (KIND == 0) contract<T, KC, KC>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
-    else if (p.strided_a) contract<T, KS, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
-    else contract<T, KC, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+    if constexpr (KIND == 0) contract<T, E, KC, KC>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+    else if (p.strided_a) contract<T, E, KS, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+    else contract<T, E, KC, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
     const bool multiplies = wave < (uint32_t)T::WAVES;
     if (slabs == (int)p.slabs) {
       if (multiplies) store_tile<T>(acc, p, i0, j0, wave);
@@ -620,8 +670,8 @@ __global__ __launch_bounds__(512) void k_glu_up_few(UpArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t f0 = blockIdx.x * 16, steps = (a.d + 31) / 32;
   f32x4 acc[2][NT];
-  const bf16_t* const w = a.w.p + (uint64_t)min(f0 + (lane & 15), a.F - 1) * a.d;
-  contract_few<2, NT>(acc, w, (uint64_t)a.F * a.d, a.x.p, a.x.ld, a.T, a.d, share_of(steps, wave, 8), share_of(steps, wave + 1, 8));
+  const bf16_t* const w = static_cast<const bf16_t*>(a.w.p) + (uint64_t)min(f0 + (lane & 15), a.F - 1) * a.d;
+  contract_few<2, NT>(acc, w, (uint64_t)a.F * a.d, static_cast<const bf16_t*>(a.x.p), a.x.ld, a.T, a.d, share_of(steps, wave, 8), share_of(steps, wave + 1, 8));
 #pragma unroll
   for (int t = 0; t < NT; ++t) { part[wave][0][t][lane] = acc[0][t]; part[wave][1][t][lane] = acc[1][t]; }
   __syncthreads();
@@ -631,16 +681,16 @@ __global__ __launch_bounds__(512) void k_glu_up_few(UpArgs a) {
 #pragma unroll
   for (int k = 1; k < 8; ++k) { g += part[k][0][t][lane]; u += part[k][1][t][lane]; }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) h[e] = gate<ACT>(g[e]) * u[e];
+  for (int e = 0; e < 4; ++e) h[e] = gate<bf16_t, ACT>(g[e]) * u[e];
   if (a.saved != nullptr) {
-    unsigned char* const b = a.saved + ((uint64_t)t * ((a.F + 15) / 16) + blockIdx.x) * SAVED_BLOCK;
+    unsigned char* const b = static_cast<unsigned char*>(a.saved) + ((uint64_t)t * ((a.F + 15) / 16) + blockIdx.x) * SAVED_BLOCK;
     uint32_t wg[3], wu[3];
     pack24(g, wg); pack24(u, wu);
     *reinterpret_cast<uint4*>(b + lane * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
     *reinterpret_cast<uint2*>(b + 1024 + lane * 8) = make_uint2(wu[1], wu[2]);
   }
   const uint32_t row = 16 * t + (lane & 15), col = f0 + 4 * (lane >> 4);
-  if (row < a.T && col < a.F) *reinterpret_cast<uint2*>(a.h + (uint64_t)row * a.F + col) = packed(h);
+  if (row < a.T && col < a.F) *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.h) + (uint64_t)row * a.F + col) = packed(h);
 }
 
 struct DownFewArgs { const bf16_t *h, *w; uint32_t T, F, d; bf16_t* y; uint32_t ldy; };
@@ -701,7 +751,7 @@ __global__ __launch_bounds__(256) void k_glu_up_rows(UpArgs a) {
   __shared__ f32x4 part[4][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 3;
   const uint32_t f0 = blockIdx.x * 4, steps = (a.d + 127) / 128;
-  const f32x4 acc = contract_rows(a.w.p + (uint64_t)(f0 + i + (wave & 1) * a.F) * a.d, a.x.p + (uint64_t)min((uint32_t)i, a.T - 1) * a.x.ld, a.d,
+  const f32x4 acc = contract_rows(static_cast<const bf16_t*>(a.w.p) + (uint64_t)(f0 + i + (wave & 1) * a.F) * a.d, static_cast<const bf16_t*>(a.x.p) + (uint64_t)min((uint32_t)i, a.T - 1) * a.x.ld, a.d,
                                   share_of(steps, wave >> 1, 2), share_of(steps, (wave >> 1) + 1, 2));
   if (lane < 4) part[wave][lane] = acc;
   __syncthreads();
@@ -709,16 +759,16 @@ __global__ __launch_bounds__(256) void k_glu_up_rows(UpArgs a) {
   const f32x4 g = part[0][i] + part[2][i], u = part[1][i] + part[3][i];
   f32x4 h;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) h[e] = gate<ACT>(g[e]) * u[e];
+  for (int e = 0; e < 4; ++e) h[e] = gate<bf16_t, ACT>(g[e]) * u[e];
   if (a.saved != nullptr) {
-    unsigned char* const b = a.saved + (uint64_t)(f0 >> 4) * SAVED_BLOCK;
+    unsigned char* const b = static_cast<unsigned char*>(a.saved) + (uint64_t)(f0 >> 4) * SAVED_BLOCK;
     const int at = 16 * ((f0 >> 2) & 3) + i;      // the lane of a fragment that has these four columns
     uint32_t wg[3], wu[3];
     pack24(g, wg); pack24(u, wu);
     *reinterpret_cast<uint4*>(b + at * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
     *reinterpret_cast<uint2*>(b + 1024 + at * 8) = make_uint2(wu[1], wu[2]);
   }
-  *reinterpret_cast<uint2*>(a.h + (uint64_t)i * a.F + f0) = packed(h);
+  *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.h) + (uint64_t)i * a.F + f0) = packed(h);
 }
 __global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
   __shared__ f32x4 part[8][4];
@@ -765,90 +815,95 @@ void launch_rows(ProfScope& ps, hipStream_t st, const UpArgs& u, const DownFewAr
   else launch_kernel(ps, k_glu_up_rows<GLU_SILU>, u.F / 4, 256, 0, st, u);
   launch_kernel(ps, k_glu_down_rows, w.d / 4, 512, 0, st, w);
 }
-template <typename T>
+template <typename T, typename E>
 void launch_up(ProfScope& ps, hipStream_t st, UpArgs a, int act) {
   a.order = order_of(a.T, a.F, T::BM, T::BN / 2);
-  if (act == GLU_GELU) launch_big<k_glu_up<T, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
-  else launch_big<k_glu_up<T, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
+  if (act == GLU_GELU) launch_big<k_glu_up<T, E, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
+  else launch_big<k_glu_up<T, E, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
 }
-template <typename T>
+template <typename T, typename E>
 void launch_dgate(ProfScope& ps, hipStream_t st, DgateArgs a, int act) {
   a.order = order_of(a.T, a.F, T::BM, T::BN);
-  if (act == GLU_GELU) launch_big<k_glu_dgate<T, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
-  else launch_big<k_glu_dgate<T, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
+  if (act == GLU_GELU) launch_big<k_glu_dgate<T, E, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
+  else launch_big<k_glu_dgate<T, E, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
 }
 constexpr uint64_t LEAST_RUN = 6;
-template <typename T>
+template <typename T, typename E>
 void plan_split(SplitArgs& a) {
   uint64_t units = 0;
-  uint32_t tiles = 0;
+  uint32_t tiles = 0, longest = 0;
   for (int k = 0; k < a.count; ++k) {
     Product& p = a.p[k];
-    p.tm = (p.M + T::BM - 1) / T::BM; p.tn = (p.N + T::BN - 1) / T::BN; p.slabs = (p.K + BK - 1) / BK; p.first = (uint32_t)units;
+    p.tm = (p.M + T::BM - 1) / T::BM; p.tn = (p.N + T::BN - 1) / T::BN; p.slabs = (p.K + DEPTH<E> - 1) / DEPTH<E>; p.first = (uint32_t)units;
     units += (uint64_t)p.tm * p.tn * p.slabs; tiles += p.tm * p.tn;
+    longest = std::max(longest, p.slabs);
   }
   a.units = units;
   const uint32_t slots = 256 * T::PER_CU;
   // Whole tiles in rounds, or all slabs in equal runs with what it costs to add the parts up, the time of about JOIN slabs; a run has LEAST_RUN of them at least.
   constexpr uint64_t JOIN = 6;
-  uint32_t longest = 0;
-  for (int k = 0; k < a.count; ++k) longest = std::max(longest, a.p[k].slabs);
   const uint64_t rounds = (tiles + slots - 1) / slots, whole = rounds * longest;
   const uint64_t groups = std::max<uint64_t>(1, std::min<uint64_t>(slots, units / LEAST_RUN)), run = (units + groups - 1) / groups + JOIN;
   a.split = run < whole && groups > 1 ? 1 : 0;
   a.groups = a.split ? (int)groups : (int)tiles;
 }
-template <typename T, int KIND>
+template <typename T, typename E, int KIND>
 void launch_split(ProfScope& ps, hipStream_t st, SplitArgs a) {
-  plan_split<T>(a);
-  launch_big<k_glu_split<T, KIND>, T>(ps, st, 8 * ((a.groups + 7) / 8), a);
+  plan_split<T, E>(a);
+  launch_big<k_glu_split<T, E, KIND>, T>(ps, st, 8 * ((a.groups + 7) / 8), a);
 }
 
 int g_force_tile = 0;
-int tile_for(int64_t M, int64_t N) {
-  if (g_force_tile != 0) return g_force_tile;
-  const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256), t128 = ((M + 127) / 128) * ((N + 127) / 128);
-  return t256 >= 200 ? 256 : t128 >= 100 ? 128 : 64;
+// The tile of products of `tiles64` tiles of 64 x 64 in all: the largest that leaves most CUs one, or, where the contraction is split over the chip (`split`),
+// some of it.  fp32: the matrix cores are sixteen times slower, and tiles beyond 128 gain nothing.
+template <typename E, typename F>
+void with_tile(size_t tiles64, bool split, F f) {
+  int tile = tiles64 >= (split ? 1600 : 3200) ? 256 : tiles64 >= (split ? 240 : 400) ? 128 : 64;
+  if (g_force_tile != 0) tile = g_force_tile;
+  if constexpr (sizeof(E) == 2) if (tile == 256) return f(T256{});
+  if (tile >= 128) f(T128{});
+  else f(T64{});
 }
 // Partial sums: two tiles for each workgroup that has a run of slabs, whether they are cut or not, so that the size grows with the number of tokens and what is
 // enough for some is for fewer.
-template <typename T>
+template <typename T, typename E>
 size_t part_bytes_of(const SplitArgs& shapes) {
   SplitArgs a = shapes;
-  plan_split<T>(a);
+  plan_split<T, E>(a);
   return (size_t)2 * std::max<uint64_t>(1, std::min<uint64_t>(256 * T::PER_CU, a.units / LEAST_RUN)) * T::BM * T::BN * 4;
 }
-size_t part_bytes(const SplitArgs& a) { return std::max({part_bytes_of<T256>(a), part_bytes_of<T128>(a), part_bytes_of<T64>(a)}); }
+template <typename E>
+size_t part_bytes(const SplitArgs& a) { return std::max({sizeof(E) == 2 ? part_bytes_of<T256, E>(a) : 0, part_bytes_of<T128, E>(a), part_bytes_of<T64, E>(a)}); }
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
-size_t most_tiles(int64_t M, int64_t N) { return (size_t)((M + 63) / 64) * ((N + 63) / 64); }
-}  // namespace
+size_t tiles64(int64_t M, int64_t N) { return (size_t)((M + 63) / 64) * ((N + 63) / 64); }
+size_t grad_tiles64(int64_t T, int d, int F) { return tiles64(T, d) + tiles64(2 * (int64_t)F, d) + tiles64(d, F); }
 
-void glu_ffn_force_tile(int t) { g_force_tile = t; }
-
-size_t glu_ffn_saved_bytes(int64_t T, int F) { return (size_t)((T + 15) / 16) * ((F + 15) / 16) * SAVED_BLOCK; }
-size_t glu_ffn_bytes(int64_t T, int d, int F) {
+template <typename E>
+size_t forward_bytes(int64_t T, int d, int F) {
   SplitArgs s{};
   s.count = 1; s.p[0].M = (uint32_t)T; s.p[0].N = d; s.p[0].K = F;
-  return up256(most_tiles(T, d) * 4) + part_bytes(s);
+  return up256(tiles64(T, d) * 4) + part_bytes<E>(s);
 }
-size_t glu_ffn_grad_bytes(int64_t T, int d, int F) {
+template <typename E>
+size_t backward_bytes(int64_t T, int d, int F) {
   SplitArgs s{};
   s.count = 3; s.p[0].M = (uint32_t)T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[1].M = 2 * F; s.p[1].N = d; s.p[1].K = (uint32_t)T; s.p[2].M = d; s.p[2].N = F; s.p[2].K = (uint32_t)T;
-  return up256((most_tiles(T, d) + most_tiles(2 * F, d) + most_tiles(d, F)) * 4) + up256((size_t)T * 2 * F * 2) + part_bytes(s);
+  return up256(grad_tiles64(T, d, F) * 4) + up256((size_t)T * 2 * F * sizeof(E)) + part_bytes<E>(s);
 }
 
-void launch_glu_ffn(hipStream_t st, const GluFfnArgs& g, void* workspace) {
-  if (g.T == 0) return;
+template <typename E>
+void forward(hipStream_t st, const GluFfnArgs& g, void* workspace) {
+  constexpr bool BF16 = sizeof(E) == 2;
   char* const ws = static_cast<char*>(workspace);
   const uint32_t T = (uint32_t)g.T, d = g.d, F = g.F;
-  const size_t ntickets = most_tiles(T, d);
-  ProfScope ps(st, F_GEMM_NT, 6.0 * T * (double)d * F);
+  const size_t ntickets = tiles64(T, d);
+  ProfScope ps(st, BF16 ? F_GEMM_NT : F_GEMM_F32, 6.0 * T * (double)d * F);
   UpArgs u{};
-  u.x = Operand{(const bf16_t*)g.x, (uint32_t)g.ldx, T}; u.w = Operand{(const bf16_t*)g.w_in, d, F};
-  u.T = T; u.F = F; u.d = d; u.h = (bf16_t*)g.hidden; u.saved = (unsigned char*)g.saved;
+  u.x = Operand{g.x, (uint32_t)g.ldx, T}; u.w = Operand{g.w_in, d, F};
+  u.T = T; u.F = F; u.d = d; u.h = g.hidden; u.saved = g.saved;
   // Few tokens without tiles.  us a call, this way / by tiles: 512 x 1368 1 token 10.2 / 13.7, 16 11.4 / 14.0, 32 12.2 / 14.3, 48 14.7 / 14.5; 1024 x 4096 1
   // 9.5 / 19.5, 5 13.1 / 19.6, 16 15.4 / 19.7, 32 20.1 / 20.2, 48 25.6 / 20.2; 2048 x 5504 1 15.0 / 27.2, 4 19.6 / 27.3, 5 27.7 / 27.3, 16 33.5 / 27.6.
-  if (g_force_tile == 0 && (T <= 4 || (T <= 32 && (uint64_t)d * F <= (1u << 22)))) {
+  if (BF16 && g_force_tile == 0 && (T <= 4 || (T <= 32 && (uint64_t)d * F <= (1u << 22)))) {
     const DownFewArgs w{(const bf16_t*)g.hidden, (const bf16_t*)g.w_out, T, F, d, (bf16_t*)g.y, (uint32_t)g.ldy};
     if (T <= 4) launch_rows(ps, st, u, w, g.act);
     else if (T <= 16) launch_few<1>(ps, st, u, w, g.act);
@@ -856,51 +911,65 @@ void launch_glu_ffn(hipStream_t st, const GluFfnArgs& g, void* workspace) {
     return;
   }
   u.tickets = (uint32_t*)ws; u.ntickets = (int)ntickets;
-  switch (tile_for(T, 2 * (int64_t)F)) {
-    case 256: launch_up<T256>(ps, st, u, g.act); break;
-    case 128: launch_up<T128>(ps, st, u, g.act); break;
-    default: launch_up<T64>(ps, st, u, g.act); break;
-  }
+  with_tile<E>(tiles64(T, 2 * (int64_t)F), false, [&](auto t) { launch_up<decltype(t), E>(ps, st, u, g.act); });
   SplitArgs s{};
   s.count = 1; s.part = (float*)(ws + up256(ntickets * 4)); s.tickets = (uint32_t*)ws;
   Product& p = s.p[0];
-  p.A = Operand{(const bf16_t*)g.hidden, F, T}; p.B = Operand{(const bf16_t*)g.w_out, F, d};
-  p.M = T; p.N = d; p.K = F; p.C = g.y; p.ldc = (uint32_t)g.ldy;
-  switch (tile_for(T, d)) {
-    case 256: launch_split<T256, 0>(ps, st, s); break;
-    case 128: launch_split<T128, 0>(ps, st, s); break;
-    default: launch_split<T64, 0>(ps, st, s); break;
-  }
+  p.A = Operand{g.hidden, F, T}; p.B = Operand{g.w_out, F, d};
+  p.M = T; p.N = d; p.K = F; p.C = g.y; p.ldc = (uint32_t)g.ldy; p.c32 = !BF16;
+  with_tile<E>(tiles64(T, d), false, [&](auto t) { launch_split<decltype(t), E, 0>(ps, st, s); });
 }
 
-void launch_glu_ffn_grad(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
+template <typename E>
+void backward(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
+  constexpr bool BF16 = sizeof(E) == 2;
   char* const ws = static_cast<char*>(workspace);
   const uint32_t T = (uint32_t)g.T, d = g.d, F = g.F;
-  const size_t ntickets = most_tiles(T, d) + most_tiles(2 * F, d) + most_tiles(d, F);
-  bf16_t* const dpre = (bf16_t*)(ws + up256(ntickets * 4));
-  ProfScope ps(st, F_GEMM_NN, 12.0 * T * (double)d * F);
+  const size_t ntickets = grad_tiles64(T, d, F);
+  void* const dpre = ws + up256(ntickets * 4);
+  ProfScope ps(st, BF16 ? F_GEMM_NN : F_GEMM_F32, 12.0 * T * (double)d * F);
   DgateArgs e{};
-  e.dy = Operand{(const bf16_t*)g.dy, (uint32_t)g.lddy, T}; e.w = Operand{(const bf16_t*)g.w_out, F, F};
-  e.T = T; e.F = F; e.d = d; e.saved = (const unsigned char*)g.saved; e.dpre = dpre; e.tickets = (uint32_t*)ws; e.ntickets = (int)ntickets;
-  switch (tile_for(T, F)) {
-    case 256: launch_dgate<T256>(ps, st, e, g.act); break;
-    case 128: launch_dgate<T128>(ps, st, e, g.act); break;
-    default: launch_dgate<T64>(ps, st, e, g.act); break;
-  }
+  e.dy = Operand{g.dy, (uint32_t)g.lddy, T}; e.w = Operand{g.w_out, F, F};
+  e.T = T; e.F = F; e.d = d; e.saved = g.saved; e.dpre = dpre; e.tickets = (uint32_t*)ws; e.ntickets = (int)ntickets;
+  with_tile<E>(tiles64(T, F), false, [&](auto t) { launch_dgate<decltype(t), E>(ps, st, e, g.act); });
   SplitArgs s{};
-  s.count = 3; s.tickets = (uint32_t*)ws; s.part = (float*)((char*)dpre + up256((size_t)T * 2 * F * 2));
-  s.p[0].A = Operand{dpre, 2 * F, T}; s.p[0].B = Operand{(const bf16_t*)g.w_in, d, d};
-  s.p[0].M = T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[0].C = g.dx; s.p[0].ldc = (uint32_t)g.lddx;
-  s.p[1].A = Operand{dpre, 2 * F, 2 * F}; s.p[1].B = Operand{(const bf16_t*)g.x, (uint32_t)g.ldx, d};
-  s.p[1].M = 2 * F; s.p[1].N = d; s.p[1].K = T; s.p[1].C = g.dw_in; s.p[1].ldc = d; s.p[1].strided_a = 1; s.p[1].c32 = g.dw_fp32;
-  s.p[2].A = Operand{(const bf16_t*)g.dy, (uint32_t)g.lddy, d}; s.p[2].B = Operand{(const bf16_t*)g.hidden, F, F};
-  s.p[2].M = d; s.p[2].N = F; s.p[2].K = T; s.p[2].C = g.dw_out; s.p[2].ldc = F; s.p[2].strided_a = 1; s.p[2].c32 = g.dw_fp32;
-  const int64_t all = most_tiles(T, d) + most_tiles(2 * F, d) + most_tiles(d, F);
-  switch (g_force_tile != 0 ? g_force_tile : all >= 16 * 100 ? 256 : all >= 4 * 60 ? 128 : 64) {
-    case 256: launch_split<T256, 1>(ps, st, s); break;
-    case 128: launch_split<T128, 1>(ps, st, s); break;
-    default: launch_split<T64, 1>(ps, st, s); break;
-  }
+  s.count = 3; s.tickets = (uint32_t*)ws; s.part = (float*)((char*)dpre + up256((size_t)T * 2 * F * sizeof(E)));
+  s.p[0].A = Operand{dpre, 2 * F, T}; s.p[0].B = Operand{g.w_in, d, d};
+  s.p[0].M = T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[0].C = g.dx; s.p[0].ldc = (uint32_t)g.lddx; s.p[0].c32 = !BF16;
+  s.p[1].A = Operand{dpre, 2 * F, 2 * F}; s.p[1].B = Operand{g.x, (uint32_t)g.ldx, d};
+  s.p[1].M = 2 * F; s.p[1].N = d; s.p[1].K = T; s.p[1].C = g.dw_in; s.p[1].ldc = d;
+  s.p[2].A = Operand{g.dy, (uint32_t)g.lddy, d}; s.p[2].B = Operand{g.hidden, F, F};
+  s.p[2].M = d; s.p[2].N = F; s.p[2].K = T; s.p[2].C = g.dw_out; s.p[2].ldc = F;
+  for (int k = 1; k < 3; ++k) { s.p[k].strided_a = 1; s.p[k].c32 = g.dw_fp32; }
+  with_tile<E>(ntickets, true, [&](auto t) { launch_split<decltype(t), E, 1>(ps, st, s); });
+}
+// fp32 operands that the tiles can load: rows in pieces of 16 bytes
+bool pieces32(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 4 == 0; }
+}  // namespace
+
+void glu_ffn_force_tile(int t) { g_force_tile = t; }
+
+size_t glu_ffn_saved_bytes(int64_t T, int F) { return (size_t)((T + 15) / 16) * ((F + 15) / 16) * SAVED_BLOCK; }
+size_t glu_ffn_bytes(int64_t T, int d, int F) { return forward_bytes<bf16_t>(T, d, F); }
+size_t glu_ffn_grad_bytes(int64_t T, int d, int F) { return backward_bytes<bf16_t>(T, d, F); }
+void launch_glu_ffn(hipStream_t st, const GluFfnArgs& g, void* workspace) { forward<bf16_t>(st, g, workspace); }
+void launch_glu_ffn_grad(hipStream_t st, const GluFfnGradArgs& g, void* workspace) { backward<bf16_t>(st, g, workspace); }
+
+size_t glu_ffn_f32_saved_bytes(int64_t T, int F) { return (size_t)T * 2 * F * 4; }
+size_t glu_ffn_f32_bytes(int64_t T, int d, int F) { return std::max(forward_bytes<float>(T, d, F), glu_ffn_plain_bytes(T, F)); }
+size_t glu_ffn_f32_grad_bytes(int64_t T, int d, int F) { return std::max(backward_bytes<float>(T, d, F), glu_ffn_plain_grad_bytes(T, F)); }
+// fp32 of any width, stride and alignment goes through the products of the MLPs; both keep g and u in the same place, so a forward call of the one
+// may be followed by a backward call of the other.
+void launch_glu_ffn_f32(hipStream_t st, const GluFfnArgs& g, void* workspace) {
+  const bool tiles = g.d % 4 == 0 && g.F % 4 == 0 && pieces32(g.x, g.ldx) && pieces32(g.y, g.ldy) && pieces32(g.w_in, 0) && pieces32(g.w_out, 0) && pieces32(g.hidden, 0);
+  if (tiles) forward<float>(st, g, workspace);
+  else launch_glu_ffn_plain(st, g, workspace);
+}
+void launch_glu_ffn_grad_f32(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
+  const bool tiles = g.d % 4 == 0 && g.F % 4 == 0 && pieces32(g.x, g.ldx) && pieces32(g.dy, g.lddy) && pieces32(g.dx, g.lddx) && pieces32(g.w_in, 0) && pieces32(g.w_out, 0) &&
+                     pieces32(g.hidden, 0) && pieces32(g.dw_in, 0) && pieces32(g.dw_out, 0);
+  if (tiles) backward<float>(st, g, workspace);
+  else launch_glu_ffn_grad_plain(st, g, workspace);
 }
 
 }  // namespace sama

@@ -1,4 +1,4 @@
-// The gated feed-forward block in fp32 (formulas: glu_ffn.hip).  The products are the fp32 matrix-core products of the framework's MLPs; the
+// The gated feed-forward block in fp32 for any width, stride and alignment (formulas, and the kernels for multiples of four: glu_ffn.hip).  The products are the fp32 matrix-core products of the framework's MLPs; the
 // gate between them is one pass over [g, u], bound by memory.  exp and erf are the full-precision ones: nothing here is rounded to fewer bits.
 #include <algorithm>
 #include "kernels.h"
@@ -52,11 +52,10 @@ GemmF32Args product(const void* A, int64_t sa_i, int64_t sa_k, const void* B, in
 }
 }  // namespace
 
-size_t glu_ffn_f32_saved_bytes(int64_t T, int F) { return (size_t)T * 2 * F * 4; }
-size_t glu_ffn_f32_bytes(int64_t T, int, int F) { return up256((size_t)T * 2 * F * 4); }
-size_t glu_ffn_f32_grad_bytes(int64_t T, int, int F) { return up256((size_t)T * F * 4) + up256((size_t)T * 2 * F * 4); }
+size_t glu_ffn_plain_bytes(int64_t T, int F) { return up256((size_t)T * 2 * F * 4); }
+size_t glu_ffn_plain_grad_bytes(int64_t T, int F) { return up256((size_t)T * F * 4) + up256((size_t)T * 2 * F * 4); }
 
-void launch_glu_ffn_f32(hipStream_t st, const GluFfnArgs& a, void* workspace) {
+void launch_glu_ffn_plain(hipStream_t st, const GluFfnArgs& a, void* workspace) {
   const int T = (int)a.T, d = a.d, F = a.F;
   float* const pre = (float*)(a.saved != nullptr ? a.saved : workspace);
   const GemmF32Args up = product(a.x, a.ldx, 1, a.w_in, 1, d, pre, 2 * (int64_t)F, T, 2 * F, d);
@@ -66,7 +65,7 @@ void launch_glu_ffn_f32(hipStream_t st, const GluFfnArgs& a, void* workspace) {
   launch_gemm_f32_batch(st, &down, 1);
 }
 
-void launch_glu_ffn_grad_f32(hipStream_t st, const GluFfnGradArgs& a, void* workspace) {
+void launch_glu_ffn_grad_plain(hipStream_t st, const GluFfnGradArgs& a, void* workspace) {
   const int T = (int)a.T, d = a.d, F = a.F;
   float* const dh = (float*)workspace;
   float* const dpre = (float*)((char*)workspace + up256((size_t)T * F * 4));

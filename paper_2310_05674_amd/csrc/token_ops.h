@@ -29,7 +29,7 @@ size_t grad_clip_bytes();
 // norm[0] = ||g||, norm[1] = the factor; out: flat fp32, or null (in place); status may be null
 void launch_grad_clip(hipStream_t, const GradTensor* g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace);
 
-// The gated feed-forward block (bf16: glu_ffn.hip, fp32: glu_ffn_f32.hip), shapes as in include/sama_ops.h.
+// The gated feed-forward block (glu_ffn.hip; fp32 that its tiles cannot load: glu_ffn_f32.hip), shapes as in include/sama_ops.h.
 enum { GLU_SILU = 0, GLU_GELU = 1 };
 struct GluFfnArgs {
   const void* x; int64_t ldx; const void *w_in, *w_out;
@@ -51,6 +51,11 @@ size_t glu_ffn_f32_bytes(int64_t T, int d, int F);
 size_t glu_ffn_f32_grad_bytes(int64_t T, int d, int F);
 void launch_glu_ffn_f32(hipStream_t, const GluFfnArgs&, void* workspace);
 void launch_glu_ffn_grad_f32(hipStream_t, const GluFfnGradArgs&, void* workspace);
+// ... of any width, stride and alignment
+size_t glu_ffn_plain_bytes(int64_t T, int F);
+size_t glu_ffn_plain_grad_bytes(int64_t T, int F);
+void launch_glu_ffn_plain(hipStream_t, const GluFfnArgs&, void* workspace);
+void launch_glu_ffn_grad_plain(hipStream_t, const GluFfnGradArgs&, void* workspace);
 void glu_ffn_force_tile(int tile);   // tuning hook: 0 = heuristic
 
 }  // namespace sama

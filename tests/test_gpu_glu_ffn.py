@@ -155,6 +155,37 @@ def test_fp32(T, d, F, act):
     assert all(torch.equal(got[k], again[k]) for k in got)
 
 
+@pytest.mark.parametrize("tile", [64, 128, 256])
+@pytest.mark.parametrize("T,d,F", [(1, 4, 4), (5, 12, 20), (33, 100, 36), (64, 64, 128), (130, 36, 1368), (257, 260, 132), (2100, 64, 68), (700, 256, 2000)])
+def test_fp32_tiles(T, d, F, tile):
+    import paper_2310_05674_amd as pkg
+    pkg.load_library().sama_dev_glu_tile(tile)
+    act = "silu" if T % 2 else "gelu"
+    i = inputs(T, d, F, "fp32", T)
+    got = run(i, act, ld=d + 4 * (T % 3))
+    check(got, exact(i, act), False)
+    again = run(i, act)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+def test_fp32_forward_and_backward_of_other_alignment():
+    """A forward call whose x begins at any float, and a backward call on an aligned copy of it."""
+    from paper_2310_05674_amd import binding as B
+    T, d, F = 90, 64, 72
+    i = inputs(T, d, F, "fp32", 2)
+    whole = torch.zeros(T * d + 1, device=DEV)
+    odd = whole[1:].view(T, d)
+    odd.copy_(i["x"])
+    scratch = lambda n: torch.empty(n, dtype=torch.uint8, device=DEV)
+    e = lambda *s: torch.empty(*s, device=DEV)
+    t = torch.float32
+    for first, second in ((odd, i["x"]), (i["x"], odd)):
+        y, hidden, saved, dx, dwi, dwo = e(T, d), e(T, F), scratch(B.glu_ffn_saved_bytes(T, F, t)), e(T, d), e(2 * F, d), e(d, F)
+        B.op_glu_ffn(first, i["w_in"], i["w_out"], y, hidden, scratch(B.glu_ffn_bytes(T, d, F, t)), saved=saved)
+        B.op_glu_ffn_grad(i["dy"], second, i["w_in"], i["w_out"], hidden, saved, dx, dwi, dwo, scratch(B.glu_ffn_grad_bytes(T, d, F, t)))
+        check(dict(y=y, hidden=hidden, dx=dx, dw_in=dwi, dw_out=dwo), exact(i, "silu"), False)
+
+
 @pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 6, 7, 8, 9, 12, 16, 17, 24, 31, 32, 48, 63, 64])
 @pytest.mark.parametrize("d,F", [(768, 2048), (1024, 4096), (520, 1368)])
 def test_few_tokens(T, d, F):
