@@ -4,10 +4,11 @@
 // 6 T d F operations forward and 12 backward in four launches:
 //   k_glu_up      both projections of a tile of tokens and hidden values in one workgroup, the rows of Wg and Wu sixteen by sixteen in turn, so that
 //                 a lane has g and u of the same values and h is all that leaves it (for training also g and u, see below)
-//   k_glu_down    y
 //   k_glu_dgate   dh, and out of it [dg, du] in the epilogue; dh is never stored
-//   k_glu_grads   dx, dW_in and dWo side by side: three products that read the same [dg, du] and none of which fills the chip alone
+//   k_glu_product y; and dx, dW_in and dWo side by side: three products that read the same [dg, du] and none of which fills the chip alone.  Where the
+//                 tiles of a product are too few, or a few too many for a round, the contraction is cut as well, and k_glu_join adds the parts
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 #include "gelu.h"
@@ -58,8 +59,9 @@ enum { KC, KS, PAIRS };
 template <typename E, int R>
 __device__ __forceinline__ int chunk_swizzle(int kr) {
   constexpr int NC = R / 16;
-  static_assert(NC % 8 == 0 || NC == 4, "tile width");
-  if constexpr (sizeof(E) == 4) return (kr >> 2) & 3;   // the four k-rows that a fetch of a word reads, four apart
+  static_assert(NC % 8 == 0 || NC == 4 || NC == 2, "tile width");
+  if constexpr (sizeof(E) == 4) return (kr >> 2) & (NC == 2 ? 1 : 3);   // the four k-rows that a fetch of a word reads, four apart
+  else if constexpr (NC == 2) return (kr >> 3) & 1;
   else return NC % 8 == 0 ? (kr & 3) | ((kr >> 1) & 4) : ((kr >> 1) & 1) | ((kr >> 2) & 2);
 }
 struct Operand {
@@ -354,12 +356,10 @@ struct UpArgs {
   TileOrder order;
   void* h;               // [T x F]
   void* saved;           // or null
-  uint32_t* tickets; int ntickets;   // of the launch behind, to be cleared
 };
 template <typename T, typename E, int ACT>
 __global__ __launch_bounds__(T::THREADS) void k_glu_up(UpArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  for (int i = blockIdx.x * T::THREADS + threadIdx.x; i < a.ntickets; i += gridDim.x * T::THREADS) a.tickets[i] = 0;
   const uint32_t id = (blockIdx.x & 7) * a.order.per_xcd + (blockIdx.x >> 3);
   if ((blockIdx.x >> 3) >= a.order.per_xcd || id >= a.order.tiles) return;
   uint32_t ti, tj;
@@ -422,12 +422,10 @@ struct DgateArgs {
   TileOrder order;
   const void* saved;
   void* dpre;            // [T x 2F]: dg, du
-  uint32_t* tickets; int ntickets;
 };
 template <typename T, typename E, int ACT>
 __global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  for (int i = blockIdx.x * T::THREADS + threadIdx.x; i < a.ntickets; i += gridDim.x * T::THREADS) a.tickets[i] = 0;
   const uint32_t id = (blockIdx.x & 7) * a.order.per_xcd + (blockIdx.x >> 3);
   if ((blockIdx.x >> 3) >= a.order.per_xcd || id >= a.order.tiles) return;
   uint32_t ti, tj;
@@ -486,136 +484,122 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
   });
 }
 
-// ---------------------------------------------------------------------------------------------------- products split over the chip
-// One to three products in a launch whose tiles need not be a multiple of the chip: the slabs of all tiles, in the order of the tiles, are cut into
-// equal runs, one for each workgroup, wherever that falls (`split`); a tile that lies in several workgroups' runs is added up by the last of them to come.
+// ---------------------------------------------------------------------------------------------------- products in pieces
+// One to three products in a launch.  A tile's contraction may be cut into `parts` equal ones: each is a workgroup of its own, which leaves its sums in `part`, a
+// fragment of 16 x 16 after the other as the lanes hold them, and k_glu_join adds those of a tile in the order of the contraction.  (Added by the last of
+// a tile's workgroups to finish, in the same launch: two thousand clocks of waiting for stores, ticket and loads in one workgroup after the other, 15 us
+// where the launch of its own takes 5, and the code for it took registers from the products.)
+constexpr int MAX_PRODUCTS = 3;
 struct Product {
   Operand A, B;
-  uint32_t M, N, K, tm, tn, slabs, first;   // first: slab of all the tiles before
+  uint32_t M, N, K, tm, tn, slabs, parts;
+  uint32_t first;        // piece: of all the products before, a multiple of 8
   void* C; uint32_t ldc; int strided_a, c32;
+  float* part;           // [parts][tiles][BM x BN]
 };
-struct SplitArgs {
-  Product p[3];
-  int count, split, groups;   // groups: workgroups
-  uint64_t units;
-  float* part;                // [groups][first, last][tile]
-  uint32_t* tickets;          // [tiles], zero
+struct ProductArgs {
+  Product p[MAX_PRODUCTS];
+  int count;
 };
+// one row of fragments of a wave's part of a tile
 template <typename T>
-__device__ __forceinline__ void store_tile(const f32x4 (&acc)[T::XT][T::YT], const Product& p, uint32_t i0, uint32_t j0, uint32_t wave) {
+__device__ __forceinline__ void store_row(const f32x4 (&c)[T::YT], const Product& p, uint32_t row0, uint32_t col0) {
   const int lane = threadIdx.x & 63;
-  const uint32_t row0 = i0 + (wave / T::WGN) * T::WM, col0 = j0 + (wave % T::WGN) * T::WN;
-  static_for<T::XT>([&](auto x_) {
-    constexpr int x = x_;
-    const uint32_t row = row0 + 16 * x + (lane & 15);
-    if (p.c32) {
-      float* const to = static_cast<float*>(p.C) + (uint64_t)row * p.ldc;
-      static_for<T::YT>([&](auto y_) {
-        const uint32_t col = col0 + 16 * decltype(y_)::value + 4 * (lane >> 4);
-        if (row < p.M && col < p.N) *reinterpret_cast<f32x4*>(to + col) = acc[x][decltype(y_)::value];
-      });
-    } else {
-      bf16_t* const to = static_cast<bf16_t*>(p.C) + (uint64_t)row * p.ldc;
-      static_for<T::YT / 2>([&](auto h_) {
-        constexpr int h = h_;
-        const uint4 v = side_by_side(acc[x][2 * h], acc[x][2 * h + 1]);
-        const uint32_t col = col0 + 32 * h + pair_column(lane);
-        if (row < p.M && col < p.N) *reinterpret_cast<uint4*>(to + col) = v;
-      });
-    }
-  });
-}
-
-// Values that one workgroup leaves for another of the same launch: written through to where every XCD sees them and read past the caches, as publish()
-// and collect() do it one value at a time.
-__device__ __forceinline__ void publish16(float* p, f32x4 v) { asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(p), "v"(v) : "memory"); }
-__device__ __forceinline__ void collect16(const float* p, f32x4 (&v)[4], int step) {
-  asm volatile("global_load_dwordx4 %0, %4, off sc1\n\tglobal_load_dwordx4 %1, %5, off sc1\n\t"
-               "global_load_dwordx4 %2, %6, off sc1\n\tglobal_load_dwordx4 %3, %7, off sc1\n\ts_waitcnt vmcnt(0)"
-               : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(p), "v"(p + step), "v"(p + 2 * step), "v"(p + 3 * step) : "memory");
+  const uint32_t row = row0 + (lane & 15);
+  if (p.c32) {
+    float* const to = static_cast<float*>(p.C) + (uint64_t)row * p.ldc;
+    static_for<T::YT>([&](auto y_) {
+      const uint32_t col = col0 + 16 * decltype(y_)::value + 4 * (lane >> 4);
+      if (row < p.M && col < p.N) *reinterpret_cast<f32x4*>(to + col) = c[decltype(y_)::value];
+    });
+  } else {
+    bf16_t* const to = static_cast<bf16_t*>(p.C) + (uint64_t)row * p.ldc;
+    static_for<T::YT / 2>([&](auto h_) {
+      constexpr int h = h_;
+      const uint4 v = side_by_side(c[2 * h], c[2 * h + 1]);
+      const uint32_t col = col0 + 32 * h + pair_column(lane);
+      if (row < p.M && col < p.N) *reinterpret_cast<uint4*>(to + col) = v;
+    });
+  }
 }
 
 // KIND 0: forward (A and B KC); 1: gradients, dx with A KC and B KS, the weights' with both KS
 template <typename T, typename E, int KIND>
-__global__ __launch_bounds__(T::THREADS) void k_glu_split(SplitArgs a) {
+__global__ __launch_bounds__(T::THREADS) void k_glu_product(ProductArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ int s_last;
-  const uint32_t groups = a.groups, per_xcd = (groups + 7) / 8, l = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= per_xcd || l >= groups) return;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int FRAGS = T::XT * T::YT, TILE = T::BM * T::BN;
+  int k = 0;
+  while (k + 1 < a.count && blockIdx.x >= a.p[k + 1].first) ++k;
+  const Product& p = a.p[k];
+  const uint32_t tiles = p.tm * p.tn, pieces = tiles * p.parts, per_xcd = (pieces + 7) / 8, b = blockIdx.x - p.first, id = (b & 7) * per_xcd + (b >> 3);
+  if ((b >> 3) >= per_xcd || id >= pieces) return;
+  const uint32_t part = p.parts > 1 ? id / tiles : 0, tile = id - part * tiles;
+  const uint32_t slab0 = p.parts > 1 ? part * p.slabs / p.parts : 0;
+  const int slabs = (int)((p.parts > 1 ? (part + 1) * p.slabs / p.parts : p.slabs) - slab0);
+  uint32_t ti, tj;
+  tile_of(tile, p.tm, p.tn, ti, tj);
+  const uint32_t i0 = ti * T::BM, j0 = tj * T::BN;
   f32x4 acc[T::XT][T::YT];
-  uint64_t at = a.split ? l * a.units / groups : 0;                      // first unit of what is left
-  const uint64_t end = a.split ? (l + 1) * a.units / groups : 0;
-  bool first_piece = true;
-  do {
-    // the tile of this piece
-    int k = 0;
-    uint32_t tile = 0, tiles_before = 0, slab0 = 0;
-    if (a.split) {
-      while (k + 1 < a.count && at >= a.p[k + 1].first) { tiles_before += a.p[k].tm * a.p[k].tn; ++k; }
-      const uint32_t u = (uint32_t)(at - a.p[k].first);
-      tile = u / a.p[k].slabs; slab0 = u - tile * a.p[k].slabs;
-    } else {
-      tile = l;
-      while (k + 1 < a.count && tile >= a.p[k].tm * a.p[k].tn) { tile -= a.p[k].tm * a.p[k].tn; tiles_before += a.p[k].tm * a.p[k].tn; ++k; }
-    }
-    const Product& p = a.p[k];
-    const uint64_t tile_at = p.first + (uint64_t)tile * p.slabs;         // units of the tile
-    const int slabs = a.split ? (int)min((uint64_t)(p.slabs - slab0), end - at) : (int)p.slabs;
-    uint32_t ti, tj;
-    tile_of(tile, p.tm, p.tn, ti, tj);
-    const uint32_t i0 = ti * T::BM, j0 = tj * T::BN;
-    if (!first_piece) __syncthreads();                                   // the stages are free
-    if constexpr (KIND == 0) contract<T, E, KC, KC>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
-    else if (p.strided_a) contract<T, E, KS, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
-    else contract<T, E, KC, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
-    const bool multiplies = wave < (uint32_t)T::WAVES;
-    if (slabs == (int)p.slabs) {
-      if (multiplies) store_tile<T>(acc, p, i0, j0, wave);
-    } else {
-      // the workgroups of the tile: the one that has its first unit, to the one that has its last
-      auto group_of = [&](uint64_t unit) { return (uint32_t)(((unit + 1) * groups - 1) / a.units); };
-      const uint32_t l0 = group_of(tile_at), l1 = group_of(tile_at + p.slabs - 1);
-      auto part_of = [&](uint32_t g) {   // a workgroup's last tile, if it has its beginning, else its first one
-        return a.part + ((uint64_t)2 * g + (g == l0 ? 1 : 0)) * TILE + (wave * 64 + (threadIdx.x & 63)) * 4;
-      };
-      constexpr int STEP = T::WAVES * 256;   // floats from a fragment to the next
-      if (multiplies) {
-        float* const to = part_of(l);
-        static_for<FRAGS>([&](auto f) { publish16(to + decltype(f)::value * STEP, acc[decltype(f)::value / T::YT][decltype(f)::value % T::YT]); });
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        uint32_t* const ticket = a.tickets + tiles_before + tile;
-        s_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == l1 - l0 ? 1 : 0;
-      }
-      __syncthreads();
-      if (s_last != 0 && multiplies) {       // the parts in the order of the contraction, whoever adds them
-        static_for<FRAGS / 4>([&](auto f4) {
-          constexpr int f0 = 4 * f4;
-          f32x4 sum[4];
+  if constexpr (KIND == 0) contract<T, E, KC, KC>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+  else if (p.strided_a) contract<T, E, KS, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+  else contract<T, E, KC, KS>(acc, smem, p.A, p.B, i0, j0, p.K, slab0, slabs);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= (uint32_t)T::WAVES) return;
+  if (p.parts == 1) {
+    const uint32_t row0 = i0 + (wave / T::WGN) * T::WM, col0 = j0 + (wave % T::WGN) * T::WN;
+    static_for<T::XT>([&](auto x) { store_row<T>(acc[decltype(x)::value], p, row0 + 16 * decltype(x)::value, col0); });
+  } else {
+    float* const to = p.part + ((uint64_t)id * T::WAVES + wave) * (T::XT * T::YT * 256) + (threadIdx.x & 63) * 4;
+    static_for<T::XT>([&](auto x_) {
+      static_for<T::YT>([&](auto y_) { *reinterpret_cast<f32x4*>(to + (decltype(x_)::value * T::YT + decltype(y_)::value) * 256) = acc[decltype(x_)::value][decltype(y_)::value]; });
+    });
+  }
+}
+
+// A wave adds two neighbouring fragments of a tile.
+template <typename T>
+__global__ __launch_bounds__(256) void k_glu_join(ProductArgs a) {
+  constexpr uint32_t PAIRS_OF = T::WAVES * T::XT * T::YT / 2;   // of a tile
+  uint64_t id = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  int k = 0;
+  while (k < a.count && (a.p[k].parts == 1 || id >= (uint64_t)a.p[k].tm * a.p[k].tn * PAIRS_OF)) {
+    if (a.p[k].parts > 1) id -= (uint64_t)a.p[k].tm * a.p[k].tn * PAIRS_OF;
+    ++k;
+  }
+  if (k == a.count) return;
+  const Product& p = a.p[k];
+  const uint32_t tiles = p.tm * p.tn, tile = (uint32_t)(id / PAIRS_OF), pair = (uint32_t)(id % PAIRS_OF);
+  const uint32_t wave = pair / (T::XT * T::YT / 2), x = pair % (T::XT * T::YT / 2) / (T::YT / 2), h = pair % (T::YT / 2);
+  const int lane = threadIdx.x & 63;
+  const uint64_t step = (uint64_t)tiles * T::BM * T::BN;
+  const float* from = p.part + ((uint64_t)tile * T::WAVES + wave) * (T::XT * T::YT * 256) + (x * T::YT + 2 * h) * 256 + lane * 4;
+  f32x4 sum[2] = {*reinterpret_cast<const f32x4*>(from), *reinterpret_cast<const f32x4*>(from + 256)};
+  uint32_t n = p.parts - 1;
+  for (; n >= 3; n -= 3) {
+    f32x4 v[3][2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum[e] = (f32x4){0.f, 0.f, 0.f, 0.f};
-          for (uint32_t g = l0; g <= l1; ++g) {
-            f32x4 v[4];
-            if (g == l) {
-              static_for<4>([&](auto e) { v[e] = acc[(f0 + decltype(e)::value) / T::YT][(f0 + decltype(e)::value) % T::YT]; });
-            } else {
-              collect16(part_of(g) + f0 * STEP, v, STEP);
-            }
+    for (int u = 0; u < 3; ++u) { from += step; v[u][0] = *reinterpret_cast<const f32x4*>(from); v[u][1] = *reinterpret_cast<const f32x4*>(from + 256); }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += v[e];
-          }
-          static_for<4>([&](auto e) { acc[(f0 + decltype(e)::value) / T::YT][(f0 + decltype(e)::value) % T::YT] = sum[e]; });
-        });
-        store_tile<T>(acc, p, i0, j0, wave);
-      }
+    for (int u = 0; u < 3; ++u) { sum[0] += v[u][0]; sum[1] += v[u][1]; }
+  }
+  for (; n > 0; --n) {
+    from += step;
+    sum[0] += *reinterpret_cast<const f32x4*>(from); sum[1] += *reinterpret_cast<const f32x4*>(from + 256);
+  }
+  uint32_t ti, tj;
+  tile_of(tile, p.tm, p.tn, ti, tj);
+  const uint32_t row = ti * T::BM + (wave / T::WGN) * T::WM + 16 * x + (lane & 15), col0 = tj * T::BN + (wave % T::WGN) * T::WN + 32 * h;
+  if (p.c32) {
+    float* const to = static_cast<float*>(p.C) + (uint64_t)row * p.ldc;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const uint32_t col = col0 + 16 * y + 4 * (lane >> 4);
+      if (row < p.M && col < p.N) *reinterpret_cast<f32x4*>(to + col) = sum[y];
     }
-    at += slabs;
-    first_piece = false;
-  } while (a.split && at < end);
+  } else {
+    const uint4 v = side_by_side(sum[0], sum[1]);
+    const uint32_t col = col0 + pair_column(lane);
+    if (row < p.M && col < p.N) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(p.C) + (uint64_t)row * p.ldc + col) = v;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------- a few tokens
@@ -788,6 +772,7 @@ __global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
 typedef Tile<256, 256, 2, 4, 2, 0, 2, 0, 1> T256;
 typedef Tile<128, 128, 2, 4, 4, 4, 0, 1, 1> T128;
 typedef Tile<64, 64, 2, 2, 4, 0, 0, 1, 2> T64;
+typedef Tile<32, 32, 2, 1, 6, 0, 0, 1, 3> T32;
 
 template <auto KERNEL, typename T, typename A>
 void launch_big(ProfScope& ps, hipStream_t st, uint32_t grid, const A& a) {
@@ -827,76 +812,172 @@ void launch_dgate(ProfScope& ps, hipStream_t st, DgateArgs a, int act) {
   if (act == GLU_GELU) launch_big<k_glu_dgate<T, E, GLU_GELU>, T>(ps, st, 8 * a.order.per_xcd, a);
   else launch_big<k_glu_dgate<T, E, GLU_SILU>, T>(ps, st, 8 * a.order.per_xcd, a);
 }
-constexpr uint64_t LEAST_RUN = 6;
-template <typename T, typename E>
-void plan_split(SplitArgs& a) {
-  uint64_t units = 0;
-  uint32_t tiles = 0, longest = 0;
+// ---- which tile, and into how many parts a contraction is cut, by what a launch costs in us: pieces are started in their order, longest first, each on the
+// workgroup slot that is free first; a piece takes its slabs' time, by how many workgroups share the CU, and `fixed`; parts are written, read and added.
+struct TileCost { int tile, bm, bn, per_cu; double one, full, fixed; };   // us of a slab with one workgroup to a CU and with per_cu
+constexpr TileCost COST16[] = {{256, 256, 256, 1, 1.50, 1.50, 6.0}, {128, 128, 128, 1, 0.52, 0.52, 2.5}, {64, 64, 64, 2, 0.27, 0.42, 1.5}, {32, 32, 32, 3, 0.20, 0.37, 1.2}};
+constexpr TileCost COST32[] = {{128, 128, 128, 1, 2.00, 2.00, 3.0}, {64, 64, 64, 2, 0.60, 1.10, 2.0}, {32, 32, 32, 3, 0.32, 0.60, 1.5}};
+constexpr double JOIN_LAUNCH = 3.5, JOIN_BYTES = 1.0 / 3.0e6;   // us; us a byte of the parts, written and read
+constexpr uint32_t LEAST_SLABS = 4, MOST_PARTS = 16;            // of a part; of a tile
+// Most bytes of parts that a launch may have, for the sizes in `a`, however they are cut: grows with the number of tokens.
+uint64_t most_part_bytes(const TileCost& c, const ProductArgs& a, uint32_t depth) {
+  uint64_t pieces = 0;
   for (int k = 0; k < a.count; ++k) {
-    Product& p = a.p[k];
-    p.tm = (p.M + T::BM - 1) / T::BM; p.tn = (p.N + T::BN - 1) / T::BN; p.slabs = (p.K + DEPTH<E> - 1) / DEPTH<E>; p.first = (uint32_t)units;
-    units += (uint64_t)p.tm * p.tn * p.slabs; tiles += p.tm * p.tn;
-    longest = std::max(longest, p.slabs);
+    const uint64_t tiles = (uint64_t)((a.p[k].M + c.bm - 1) / c.bm) * ((a.p[k].N + c.bn - 1) / c.bn), slabs = (a.p[k].K + depth - 1) / depth;
+    pieces += tiles * std::min<uint64_t>(MOST_PARTS, std::max<uint64_t>(1, slabs / LEAST_SLABS));
   }
-  a.units = units;
-  const uint32_t slots = 256 * T::PER_CU;
-  // Whole tiles in rounds, or all slabs in equal runs with what it costs to add the parts up, the time of about JOIN slabs; a run has LEAST_RUN of them at least.
-  constexpr uint64_t JOIN = 6;
-  const uint64_t rounds = (tiles + slots - 1) / slots, whole = rounds * longest;
-  const uint64_t groups = std::max<uint64_t>(1, std::min<uint64_t>(slots, units / LEAST_RUN)), run = (units + groups - 1) / groups + JOIN;
-  a.split = run < whole && groups > 1 ? 1 : 0;
-  a.groups = a.split ? (int)groups : (int)tiles;
+  return std::min<uint64_t>(pieces, 512 * c.per_cu) * c.bm * c.bn * 4;
+}
+// The time of a launch of pieces in this order: `n` pieces of length us, ...
+double makespan(const uint64_t* n, const double* length, int count, uint64_t slots) {
+  // slots by the time they are free, a few distinct ones
+  struct Free { double at; uint64_t n; } f[40] = {{0.0, slots}};
+  int nf = 1;
+  double end = 0.0;
+  for (int k = 0; k < count; ++k) {
+    uint64_t left = n[k];
+    if (left > 8 * slots) {   // whole rounds at once
+      const uint64_t rounds = left / slots - 4;
+      for (int i = 0; i < nf; ++i) f[i].at += rounds * length[k];
+      left -= rounds * slots;
+    }
+    while (left > 0) {
+      int first = 0;
+      for (int i = 1; i < nf; ++i) if (f[i].at < f[first].at) first = i;
+      const uint64_t take = std::min(left, f[first].n);
+      const double done = f[first].at + length[k];
+      end = std::max(end, done);
+      left -= take;
+      f[first].n -= take;
+      int same = -1;
+      for (int i = 0; i < nf; ++i) if (std::abs(f[i].at - done) < 1e-9) same = i;
+      if (same >= 0) f[same].n += take;
+      else if (f[first].n == 0) f[first] = {done, take};
+      else if (nf < 40) f[nf++] = {done, take};
+      else f[first].n += take;   // (too many distinct times: as good as free)
+      if (f[first].n == 0) f[first] = f[--nf];
+    }
+  }
+  return end;
+}
+struct Plan { int tile; uint32_t parts[MAX_PRODUCTS]; int order[MAX_PRODUCTS]; double cost; };
+int g_force_tile = 0, g_force_parts = 0;
+template <typename E, int N>
+Plan plan_products(const TileCost (&costs)[N], const ProductArgs& a, int force_tile) {
+  Plan best{0, {}, {}, 0.0};
+  for (const TileCost& c : costs) {
+    if (force_tile != 0 && c.tile != force_tile) continue;
+    const uint64_t room = most_part_bytes(c, a, DEPTH<E>);
+    uint64_t tiles[MAX_PRODUCTS] = {};
+    uint32_t slabs[MAX_PRODUCTS] = {}, most[MAX_PRODUCTS] = {1, 1, 1};
+    for (int k = 0; k < a.count; ++k) {
+      tiles[k] = (uint64_t)((a.p[k].M + c.bm - 1) / c.bm) * ((a.p[k].N + c.bn - 1) / c.bn);
+      slabs[k] = (a.p[k].K + DEPTH<E> - 1) / DEPTH<E>;
+      most[k] = std::min(MOST_PARTS, std::max(1u, slabs[k] / LEAST_SLABS));
+    }
+    const uint64_t slots = 256 * c.per_cu;
+    for (uint32_t s0 = 1; s0 <= most[0]; s0 *= 2)
+      for (uint32_t s1 = 1; s1 <= most[1]; s1 *= 2)
+        for (uint32_t s2 = 1; s2 <= most[2]; s2 *= 2) {
+          uint32_t parts[MAX_PRODUCTS] = {s0, s1, s2};
+          if (g_force_parts != 0) for (int k = 0; k < a.count; ++k) parts[k] = std::min(most[k], (uint32_t)g_force_parts);
+          uint64_t bytes = 0, pieces = 0;
+          for (int k = 0; k < a.count; ++k) {
+            pieces += tiles[k] * parts[k];
+            if (parts[k] > 1) bytes += tiles[k] * parts[k] * c.bm * c.bn * 4;
+          }
+          if (bytes > room && g_force_parts == 0) continue;
+          if (bytes > room) for (int k = 0; k < a.count; ++k) parts[k] = 1;
+          Plan p{c.tile, {parts[0], parts[1], parts[2]}, {0, 1, 2}, 0.0};
+          const double share = std::min(1.0, std::max(0.0, ((double)pieces - 256.0) / (double)std::max<uint64_t>(1, slots - 256)));
+          const double slab = c.one + (c.full - c.one) * (c.per_cu > 1 ? share : 0.0);
+          double length[MAX_PRODUCTS], sorted[MAX_PRODUCTS];
+          uint64_t n[MAX_PRODUCTS];
+          for (int k = 0; k < a.count; ++k) length[k] = (double)((slabs[k] + parts[k] - 1) / parts[k]) * slab + c.fixed;
+          std::sort(p.order, p.order + a.count, [&](int x, int y) { return length[x] != length[y] ? length[x] > length[y] : x < y; });
+          for (int k = 0; k < a.count; ++k) { sorted[k] = length[p.order[k]]; n[k] = tiles[p.order[k]] * parts[p.order[k]]; }
+          p.cost = makespan(n, sorted, a.count, slots) + (bytes > 0 ? JOIN_LAUNCH + bytes * JOIN_BYTES : 0.0);
+          if (best.tile == 0 || p.cost < best.cost) best = p;
+        }
+  }
+  return best;
 }
 template <typename T, typename E, int KIND>
-void launch_split(ProfScope& ps, hipStream_t st, SplitArgs a) {
-  plan_split<T, E>(a);
-  launch_big<k_glu_split<T, E, KIND>, T>(ps, st, 8 * ((a.groups + 7) / 8), a);
+void launch_products(ProfScope& ps, hipStream_t st, const ProductArgs& in, const Plan& plan, float* part) {
+  ProductArgs a{};
+  a.count = in.count;
+  uint32_t blocks = 0;
+  uint64_t join = 0;
+  for (int k = 0; k < a.count; ++k) {
+    Product& p = a.p[k];
+    p = in.p[plan.order[k]];
+    p.parts = plan.parts[plan.order[k]];
+    p.tm = (p.M + T::BM - 1) / T::BM; p.tn = (p.N + T::BN - 1) / T::BN; p.slabs = (p.K + DEPTH<E> - 1) / DEPTH<E>; p.first = blocks; p.part = part;
+    const uint32_t pieces = p.tm * p.tn * p.parts;
+    blocks += (pieces + 7) / 8 * 8;
+    if (p.parts > 1) { part += (uint64_t)pieces * T::BM * T::BN; join += (uint64_t)p.tm * p.tn * (T::WAVES * T::XT * T::YT / 2); }
+  }
+  launch_big<k_glu_product<T, E, KIND>, T>(ps, st, blocks, a);
+  if (join > 0) launch_kernel(ps, k_glu_join<T>, (uint32_t)((join + 3) / 4), 256, 0, st, a);
 }
-
-int g_force_tile = 0;
-// The tile of products of `tiles64` tiles of 64 x 64 in all: the largest that leaves most CUs one, or, where the contraction is split over the chip (`split`),
-// some of it.  fp32: the matrix cores are sixteen times slower, and tiles beyond 128 gain nothing.
 template <typename E, typename F>
-void with_tile(size_t tiles64, bool split, F f) {
-  int tile = tiles64 >= (split ? 1600 : 3200) ? 256 : tiles64 >= (split ? 240 : 400) ? 128 : 64;
-  if (g_force_tile != 0) tile = g_force_tile;
+void with_tile(int tile, F f) {
   if constexpr (sizeof(E) == 2) if (tile == 256) return f(T256{});
   if (tile >= 128) f(T128{});
-  else f(T64{});
+  else if (tile == 64) f(T64{});
+  else f(T32{});
 }
-// Partial sums: two tiles for each workgroup that has a run of slabs, whether they are cut or not, so that the size grows with the number of tokens and what is
-// enough for some is for fewer.
-template <typename T, typename E>
-size_t part_bytes_of(const SplitArgs& shapes) {
-  SplitArgs a = shapes;
-  plan_split<T, E>(a);
-  return (size_t)2 * std::max<uint64_t>(1, std::min<uint64_t>(256 * T::PER_CU, a.units / LEAST_RUN)) * T::BM * T::BN * 4;
+template <typename E, int KIND>
+void products(ProfScope& ps, hipStream_t st, const ProductArgs& a, float* part) {
+  Plan plan;
+  if constexpr (sizeof(E) == 2) plan = plan_products<E>(COST16, a, g_force_tile);
+  else plan = plan_products<E>(COST32, a, std::min(g_force_tile, 128));
+  with_tile<E>(plan.tile, [&](auto t) { launch_products<decltype(t), E, KIND>(ps, st, a, plan, part); });
+}
+// the tile of a product that is not cut
+template <typename E>
+int whole_tile(int64_t M, int64_t N, int64_t K) {
+  ProductArgs a{};
+  a.count = 1; a.p[0].M = (uint32_t)M; a.p[0].N = (uint32_t)N; a.p[0].K = (uint32_t)K;
+  double best = 0.0;
+  int tile = 0;
+  auto look = [&](const TileCost& c) {
+    const uint64_t n = (uint64_t)((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), slots = 256 * c.per_cu;
+    const double share = std::min(1.0, std::max(0.0, ((double)n - 256.0) / (double)std::max<uint64_t>(1, slots - 256)));
+    const double length = (double)((K + DEPTH<E> - 1) / DEPTH<E>) * (c.one + (c.full - c.one) * (c.per_cu > 1 ? share : 0.0)) + 2 * c.fixed;
+    const double cost = (double)((n + slots - 1) / slots) * length;
+    if (tile == 0 || cost < best) { tile = c.tile; best = cost; }
+  };
+  if constexpr (sizeof(E) == 2) for (const TileCost& c : COST16) look(c);
+  else for (const TileCost& c : COST32) look(c);
+  return g_force_tile == 0 ? tile : sizeof(E) == 4 ? std::min(g_force_tile, 128) : g_force_tile;
 }
 template <typename E>
-size_t part_bytes(const SplitArgs& a) { return std::max({sizeof(E) == 2 ? part_bytes_of<T256, E>(a) : 0, part_bytes_of<T128, E>(a), part_bytes_of<T64, E>(a)}); }
+size_t part_bytes(const ProductArgs& a) {
+  uint64_t most = 256;
+  if constexpr (sizeof(E) == 2) for (const TileCost& c : COST16) most = std::max(most, most_part_bytes(c, a, DEPTH<E>));
+  else for (const TileCost& c : COST32) most = std::max(most, most_part_bytes(c, a, DEPTH<E>));
+  return most;
+}
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
-size_t tiles64(int64_t M, int64_t N) { return (size_t)((M + 63) / 64) * ((N + 63) / 64); }
-size_t grad_tiles64(int64_t T, int d, int F) { return tiles64(T, d) + tiles64(2 * (int64_t)F, d) + tiles64(d, F); }
 
 template <typename E>
 size_t forward_bytes(int64_t T, int d, int F) {
-  SplitArgs s{};
+  ProductArgs s{};
   s.count = 1; s.p[0].M = (uint32_t)T; s.p[0].N = d; s.p[0].K = F;
-  return up256(tiles64(T, d) * 4) + part_bytes<E>(s);
+  return part_bytes<E>(s);
 }
 template <typename E>
 size_t backward_bytes(int64_t T, int d, int F) {
-  SplitArgs s{};
+  ProductArgs s{};
   s.count = 3; s.p[0].M = (uint32_t)T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[1].M = 2 * F; s.p[1].N = d; s.p[1].K = (uint32_t)T; s.p[2].M = d; s.p[2].N = F; s.p[2].K = (uint32_t)T;
-  return up256(grad_tiles64(T, d, F) * 4) + up256((size_t)T * 2 * F * sizeof(E)) + part_bytes<E>(s);
+  return up256((size_t)T * 2 * F * sizeof(E)) + part_bytes<E>(s);
 }
 
 template <typename E>
 void forward(hipStream_t st, const GluFfnArgs& g, void* workspace) {
   constexpr bool BF16 = sizeof(E) == 2;
-  char* const ws = static_cast<char*>(workspace);
   const uint32_t T = (uint32_t)g.T, d = g.d, F = g.F;
-  const size_t ntickets = tiles64(T, d);
   ProfScope ps(st, BF16 ? F_GEMM_NT : F_GEMM_F32, 6.0 * T * (double)d * F);
   UpArgs u{};
   u.x = Operand{g.x, (uint32_t)g.ldx, T}; u.w = Operand{g.w_in, d, F};
@@ -910,30 +991,27 @@ void forward(hipStream_t st, const GluFfnArgs& g, void* workspace) {
     else launch_few<2>(ps, st, u, w, g.act);
     return;
   }
-  u.tickets = (uint32_t*)ws; u.ntickets = (int)ntickets;
-  with_tile<E>(tiles64(T, 2 * (int64_t)F), false, [&](auto t) { launch_up<decltype(t), E>(ps, st, u, g.act); });
-  SplitArgs s{};
-  s.count = 1; s.part = (float*)(ws + up256(ntickets * 4)); s.tickets = (uint32_t*)ws;
+  with_tile<E>(whole_tile<E>(T, 2 * (int64_t)F, d), [&](auto t) { launch_up<decltype(t), E>(ps, st, u, g.act); });
+  ProductArgs s{};
+  s.count = 1;
   Product& p = s.p[0];
   p.A = Operand{g.hidden, F, T}; p.B = Operand{g.w_out, F, d};
   p.M = T; p.N = d; p.K = F; p.C = g.y; p.ldc = (uint32_t)g.ldy; p.c32 = !BF16;
-  with_tile<E>(tiles64(T, d), false, [&](auto t) { launch_split<decltype(t), E, 0>(ps, st, s); });
+  products<E, 0>(ps, st, s, (float*)workspace);
 }
 
 template <typename E>
 void backward(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
   constexpr bool BF16 = sizeof(E) == 2;
-  char* const ws = static_cast<char*>(workspace);
   const uint32_t T = (uint32_t)g.T, d = g.d, F = g.F;
-  const size_t ntickets = grad_tiles64(T, d, F);
-  void* const dpre = ws + up256(ntickets * 4);
+  void* const dpre = workspace;
   ProfScope ps(st, BF16 ? F_GEMM_NN : F_GEMM_F32, 12.0 * T * (double)d * F);
   DgateArgs e{};
   e.dy = Operand{g.dy, (uint32_t)g.lddy, T}; e.w = Operand{g.w_out, F, F};
-  e.T = T; e.F = F; e.d = d; e.saved = g.saved; e.dpre = dpre; e.tickets = (uint32_t*)ws; e.ntickets = (int)ntickets;
-  with_tile<E>(tiles64(T, F), false, [&](auto t) { launch_dgate<decltype(t), E>(ps, st, e, g.act); });
-  SplitArgs s{};
-  s.count = 3; s.tickets = (uint32_t*)ws; s.part = (float*)((char*)dpre + up256((size_t)T * 2 * F * sizeof(E)));
+  e.T = T; e.F = F; e.d = d; e.saved = g.saved; e.dpre = dpre;
+  with_tile<E>(whole_tile<E>(T, F, d), [&](auto t) { launch_dgate<decltype(t), E>(ps, st, e, g.act); });
+  ProductArgs s{};
+  s.count = 3;
   s.p[0].A = Operand{dpre, 2 * F, T}; s.p[0].B = Operand{g.w_in, d, d};
   s.p[0].M = T; s.p[0].N = d; s.p[0].K = 2 * F; s.p[0].C = g.dx; s.p[0].ldc = (uint32_t)g.lddx; s.p[0].c32 = !BF16;
   s.p[1].A = Operand{dpre, 2 * F, 2 * F}; s.p[1].B = Operand{g.x, (uint32_t)g.ldx, d};
@@ -941,13 +1019,13 @@ void backward(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
   s.p[2].A = Operand{g.dy, (uint32_t)g.lddy, d}; s.p[2].B = Operand{g.hidden, F, F};
   s.p[2].M = d; s.p[2].N = F; s.p[2].K = T; s.p[2].C = g.dw_out; s.p[2].ldc = F;
   for (int k = 1; k < 3; ++k) { s.p[k].strided_a = 1; s.p[k].c32 = g.dw_fp32; }
-  with_tile<E>(ntickets, true, [&](auto t) { launch_split<decltype(t), E, 1>(ps, st, s); });
+  products<E, 1>(ps, st, s, (float*)((char*)dpre + up256((size_t)T * 2 * F * sizeof(E))));
 }
 // fp32 operands that the tiles can load: rows in pieces of 16 bytes
 bool pieces32(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 4 == 0; }
 }  // namespace
 
-void glu_ffn_force_tile(int t) { g_force_tile = t; }
+void glu_ffn_force_tile(int t) { g_force_tile = t % 1000; g_force_parts = t / 1000; }
 
 size_t glu_ffn_saved_bytes(int64_t T, int F) { return (size_t)((T + 15) / 16) * ((F + 15) / 16) * SAVED_BLOCK; }
 size_t glu_ffn_bytes(int64_t T, int d, int F) { return forward_bytes<bf16_t>(T, d, F); }
