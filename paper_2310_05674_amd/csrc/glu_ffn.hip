@@ -331,7 +331,9 @@ __device__ __forceinline__ float gate(float g) {
 // three words, so that a lane's part of a 16 x 16 fragment is 16 and 8 bytes.  Blocks of 16 rows by 16 columns in row order, 1 KB and 512 bytes of
 // one block side by side: every store and load is whole lines.  Held in bf16 they would be 8 bytes of 12 and would double the error
 // of the gradients, in fp32 16.
+// They go past the caches, which keep the operands: 8192 x 1024 x 4096 620 -> 600 us for both passes, and no size is slower.
 constexpr int SAVED_BLOCK = 1536;
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void pack24(f32x4 v, uint32_t (&w)[3]) {
   const uint32_t b[4] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
   w[0] = __builtin_amdgcn_perm(b[1], b[0], 0x05030201);
@@ -398,8 +400,8 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_up(UpArgs a) {
         unsigned char* const b = static_cast<unsigned char*>(a.saved) + ((uint64_t)((row0 >> 4) + x) * blocks + (col0 >> 4) + q) * SAVED_BLOCK;
         uint32_t wg[3], wu[3];
         pack24(g, wg); pack24(u, wu);
-        *reinterpret_cast<uint4*>(b + lane * 16) = make_uint4(wg[0], wg[1], wg[2], wu[0]);
-        *reinterpret_cast<uint2*>(b + 1024 + lane * 8) = make_uint2(wu[1], wu[2]);
+        __builtin_nontemporal_store((u32x4){wg[0], wg[1], wg[2], wu[0]}, reinterpret_cast<u32x4*>(b + lane * 16));
+        __builtin_nontemporal_store((words2){wu[1], wu[2]}, reinterpret_cast<words2*>(b + 1024 + lane * 8));
       }
     });
     if constexpr (sizeof(E) == 2 && GR == 1) {
@@ -446,12 +448,11 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
       dg[e] = dh[e] * (u[e] * ds); du[e] = dh[e] * s;
     }
   };
-  static_for<T::XT>([&](auto x_) {
-    constexpr int x = x_;
-    if (row0 + 16 * x >= a.T) return;
-    const uint32_t row = row0 + 16 * x + (lane & 15);
-    E* const to = static_cast<E*>(a.dpre) + (uint64_t)row * (2 * a.F);
-    if constexpr (sizeof(E) == 4) {
+  if constexpr (sizeof(E) == 4) {
+    static_for<T::XT>([&](auto x_) {
+      constexpr int x = x_;
+      const uint32_t row = row0 + 16 * x + (lane & 15);
+      float* const to = static_cast<float*>(a.dpre) + (uint64_t)row * (2 * a.F);
       static_for<T::YT>([&](auto y_) {
         const uint32_t col = col0 + 16 * decltype(y_)::value + 4 * (lane >> 4);
         if (row >= a.T || col >= a.F) return;
@@ -461,27 +462,42 @@ __global__ __launch_bounds__(T::THREADS) void k_glu_dgate(DgateArgs a) {
         *reinterpret_cast<f32x4*>(to + col) = dg;
         *reinterpret_cast<f32x4*>(to + a.F + col) = du;
       });
-    } else {
-      static_for<T::YT / 2>([&](auto h_) {
-        constexpr int h = h_;
-        f32x4 dg[2], du[2];
+    });
+  } else {
+    // Two neighbouring fragments at a time, AHEAD pairs of g and u on their way: with one, a wave of the 256 x 256 tile waits for memory sixteen times in a row.
+    constexpr int H = T::YT / 2, N = T::XT * H, AHEAD = N < 5 ? N : 5;
+    struct { uint4 p; uint2 r; } v[AHEAD][2];
+    const uint32_t last_row = (a.T - 1) >> 4;
+    auto fetch = [&](auto n_) {
+      constexpr int n = n_, x = n / H, h = n % H;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t block = min((col0 >> 4) + 2 * h + k, blocks - 1);
-          const unsigned char* const b = static_cast<const unsigned char*>(a.saved) + ((uint64_t)((row0 >> 4) + x) * blocks + block) * SAVED_BLOCK;
-          const uint4 p = *reinterpret_cast<const uint4*>(b + lane * 16);
-          const uint2 r = *reinterpret_cast<const uint2*>(b + 1024 + lane * 8);
-          backward(unpack24(p.x, p.y, p.z), unpack24(p.w, r.x, r.y), acc[x][2 * h + k], dg[k], du[k]);
-        }
-        const uint4 vg = side_by_side(dg[0], dg[1]), vu = side_by_side(du[0], du[1]);
-        const uint32_t col = col0 + 32 * h + pair_column(lane);
-        if (row < a.T && col < a.F) {
-          *reinterpret_cast<uint4*>(to + col) = vg;
-          *reinterpret_cast<uint4*>(to + a.F + col) = vu;
-        }
-      });
-    }
-  });
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t block = min((col0 >> 4) + 2 * h + k, blocks - 1);
+        const unsigned char* const b = static_cast<const unsigned char*>(a.saved) + ((uint64_t)min((row0 >> 4) + x, last_row) * blocks + block) * SAVED_BLOCK;
+        v[n % AHEAD][k].p = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(b + lane * 16)));
+        v[n % AHEAD][k].r = __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const words2*>(b + 1024 + lane * 8)));
+      }
+    };
+    static_for<AHEAD>([&](auto n) { fetch(n); });
+    static_for<N>([&](auto n_) {
+      constexpr int n = n_, x = n / H, h = n % H;
+      f32x4 dg[2], du[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint4 p = v[n % AHEAD][k].p;
+        const uint2 r = v[n % AHEAD][k].r;
+        backward(unpack24(p.x, p.y, p.z), unpack24(p.w, r.x, r.y), acc[x][2 * h + k], dg[k], du[k]);
+      }
+      if constexpr (n + AHEAD < N) fetch(std::integral_constant<int, n + AHEAD>{});
+      const uint4 vg = side_by_side(dg[0], dg[1]), vu = side_by_side(du[0], du[1]);
+      const uint32_t row = row0 + 16 * x + (lane & 15), col = col0 + 32 * h + pair_column(lane);
+      bf16_t* const to = static_cast<bf16_t*>(a.dpre) + (uint64_t)row * (2 * a.F) + col;
+      if (row < a.T && col < a.F) {
+        *reinterpret_cast<uint4*>(to) = vg;
+        *reinterpret_cast<uint4*>(to + a.F) = vu;
+      }
+    });
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------- products in pieces
