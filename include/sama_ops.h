@@ -158,7 +158,8 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
  *    device, by `choice`: four bits for each sixteenth of the rows, the lowest for up to one, each 1 (256 x 192), 2 (256 x 128), 4 (128 x 96) or
  *    5 (128 x 64), anything else is SAMA_EINVAL; 0 = the heuristic (default).  No bit of a result depends on it.
  *  - sama_dev_gemm_counts(counts, 2): HOST counts since the last call: launches of that kernel for forward products and for input gradients.
- *  - sama_dev_glu_tile(t + 1000 p): the products of the gated feed-forward block use the t x t tile, t = 32, 64, 128 or 256 (fp32: 128 at most), and cut their
+ *  - sama_dev_glu_tile(t + 1000 p): the products of the gated feed-forward block use the t x t tile, t = 32, 64, 128 or 256, or 256 x 128 for t = 192
+ *    (fp32: 128 at most), and cut their
  *    contractions into p parts where these are long enough (p = 0: by the heuristic); 0 = the heuristic for both (default).  The order of the sums goes with p.
  *  - sama_dev_side_stream(0): the encoder's backward passes keep every launch on the context's stream (a per-kernel profile
  *    wants one stream); 1 = default: weight gradients and optimizer slices run on the library's second stream where rows and

@@ -227,16 +227,14 @@ __device__ __forceinline__ void contract(f32x4 (&acc)[T::XT][T::YT], unsigned ch
   auto fetchA = [&](const unsigned char* s, int x, int ks) { return fetch(s, std::bool_constant<SA == KS>{}, std::integral_constant<int, T::BM>{}, fa, x, ks); };
   auto fetchB = [&](const unsigned char* s, int y, int ks) { return fetch(s + T::A_BYTES, std::bool_constant<SB == KS>{}, std::integral_constant<int, T::BN>{}, fb, y, ks); };
 
-  constexpr int YP = T::YP, NP = T::NP, NT = STEPS * NP, NM = XT * YP;   // pieces of a slab, products of a piece
+  // pieces of a slab, products of a piece: in fp32 four for each pair of fragments, all pairs before the next four, so that none waits for the one before it
+  constexpr int YP = T::YP, NP = T::NP, NT = STEPS * NP, SUB = sizeof(E) == 4 ? 4 : 1, NM = XT * YP * SUB;
   static_assert(NT % 2 == 0, "operand double buffer parity");
   Frag av[2][XT], bv[2][YP];
   auto mfma = [&](auto t, auto m) {
-    constexpr int T_ = t, ks = T_ / NP, y0 = T_ % NP * YP, x = m / YP, yy = m % YP, y = (x & 1) ? YP - 1 - yy : yy;
-    if constexpr (sizeof(E) == 4) {
-      static_for<4>([&](auto e) { acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[T_ & 1][y][decltype(e)::value], av[ks & 1][x][decltype(e)::value], acc[x][y0 + y], 0, 0, 0); });
-    } else {
-      acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[T_ & 1][y], av[ks & 1][x], acc[x][y0 + y], 0, 0, 0);
-    }
+    constexpr int T_ = t, M_ = m % (XT * YP), ks = T_ / NP, y0 = T_ % NP * YP, x = M_ / YP, yy = M_ % YP, y = (x & 1) ? YP - 1 - yy : yy;
+    if constexpr (sizeof(E) == 4) acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[T_ & 1][y][m / (XT * YP)], av[ks & 1][x][m / (XT * YP)], acc[x][y0 + y], 0, 0, 0);
+    else acc[x][y0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[T_ & 1][y], av[ks & 1][x], acc[x][y0 + y], 0, 0, 0);
   };
   constexpr int READS = YP + XT;
   auto operands = [](int t) { return YP + (t % NP == 0 ? XT : 0); };
@@ -786,6 +784,7 @@ __global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
 
 // ---------------------------------------------------------------------------------------------------- launches
 typedef Tile<256, 256, 2, 4, 2, 0, 2, 0, 1> T256;
+typedef Tile<256, 128, 4, 2, 3, 4, 2, 2, 1> T192;   // (the number between: 192)
 typedef Tile<128, 128, 2, 4, 4, 4, 0, 1, 1> T128;
 typedef Tile<64, 64, 2, 2, 4, 0, 0, 1, 2> T64;
 typedef Tile<32, 32, 2, 1, 6, 0, 0, 1, 3> T32;
@@ -831,7 +830,7 @@ void launch_dgate(ProfScope& ps, hipStream_t st, DgateArgs a, int act) {
 // ---- which tile, and into how many parts a contraction is cut, by what a launch costs in us: pieces are started in their order, longest first, each on the
 // workgroup slot that is free first; a piece takes its slabs' time, by how many workgroups share the CU, and `fixed`; parts are written, read and added.
 struct TileCost { int tile, bm, bn, per_cu; double one, full, fixed; };   // us of a slab with one workgroup to a CU and with per_cu
-constexpr TileCost COST16[] = {{256, 256, 256, 1, 1.50, 1.50, 6.0}, {128, 128, 128, 1, 0.52, 0.52, 2.5}, {64, 64, 64, 2, 0.27, 0.42, 1.5}, {32, 32, 32, 3, 0.20, 0.37, 1.2}};
+constexpr TileCost COST16[] = {{256, 256, 256, 1, 1.50, 1.50, 6.0}, {192, 256, 128, 1, 0.85, 0.85, 4.0}, {128, 128, 128, 1, 0.52, 0.52, 2.5}, {64, 64, 64, 2, 0.27, 0.42, 1.5}, {32, 32, 32, 3, 0.20, 0.37, 1.2}};
 constexpr TileCost COST32[] = {{128, 128, 128, 1, 2.00, 2.00, 3.0}, {64, 64, 64, 2, 0.60, 1.10, 2.0}, {32, 32, 32, 3, 0.32, 0.60, 1.5}};
 constexpr double JOIN_LAUNCH = 3.5, JOIN_BYTES = 1.0 / 3.0e6;   // us; us a byte of the parts, written and read
 constexpr uint32_t LEAST_SLABS = 4, MOST_PARTS = 16;            // of a part; of a tile
@@ -905,8 +904,7 @@ Plan plan_products(const TileCost (&costs)[N], const ProductArgs& a, int force_t
           if (bytes > room && g_force_parts == 0) continue;
           if (bytes > room) for (int k = 0; k < a.count; ++k) parts[k] = 1;
           Plan p{c.tile, {parts[0], parts[1], parts[2]}, {0, 1, 2}, 0.0};
-          const double share = std::min(1.0, std::max(0.0, ((double)pieces - 256.0) / (double)std::max<uint64_t>(1, slots - 256)));
-          const double slab = c.one + (c.full - c.one) * (c.per_cu > 1 ? share : 0.0);
+          const double slab = pieces <= 256 ? c.one : c.full;   // with one more some CU has two, and the launch waits for it
           double length[MAX_PRODUCTS], sorted[MAX_PRODUCTS];
           uint64_t n[MAX_PRODUCTS];
           for (int k = 0; k < a.count; ++k) length[k] = (double)((slabs[k] + parts[k] - 1) / parts[k]) * slab + c.fixed;
@@ -938,7 +936,10 @@ void launch_products(ProfScope& ps, hipStream_t st, const ProductArgs& in, const
 }
 template <typename E, typename F>
 void with_tile(int tile, F f) {
-  if constexpr (sizeof(E) == 2) if (tile == 256) return f(T256{});
+  if constexpr (sizeof(E) == 2) {
+    if (tile == 256) return f(T256{});
+    if (tile == 192) return f(T192{});
+  }
   if (tile >= 128) f(T128{});
   else if (tile == 64) f(T64{});
   else f(T32{});
@@ -959,8 +960,7 @@ int whole_tile(int64_t M, int64_t N, int64_t K) {
   int tile = 0;
   auto look = [&](const TileCost& c) {
     const uint64_t n = (uint64_t)((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), slots = 256 * c.per_cu;
-    const double share = std::min(1.0, std::max(0.0, ((double)n - 256.0) / (double)std::max<uint64_t>(1, slots - 256)));
-    const double length = (double)((K + DEPTH<E> - 1) / DEPTH<E>) * (c.one + (c.full - c.one) * (c.per_cu > 1 ? share : 0.0)) + 2 * c.fixed;
+    const double length = (double)((K + DEPTH<E> - 1) / DEPTH<E>) * (n <= 256 ? c.one : c.full) + 2 * c.fixed;
     const double cost = (double)((n + slots - 1) / slots) * length;
     if (tile == 0 || cost < best) { tile = c.tile; best = cost; }
   };

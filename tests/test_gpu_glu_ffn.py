@@ -117,7 +117,7 @@ SHAPES = [(1, 8, 8), (2, 64, 64), (7, 16, 24), (8, 200, 520), (9, 72, 40), (16, 
           (257, 256, 512), (300, 72, 1368), (513, 328, 264)]
 
 
-@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256, 3064])
+@pytest.mark.parametrize("tile", [0, 32, 64, 128, 192, 256, 3064])
 @pytest.mark.parametrize("T,d,F", SHAPES)
 def test_bf16(T, d, F, tile):
     import paper_2310_05674_amd as pkg
@@ -132,7 +132,7 @@ def test_bf16(T, d, F, tile):
     assert torch.equal(alone["y"], got["y"])
 
 
-@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256, 2032, 5064, 3128, 2256, 16256])
+@pytest.mark.parametrize("tile", [0, 32, 64, 128, 192, 256, 2032, 5064, 3128, 4192, 2256, 16256])
 @pytest.mark.parametrize("T,d,F", [(8, 64, 8192), (100, 128, 4104), (2100, 64, 72), (1000, 136, 3000), (4100, 256, 256), (700, 1024, 512)])
 def test_bf16_split_contractions(T, d, F, tile):
     """Few tiles and long contractions: sums over several workgroups, in every product that may be cut."""
