@@ -6,7 +6,7 @@ each text weighted by the net w(l; lambda)) with clipped gradients and Adam, the
 theta +- eps v, and Adam on lambda with the finite difference of the two weight gradients.
 
   lookup      op_embedding       fp32 master table -> bf16 activations, padding gives zeros
-  blocks      op_glu_ffn         and op_glu_ffn_grad, bf16 with fp32 sums, weights' gradients in fp32
+  blocks      op_glu_ffn         and op_glu_ffn_grad, bf16 with fp32 sums, weights' gradients in fp32; the passes at theta +- eps v in fp32
   table       op_embedding_grad  by sorted tokens
   clipping    op_grad_clip       all tensors into the flat gradient
   solver      op_adam            refreshes the bf16 working copy of the matrices
@@ -61,21 +61,37 @@ class GatedTokenModel:
             at += n
         return out
 
-    def forward(self, ids, keep=True, theta=None):
-        """logits [n, C] of ids [n, S] at theta (default: the model's own); `keep`: for a backward pass."""
+    def share(self, ids):
+        """What each token is of its text's mean."""
+        real = (ids != PAD).float()
+        return real / real.sum(1, keepdim=True)
+
+    def forward(self, ids, keep=True):
+        """logits [n, C] of ids [n, S]; `keep`: for a backward pass."""
         n, S = ids.shape
         T = n * S
-        master = self.views(self.theta if theta is None else theta)
-        work = self.views(self.theta16 if theta is None else theta[:self.n16].to(torch.bfloat16))
+        master, work = self.views(self.theta), self.views(self.theta16)
         B.op_embedding(master[2 * self.L], ids.view(-1), self.x[0][:T], scale=self.d ** 0.5, pad_id=PAD)
         for l in range(self.L):
             y = self.x[l + 1][:T]
             B.op_glu_ffn(self.x[l][:T], work[2 * l], work[2 * l + 1], y, self.hidden[l][:T], self.ws, act=self.act, saved=self.saved[l] if keep else None)
             y += self.x[l][:T]
-        self.real = (ids != PAD).float()
-        self.share = self.real / self.real.sum(1, keepdim=True)                       # of a text's mean
-        self.pooled = torch.bmm(self.share[:, None, :], self.x[self.L][:T].view(n, S, self.d).float())[:, 0]
+        self.pooled = torch.bmm(self.share(ids)[:, None, :], self.x[self.L][:T].view(n, S, self.d).float())[:, 0]
         return self.pooled @ master[-1].t()
+
+    def forward_at(self, ids, theta):
+        """logits at other parameters, in fp32: theta +- eps v differs from theta by less than half a bf16 ulp of most weights."""
+        n, S = ids.shape
+        T = n * S
+        p = self.views(theta)
+        new = lambda *s: torch.empty(*s, device="cuda")
+        x, y, hidden = new(T, self.d), new(T, self.d), new(T, self.F)
+        ws = torch.empty(B.glu_ffn_bytes(T, self.d, self.F, torch.float32), dtype=torch.uint8, device="cuda")
+        B.op_embedding(p[2 * self.L], ids.view(-1), x, scale=self.d ** 0.5, pad_id=PAD)
+        for l in range(self.L):
+            B.op_glu_ffn(x, p[2 * l], p[2 * l + 1], y, hidden, ws, act=self.act)
+            x += y
+        return torch.bmm(self.share(ids)[:, None, :], x.view(n, S, self.d))[:, 0] @ p[-1].t()
 
     def backward(self, ids, dlogits):
         """Gradients of sum(dlogits * logits) of the last forward pass into self.grads."""
@@ -83,7 +99,7 @@ class GatedTokenModel:
         T = n * S
         work, master = self.views(self.theta16), self.views(self.theta)
         torch.mm(dlogits.t(), self.pooled, out=self.grads[-1])
-        dx = (self.share[:, :, None] * (dlogits @ master[-1])[:, None, :]).reshape(T, self.d).to(torch.bfloat16)
+        dx = (self.share(ids)[:, :, None] * (dlogits @ master[-1])[:, None, :]).reshape(T, self.d).to(torch.bfloat16)
         for l in reversed(range(self.L)):
             dx_in = torch.empty_like(dx)
             B.op_glu_ffn_grad(dx, self.x[l][:T], work[2 * l], work[2 * l + 1], self.hidden[l][:T], self.saved[l], dx_in, self.grads[2 * l],
@@ -107,12 +123,15 @@ class GatedTokenModel:
 
 
 class WeightNet:
-    """w(l; lambda) = sigmoid(W2 relu(W1 l + b1) + b2), its gradient in lambda and Adam on it."""
+    """w(l; lambda) = sigmoid(W2 relu(W1 l + b1) + b2), its gradient in lambda and Adam on it.
+
+    It starts flat and moves slowly: the losses at theta +- eps v move the net's input as well as what it multiplies, so the finite difference is of
+    w'(l) l + w, which has the sign of w only while the net is not steep where it is saturated."""
 
     def __init__(self, H, lr, seed=1):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         n = lambda k, std=1.0: torch.randn(k, device="cuda", generator=gen) * std
-        self.p = [n(H), n(H), n(H, H ** -0.5), torch.zeros(1, device="cuda")]
+        self.p = [n(H, 0.3), n(H), n(H, 0.3 * H ** -0.5), torch.zeros(1, device="cuda")]
         self.m, self.s = [torch.zeros_like(p) for p in self.p], [torch.zeros_like(p) for p in self.p]
         self.lr, self.t = lr, 0
 
@@ -155,7 +174,7 @@ def iteration(model, net, train, meta, lr=1e-3, alpha=0.1, max_norm=1.0):
     model.backward(mids, d / len(my))
     if model.t >= 2:                                   # after one step from zero moments the adaptation is nothing but rounding
         model.adapt(lr, alpha)
-        plus, minus = (net.grad(cross_entropy(model.forward(ids, keep=False, theta=model.theta + s * model.eps[0] * model.vdir), y)[0]) for s in (1.0, -1.0))
+        plus, minus = (net.grad(cross_entropy(model.forward_at(ids, model.theta + s * model.eps[0] * model.vdir), y)[0]) for s in (1.0, -1.0))
         net.step([(b - a) / (2 * model.eps[0]) for a, b in zip(plus, minus)])
         model.nudge()
     return losses.mean(), weights
@@ -176,7 +195,7 @@ def texts(n, S, V, C, noise, seed, teacher):
 
 def main(iterations=60):
     V, S, C = 2000, 40, 4
-    model, net = GatedTokenModel(V, 128, 344, 2, C, rows=64 * S), WeightNet(32, 3e-2)
+    model, net = GatedTokenModel(V, 128, 344, 2, C, rows=64 * S), WeightNet(32, 3e-3)
     teacher = torch.randn(V, C, device="cuda", generator=torch.Generator(device="cuda").manual_seed(9))
     for it in range(iterations):
         ids, y, flip = texts(64, S, V, C, 0.3, 100 + it, teacher)

@@ -52,3 +52,12 @@ def test_it_learns(example):
     assert right > 0.5                       # of four classes
     assert int(model.status) == 0 and np.isfinite(float(model.norm[0]))
     assert all(bool(torch.isfinite(q).all()) for q in net.p)
+
+
+def test_the_weights_tell_wrong_labels(example):
+    """30 % of the training labels are wrong: the net has to give such texts less weight, and the rest more than half."""
+    model, net = example.main(150)
+    teacher = torch.randn(2000, 4, device="cuda", generator=torch.Generator(device="cuda").manual_seed(9))
+    ids, y, flip = example.texts(64, 40, 2000, 4, 0.3, 78, teacher)
+    w = net(example.cross_entropy(model.forward(ids, keep=False), y)[0])
+    assert float(w[~flip].mean()) > 0.5 and float(w[flip].mean()) < float(w[~flip].mean()) - 0.1
