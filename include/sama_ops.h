@@ -106,8 +106,9 @@ sama_status sama_op_embedding(const void* table, int32_t table_dtype, int64_t ld
 
 /* Its gradient: grad[v][:] = scale * sum over the i with id_i = v of dy[i][:], in ascending i (dy [n x d], grad [V x d]).  Padding contributes
  * nothing and its rows of dy are not read.  accumulate = 0: every row of grad is written, zeros where no token has the id; 1: the sums are
- * added to grad (a table that is also the output matrix), and rows without a token are left alone.  n at most 2^30.  workspace: DEVICE,
- * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for sizes that the call refuses), which suffices for fewer tokens too. */
+ * added to grad (a table that is also the output matrix), and rows without a token are left alone.  V is at most 2^30, n below 2^30, and so is n
+ * times the pieces of a row (64 lanes' loads of 16 bytes each, of a value where rows do not consist of such).  workspace: DEVICE,
+ * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for n, V or d out of range), which suffices for fewer tokens too. */
 size_t sama_op_embedding_grad_bytes(int64_t n, int32_t V, int32_t d);
 sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_dy, const int32_t* ids, int64_t n, int32_t V, int32_t d,
                                    float scale, int32_t pad_id, int32_t accumulate, void* grad, int32_t grad_dtype, int64_t ld_grad,
@@ -128,8 +129,8 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
  * x, y [T x d] with row strides ldx, ldy; w_in [2F x d], rows 0..F-1 = Wg, F..2F-1 = Wu; w_out [d x F]; hidden [T x F], receives h.  Matrices
  * without a stride are dense.  act: SAMA_ACT_SILU (g / (1 + exp(-g))) or SAMA_ACT_GELU (with the error function).
  * dtype SAMA_DTYPE_BF16: everything in bf16 with fp32 accumulation; h is rounded once, as y is.  d, F and the strides are multiples of 8 and
- * pointers 16-byte aligned; strides at most 2^21, d F below 2^29.  SAMA_DTYPE_FP32: any d, F, stride and alignment of a value.  T at most 2^22, 0 does
- * nothing.  saved: DEVICE, sama_op_glu_ffn_saved_bytes() bytes, 16-byte aligned, receives what the backward call needs besides hidden (a layout
+ * pointers 16-byte aligned.  SAMA_DTYPE_FP32: any d, F, stride and alignment of a value.  Strides at most 2^21, d and F at most 2^20, d F below 2^29
+ * (fp32: 2^28).  T at most 2^22, 0 does nothing.  saved: DEVICE, sama_op_glu_ffn_saved_bytes() bytes, 16-byte aligned, receives what the backward call needs besides hidden (a layout
  * of the library's own), or NULL.  workspace: DEVICE, 256-byte aligned, sama_op_glu_ffn_bytes() bytes.  The size functions return 0 for sizes
  * that the calls refuse; a size for T tokens suffices for fewer.  What a token gets may depend in its last bits on how many tokens it comes with; the same call gives the same bits. */
 enum { SAMA_ACT_SILU = 0, SAMA_ACT_GELU = 1 };
@@ -158,9 +159,9 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
  *    device, by `choice`: four bits for each sixteenth of the rows, the lowest for up to one, each 1 (256 x 192), 2 (256 x 128), 4 (128 x 96) or
  *    5 (128 x 64), anything else is SAMA_EINVAL; 0 = the heuristic (default).  No bit of a result depends on it.
  *  - sama_dev_gemm_counts(counts, 2): HOST counts since the last call: launches of that kernel for forward products and for input gradients.
- *  - sama_dev_glu_tile(t + 1000 p): the products of the gated feed-forward block use the t x t tile, t = 32, 64, 128 or 256, or 256 x 128 for t = 192
- *    (fp32: 128 at most), and cut their
- *    contractions into p parts where these are long enough (p = 0: by the heuristic); 0 = the heuristic for both (default).  The order of the sums goes with p.
+ *  - sama_dev_glu_tile(t + 1000 p): the products of the gated feed-forward block use the t x t tile, t = 32, 64, 128 or 256, or 256 x 128 for
+ *    t = 192 (fp32: 128 at most), and cut their contractions into p parts where these are long enough (p = 0: by the heuristic); 0 = the
+ *    heuristic for both (default).  The order of the sums goes with p.
  *  - sama_dev_side_stream(0): the encoder's backward passes keep every launch on the context's stream (a per-kernel profile
  *    wants one stream); 1 = default: weight gradients and optimizer slices run on the library's second stream where rows and
  *    layers are large enough for it; 2: they do for every size.  Any other value means 1.  A base step keeps its bits; a

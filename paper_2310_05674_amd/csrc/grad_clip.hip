@@ -10,6 +10,7 @@
 // their first unit is on its way.  The second kernel walks the units backwards: the end of the gradients is what the last-level cache still holds.
 #include <algorithm>
 #include <cmath>
+#include "../../include/sama_ops.h"
 #include "kernels.h"
 #include "token_ops.h"
 
@@ -203,18 +204,19 @@ __global__ __launch_bounds__(THREADS) void k_clip(ClipTable t) {
 
 size_t grad_clip_bytes() { return PARTIALS * sizeof(double); }
 
-void launch_grad_clip(hipStream_t st, const GradTensor* g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace) {
+void launch_grad_clip(hipStream_t st, const GradList& g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace) {
   // launches: the next tensors that are not empty, up to TENSORS of them and 2^30 units
   auto next = [&](int64_t& k, int64_t& flat, ClipTable& t) {
     t.count = t.units = 0;
     for (uint32_t& w : t.bf16) w = 0;
     for (; k < count && t.count < TENSORS; ++k) {
-      if (g[k].n == 0) continue;
-      const int64_t each = g[k].bf16 ? UNIT_BYTES / 2 : UNIT_BYTES / 4, units = (g[k].n + each - 1) / each;
+      if (g.n[k] == 0) continue;
+      const bool bf16 = g.dtype[k] == SAMA_DTYPE_BF16;
+      const int64_t each = bf16 ? UNIT_BYTES / 2 : UNIT_BYTES / 4, units = (g.n[k] + each - 1) / each;
       if (t.count > 0 && t.units + units > (1 << 30)) break;
-      t.p[t.count] = g[k].p; t.n[t.count] = g[k].n; t.to[t.count] = flat; t.first[t.count] = t.units;
-      if (g[k].bf16) t.bf16[t.count >> 5] |= 1u << (t.count & 31);
-      flat += g[k].n; t.units += (int)units; ++t.count;
+      t.p[t.count] = g.p[k]; t.n[t.count] = g.n[k]; t.to[t.count] = flat; t.first[t.count] = t.units;
+      if (bf16) t.bf16[t.count >> 5] |= 1u << (t.count & 31);
+      flat += g.n[k]; t.units += (int)units; ++t.count;
     }
     t.first[t.count] = t.units;
   };

@@ -4,7 +4,6 @@
 #include <math.h>
 #include <mutex>
 #include <string>
-#include <vector>
 #include "../../include/sama_ops.h"
 #include "kernels.h"
 #include "token_ops.h"
@@ -64,7 +63,9 @@ const char* check_embedding(const int32_t* ids, int64_t n, int32_t V, int32_t d,
 const char* check_glu(int64_t T, int32_t d, int32_t F, int32_t dtype) {
   if (!is_dtype(dtype)) return "dtype must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16";
   if (T < 0 || T > ((int64_t)1 << 22)) return "T must be 0 to 2^22";
-  if (d < 1 || F < 1 || (int64_t)d * F >= ((int64_t)1 << 29)) return "d and F must be positive and d F below 2^29";
+  // offsets in a tile's slab are 32 bits: 255 rows of 2 F values, F + 127 rows of d values
+  if (d < 1 || F < 1 || d > (1 << 20) || F > (1 << 20)) return "d and F must be 1 to 2^20";
+  if ((int64_t)d * F >= ((int64_t)1 << (dtype == SAMA_DTYPE_BF16 ? 29 : 28))) return "d F must be below 2^29 in bf16, 2^28 in fp32";
   if (dtype == SAMA_DTYPE_BF16 && (d % 8 != 0 || F % 8 != 0)) return "d and F must be multiples of 8 in bf16";
   return nullptr;
 }
@@ -263,6 +264,7 @@ sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_
   EmbeddingGradArgs a{};
   a.dy = dy; a.ldy = ld_dy; a.dy_bf16 = dy_dtype == SAMA_DTYPE_BF16; a.ids = ids; a.n = n; a.V = V; a.d = d; a.scale = scale; a.pad = pad_id;
   a.accumulate = accumulate != 0; a.grad = grad; a.ldg = ld_grad; a.grad_bf16 = grad_dtype == SAMA_DTYPE_BF16;
+  if (!embedding_grad_fits(a)) return refuse(op, "V above 2^30, or more tokens of this width than a launch has room for");
   (void)hipGetLastError();
   launch_embedding_grad((hipStream_t)hip_stream, a, workspace);
   return launched(op);
@@ -281,7 +283,6 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
     (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_grad_clip_bytes()");
     return SAMA_EWORKSPACE;
   }
-  std::vector<GradTensor> list((size_t)count);
   int64_t total = 0;
   for (int64_t k = 0; k < count; ++k) {
     if (!is_dtype(dtypes[k])) return refuse(op, "types must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16");
@@ -289,10 +290,9 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
       return refuse(op, "a gradient is null, misaligned or of a negative size");
     total += counts[k];
     if (total > ((int64_t)1 << 40)) return refuse(op, "more than 2^40 values");
-    list[k] = GradTensor{grads[k], counts[k], dtypes[k] == SAMA_DTYPE_BF16};
   }
   (void)hipGetLastError();
-  launch_grad_clip((hipStream_t)hip_stream, list.data(), count, max_norm, norm_out, out, status, workspace);
+  launch_grad_clip((hipStream_t)hip_stream, GradList{grads, counts, dtypes}, count, max_norm, norm_out, out, status, workspace);
   return launched(op);
 }
 

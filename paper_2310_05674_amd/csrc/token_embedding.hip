@@ -629,6 +629,11 @@ size_t embedding_grad_bytes(int64_t n, int V, int d) {
   return std::max({plan_grad(n, V, d, 8).bytes, plan_grad(n, V, d, 4).bytes, plan_grad(n, V, d, 1).bytes});
 }
 
+bool embedding_grad_fits(const EmbeddingGradArgs& e) {
+  const GradPlan g = plan_grad(e.n, e.V, e.d, grad_vec(e));
+  return e.V <= (1 << 30) && g.chunks * g.slices < ((int64_t)1 << 32) / (SUM_WAVES * 64);
+}
+
 void launch_embedding_grad(hipStream_t st, const EmbeddingGradArgs& e, void* workspace) {
   const int vec = grad_vec(e);
   const GradPlan g = plan_grad(e.n, e.V, e.d, vec);

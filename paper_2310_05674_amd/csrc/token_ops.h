@@ -22,12 +22,13 @@ struct EmbeddingGradArgs {
   void* grad; int64_t ldg; bool grad_bf16;
 };
 size_t embedding_grad_bytes(int64_t n, int V, int d);
+bool embedding_grad_fits(const EmbeddingGradArgs&);   // its launches have less than 2^32 threads
 void launch_embedding_grad(hipStream_t, const EmbeddingGradArgs&, void* workspace);
 
-struct GradTensor { void* p; int64_t n; bool bf16; };
+struct GradList { void* const* p; const int64_t* n; const int32_t* dtype; };   // SAMA_DTYPE_*
 size_t grad_clip_bytes();
 // norm[0] = ||g||, norm[1] = the factor; out: flat fp32, or null (in place); status may be null
-void launch_grad_clip(hipStream_t, const GradTensor* g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace);
+void launch_grad_clip(hipStream_t, const GradList& g, int64_t count, double max_norm, float* norm, float* out, int64_t* status, void* workspace);
 
 // The gated feed-forward block (glu_ffn.hip; fp32 that its tiles cannot load: glu_ffn_f32.hip), shapes as in include/sama_ops.h.
 enum { GLU_SILU = 0, GLU_GELU = 1 };

@@ -97,3 +97,18 @@ def test_feed_forward_refusals(lib):
             sizes = [f(T, 520, 1368, dtype) for T in list(range(0, 3000, 23)) + [8192, 65536, 2 ** 22]]
             assert sizes == sorted(sizes)             # what suffices for many tokens suffices for fewer
             assert f(2 ** 22, 4096, 16384, dtype) > 0
+
+
+def test_sizes_beyond_a_launch(lib):
+    """Sizes whose offsets or launches would not fit 32 bits are refused, whatever the workspace."""
+    grad = dict(dy=P, dt=F32, ldy=2 ** 16, ids=P, n=2 ** 30, V=10, d=2 ** 16, scale=1.0, pad=-1, acc=0, grad=P, gt=F32, ldg=2 ** 16, ws=P, wb=2 ** 62, st=None)
+    refused(lib, "sama_op_embedding_grad", grad, [dict(), dict(d=1), dict(dt=BF16), dict(n=3, d=64, V=2 ** 30 + 1)])
+    for dtype in (BF16, F32):
+        for d, F in ((8, 2 ** 20 + 8), (2 ** 20 + 8, 8), (2 ** 15, 2 ** 14) if dtype == BF16 else (2 ** 14, 2 ** 14)):
+            up = dict(x=P, ldx=2 ** 21, wi=P, wo=P, T=5, d=d, F=F, act=0, dtype=dtype, y=P, ldy=2 ** 21, hidden=P, saved=None, ws=P, wb=2 ** 62, st=None)
+            refused(lib, "sama_op_glu_ffn", up, [dict()])
+            down = dict(dy=P, lddy=2 ** 21, x=P, ldx=2 ** 21, wi=P, wo=P, hidden=P, saved=P, T=5, d=d, F=F, act=0, dtype=dtype, dx=P, lddx=2 ** 21, dwi=P, dwo=P,
+                        dwt=dtype, ws=P, wb=2 ** 62, st=None)
+            refused(lib, "sama_op_glu_ffn_grad", down, [dict()])
+            assert lib.sama_op_glu_ffn_bytes(5, d, F, dtype) == lib.sama_op_glu_ffn_grad_bytes(5, d, F, dtype) == 0
+        assert lib.sama_op_glu_ffn_bytes(5, 8, 2 ** 20, dtype) > 0 and lib.sama_op_glu_ffn_grad_bytes(5, 2 ** 20, 8, dtype) > 0
