@@ -3,7 +3,7 @@
 // table's gradient once.
 //
 // The gradient sorts the tokens by id, which gives every id's rows one after the other in ascending i, and sums each run in a fixed
-// order in 32 bits: the same bits from call to call, without an atomic on a sum.  Two launches.
+// order in 32 bits: the same bits from call to call, without an atomic on a sum.  Two launches, and for a few tokens one (k_token_few).
 //   k_token_sort   A workgroup owns every 256th id and looks through all tokens, 16 waves a section of them each: it counts its ids and
 //                  those of the workgroups before it, turns the counts into places, and puts its tokens there, a wave 64 at a time in order
 //                  (ranks among equal ids by ballots).  Every 256th and not 256th parts of the table: the low ids are the frequent ones of
@@ -187,6 +187,31 @@ IdOrder order_of(int V) {
   return o;
 }
 
+// lanes of the set below this one, + from
+__device__ __forceinline__ int rank_in(uint64_t lanes, int from) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, from));
+}
+// the lanes of `among` that have this lane's id, of `bits` bits: of the first few ids that there are one by one, then by a ballot for each bit
+__device__ __forceinline__ uint64_t lanes_with(int id, uint64_t among, int bits) {
+  uint64_t same = 0, left = among;
+#pragma unroll 1
+  for (int k = 0; k < 4 && left != 0; ++k) {
+    const int v = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+    const uint64_t with = __ballot(id == v) & left;
+    if (id == v) same = with;
+    left &= ~with;
+  }
+  if (left == 0) return same;
+  uint64_t rest = left;
+  for (int k = 0; k < bits; ++k) {
+    const bool set = (id >> k) & 1;
+    const uint64_t with = __ballot(set);
+    rest &= set ? with : ~with;
+  }
+  return left >> (threadIdx.x & 63) & 1 ? rest : same;
+}
+typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));   // a load of 16 bytes wants no more than a word's alignment
+
 struct SortArgs {
   const int32_t* ids; int n, V, pad;
   IdOrder o;
@@ -237,27 +262,6 @@ __global__ __launch_bounds__(SORT_THREADS) void k_token_sort(SortArgs a) {
   const int first = (int)min((int64_t)wave * section, (int64_t)n), last = (int)min((int64_t)first + section, (int64_t)n);
   const int bits = range > 1 ? 32 - __builtin_clz(range - 1) : 0;
   auto clamped = [&](int id) { return min(max(id, 0), most); };
-  auto rank_in = [&](uint64_t lanes, int from) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, from)); };
-  // the lanes of `among` that have this lane's id: of the first few ids that there are one by one, then by a ballot for each bit
-  auto equals = [&](int id, uint64_t among) {
-    uint64_t same = 0, left = among;
-#pragma unroll 1
-    for (int k = 0; k < 4 && left != 0; ++k) {
-      const int v = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-      const uint64_t with = __ballot(id == v) & left;
-      if (id == v) same = with;
-      left &= ~with;
-    }
-    if (left == 0) return same;
-    uint64_t rest = left;
-    for (int k = 0; k < bits; ++k) {
-      const bool set = (id >> k) & 1;
-      const uint64_t with = __ballot(set);
-      rest &= set ? with : ~with;
-    }
-    return left >> lane & 1 ? rest : same;
-  };
-  typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));   // a load of 16 bytes wants no more than a word's alignment
   const int room = section <= 1 << LIST_BITS ? LIST : 0;
   int below = 0, listed = 0;                 // tokens of workgroups before this one, of this one: the same in every lane
   auto look = [&](int i0, i4 now, auto whole) {
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_token_sort(SortArgs a) {
   each([&](int id, int) {
     uint64_t some = __ballot(id >= 0);
     if (some == 0) return;
-    some = equals(id, some);
+    some = lanes_with(id, some, bits);
     if (id >= 0 && rank_in(some, 0) == 0) mine[id] += __popcll(some);   // the first of each id: no two lanes at one place
   });
   __syncthreads();
@@ -369,7 +373,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_token_sort(SortArgs a) {
   each([&](int id, int token) {   // (each wave reads and changes its own places)
     uint64_t peers = __ballot(id >= 0);
     if (peers == 0) return;
-    peers = equals(id, peers);
+    peers = lanes_with(id, peers, bits);
     if (id >= 0) {
       const int rank = rank_in(peers, 0), to = mine[id];
       a.order[to + rank] = token;
@@ -410,6 +414,25 @@ __device__ __forceinline__ void collect_values(const float* p, float (&f)[VEC]) 
     }
 }
 
+template <typename TO, int VEC>
+__device__ __forceinline__ void put_sum(TO* p, const float (&s)[VEC], float scale, int accumulate) {
+  float f[VEC];
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) f[k] = s[k] * scale;
+  if (accumulate) {
+    constexpr int STEP = sizeof(TO) == 4 && VEC == 8 ? 4 : VEC;
+#pragma unroll
+    for (int k0 = 0; k0 < VEC; k0 += STEP) {
+      Values<TO, STEP> old;
+      float o[STEP];
+      old.load(p + k0); old.get(o);
+#pragma unroll
+      for (int k = 0; k < STEP; ++k) f[k0 + k] += o[k];
+    }
+  }
+  put_once(p, f);
+}
+
 template <typename TI, typename TO, int VEC, int P>
 __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   constexpr int CHUNK = SUM_WAVES * P, SLICE = 64 * VEC;
@@ -433,29 +456,7 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   const TI* const dy = static_cast<const TI*>(a.dy) + (have ? col : 0);
   TO* const grad = static_cast<TO*>(a.grad);
   auto finish = [&](int id, const float (&s)[VEC]) {
-    if (!have) return;
-    TO* const p = grad + (int64_t)id * a.ldg + col;
-    float f[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) f[k] = s[k] * a.scale;
-    if (a.accumulate) {
-      Values<TO, (sizeof(TO) == 4 && VEC == 8) ? 4 : VEC> old;
-      if constexpr (sizeof(TO) == 4 && VEC == 8) {
-        float o[4];
-        old.load(p); old.get(o);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[k] += o[k];
-        old.load(p + 4); old.get(o);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[4 + k] += o[k];
-      } else {
-        float o[VEC];
-        old.load(p); old.get(o);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) f[k] += o[k];
-      }
-    }
-    put_once(p, f);
+    if (have) put_sum(grad + (int64_t)id * a.ldg + col, s, a.scale, a.accumulate);
   };
   auto head_out = [&](const float (&s)[VEC]) {
 #pragma unroll
@@ -568,6 +569,151 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
   }
 }
 
+// ---------------------------------------------------------------------------------------------------- gradient: few tokens in one launch
+// A workgroup owns every 256th id and a slice of the columns: it looks through all ids, lists its tokens in order, sorts them by id in LDS, sums
+// the runs, a wave an equal share of the sorted rows, and zeroes its other rows meanwhile.  Nobody waits for another workgroup, nothing passes through
+// memory.  What bounds it is one launch and the id with the most tokens, whose rows one CU reads at 45 GB/s, while the two launches above spread them over
+// the chip but cost one more and the way through memory between them.  us, two launches / this one, ids by Zipf's law of exponent 1.1 (the most frequent 13 %):
+//   tokens                 64           256          703          1024         1400
+//   8192 x 256      9.6 / 5.6                 10.8 / 6.7
+//   8192 x 512     10.3 / 7.5   11.2 / 7.7   11.7 / 8.6   11.9 / 11.6  12.4 / 12.8
+//   2000 x 768      9.0 / 8.3   10.2 / 9.0   10.4 / 9.7   10.9 / 9.9   12.0 / 10.4
+//   8192 x 1024    12.2 / 12.7  13.1 / 13.3  13.7 / 14.3  14.4 / 14.6  14.8 / 16.1
+//   30522 x 768    19.4 / 17.9               20.6 / 23.6  (2048: 22.7 / 31.6)
+// and with 703 tokens of 8192 x 256 of which half have one id 10.9 / 10.5, all 12.5 / 19.5.  So: up to 1024 tokens, up to 24 MB of gradient to be
+// written (zeroing more than that a row at a time is slower than by the 256 workgroups of the sort), up to four slices.
+constexpr int FEW_TOKENS = 1024, FEW_WAVES = FEW_TOKENS / 64, FEW_BITS = 16, FEW_SLICES = 4;   // a thread looks at one id; bits of a token in the list
+constexpr int64_t FEW_BYTES = 24 << 20;
+struct FewArgs {
+  const void* dy; int64_t ldy;
+  const int32_t* ids; int n, V, d, pad, bits, slices;   // bits of id / 256
+  float scale; int accumulate;
+  void* grad; int64_t ldg;
+};
+template <typename TI, typename TO, int VEC>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_token_few(FewArgs a) {
+  constexpr int GROUPS = 256, SLICE = 64 * VEC, HEADS = FEW_WAVES * SLICE;
+  __shared__ __attribute__((aligned(16))) uint32_t s_work[HEADS > FEW_TOKENS ? HEADS : FEW_TOKENS];   // the list, later the waves' parts of runs that began before them
+  __shared__ uint32_t s_sorted[FEW_TOKENS];
+  __shared__ __attribute__((aligned(16))) int32_t s_count[SORT_RANGE], s_to[SORT_RANGE];              // of each id: its tokens, where they go (in the end: where they end)
+  __shared__ int32_t s_wave[FEW_WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int own = blockIdx.x / a.slices, slice = blockIdx.x - own * a.slices;
+  const int pad = a.pad >= 0 ? a.pad : INT32_MIN, most = a.V - 1, n = a.n;
+  const int t = tid < n ? a.ids[tid] : 0;
+  if (tid < SORT_RANGE) s_count[tid] = 0;
+  __syncthreads();
+  // ---- this workgroup's tokens, in order (the atomics are on counts)
+  const int clamped = min(max(t, 0), most), local = clamped >> 8;
+  const bool here = tid < n && max(t, -1) != pad && (clamped & (GROUPS - 1)) == own;
+  const uint64_t tokens = __ballot(here);
+  if (here) atomicAdd(&s_count[local], 1);
+  if (lane == 0) s_wave[wave] = __popcll(tokens);
+  __syncthreads();
+  int m = 0, before_me = 0;
+#pragma unroll
+  for (int w = 0; w < FEW_WAVES; ++w) {
+    if (w < wave) before_me += s_wave[w];
+    m += s_wave[w];
+  }
+  if (here) s_work[rank_in(tokens, before_me)] = (uint32_t)tid | (uint32_t)local << FEW_BITS;
+  __syncthreads();
+  const int col = slice * SLICE + lane * VEC;
+  const bool have = col < a.d;                                      // (d is a multiple of VEC)
+  TO* const grad = static_cast<TO*>(a.grad) + (int64_t)own * a.ldg + (have ? col : 0);
+  const int64_t next = (int64_t)GROUPS * a.ldg;
+  // ---- one wave sorts them, the others zero the rows of the ids that have none
+  if (wave == 0) {
+    static_assert(SORT_RANGE == 64 * 8, "ids of a lane");
+    int c[8], sum = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { c[k] = s_count[8 * lane + k]; sum += c[k]; }
+    int upto = sum;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int v = __shfl_up(upto, s, 64);
+      if (lane >= s) upto += v;
+    }
+    upto -= sum;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { s_to[8 * lane + k] = upto; upto += c[k]; }
+    for (int k0 = 0; k0 < m; k0 += 64) {
+      const bool there = k0 + lane < m;
+      const uint32_t v = there ? s_work[k0 + lane] : 0;
+      const int id = there ? (int)(v >> FEW_BITS) : -1;
+      const uint64_t same = lanes_with(id, __ballot(there), a.bits);
+      if (there) {
+        const int rank = rank_in(same, 0), to = s_to[id];
+        s_sorted[to + rank] = v;
+        if (rank == 0) s_to[id] = to + __popcll(same);
+      }
+    }
+  } else if (!a.accumulate && have) {
+    const int rows = own > most ? 0 : (most - own) / GROUPS + 1;
+    const float zero[VEC] = {};
+    for (int r = wave - 1; r < rows; r += FEW_WAVES - 1)
+      if (s_count[r] == 0) put(grad + r * next, zero);
+  }
+  __syncthreads();
+  // ---- the sums
+  const int P = (m + FEW_WAVES - 1) / FEW_WAVES, q0 = min(wave * P, m), q1 = min(q0 + P, m);
+  float* const s_head = reinterpret_cast<float*>(s_work);
+  const TI* const dy = static_cast<const TI*>(a.dy) + (have ? col : 0);
+  auto head_out = [&](const float (&s)[VEC]) {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) s_head[wave * SLICE + k * 64 + lane] = s[k];
+  };
+  auto finish = [&](int id, const float (&s)[VEC]) {
+    if (have) put_sum(grad + id * next, s, a.scale, a.accumulate);
+  };
+  float acc[VEC] = {};
+  int open = -1;             // the run at the wave's end began here and goes on behind it
+  if (q0 < q1) {
+    const int before = q0 > 0 ? (int)(__builtin_amdgcn_readfirstlane(s_sorted[q0 - 1]) >> FEW_BITS) : -1;
+    const int behind = q1 < m ? (int)(__builtin_amdgcn_readfirstlane(s_sorted[q1]) >> FEW_BITS) : -1;
+    constexpr int B = 8;
+    int run = before;
+    bool began = false;
+    for (int j0 = q0; j0 < q1; j0 += B) {
+      const uint32_t mine = s_sorted[min(j0 + (lane & (B - 1)), q1 - 1)];
+      Values<TI, VEC> v[B];
+#pragma unroll
+      for (int j = 0; j < B; ++j)
+        if (j == 0 || j0 + j < q1) v[j] = load_once<TI, VEC>(dy + (int64_t)(__builtin_amdgcn_readlane(mine, j) & ((1u << FEW_BITS) - 1)) * a.ldy);
+#pragma unroll
+      for (int j = 0; j < B; ++j) {
+        if (j0 + j >= q1) break;
+        const int id = (int)((uint32_t)__builtin_amdgcn_readlane(mine, j) >> FEW_BITS);
+        float f[VEC];
+        v[j].get(f);
+        if (id != run) {
+          if (j0 + j > q0) {
+            if (began) finish(run, acc);
+            else head_out(acc);
+          }
+          run = id; began = true;
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) acc[k] = f[k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) acc[k] += f[k];
+        }
+      }
+    }
+    if (!began) head_out(acc);
+    else if (run == behind) open = run;
+    else finish(run, acc);
+  }
+  __syncthreads();
+  if (open >= 0) {
+    const int last = (s_to[open] - 1) / P;
+    for (int w = wave + 1; w <= last; ++w)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) acc[k] += s_head[w * SLICE + k * 64 + lane];
+    finish(open, acc);
+  }
+}
+
 // Sorted rows of a wave: the most of 16 to 1 that leave the chip 512 workgroups.
 int sum_rows(int64_t n, int slices) {
   int p = 16;
@@ -606,6 +752,13 @@ void launch_sum(hipStream_t st, ProfScope& ps, const SumArgs& s, const GradPlan&
   }
 }
 
+template <typename TI, typename TO>
+void launch_few(hipStream_t st, ProfScope& ps, const FewArgs& a, int vec) {
+  constexpr int VEC = sizeof(TI) == 2 ? 8 : 4;
+  if (vec > 1) launch_kernel(ps, k_token_few<TI, TO, VEC>, 256 * slices_of(a.d, VEC), FEW_WAVES * 64, 0, st, a);
+  else launch_kernel(ps, k_token_few<TI, TO, 1>, 256 * slices_of(a.d, 1), FEW_WAVES * 64, 0, st, a);
+}
+
 // Values a lane takes: 16 bytes of dy, where every row of dy and of the gradient allows it.
 int grad_vec(const EmbeddingGradArgs& a) {
   const int se = a.dy_bf16 ? 2 : 4, ge = a.grad_bf16 ? 2 : 4, vec = a.dy_bf16 ? 8 : 4;
@@ -639,6 +792,18 @@ void launch_embedding_grad(hipStream_t st, const EmbeddingGradArgs& e, void* wor
   const GradPlan g = plan_grad(e.n, e.V, e.d, vec);
   char* const ws = static_cast<char*>(workspace);
   ProfScope ps(st, F_OTHER, 0.0);
+  if (e.n <= FEW_TOKENS && order_of(e.V).lg == 8 && g.slices <= FEW_SLICES && (e.accumulate || e.V * (int64_t)e.d * (e.grad_bf16 ? 2 : 4) <= FEW_BYTES)) {
+    FewArgs a{};
+    a.dy = e.dy; a.ldy = e.ldy; a.ids = e.ids; a.n = (int)e.n; a.V = e.V; a.d = e.d; a.pad = e.pad;
+    while (order_of(e.V).range > 1 << a.bits) ++a.bits;
+    a.slices = g.slices;
+    a.scale = e.scale; a.accumulate = e.accumulate; a.grad = e.grad; a.ldg = e.ldg;
+    if (e.dy_bf16 && e.grad_bf16) launch_few<bf16_t, bf16_t>(st, ps, a, vec);
+    else if (e.dy_bf16) launch_few<bf16_t, float>(st, ps, a, vec);
+    else if (e.grad_bf16) launch_few<float, bf16_t>(st, ps, a, vec);
+    else launch_few<float, float>(st, ps, a, vec);
+    return;
+  }
   SortArgs s{};
   s.ids = e.ids; s.n = (int)e.n; s.V = e.V; s.pad = e.pad;
   s.o = order_of(e.V);

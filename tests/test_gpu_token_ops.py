@@ -331,3 +331,36 @@ def test_clipping_gives_the_same_bits():
     grads = gradients([70001, 5, 2 ** 20], 3, ("fp32", "bf16"))
     a, b = torch.empty(70006 + 2 ** 20, device=DEV), torch.empty(70006 + 2 ** 20, device=DEV)
     assert tuple(clip(grads, 0.1, out=a)) == tuple(clip(grads, 0.1, out=b)) and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dy_t,grad_t", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("n,V,d", [(1024, 300, 256), (1025, 300, 256), (1024, 131072, 24), (1024, 131073, 24), (700, 257, 1024), (700, 257, 1032), (700, 257, 2048), (700, 257, 2056),
+                                   (333, 255, 250), (333, 256, 260), (1, 131072, 40), (63, 200000, 40), (1023, 30522, 264)])
+def test_token_gradient_of_few_tokens(n, V, d, dy_t, grad_t):
+    """Both sides of where one launch takes over from two: tokens, ids, slices of the columns (16-byte pieces or not) and bytes of the gradient, with
+    long runs, with padding and on top of what is there."""
+    for kind in ("zipf", "same", "runs"):
+        dy, ids = values(n + d, n, d).to(T[dy_t]), token_ids(kind, n, V, n + V)
+        got = grad_of(dy, ids, V, grad_t, scale=1.25)
+        check_grad(dy, ids, V, got, 1.25)
+        assert torch.equal(got, grad_of(dy, ids, V, grad_t, scale=1.25))
+    ids = token_ids("zipf", n, V, 9)
+    ids[::3] = 2
+    dy[ids == 2] = float("nan")
+    check_grad(torch.nan_to_num(dy.float()), ids, V, grad_of(dy, ids, V, grad_t, scale=0.5, pad_id=2), 0.5, pad=2)
+
+
+@pytest.mark.parametrize("n", [0, 1, 700, 1024, 1025])
+@pytest.mark.parametrize("V,d", [(300, 256), (131072, 64), (200000, 40)])
+def test_token_gradient_of_few_tokens_on_top(n, V, d):
+    from paper_2310_05674_amd import binding as B
+    dy, ids = values(n + 1, n, d), token_ids("zipf", n, V, 3)
+    grad = values(6, V, d)
+    before = f64(grad)
+    ws = torch.full((B.embedding_grad_bytes(n, V, d),), 0xa5, dtype=torch.uint8, device=DEV)
+    B.op_embedding_grad(dy, ids, grad, ws, scale=0.75, accumulate=True)
+    check_grad(dy, ids, V, grad, 0.75, start=before)
+    unseen = np.setdiff1d(np.arange(V), ids.cpu().numpy())
+    assert np.array_equal(f64(grad)[unseen], before[unseen])
+    B.op_embedding_grad(dy, ids, grad, ws, scale=0.75)
+    check_grad(dy, ids, V, grad, 0.75)
