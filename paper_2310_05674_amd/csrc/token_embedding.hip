@@ -574,16 +574,16 @@ __global__ __launch_bounds__(SUM_WAVES * 64) void k_token_sum(SumArgs a) {
 // the runs, a wave an equal share of the sorted rows, and zeroes its other rows meanwhile.  Nobody waits for another workgroup, nothing passes through
 // memory.  What bounds it is one launch and the id with the most tokens, whose rows one CU reads at 45 GB/s, while the two launches above spread them over
 // the chip but cost one more and the way through memory between them.  us, two launches / this one, ids by Zipf's law of exponent 1.1 (the most frequent 13 %):
-//   tokens                 64           256          703          1024         1400
-//   8192 x 256      9.6 / 5.6                 10.8 / 6.7
-//   8192 x 512     10.3 / 7.5   11.2 / 7.7   11.7 / 8.6   11.9 / 11.6  12.4 / 12.8
-//   2000 x 768      9.0 / 8.3   10.2 / 9.0   10.4 / 9.7   10.9 / 9.9   12.0 / 10.4
-//   8192 x 1024    12.2 / 12.7  13.1 / 13.3  13.7 / 14.3  14.4 / 14.6  14.8 / 16.1
-//   30522 x 768    19.4 / 17.9               20.6 / 23.6  (2048: 22.7 / 31.6)
-// and with 703 tokens of 8192 x 256 of which half have one id 10.9 / 10.5, all 12.5 / 19.5.  So: up to 1024 tokens, up to 24 MB of gradient to be
-// written (zeroing more than that a row at a time is slower than by the 256 workgroups of the sort), up to four slices.
+//   tokens            64           256          703          1024
+//   8192 x 256     9.6 / 5.5                 10.8 / 6.2
+//   8192 x 512    10.3 / 6.1   11.2 / 6.5    11.7 / 9.4   11.9 / 11.4
+//   2000 x 768     9.0 / 6.5   10.2 / 6.8    10.4 / 7.4   10.9 / 7.8
+//   8192 x 1024   12.2 / 10.5  13.1 / 11.1   13.7 / 12.4  14.4 / 14.5
+//   30522 x 512   15.4 / 12.7  16.1 / 15.0   16.7 / 16.7  16.7 / 18.7
+// 703 tokens of 8192 x 256, half of them of one id: 10.9 / 10.5, all: 12.5 / 19.5.  So: up to 1024 tokens, up to 32 MB of gradient to be written (a workgroup's
+// rows are 256 apart: zeroing more than that takes longer than in the sort's own share), up to four slices.
 constexpr int FEW_TOKENS = 1024, FEW_WAVES = FEW_TOKENS / 64, FEW_BITS = 16, FEW_SLICES = 4;   // a thread looks at one id; bits of a token in the list
-constexpr int64_t FEW_BYTES = 24 << 20;
+constexpr int64_t FEW_BYTES = 32 << 20;
 struct FewArgs {
   const void* dy; int64_t ldy;
   const int32_t* ids; int n, V, d, pad, bits, slices;   // bits of id / 256
