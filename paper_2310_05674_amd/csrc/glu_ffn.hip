@@ -11,7 +11,6 @@
 #include <cmath>
 #include <type_traits>
 #include <utility>
-#include "gelu.h"
 #include "kernels.h"
 #include "token_ops.h"
 
@@ -301,15 +300,25 @@ __device__ __forceinline__ uint4 side_by_side(f32x4 a, f32x4 b) {
 __device__ __forceinline__ int pair_column(int lane) { return 16 * ((lane >> 4) & 1) + 8 * (lane >> 5); }
 
 // The gate and its derivative: silu(g) = g s, silu'(g) = s + g s (1 - s) with s = 1 / (1 + exp(-g)); gelu(g) = g P(g), gelu'(g) = P(g) + g p(g) with the
-// normal distribution P and its density p.
-// In fp32 with the full-precision exp and erf, in bf16 with the fast ones, whose error is 1e-6.
+// normal distribution P and its density p.  In fp32 with the full-precision exp and erf.  In bf16, where the result is rounded to 2^-9 of itself, with the
+// hardware's exp2 and reciprocal, and P through its logarithm, which is smooth: P(-x) = 2^q(x) for x >= 0 with a q of degree seven, fitted here to log2 P(-x) on
+// [0, 7.5] (Chebyshev points, errors beyond 3.5 counting less).  Its errors: 4e-6 of P down to -3.5, 5e-5 down to -6, 6e-7 of gelu anywhere; q falls
+// on to minus infinity.  An exp2 and eight multiply-adds, where an erf by exp and reciprocal is twice that, and the epilogue of a tile has nothing to hide it
+// behind: both projections of 4096 x 768 x 2048 29.3 us instead of 30.9, 26.0 without any gate.
+__device__ __forceinline__ float normal_cdf(float g) {
+  const float x = fabsf(g);
+  float q = -1.72933608e-06f;
+  q = fmaf(q, x, 5.9637081e-05f); q = fmaf(q, x, -0.000916504301f); q = fmaf(q, x, 0.00845899247f); q = fmaf(q, x, -0.0538729616f);
+  q = fmaf(q, x, -0.458539814f); q = fmaf(q, x, -1.15122414f); q = fmaf(q, x, -0.999997795f);
+  const float below = __builtin_amdgcn_exp2f(q);
+  return g < 0.f ? below : 1.f - below;
+}
 template <typename E, int ACT>
 __device__ __forceinline__ void gate_and_slope(float g, float& a, float& da) {
   if constexpr (ACT == GLU_GELU) {
-    float erfz, ez;
-    if constexpr (sizeof(E) == 4) { erfz = erff(g * 0.70710678118654752f); ez = expf(-0.5f * g * g); }
-    else erf_and_gauss(g * 0.70710678118654752f, erfz, ez);
-    const float cdf = 0.5f * (1.f + erfz);
+    float cdf, ez;
+    if constexpr (sizeof(E) == 4) { cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f)); ez = expf(-0.5f * g * g); }
+    else { cdf = normal_cdf(g); ez = __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g); }
     a = g * cdf; da = fmaf(g * 0.39894228040143268f, ez, cdf);
   } else {
     float s;
@@ -831,7 +840,7 @@ void launch_dgate(ProfScope& ps, hipStream_t st, DgateArgs a, int act) {
 // workgroup slot that is free first; a piece takes its slabs' time, by how many workgroups share the CU, and `fixed`; parts are written, read and added.
 struct TileCost { int tile, bm, bn, per_cu; double one, full, fixed; };   // us of a slab with one workgroup to a CU and with per_cu
 constexpr TileCost COST16[] = {{256, 256, 256, 1, 1.50, 1.50, 6.0}, {192, 256, 128, 1, 0.85, 0.85, 4.0}, {128, 128, 128, 1, 0.52, 0.52, 2.5}, {64, 64, 64, 2, 0.27, 0.42, 1.5}, {32, 32, 32, 3, 0.20, 0.37, 1.2}};
-constexpr TileCost COST32[] = {{128, 128, 128, 1, 2.00, 2.00, 3.0}, {64, 64, 64, 2, 0.60, 1.10, 2.0}, {32, 32, 32, 3, 0.32, 0.60, 1.5}};
+constexpr TileCost COST32[] = {{128, 128, 128, 1, 2.00, 2.00, 3.0}, {64, 64, 64, 2, 0.72, 1.10, 2.0}, {32, 32, 32, 3, 0.32, 0.60, 1.5}};
 constexpr double JOIN_LAUNCH = 3.5, JOIN_BYTES = 1.0 / 3.0e6;   // us; us a byte of the parts, written and read
 constexpr uint32_t LEAST_SLABS = 4, MOST_PARTS = 16;            // of a part; of a tile
 // Most bytes of parts that a launch may have, for the sizes in `a`, however they are cut: grows with the number of tokens.
