@@ -116,7 +116,9 @@ struct LookupArgs {
 };
 
 // A block takes `rows` rows, its threads the pieces of VEC values of all of them one after the other, U of them at a time so that
-// the loads of the ids, then those of the rows, are under way together.
+// the loads of the ids, then those of the rows, are under way together.  Bound by memory: 32768 tokens of 1024, a quarter of them padding, from an fp32 table
+// into bf16 in 21.0 us, 90 MB of distinct rows and output (4.3 TB/s; 168 MB with what the caches answer); 128 tokens of 256 in 5.7, which is the call: the
+// kernel takes 2.4.
 template <typename TI, typename TO, int VEC, int U>
 __global__ __launch_bounds__(256) void k_embedding(LookupArgs a) {
   const TI* const table = static_cast<const TI*>(a.table);
@@ -154,7 +156,7 @@ template <typename TI, typename TO, int VEC>
 void launch_lookup(hipStream_t st, ProfScope& ps, LookupArgs a) {
   a.pieces = a.d / VEC;
   a.magic = a.pieces == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.pieces - 1) / a.pieces);
-  // four pieces a thread where that leaves 1024 blocks and more
+  // four pieces a thread where that leaves 1024 blocks and more, else one (the first of the above U1_BATCH us with one)
   const bool many = a.n * a.pieces >= (int64_t)1024 * 1024;
   a.rows = (int)std::max<int64_t>(1, (many ? 1024 : 256) / a.pieces);
   const uint32_t blocks = (uint32_t)std::min<int64_t>((a.n + a.rows - 1) / a.rows, 1 << 20);
@@ -165,6 +167,7 @@ template <typename TI, typename TO>
 void launch_lookup(hipStream_t st, ProfScope& ps, const LookupArgs& a) {
   constexpr int VEC = sizeof(TI) == 2 && sizeof(TO) == 2 ? 8 : 4;
   const uintptr_t at = (uintptr_t)a.table | (uintptr_t)(a.ldt * sizeof(TI)), to = (uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(TO));
+  // rows in pieces of 16 bytes (of the fp32 side) where both sides allow it: 32768 x 1024, ids evenly spread, 30.3 us, a value at a time 44.1
   const bool wide = a.d % VEC == 0 && at % (VEC * sizeof(TI)) == 0 && to % (VEC * sizeof(TO)) == 0;
   if (wide) launch_lookup<TI, TO, VEC>(st, ps, a);
   else launch_lookup<TI, TO, 1>(st, ps, a);
@@ -714,7 +717,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_token_few(FewArgs a) {
   }
 }
 
-// Sorted rows of a wave: the most of 16 to 1 that leave the chip 512 workgroups.
+// Sorted rows of a wave: the most of 16 to 1 that leave the chip 512 workgroups.  4096 tokens of 768 into 30522 rows 23.7 us, with 256 workgroups 23.6, with
+// 1024 26.8; 65521 of 1024 the same with all.
 int sum_rows(int64_t n, int slices) {
   int p = 16;
   while (p > 1 && (n + SUM_WAVES * p - 1) / (SUM_WAVES * p) * slices < 512) p /= 2;
@@ -759,7 +763,8 @@ void launch_few(hipStream_t st, ProfScope& ps, const FewArgs& a, int vec) {
   else launch_kernel(ps, k_token_few<TI, TO, 1>, 256 * slices_of(a.d, 1), FEW_WAVES * 64, 0, st, a);
 }
 
-// Values a lane takes: 16 bytes of dy, where every row of dy and of the gradient allows it.
+// Values a lane takes: 16 bytes of dy, where every row of dy and of the gradient allows it: 4096 tokens of 768, ids evenly spread, into 30522 rows 23.6 us, a
+// value at a time 25.8.
 int grad_vec(const EmbeddingGradArgs& a) {
   const int se = a.dy_bf16 ? 2 : 4, ge = a.grad_bf16 ? 2 : 4, vec = a.dy_bf16 ? 8 : 4;
   const uintptr_t at = (uintptr_t)a.dy | (uintptr_t)(a.ldy * se), to = (uintptr_t)a.grad | (uintptr_t)(a.ldg * ge);
