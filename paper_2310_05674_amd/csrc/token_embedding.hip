@@ -2,6 +2,9 @@
 // of dy[i].  Both move bytes: a row of the table and of the output for each token; the real rows of dy once and every row of the
 // table's gradient once.
 //
+// Measured on an MI355X: the lookup beside its kernel; the gradient of 4096 tokens of 768 into 30522 rows of fp32 23.7 us for 106 MB (94 MB of them written: 13.5
+// us by themselves), of 65521 tokens of 1024 in bf16, a quarter padding, into 50304 rows 78 us for 307 MB; of 703 tokens of 256 into 8192 rows 6.2 us.
+//
 // The gradient sorts the tokens by id, which gives every id's rows one after the other in ascending i, and sums each run in a fixed
 // order in 32 bits: the same bits from call to call, without an atomic on a sum.  Two launches, and for a few tokens one (k_token_few).
 //   k_token_sort   A workgroup owns every 256th id and looks through all tokens, 16 waves a section of them each: it counts its ids and
@@ -10,7 +13,8 @@
 //                  most vocabularies, and one workgroup had half of the tokens.  No workgroup waits for another.
 //                  Beside each a second one zeroes a share of the gradient: for a vocabulary of 30522 and 4096 tokens that is most of all
 //                  bytes, and sorting hides behind it.  Zeroing only the rows that stay so, in the launch behind this one, moves a fifth
-//                  less and takes longer.
+//                  less and takes longer; so does leaving just those there that do not hide behind the sort (30 us instead of 24 for the first
+//                  of the above, 78 to 91 instead of 78 for the second).
 //   k_token_sum    8 waves of `P` sorted rows each and a slice of the columns.  Runs inside a wave go out directly, runs over waves
 //                  are joined through LDS, runs over workgroups through partial sums that the last of them to finish adds in order.
 //                  A fixed number of rows to a workgroup and not of ids: texts have one token in ten the same, and padding more.
@@ -156,7 +160,7 @@ template <typename TI, typename TO, int VEC>
 void launch_lookup(hipStream_t st, ProfScope& ps, LookupArgs a) {
   a.pieces = a.d / VEC;
   a.magic = a.pieces == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.pieces - 1) / a.pieces);
-  // four pieces a thread where that leaves 1024 blocks and more, else one (the first of the above U1_BATCH us with one)
+  // four pieces a thread where that leaves 1024 blocks and more, else one (the first of the above 25.5 us with one, the second 5.7 with either)
   const bool many = a.n * a.pieces >= (int64_t)1024 * 1024;
   a.rows = (int)std::max<int64_t>(1, (many ? 1024 : 256) / a.pieces);
   const uint32_t blocks = (uint32_t)std::min<int64_t>((a.n + a.rows - 1) / a.rows, 1 << 20);
