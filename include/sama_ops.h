@@ -96,8 +96,8 @@ sama_status sama_op_nudge(float* theta, const float* vdir, const float* eps_ptr,
  * Types are SAMA_DTYPE_*; fp32 and bf16 may be mixed where a type is given for each side.  Strides (ld*) are in values, at least the row's length.
  * Any length, alignment (of a value) and stride is accepted; rows whose length, start and stride are multiples of 16 bytes are moved in
  * pieces of that size.  Sums are held in 32 bits or more, in a fixed order: the same call gives the same bits.  Workspaces need 256-byte
- * alignment and nothing in them beforehand; calls that overlap in time need one each.  An argument that is refused gives SAMA_EINVAL,
- * launches nothing, and sama_op_last_error() says which. */
+ * alignment and nothing in them beforehand; calls that overlap in time need one each.  Outputs must not overlap inputs, one another or the
+ * workspace.  An argument that is refused gives SAMA_EINVAL, launches nothing, and sama_op_last_error() says which. */
 
 /* out[i][:] = scale * table[id_i][:] for n tokens (table [V x d]).  Ids outside [0, V) are clamped into it, as everywhere in this
  * library; pad_id >= 0: the rows of that id (before clamping) are zero whatever the table holds there, -1: there is no such id. */
@@ -132,7 +132,8 @@ sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* 
  * pointers 16-byte aligned.  SAMA_DTYPE_FP32: any d, F, stride and alignment of a value.  Strides at most 2^21, d and F at most 2^20, d F below 2^29
  * (fp32: 2^28).  T at most 2^22, 0 does nothing.  saved: DEVICE, sama_op_glu_ffn_saved_bytes() bytes, 16-byte aligned, receives what the backward call needs besides hidden (a layout
  * of the library's own), or NULL.  workspace: DEVICE, 256-byte aligned, sama_op_glu_ffn_bytes() bytes.  The size functions return 0 for sizes
- * that the calls refuse; a size for T tokens suffices for fewer.  What a token gets may depend in its last bits on how many tokens it comes with; the same call gives the same bits. */
+ * that the calls refuse; a size for T tokens suffices for fewer.  What a token gets may depend in its last bits on how many tokens it comes
+ * with; the same call gives the same bits. */
 enum { SAMA_ACT_SILU = 0, SAMA_ACT_GELU = 1 };
 size_t sama_op_glu_ffn_bytes(int64_t T, int32_t d, int32_t F, int32_t dtype);
 size_t sama_op_glu_ffn_saved_bytes(int64_t T, int32_t F, int32_t dtype);

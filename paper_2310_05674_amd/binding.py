@@ -422,17 +422,15 @@ def _torch():
     return torch
 
 
-def _dtype(t):
-    """SAMA_DTYPE_* of a tensor (-1, which the library refuses, for any other type)."""
-    if not _DTYPES:
-        _torch()
-    return _DTYPES.get(t.dtype, -1)
+_torch_c = None
 
 
 def _raw_stream():
     """The current stream of the current device, as a number."""
-    c = _torch()._C
-    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+    global _torch_c
+    if _torch_c is None:
+        _torch_c = _torch()._C
+    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())
 
 
 def _rows(t, d, what):
@@ -450,6 +448,13 @@ def _ids(ids, n):
         raise ValueError(f"ids: expected {n} contiguous int32 values on the GPU")
 
 
+def _space(t):
+    """Bytes of a workspace."""
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError("workspace: expected contiguous memory on the GPU")
+    return t.nbytes
+
+
 def _op(rc, name):
     if rc != 0:
         raise SamaError(rc, load_library().sama_op_last_error().decode() or name + " failed")
@@ -458,12 +463,17 @@ def _op(rc, name):
 def op_embedding(table, ids, out, *, scale=1.0, pad_id=-1):
     """out[i] = scale * table[ids[i]] through sama_op_embedding.  table [V, d] and out [n, d]: fp32 or bf16 CUDA tensors with contiguous rows; ids: n
     int32 values; rows of pad_id come out as zeros."""
-    V, d = table.shape
-    n = out.shape[0]
     stream = _raw_stream()
+    V, d = table.shape
+    n, width = out.shape
+    # (a lookup of a text takes the time of this function and of a launch: what most calls are is seen in few steps)
+    ld, step = table.stride()
+    ldo, step_out = out.stride()
+    if not (step == 1 and step_out == 1 and width == d and n > 1 and V > 1 and table.is_cuda and out.is_cuda):
+        ld, ldo = _rows(table, d, "table"), _rows(out, d, "out")
     _ids(ids, n)
-    rc = load_library().sama_op_embedding(table.data_ptr(), _dtype(table), _rows(table, d, "table"), ids.data_ptr(), n, V, d, scale, pad_id,
-                                          out.data_ptr(), _dtype(out), _rows(out, d, "out"), stream)
+    rc = (_lib or load_library()).sama_op_embedding(table.data_ptr(), _DTYPES.get(table.dtype, -1), ld, ids.data_ptr(), n, V, d, scale, pad_id, out.data_ptr(),
+                                                    _DTYPES.get(out.dtype, -1), ldo, stream)
     if rc != 0:
         _op(rc, "sama_op_embedding")
 
@@ -475,12 +485,16 @@ def embedding_grad_bytes(n, V, d):
 def op_embedding_grad(dy, ids, grad, workspace, *, scale=1.0, pad_id=-1, accumulate=False):
     """grad[v] = scale * the sum of dy over the tokens with id v (added to grad with `accumulate`) through sama_op_embedding_grad.  dy [n, d], grad
     [V, d]: fp32 or bf16; workspace: uint8, embedding_grad_bytes(n, V, d)."""
-    n, d = dy.shape
     stream = _raw_stream()
+    n, d = dy.shape
+    V, width = grad.shape
+    ld, step = dy.stride()
+    ldg, step_grad = grad.stride()
+    if not (step == 1 and step_grad == 1 and width == d and n > 1 and V > 1 and dy.is_cuda and grad.is_cuda):
+        ld, ldg = _rows(dy, d, "dy"), _rows(grad, d, "grad")
     _ids(ids, n)
-    rc = load_library().sama_op_embedding_grad(dy.data_ptr(), _dtype(dy), _rows(dy, d, "dy"), ids.data_ptr(), n, grad.shape[0], d, scale, pad_id,
-                                               1 if accumulate else 0, grad.data_ptr(), _dtype(grad), _rows(grad, d, "grad"), workspace.data_ptr(),
-                                               workspace.numel(), stream)
+    rc = (_lib or load_library()).sama_op_embedding_grad(dy.data_ptr(), _DTYPES.get(dy.dtype, -1), ld, ids.data_ptr(), n, V, d, scale, pad_id, 1 if accumulate else 0,
+                                                         grad.data_ptr(), _DTYPES.get(grad.dtype, -1), ldg, workspace.data_ptr(), _space(workspace), stream)
     if rc != 0:
         _op(rc, "sama_op_embedding_grad")
 
@@ -501,14 +515,14 @@ def op_grad_clip(grads, max_norm, norm, workspace, *, out=None, status=None):
     for g in grads:
         if not (g.is_contiguous() and g.is_cuda):
             raise ValueError("grads: expected contiguous CUDA tensors")
-    if norm.dtype != torch.float32 or norm.numel() < 2 or not norm.is_contiguous():
-        raise ValueError("norm: expected two contiguous fp32 values")
-    if out is not None and (out.dtype != torch.float32 or out.numel() != sum(counts) or not out.is_contiguous()):
-        raise ValueError(f"out: expected {sum(counts)} contiguous fp32 values")
-    if status is not None and (status.dtype != torch.int64 or status.numel() < 1):
-        raise ValueError("status: expected an int64 value")
+    if norm.dtype != torch.float32 or norm.numel() < 2 or not norm.is_contiguous() or not norm.is_cuda:
+        raise ValueError("norm: expected two contiguous fp32 values on the GPU")
+    if out is not None and (out.dtype != torch.float32 or out.numel() != sum(counts) or not out.is_contiguous() or not out.is_cuda):
+        raise ValueError(f"out: expected {sum(counts)} contiguous fp32 values on the GPU")
+    if status is not None and (status.dtype != torch.int64 or status.numel() < 1 or not status.is_cuda):
+        raise ValueError("status: expected an int64 value on the GPU")
     rc = load_library().sama_op_grad_clip(n, pointers.buffer_info()[0], counts.buffer_info()[0], dtypes.buffer_info()[0], max_norm, _p(out), _p(norm),
-                                          _p(status), _p(workspace), workspace.numel(), _raw_stream())
+                                          _p(status), _p(workspace), _space(workspace), _raw_stream())
     if rc != 0:
         _op(rc, "sama_op_grad_clip")
 
@@ -558,8 +572,8 @@ def op_glu_ffn(x, w_in, w_out, y, hidden, workspace, *, act="silu", saved=None):
     _dense(w_in, (2 * F, d), t, "w_in"); _dense(w_out, (d, F), t, "w_out"); _dense(hidden, (T, F), t, "hidden")
     if saved is not None:
         _scratch(saved, glu_ffn_saved_bytes(T, F, t), "saved")
-    _op(load_library().sama_op_glu_ffn(_p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), T, d, F, ACT[act], _glu_dtype(t), _p(y),
-                                       _glu_rows(y, T, d, t, "y"), _p(hidden), _p(saved), _p(workspace), workspace.numel(), _raw_stream()), "sama_op_glu_ffn")
+    _op(load_library().sama_op_glu_ffn(_p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), T, d, F, ACT.get(act, -1), _glu_dtype(t), _p(y),
+                                       _glu_rows(y, T, d, t, "y"), _p(hidden), _p(saved), _p(workspace), _space(workspace), _raw_stream()), "sama_op_glu_ffn")
 
 
 def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, workspace, *, act="silu"):
@@ -571,5 +585,5 @@ def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, worksp
     _dense(dw_in, (2 * F, d), dw_in.dtype, "dw_in"); _dense(dw_out, (d, F), dw_in.dtype, "dw_out")
     _scratch(saved, glu_ffn_saved_bytes(T, F, t), "saved")
     _op(load_library().sama_op_glu_ffn_grad(_p(dy), _glu_rows(dy, T, d, t, "dy"), _p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), _p(hidden),
-                                            _p(saved), T, d, F, ACT[act], _glu_dtype(t), _p(dx), _glu_rows(dx, T, d, t, "dx"), _p(dw_in), _p(dw_out),
-                                            _glu_dtype(dw_in.dtype), _p(workspace), workspace.numel(), _raw_stream()), "sama_op_glu_ffn_grad")
+                                            _p(saved), T, d, F, ACT.get(act, -1), _glu_dtype(t), _p(dx), _glu_rows(dx, T, d, t, "dx"), _p(dw_in), _p(dw_out),
+                                            _glu_dtype(dw_in.dtype), _p(workspace), _space(workspace), _raw_stream()), "sama_op_glu_ffn_grad")

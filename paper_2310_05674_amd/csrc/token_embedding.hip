@@ -121,7 +121,7 @@ struct LookupArgs {
 
 // A block takes `rows` rows, its threads the pieces of VEC values of all of them one after the other, U of them at a time so that
 // the loads of the ids, then those of the rows, are under way together.  Bound by memory: 32768 tokens of 1024, a quarter of them padding, from an fp32 table
-// into bf16 in 21.0 us, 90 MB of distinct rows and output (4.3 TB/s; 168 MB with what the caches answer); 128 tokens of 256 in 5.7, which is the call: the
+// into bf16 in 21.0 us, 90 MB of distinct rows and output (4.3 TB/s; 168 MB with what the caches answer); 128 tokens of 256 in 5.2, which is the call: the
 // kernel takes 2.4.
 template <typename TI, typename TO, int VEC, int U>
 __global__ __launch_bounds__(256) void k_embedding(LookupArgs a) {
@@ -160,7 +160,7 @@ template <typename TI, typename TO, int VEC>
 void launch_lookup(hipStream_t st, ProfScope& ps, LookupArgs a) {
   a.pieces = a.d / VEC;
   a.magic = a.pieces == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + a.pieces - 1) / a.pieces);
-  // four pieces a thread where that leaves 1024 blocks and more, else one (the first of the above 25.5 us with one, the second 5.7 with either)
+  // four pieces a thread where that leaves 1024 blocks and more, else one (the first of the above 25.5 us with one, the second the same with either)
   const bool many = a.n * a.pieces >= (int64_t)1024 * 1024;
   a.rows = (int)std::max<int64_t>(1, (many ? 1024 : 256) / a.pieces);
   const uint32_t blocks = (uint32_t)std::min<int64_t>((a.n + a.rows - 1) / a.rows, 1 << 20);

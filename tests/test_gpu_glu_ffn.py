@@ -304,3 +304,43 @@ def test_in_a_graph_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
+
+
+def test_what_the_binding_refuses():
+    """On the host, other types or shapes, an unknown gate: an error that launches nothing."""
+    from paper_2310_05674_amd import binding as B
+    T, d, F = 5, 64, 72
+    new = lambda *s, dtype=torch.bfloat16, device=DEV: torch.zeros(*s, dtype=dtype, device=device)
+    good = dict(x=new(T, d), w_in=new(2 * F, d), w_out=new(d, F), y=new(T, d), hidden=new(T, F), ws=new(B.glu_ffn_bytes(T, d, F, torch.bfloat16), dtype=torch.uint8), act="silu",
+                saved=new(B.glu_ffn_saved_bytes(T, F, torch.bfloat16), dtype=torch.uint8))
+
+    def forward(**change):
+        a = dict(good, **change)
+        B.op_glu_ffn(a["x"], a["w_in"], a["w_out"], a["y"], a["hidden"], a["ws"], act=a["act"], saved=a["saved"])
+
+    forward()
+    for k in ("x", "w_in", "w_out", "y", "hidden", "ws", "saved"):
+        with pytest.raises(ValueError):
+            forward(**{k: good[k].cpu()})
+    for bad in (dict(w_in=new(F, d)), dict(y=new(T + 1, d)), dict(y=new(T, d, dtype=torch.float32)), dict(hidden=new(T, F + 8)), dict(saved=good["saved"][:-1]), dict(x=new(T, 2 * d)[:, ::2])):
+        with pytest.raises(ValueError):
+            forward(**bad)
+    for bad in (dict(act="relu"), dict(ws=good["ws"][:-1])):
+        with pytest.raises(B.SamaError):
+            forward(**bad)
+    back = dict(dy=new(T, d), dx=new(T, d), dwi=new(2 * F, d), dwo=new(d, F), ws=new(B.glu_ffn_grad_bytes(T, d, F, torch.bfloat16), dtype=torch.uint8))
+
+    def backward(**change):
+        a = dict(good, **dict(back, **change))
+        B.op_glu_ffn_grad(a["dy"], a["x"], a["w_in"], a["w_out"], a["hidden"], a["saved"], a["dx"], a["dwi"], a["dwo"], a["ws"], act=a["act"])
+
+    backward()
+    for k in back:
+        with pytest.raises(ValueError):
+            backward(**{k: back[k].cpu()})
+    for bad in (dict(dwi=new(2 * F, d + 8)), dict(dwo=new(d, F, dtype=torch.float32)), dict(dx=new(T, d, dtype=torch.float32))):
+        with pytest.raises(ValueError):
+            backward(**bad)
+    for bad in (dict(act="tanh"), dict(ws=back["ws"][:-1])):
+        with pytest.raises(B.SamaError):
+            backward(**bad)

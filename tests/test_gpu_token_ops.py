@@ -364,3 +364,29 @@ def test_token_gradient_of_few_tokens_on_top(n, V, d):
     assert np.array_equal(f64(grad)[unseen], before[unseen])
     B.op_embedding_grad(dy, ids, grad, ws, scale=0.75)
     check_grad(dy, ids, V, grad, 0.75)
+
+
+def test_tensors_that_the_binding_refuses():
+    """On the host, wrong types, strided rows of values: the binding says so before the library sees a pointer."""
+    from paper_2310_05674_amd import binding as B
+    new = lambda *s, dtype=torch.float32, device=DEV: torch.zeros(*s, dtype=dtype, device=device)
+    table, ids, out, grad = new(10, 8), new(5, dtype=torch.int32), new(5, 8), new(10, 8)
+    ws, clip = new(B.embedding_grad_bytes(5, 10, 8), dtype=torch.uint8), new(B.grad_clip_bytes(), dtype=torch.uint8)
+    norm, status = new(2), new(1, dtype=torch.int64)
+    for bad in (dict(table=new(10, 8, device="cpu")), dict(out=new(5, 8, device="cpu")), dict(ids=ids.cpu()), dict(ids=ids.long()), dict(ids=new(4, dtype=torch.int32)), dict(out=new(5, 7)),
+                dict(table=new(10, 16)[:, ::2]), dict(out=new(8, 5).t())):
+        a = dict(dict(table=table, ids=ids, out=out), **bad)
+        with pytest.raises(ValueError):
+            B.op_embedding(a["table"], a["ids"], a["out"])
+    for bad in (dict(dy=out.cpu()), dict(grad=grad.cpu()), dict(ids=ids.cpu()), dict(ws=ws.cpu()), dict(grad=new(10, 7)), dict(dy=new(5, 16)[:, ::2]), dict(ws=new(2 * ws.numel(), dtype=torch.uint8)[::2])):
+        a = dict(dict(dy=out, ids=ids, grad=grad, ws=ws), **bad)
+        with pytest.raises(ValueError):
+            B.op_embedding_grad(a["dy"], a["ids"], a["grad"], a["ws"])
+    for bad in (dict(g=[grad.cpu()]), dict(g=[new(8, 10).t()]), dict(norm=norm.cpu()), dict(norm=norm.double()), dict(out=new(80, device="cpu")), dict(out=new(79)), dict(status=status.cpu()),
+                dict(status=status.int()), dict(ws=clip.cpu())):
+        a = dict(dict(g=[grad], norm=norm, out=None, status=None, ws=clip), **bad)
+        with pytest.raises(ValueError):
+            B.op_grad_clip(a["g"], 1.0, a["norm"], a["ws"], out=a["out"], status=a["status"])
+    for half in (table.half(), ):
+        with pytest.raises(B.SamaError):
+            B.op_embedding(half, ids, out)
