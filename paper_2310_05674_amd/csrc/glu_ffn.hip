@@ -805,8 +805,11 @@ __global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
 typedef Tile<256, 256, 2, 4, 2, 0, 2, 0, 1> T256;
 typedef Tile<256, 128, 4, 2, 3, 4, 2, 2, 1> T192;   // (the number between: 192)
 typedef Tile<128, 128, 2, 4, 4, 4, 0, 1, 1> T128;
-typedef Tile<64, 64, 2, 2, 4, 0, 0, 1, 2> T64;
-typedef Tile<32, 32, 2, 1, 6, 0, 0, 1, 3> T32;
+// Waves that only load also in the small ones: a wave that multiplies between its barriers asks for the next slab too late when there are two or three to a
+// SIMD.  us without / with, forward and backward: fp32 512 x 256 x 688 50.2 / 45.5, 6299 x 264 x 528 220 / 205; bf16 300 x 768 x 2048 41.1 / 36.8, 700 x 512 x 1368
+// 36.2 / 35.1, 2100 x 80 x 216 29.5 / 26.5.
+typedef Tile<64, 64, 2, 2, 4, 4, 0, 1, 2> T64;
+typedef Tile<32, 32, 2, 1, 6, 2, 0, 1, 3> T32;
 
 template <auto KERNEL, typename T, typename A>
 void launch_big(ProfScope& ps, hipStream_t st, uint32_t grid, const A& a) {
