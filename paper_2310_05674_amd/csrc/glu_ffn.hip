@@ -798,7 +798,7 @@ __global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
 //   256 x 256     155      68 + 16      127       307 + 15         28.8     22.4 + 10.7
 //   256 x 128     158      58           130       347 + 10         27.6     18.0 + 7.3
 //   128 x 128     212      76           126       346              33.1     17.2
-//   64 x 64       286     113           160       609              54.9     26.0
+//   64 x 64       268      110         149       604              44.9     21.2
 // The large tiles read the least from LDS for a product and are bound by power in the loop (1.5 us of a slab; k_glu_up without its epilogue 126 us); what is left is
 // the epilogue, whose 67 MB of h and 201 MB of g and u nothing hides: two workgroups to a CU, workgroups out of step and deeper stages gained nothing.  The
 // smaller ones are for sizes whose large tiles do not fill the chip.  128 x 96 for y, whose 256 tiles the second size would fill exactly, takes 16.2 us.
@@ -1074,8 +1074,8 @@ void launch_glu_ffn_grad(hipStream_t st, const GluFfnGradArgs& g, void* workspac
 size_t glu_ffn_f32_saved_bytes(int64_t T, int F) { return (size_t)T * 2 * F * 4; }
 size_t glu_ffn_f32_bytes(int64_t T, int d, int F) { return std::max(forward_bytes<float>(T, d, F), glu_ffn_plain_bytes(T, F)); }
 size_t glu_ffn_f32_grad_bytes(int64_t T, int d, int F) { return std::max(backward_bytes<float>(T, d, F), glu_ffn_plain_grad_bytes(T, F)); }
-// fp32 whose rows are pieces of 16 bytes goes through the tiles: 512 x 256 x 688 with gelu 50 us forward and backward, of any width, stride and alignment through the
-// products of the MLPs: 512 x 255 x 687 69 us (forward alone 20.6 and 21.6); both keep g and u in the same place, so a forward call of the one
+// fp32 whose rows are pieces of 16 bytes goes through the tiles: 512 x 256 x 688 with gelu 45.5 us forward and backward, of any width, stride and alignment through the
+// products of the MLPs: 512 x 255 x 687 69 us; both keep g and u in the same place, so a forward call of the one
 // may be followed by a backward call of the other.
 void launch_glu_ffn_f32(hipStream_t st, const GluFfnArgs& g, void* workspace) {
   const bool tiles = g.d % 4 == 0 && g.F % 4 == 0 && pieces32(g.x, g.ldx) && pieces32(g.y, g.ldy) && pieces32(g.w_in, 0) && pieces32(g.w_out, 0) && pieces32(g.hidden, 0);
