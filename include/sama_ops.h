@@ -161,8 +161,8 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
  *    5 (128 x 64), anything else is SAMA_EINVAL; 0 = the heuristic (default).  No bit of a result depends on it.
  *  - sama_dev_gemm_counts(counts, 2): HOST counts since the last call: launches of that kernel for forward products and for input gradients.
  *  - sama_dev_glu_tile(t + 1000 p): the products of the gated feed-forward block use the t x t tile, t = 32, 64, 128 or 256, or 256 x 128 for
- *    t = 192 (fp32: 128 at most), and cut their contractions into p parts where these are long enough (p = 0: by the heuristic); 0 = the
- *    heuristic for both (default).  The order of the sums goes with p.
+ *    t = 192 (fp32: 128 at most), and cut their contractions into p parts where these are long enough (t = 0 or p = 0: by the heuristic); 0 = the
+ *    heuristic for both (default).  The order of the sums goes with p.  Anything else is SAMA_EINVAL and leaves the switch as it was.
  *  - sama_dev_side_stream(0): the encoder's backward passes keep every launch on the context's stream (a per-kernel profile
  *    wants one stream); 1 = default: weight gradients and optimizer slices run on the library's second stream where rows and
  *    layers are large enough for it; 2: they do for every size.  Any other value means 1.  A base step keeps its bits; a
@@ -172,7 +172,7 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
 void sama_dev_gemm_shape(int32_t id);
 sama_status sama_dev_gemm_rows(uint64_t choice);
 sama_status sama_dev_gemm_counts(int64_t* counts, int32_t n);
-void sama_dev_glu_tile(int32_t tile);
+sama_status sama_dev_glu_tile(int32_t tile);
 void sama_dev_side_stream(int32_t mode);
 void sama_dev_side_sink(int32_t on);
 

@@ -133,7 +133,7 @@ def load_library():
     L.sama_op_glu_ffn.restype = C.c_int; L.sama_op_glu_ffn.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, vp, sz, vp]
     L.sama_op_glu_ffn_grad.restype = C.c_int
     L.sama_op_glu_ffn_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, sz, vp]
-    L.sama_dev_glu_tile.restype = None; L.sama_dev_glu_tile.argtypes = [i32]
+    L.sama_dev_glu_tile.restype = C.c_int; L.sama_dev_glu_tile.argtypes = [i32]
     _lib = L
     return L
 

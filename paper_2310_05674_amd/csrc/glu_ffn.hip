@@ -9,6 +9,7 @@
 //                 tiles of a product are too few, or a few too many for a round, the contraction is cut as well, and k_glu_join adds the parts
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 #include <type_traits>
 #include <utility>
 #include "kernels.h"
@@ -1063,7 +1064,12 @@ void backward(hipStream_t st, const GluFfnGradArgs& g, void* workspace) {
 bool pieces32(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 4 == 0; }
 }  // namespace
 
-void glu_ffn_force_tile(int t) { g_force_tile = t % 1000; g_force_parts = t / 1000; }
+bool glu_ffn_force_tile(int t) {
+  const int tile = t % 1000;
+  if (t < 0 || (tile != 0 && std::none_of(std::begin(COST16), std::end(COST16), [&](const TileCost& c) { return c.tile == tile; }))) return false;   // no plan would have it
+  g_force_tile = tile; g_force_parts = t / 1000;
+  return true;
+}
 
 size_t glu_ffn_saved_bytes(int64_t T, int F) { return (size_t)((T + 15) / 16) * ((F + 15) / 16) * SAVED_BLOCK; }
 size_t glu_ffn_bytes(int64_t T, int d, int F) { return forward_bytes<bf16_t>(T, d, F); }

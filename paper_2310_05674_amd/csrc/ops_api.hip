@@ -364,6 +364,6 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
   else launch_glu_ffn_grad_f32((hipStream_t)hip_stream, a, workspace);
   return launched(op);
 }
-void sama_dev_glu_tile(int32_t tile) { glu_ffn_force_tile(tile); }
+sama_status sama_dev_glu_tile(int32_t tile) { return glu_ffn_force_tile(tile) ? SAMA_OK : SAMA_EINVAL; }
 
 }  // extern "C"

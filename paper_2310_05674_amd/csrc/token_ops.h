@@ -57,6 +57,6 @@ size_t glu_ffn_plain_bytes(int64_t T, int F);
 size_t glu_ffn_plain_grad_bytes(int64_t T, int F);
 void launch_glu_ffn_plain(hipStream_t, const GluFfnArgs&, void* workspace);
 void launch_glu_ffn_grad_plain(hipStream_t, const GluFfnGradArgs&, void* workspace);
-void glu_ffn_force_tile(int tile);   // tuning hook: 0 = heuristic
+bool glu_ffn_force_tile(int tile);   // tuning hook: 0 = heuristic; false for a tile that there is not
 
 }  // namespace sama

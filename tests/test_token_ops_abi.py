@@ -112,3 +112,14 @@ def test_sizes_beyond_a_launch(lib):
             refused(lib, "sama_op_glu_ffn_grad", down, [dict()])
             assert lib.sama_op_glu_ffn_bytes(5, d, F, dtype) == lib.sama_op_glu_ffn_grad_bytes(5, d, F, dtype) == 0
         assert lib.sama_op_glu_ffn_bytes(5, 8, 2 ** 20, dtype) > 0 and lib.sama_op_glu_ffn_grad_bytes(5, 2 ** 20, 8, dtype) > 0
+
+
+def test_tile_switch_refusals(lib):
+    """The development switch takes the tiles that there are, alone or with a number of parts; anything else is refused and changes nothing."""
+    try:
+        for tile in (32, 64, 128, 192, 256, 3064, 16256, 4000, 0):
+            assert lib.sama_dev_glu_tile(tile) == 0, tile
+        for tile in (1, 16, 31, 33, 96, 127, 129, 255, 257, 512, 999, 1001, 2100, 3065, -1, -32, -64, -1000, -3064, 2 ** 31 - 1, -2 ** 31):
+            assert lib.sama_dev_glu_tile(tile) == 1, tile
+    finally:
+        lib.sama_dev_glu_tile(0)
