@@ -434,12 +434,12 @@ def _raw_stream():
 
 
 def _rows(t, d, what):
-    """A 2-D tensor on the GPU whose rows are d neighbouring values -> its row stride."""
+    """A 2-D tensor on the GPU whose rows are d neighbouring values -> its row stride (of a single row: its length, whatever the stride says)."""
     shape = t.shape
     if len(shape) == 2 and shape[1] == d and t.is_cuda:
         ld, step = t.stride()
         if step == 1 or d == 1 or shape[0] == 0:
-            return ld if shape[0] > 1 else max(d, ld)
+            return ld if shape[0] > 1 else d
     raise ValueError(f"{what}: expected a [n, {d}] CUDA tensor with contiguous rows, got {tuple(shape)}, strides {t.stride()}")
 
 

@@ -390,3 +390,34 @@ def test_tensors_that_the_binding_refuses():
     for half in (table.half(), ):
         with pytest.raises(B.SamaError):
             B.op_embedding(half, ids, out)
+
+
+def test_one_row_of_any_stride():
+    """A matrix of one row has no stride to speak of: torch calls it contiguous whatever it is a row of, and the operators take it."""
+    from paper_2310_05674_amd import binding as B
+    t, d, F, V = torch.bfloat16, 136, 72, 40
+
+    def row(seed, width):
+        whole = torch.zeros(2, width, dtype=t, device=DEV)
+        whole[:1, :d].copy_(values(seed, 1, d))
+        return whole[:1, :d]
+
+    scratch = lambda n: torch.empty(n, dtype=torch.uint8, device=DEV)
+    new = lambda *s: torch.empty(*s, dtype=t, device=DEV)
+    w_in, w_out = (values(1, 2 * F, d) * 0.1).to(t), (values(2, d, F) * 0.1).to(t)
+    for width in (d + 1, 2 ** 21 + 8):                        # odd, and beyond what the strides of several rows may be
+        x, dy, y, dx = (row(k, width) for k in (3, 4, 5, 6))
+        assert x.is_contiguous() and x.stride(0) == width
+        out = []
+        for a, b, c, e in ((x, dy, y, dx), (new(1, d).copy_(x), new(1, d).copy_(dy), new(1, d), new(1, d))):
+            hidden, saved, dwi, dwo = new(1, F), scratch(B.glu_ffn_saved_bytes(1, F, t)), new(2 * F, d), new(d, F)
+            B.op_glu_ffn(a, w_in, w_out, c, hidden, scratch(B.glu_ffn_bytes(1, d, F, t)), saved=saved)
+            B.op_glu_ffn_grad(b, a, w_in, w_out, hidden, saved, e, dwi, dwo, scratch(B.glu_ffn_grad_bytes(1, d, F, t)))
+            out.append([v.clone() for v in (c, e, hidden, dwi, dwo)])
+        assert all(torch.equal(p, q) for p, q in zip(*out))
+        table, ids = values(7, V, d).to(t), torch.full((1,), 17, dtype=torch.int32, device=DEV)
+        B.op_embedding(table, ids, y, scale=2.0)
+        assert torch.equal(y[0], (table[17].float() * 2.0).to(t))
+        grad = new(V, d)
+        B.op_embedding_grad(dy, ids, grad, scratch(B.embedding_grad_bytes(1, V, d)))
+        assert torch.equal(grad[17], dy[0]) and not grad[:17].any() and not grad[18:].any()
