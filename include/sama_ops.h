@@ -118,7 +118,8 @@ sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_
  * factor = min(1, max_norm / (norm + 1e-6)).  grads, counts, dtypes: HOST arrays of `count` DEVICE pointers, numbers of values and types.
  * out: DEVICE fp32 [sum of counts], receives factor * g of all tensors one after the other (the flat gradient of sama_op_adam), or NULL: the
  * gradients are scaled in place, and not touched where the factor is 1.  max_norm > 0; infinity gives the norm alone (out receives copies).
- * norm_out: DEVICE fp32 [2] = {norm, factor}.  status: DEVICE, or NULL: 1 if the norm is not finite, in which case the factor is 1, else 0.
+ * norm_out: DEVICE fp32 [2] = {norm, factor}, each rounded to fp32 (a finite norm beyond its range to infinity; what is applied is not the rounded factor
+ * where that is below 2^-100, but one of all 24 bits).  status: DEVICE, or NULL: 1 if the norm is not finite, in which case the factor is 1, else 0.
  * workspace: DEVICE, sama_op_grad_clip_bytes() bytes.  The tensors must not overlap one another nor out. */
 size_t sama_op_grad_clip_bytes(void);
 sama_status sama_op_grad_clip(int64_t count, void* const* grads, const int64_t* counts, const int32_t* dtypes, float max_norm, float* out,

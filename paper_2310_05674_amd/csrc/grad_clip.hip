@@ -135,10 +135,16 @@ __global__ __launch_bounds__(THREADS) void k_square_sums(ClipTable t) {
 // Results go past the caches, which keep the gradients for the second reading instead, and the next norm does not wait for them to be written back: the 217 MB
 // above take 196 us with ordinary stores instead of 156, the 25 MB the same with both.
 __device__ __forceinline__ void store_once(char* p, f32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(p)); }
+// The factor as two, applied one after the other: 1 and itself, or 2^-64 and 2^64 times itself where it is so small that fp32 would hold it in fewer bits (norms beyond
+// fp32's range).  The first product is exact, unless the second rounds to zero.
+struct Factor {
+  float first, second;
+  __device__ __forceinline__ float operator()(float x) const { return x * first * second; }
+};
 // One unit, whose values are in v if it is a whole one, times f to `dest` (the tensor's place): bf16 in place, else fp32.
-__device__ __forceinline__ void scale_unit(const Unit& u, const uint4 (&v)[PER], void* dest, bool to_bf16, float f) {
+__device__ __forceinline__ void scale_unit(const Unit& u, const uint4 (&v)[PER], void* dest, bool to_bf16, Factor f) {
   auto one = [&](int64_t i) {
-    const float x = value_at(u, i) * f;
+    const float x = f(value_at(u, i));
     if (to_bf16) static_cast<bf16_t*>(dest)[i] = f32_to_bf16(x);
     else static_cast<float*>(dest)[i] = x;
   };
@@ -150,14 +156,14 @@ __device__ __forceinline__ void scale_unit(const Unit& u, const uint4 (&v)[PER],
       const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
       const int piece = i * THREADS + threadIdx.x;
       if (!u.half) {
-        store_once(at + piece * 16, (f32x4){__uint_as_float(w[0]) * f, __uint_as_float(w[1]) * f, __uint_as_float(w[2]) * f, __uint_as_float(w[3]) * f});
+        store_once(at + piece * 16, (f32x4){f(__uint_as_float(w[0])), f(__uint_as_float(w[1])), f(__uint_as_float(w[2])), f(__uint_as_float(w[3]))});
       } else if (to_bf16) {
-        *reinterpret_cast<uint4*>(at + piece * 16) = make_uint4(pack_bf16x2(low(w[0]) * f, high(w[0]) * f), pack_bf16x2(low(w[1]) * f, high(w[1]) * f),
-                                                                pack_bf16x2(low(w[2]) * f, high(w[2]) * f), pack_bf16x2(low(w[3]) * f, high(w[3]) * f));
+        *reinterpret_cast<uint4*>(at + piece * 16) = make_uint4(pack_bf16x2(f(low(w[0])), f(high(w[0]))), pack_bf16x2(f(low(w[1])), f(high(w[1]))),
+                                                                pack_bf16x2(f(low(w[2])), f(high(w[2]))), pack_bf16x2(f(low(w[3])), f(high(w[3]))));
       } else {
         const int first = 2 * i * THREADS + threadIdx.x;
-        store_once(at + first * 16, (f32x4){low(w[0]) * f, high(w[0]) * f, low(w[1]) * f, high(w[1]) * f});
-        store_once(at + (first + THREADS) * 16, (f32x4){low(w[2]) * f, high(w[2]) * f, low(w[3]) * f, high(w[3]) * f});
+        store_once(at + first * 16, (f32x4){f(low(w[0])), f(high(w[0])), f(low(w[1])), f(high(w[1]))});
+        store_once(at + (first + THREADS) * 16, (f32x4){f(low(w[2])), f(high(w[2])), f(low(w[3])), f(high(w[3]))});
       }
     }
   } else {
@@ -186,7 +192,9 @@ __global__ __launch_bounds__(THREADS) void k_clip(ClipTable t) {
   for (int i = 0; i < PARTIALS / THREADS; ++i) s += part[i];
   const double norm = sqrt(block_sum64(s, red));
   const bool finite = norm <= 1.7976931348623157e308;
-  const float factor = finite ? (float)fmin(1.0, t.max_norm / (norm + 1e-6)) : 1.f;
+  const double exact = finite ? fmin(1.0, t.max_norm / (norm + 1e-6)) : 1.0;
+  const float factor = (float)exact;
+  const Factor scale = exact < 0x1p-100 ? Factor{0x1p-64f, (float)(exact * 0x1p64)} : Factor{1.f, factor};
   if (t.norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) {
     t.norm[0] = (float)norm; t.norm[1] = factor;
     if (t.status != nullptr) *t.status = finite ? 0 : 1;
@@ -198,8 +206,8 @@ __global__ __launch_bounds__(THREADS) void k_clip(ClipTable t) {
       u = unit_at(t, k, unit);
       if (u.whole()) load_whole(u, t.out != nullptr && u.half, v);
     }
-    if (t.out != nullptr) scale_unit(u, v, t.out + t.to[k], false, factor);
-    else scale_unit(u, v, t.p[k], u.half != 0, factor);
+    if (t.out != nullptr) scale_unit(u, v, t.out + t.to[k], false, scale);
+    else scale_unit(u, v, t.p[k], u.half != 0, scale);
   }
 }
 }  // namespace

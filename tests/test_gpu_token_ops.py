@@ -421,3 +421,21 @@ def test_one_row_of_any_stride():
         grad = new(V, d)
         B.op_embedding_grad(dy, ids, grad, scratch(B.embedding_grad_bytes(1, V, d)))
         assert torch.equal(grad[17], dy[0]) and not grad[:17].any() and not grad[18:].any()
+
+
+@pytest.mark.parametrize("grad_t", ["fp32", "bf16"])
+def test_clipping_by_a_factor_below_the_normal_numbers(grad_t):
+    """A norm of 2e40, which is beyond fp32, takes a factor of 5e-41, which fp32 holds in seventeen bits: the results keep theirs.  Two products, each with one
+    rounding, of a factor rounded once; bf16 in place rounds once more."""
+    g = torch.full((5000,), 3e38, device=DEV).to(T[grad_t])
+    g[::7] *= -0.5; g[1::7] = 1e-3; g[2::7] = 0.0
+    b = f64(g)
+    norm = np.sqrt(np.sum(b * b))
+    out, status = torch.empty(5000, device=DEV), torch.full((1,), 7, dtype=torch.int64, device=DEV)
+    for dest in (out, None):
+        got = clip([g], 1.0, out=dest, status=status)
+        # the norm is known in 64 bits: it is finite and it clips; as an fp32 value it is infinite
+        assert got[0] == np.inf and abs(got[1] * norm - 1) < 1e-4 and int(status) == 0
+    for t in (out, g):
+        bar = 3.1 * U32 + (U16 * 1.001 if t.dtype == torch.bfloat16 else 0)
+        assert np.all(np.abs(f64(t) - b / norm) <= bar * np.abs(b / norm) + 2.0 ** -133), float(np.max(np.abs(f64(t) * norm - b) / (np.abs(b) + 1e-30)))
