@@ -439,3 +439,38 @@ def test_clipping_by_a_factor_below_the_normal_numbers(grad_t):
     for t in (out, g):
         bar = 3.1 * U32 + (U16 * 1.001 if t.dtype == torch.bfloat16 else 0)
         assert np.all(np.abs(f64(t) - b / norm) <= bar * np.abs(b / norm) + 2.0 ** -133), float(np.max(np.abs(f64(t) * norm - b) / (np.abs(b) + 1e-30)))
+
+
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+@pytest.mark.parametrize("types", [("fp32",), ("bf16",), ("bf16", "fp32"), ("fp32", "bf16", "bf16")])
+def test_clipping_by_blocks_of_several_units(types, max_norm):
+    """More units of 32 KB than there are blocks: a block walks a run of them, over parts of units, over the ends of tensors and from one type to the other.  More
+    tensors than a launch takes, so that the runs begin anew; every one begins off 16 bytes, and after the first odd one so does its place in `out`."""
+    sizes = [2 ** 25 + 8191, 3, 2 ** 25 - 5, 16385, 1, 2 ** 23 + 77] + [8191 + 4099 * (k % 7) for k in range(120)] + [2 ** 24 + 1, 0, 40000]
+    grads, total = [], sum(sizes)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    for k, n in enumerate(sizes):
+        whole = torch.randn(n + 8, device=DEV, generator=gen).mul_(10.0 ** -(k % 3)).to(T[types[k % len(types)]])
+        grads.append(whole[k % 4:k % 4 + n])
+    units = sum(-(-n // (16384 if g.dtype == torch.bfloat16 else 8192)) for n, g in zip(sizes[:100], grads))
+    assert units > 4096
+    # norm in 64 bits on the GPU, tensor by tensor
+    norm = float(sum((g.double() ** 2).sum() for g in grads) ** 0.5)
+    factor = min(1.0, max_norm / (norm + 1e-6))
+    before = [g.clone() for g in grads]
+    out = torch.full((total + 1,), 3.0, device=DEV)[1:]
+    for dest in (out, None):
+        got = clip(grads, max_norm, out=dest)
+        assert abs(got[0] - norm) <= 1.01 * U32 * norm and abs(got[1] - factor) <= 1.01 * U32 * factor
+        at = 0
+        for g, b in zip(grads, before):
+            if dest is not None:
+                assert torch.equal(g, b)
+                got_g, bar = out[at:at + g.numel()], 2.1 * U32
+            else:
+                got_g, bar = g, 2.1 * U32 + (U16 * 1.001 if g.dtype == torch.bfloat16 else 0)
+            at += g.numel()
+            if factor == 1.0:
+                assert torch.equal(got_g.float(), b.float())
+            want = b.double() * factor
+            assert bool(((got_g.double() - want).abs() <= bar * want.abs()).all())
