@@ -474,3 +474,25 @@ def test_clipping_by_blocks_of_several_units(types, max_norm):
                 assert torch.equal(got_g.float(), b.float())
             want = b.double() * factor
             assert bool(((got_g.double() - want).abs() <= bar * want.abs()).all())
+
+
+@pytest.mark.parametrize("table_t,out_t", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("n,V,d", [(32769, 50, 256), (4099, 60, 1030), (4097, 33, 2048), (1100003, 9, 1), (70001, 700, 120), (1048577, 3, 1030), (1048579, 3, 4104)])
+def test_lookup_of_many(n, V, d, table_t, out_t):
+    """Sizes where a thread takes four pieces at a time, whole ones and value by value; with more than 2^20 blocks of one row, where a block goes on to more rows, and
+    outputs of more than 2^32 values; ids beyond the table, and padding."""
+    from paper_2310_05674_amd import binding as B
+    vec = 8 if table_t == out_t == "bf16" else 4
+    pieces = d // vec if d % vec == 0 else d
+    assert n * pieces >= 2 ** 20
+    table = values(n + d, V, d).to(T[table_t])
+    ids = token_ids("outside", n, V, n)
+    out = torch.full((n + 1, d), 9.0, dtype=T[out_t], device=DEV)
+    B.op_embedding(table, ids, out[:n], scale=1.7, pad_id=2)
+    scaled = (table.float() * torch.tensor(1.7, device=DEV)).to(T[out_t])
+    for i0 in range(0, n, 2 ** 17):
+        t = ids[i0:i0 + 2 ** 17]
+        want = scaled[t.clamp(0, V - 1).long()]
+        want[t == 2] = 0
+        assert torch.equal(out[i0:min(i0 + 2 ** 17, n)], want)
+    assert bool((out[n] == 9.0).all())
