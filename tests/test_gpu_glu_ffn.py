@@ -344,3 +344,20 @@ def test_what_the_binding_refuses():
     for bad in (dict(act="tanh"), dict(ws=back["ws"][:-1])):
         with pytest.raises(B.SamaError):
             backward(**bad)
+
+
+@pytest.mark.parametrize("dtype,T,d,F", [("bf16", 270001, 64, 8008), ("fp32", 270001, 64, 8004), ("fp32", 135001, 63, 8001)])
+def test_offsets_beyond_32_bits(dtype, T, d, F):
+    """More than 2^31 hidden values (the last: gates), and twice as many gates and gradients of them; checked a few thousand tokens at a time.  A sum over T tokens is
+    within (T + 2) u of the sum of their sizes, which is at most the number of pieces times the bars of the pieces added up."""
+    i = inputs(T, d, F, dtype, 1)
+    got = run(i, "silu", dw="fp32")
+    step, bars, sums = 13000, {}, {}
+    for t0 in range(0, T, step):
+        part = dict(i, x=i["x"][t0:t0 + step], dy=i["dy"][t0:t0 + step])
+        want = exact(part, "silu")
+        check({k: got[k][t0:t0 + step] for k in ("y", "hidden", "dx")}, want, dtype == "bf16")
+        for k in ("dw_in", "dw_out"):
+            sums[k] = want[k][0] + sums.get(k, 0.0)
+            bars[k] = want[k][1] + bars.get(k, 0.0)
+    check({k: got[k] for k in sums}, {k: (sums[k], bars[k] * -(-T // step)) for k in sums}, dtype == "bf16")

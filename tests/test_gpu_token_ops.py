@@ -496,3 +496,43 @@ def test_lookup_of_many(n, V, d, table_t, out_t):
         want[t == 2] = 0
         assert torch.equal(out[i0:min(i0 + 2 ** 17, n)], want)
     assert bool((out[n] == 9.0).all())
+
+
+@pytest.mark.parametrize("dy_t,grad_t", [("bf16", "bf16"), ("fp32", "fp32")])
+def test_token_gradient_beyond_32_bits(dy_t, grad_t):
+    """More than 2^31 values of dy and of the gradient: ids from the whole table, and again on top of what is there."""
+    from paper_2310_05674_amd import binding as B
+    n, V, d = 2 ** 21 + 7, 2 ** 21 + 5, 1032
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    ids = torch.randint(0, V, (n,), device=DEV, generator=gen, dtype=torch.int32)
+    ids[::5] = V - 1 - ids[::5] % 3                       # two hundred thousand tokens each of the last three
+    dy = torch.randint(-1, 2, (n, d), device=DEV, generator=gen, dtype=torch.int8).to(T[dy_t])   # every sum is an integer, and exact in fp32
+    grad = torch.full((V, d), 7.0, dtype=T[grad_t], device=DEV)
+    ws = torch.empty(B.embedding_grad_bytes(n, V, d), dtype=torch.uint8, device=DEV)
+    for accumulate in (False, True):
+        B.op_embedding_grad(dy, ids, grad, ws, scale=2.0, accumulate=accumulate)
+        for c in range(0, d, 258):
+            want = torch.zeros(V, 258, device=DEV).index_add_(0, ids, dy[:, c:c + 258].float()).mul_(2.0).to(T[grad_t])
+            if accumulate:
+                want = (want.float() + torch.zeros(V, 258, device=DEV).index_add_(0, ids, dy[:, c:c + 258].float()).mul_(2.0)).to(T[grad_t])
+            assert torch.equal(grad[:, c:c + 258], want)
+
+
+def test_token_gradient_of_more_tokens_than_a_list_numbers():
+    """More than 2^23 tokens to a wave of the sort, which then looks through them again, and a run over half a million workgroups."""
+    from paper_2310_05674_amd import binding as B
+    n, V = 2 ** 27 + 700 * 450 + 3, 700
+    i = torch.arange(n, device=DEV, dtype=torch.int32)
+    half = n // 2 // V * V
+    ids = torch.where(i < half, 5, i % V)
+    dy = torch.randint(-1, 2, (n, 1), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1), dtype=torch.int8).float()   # sums are integers below 2^24
+    grad = torch.full((V, 1), 7.0, device=DEV)
+    ws = torch.empty(B.embedding_grad_bytes(n, V, 1), dtype=torch.uint8, device=DEV)
+    B.op_embedding_grad(dy, ids, grad, ws, scale=1.0)
+    want = torch.zeros(V, dtype=torch.float64, device=DEV)
+    rest = dy[half:, 0].double()
+    whole = len(rest) // V * V
+    want += rest[:whole].view(-1, V).sum(0)
+    want[:len(rest) - whole] += rest[whole:]
+    want[5] += dy[:half, 0].double().sum()
+    assert torch.equal(grad[:, 0].double(), want)
