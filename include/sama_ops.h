@@ -94,7 +94,7 @@ sama_status sama_op_nudge(float* theta, const float* vdir, const float* eps_ptr,
 /* ---- Operators of a token model's base step beyond the encoder's own: a scaled embedding, clipped gradients, and a gated
  * feed-forward block.
  * Types are SAMA_DTYPE_*; fp32 and bf16 may be mixed where a type is given for each side.  Strides (ld*) are in values, at least the row's length.
- * Any length, alignment (of a value) and stride is accepted; rows whose length, start and stride are multiples of 16 bytes are moved in
+ * Any length, alignment (of a value) and stride is accepted, but for the bf16 block, see there; rows whose length, start and stride are multiples of 16 bytes are moved in
  * pieces of that size.  Sums are held in 32 bits or more, in a fixed order: the same call gives the same bits.  Workspaces need 256-byte
  * alignment and nothing in them beforehand; calls that overlap in time need one each.  Outputs must not overlap inputs, one another or the
  * workspace.  An argument that is refused gives SAMA_EINVAL, launches nothing, and sama_op_last_error() says which. */
@@ -106,9 +106,9 @@ sama_status sama_op_embedding(const void* table, int32_t table_dtype, int64_t ld
 
 /* Its gradient: grad[v][:] = scale * sum over the i with id_i = v of dy[i][:], in ascending i (dy [n x d], grad [V x d]).  Padding contributes
  * nothing and its rows of dy are not read.  accumulate = 0: every row of grad is written, zeros where no token has the id; 1: the sums are
- * added to grad (a table that is also the output matrix), and rows without a token are left alone.  V is at most 2^30, n below 2^30, and so is n
- * times the pieces of a row (64 lanes' loads of 16 bytes each, of a value where rows do not consist of such).  workspace: DEVICE,
- * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for n, V or d out of range), which suffices for fewer tokens too. */
+ * added to grad (a table that is also the output matrix), and rows without a token are left alone.  V is at most 2^30; n, up to
+ * the next multiple of 128, times the pieces of a row (64 lanes' loads of 16 bytes each, of a value where rows do not consist of such) is below 2^30.  workspace: DEVICE,
+ * sama_op_embedding_grad_bytes(n, V, d) bytes (0 for n below 0 or above 2^30, V or d below 1), which suffices for fewer tokens too. */
 size_t sama_op_embedding_grad_bytes(int64_t n, int32_t V, int32_t d);
 sama_status sama_op_embedding_grad(const void* dy, int32_t dy_dtype, int64_t ld_dy, const int32_t* ids, int64_t n, int32_t V, int32_t d,
                                    float scale, int32_t pad_id, int32_t accumulate, void* grad, int32_t grad_dtype, int64_t ld_grad,

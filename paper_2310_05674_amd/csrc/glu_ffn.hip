@@ -301,10 +301,12 @@ __device__ __forceinline__ uint4 side_by_side(f32x4 a, f32x4 b) {
 __device__ __forceinline__ int pair_column(int lane) { return 16 * ((lane >> 4) & 1) + 8 * (lane >> 5); }
 
 // The gate and its derivative: silu(g) = g s, silu'(g) = s + g s (1 - s) with s = 1 / (1 + exp(-g)); gelu(g) = g P(g), gelu'(g) = P(g) + g p(g) with the
-// normal distribution P and its density p.  In fp32 with the full-precision exp and erf.  In bf16, where the result is rounded to 2^-9 of itself, with the
+// normal distribution P and its density p.  In fp32 with the full-precision exp and erf: 1 + erf leaves
+// P within 6e-8, which below -5 is as large as P.  In bf16, where the result is rounded to 2^-9 of itself, with the
 // hardware's exp2 and reciprocal, and P through its logarithm, which is smooth: P(-x) = 2^q(x) for x >= 0 with a q of degree seven, fitted here to log2 P(-x) on
-// [0, 7.5] (Chebyshev points, errors beyond 3.5 counting less).  Its errors: 4e-6 of P down to -3.5, 5e-5 down to -6, 6e-7 of gelu anywhere; q falls
-// on to minus infinity.  An exp2 and eight multiply-adds, where an erf by exp and reciprocal is twice that, and the epilogue of a tile has nothing to hide it
+// [0, 7.5] (Chebyshev points, errors beyond 3.5 counting less).  Its errors: 4e-6 of P down to -3.5, 5e-5 down to -6, 1.6e-4 down to -7.5, where P is 3e-14; behind the fitted end
+// they pass the rounding to bf16 (2 % at -9, two thirds at -12), of a P of 1e-19 and less, while q falls on to minus infinity.  Of gelu 6e-7
+// anywhere.  An exp2 and eight multiply-adds, where an erf by exp and reciprocal is twice that, and the epilogue of a tile has nothing to hide it
 // behind: both projections of 4096 x 768 x 2048 29.3 us instead of 30.9, 26.0 without any gate.
 __device__ __forceinline__ float normal_cdf(float g) {
   const float x = fabsf(g);
@@ -804,7 +806,7 @@ __global__ __launch_bounds__(512) void k_glu_down_rows(DownFewArgs a) {
 // the epilogue, whose 67 MB of h and 201 MB of g and u nothing hides: two workgroups to a CU, workgroups out of step and deeper stages gained nothing.  The
 // smaller ones are for sizes whose large tiles do not fill the chip.  128 x 96 for y, whose 256 tiles the second size would fill exactly, takes 16.2 us.
 typedef Tile<256, 256, 2, 4, 2, 0, 2, 0, 1> T256;
-typedef Tile<256, 128, 4, 2, 3, 4, 2, 2, 1> T192;   // (the number between: 192)
+typedef Tile<256, 128, 4, 2, 3, 4, 2, 2, 1> T192;   // (the number between: 192; the weights' gradients in bf16 keep 3 of its registers in scratch, 16 bytes a lane)
 typedef Tile<128, 128, 2, 4, 4, 4, 0, 1, 1> T128;
 // Waves that only load also in the small ones: a wave that multiplies between its barriers asks for the next slab too late when there are two or three to a
 // SIMD.  us without / with, forward and backward: fp32 512 x 256 x 688 50.2 / 45.5, 6299 x 264 x 528 220 / 205; bf16 300 x 768 x 2048 41.1 / 36.8, 700 x 512 x 1368
@@ -852,6 +854,10 @@ void launch_dgate(ProfScope& ps, hipStream_t st, DgateArgs a, int act) {
 }
 // ---- which tile, and into how many parts a contraction is cut, by what a launch costs in us: pieces are started in their order, longest first, each on the
 // workgroup slot that is free first; a piece takes its slabs' time, by how many workgroups share the CU, and `fixed`; parts are written, read and added.
+// The times are those of operands with the contraction contiguous, and of the 64 x 64 and 32 x 32 tiles before these had waves that only load.  Where they are off, us
+// planned / taken: y of 4096 x 768 x 2048 in 64 x 64 tiles 29.9 / 21.2; 67 MB of parts 26 / 14 to 16; the gradients of 8192 x 1024 x 4096, whose operands run along the other
+// index (1.8 us of a 256 x 256 slab), 252 / 293 to 310.  Training, every launch in one tile / as planned: 1021 x 520 x 1368 52.0 at best (64 x 64) / 47.7,
+// 4096 x 768 x 2048 156.2 (128 x 128) / 152.6.
 struct TileCost { int tile, bm, bn, per_cu; double one, full, fixed; };   // us of a slab with one workgroup to a CU and with per_cu
 constexpr TileCost COST16[] = {{256, 256, 256, 1, 1.50, 1.50, 6.0}, {192, 256, 128, 1, 0.85, 0.85, 4.0}, {128, 128, 128, 1, 0.52, 0.52, 2.5}, {64, 64, 64, 2, 0.27, 0.42, 1.5}, {32, 32, 32, 3, 0.20, 0.37, 1.2}};
 constexpr TileCost COST32[] = {{128, 128, 128, 1, 2.00, 2.00, 3.0}, {64, 64, 64, 2, 0.72, 1.10, 2.0}, {32, 32, 32, 3, 0.32, 0.60, 1.5}};

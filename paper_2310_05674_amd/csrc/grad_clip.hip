@@ -9,7 +9,9 @@
 // models of up to TENSORS tensors: the blocks of the second add the partial sums up for themselves instead of waiting for a last block, while
 // their first unit is on its way.  Up to PARTIALS blocks: 217 MB of bf16 matrices and fp32 vectors into 434 MB of flat gradient take 148 us (5.9 TB/s of
 // what is read twice and written), with 2048 blocks 154, and 154 with 4096 blocks that walk backwards in the second kernel, towards what the last-level
-// cache should still hold; 25 MB in place, out of the caches, 17.3 us, of which two launches are a third.
+// cache should still hold; 25 MB into a flat gradient, out of the caches, 17.3 us, of which two launches are a third.  Matrices alone, into `out` / in place: 6.3 million fp32
+// values 16.0 / 16.0, 108 million 246 / 268, in bf16 146 / 130.  A tensor whose place in `out` is off 16 bytes (any behind one of odd length) goes out value by value and
+// is read once more: 319 for 246, bf16 255 for 146.
 #include <algorithm>
 #include <cmath>
 #include "../../include/sama_ops.h"
