@@ -79,7 +79,7 @@ sama_status sama_op_adapt_norm_static(const float* g, const float* m, const floa
                                       int64_t n, int64_t t, float lr, float beta1, float beta2, float eps, float alpha,
                                       float* scalars, int64_t* status, void* hip_stream);
 /* Text of the last error of an op-level call on this thread (HOST string owned by the library, "" if none); set by
- * sama_op_adapt_norm_static and the calls of a token model's step below. */
+ * sama_op_adapt_norm_static and the calls of a token model's step and sequences below. */
 const char* sama_op_last_error(void);
 
 /* Low halves of theta +- eps v against the bf16 working copy (Eq. 5): lo_p/lo_m[k] = bf16((theta[k] +- eps v[k]) -
@@ -150,6 +150,63 @@ size_t sama_op_glu_ffn_grad_bytes(int64_t T, int32_t d, int32_t F, int32_t dtype
 sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_in, const void* w_out, const void* hidden,
                                  const void* saved, int64_t T, int32_t d, int32_t F, int32_t act, int32_t dtype, void* dx, int64_t lddx,
                                  void* dw_in, void* dw_out, int32_t dw_dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- Operators of a token model's sequences: rotary positions, attention within spans of keys, distillation from a teacher's top logits.
+ * Types, streams, workspaces, overlap, order of sums and refusals as above.  [tokens][heads][width] tensors have a stride between tokens (ld) and one between heads (hs), in
+ * values, each at least the width; the width is dense.  So the parts of a product's rows [T][(Hq + 2 Hk) D] can be taken in place, and [heads][tokens][width] as well. */
+
+/* Rotary positions.  Of each head's D values the first R = 2 sum(sections) turn in pairs, pair i (i = 0 .. R/2 - 1) by phi = positions[a][t] base^(-2 i / R):
+ *     (x, y) -> (x cos phi - y sin phi, x sin phi + y cos phi);  inverse = 1: by -phi, which is also the gradient.
+ * neighbours = 0: pair i is values i and i + R/2; 1: values 2 i and 2 i + 1.  sections: HOST array [axes] of numbers of pairs: the first sections[0] turn by axis a = 0, the next
+ * sections[1] by axis 1 and so on (time, height and width of a video; text has one axis).  positions: DEVICE int32 [axes][T], any value.  The other D - R values are copied.  Angles are
+ * formed in 64 bits.  x and out [T][H][D] in dtype; out may be x itself, with the same strides.  axes 1 to 4, R 2 to 256, H D up to 2^20, T up to 2^23. */
+sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, int32_t H, int32_t D, int32_t dtype, const int32_t* positions, int32_t axes,
+                           const int32_t* sections, double base, int32_t neighbours, int32_t inverse, void* out, int64_t ldo, int64_t hso, void* hip_stream);
+
+/* Attention.  Query i of head h sees the keys begin <= j < end of its span (spans: DEVICE int32 [Tq][2], clipped to [0, Tk)) of key head h Hk / Hq:
+ *     s_j = scale q_i . k_j;  with cap > 0: s_j = cap tanh(s_j / cap);  with slopes: s_j -= slopes[h] |at_i - j|
+ *     p = softmax of s over those j,  out_i = sum_j p_j v_j,  lse_i = log sum_j exp(s_j)
+ * A query that sees nothing has out = 0 and lse = minus infinity.  Spans of packed documents come from sama_op_attention_spans; a cache per text, rows of padding,
+ * windows or any other interval of keys for each query can be given as well, in any order.  Keys and values that a query does not see do not reach it, whatever they hold; a value that is not finite
+ * reaches those that see it as one that is not finite, if not the same.
+ * q, out [Tq][Hq][D], k, v [Tk][Hk][D]; Hq a multiple of Hk, at most 64 times it; D a multiple of 8 up to 128; strides multiples of 16 bytes, ld at most 2^21, (Hq/Hk - 1) hs of q and dout
+ * below 2^30 bytes; pointers 16-byte aligned; Tq Hq and Tk Hk up to 2^28.  at: DEVICE int32 [Tq], the place of each query among the keys, or NULL: query i is beside key i (Tq = Tk).
+ * slopes: DEVICE fp32 [Hq], or NULL; constants, they get no gradient.  lse: DEVICE fp32 [Tq][Hq], natural logarithm, or NULL.  scale > 0; cap 0: none.
+ * bf16: probabilities are rounded to bf16 before their product with v, sums are fp32; fp32: nothing is rounded.  workspace: sama_op_attention_bytes(), for these very sizes (0 for sizes that are refused). */
+typedef struct { void* p; int64_t ld, hs; } sama_heads;
+typedef struct {
+  sama_heads q, k, v, out;
+  const int32_t *spans, *at;
+  const float* slopes;
+  float* lse;
+  int64_t Tq, Tk;
+  int32_t Hq, Hk, D, dtype;
+  float scale, cap;
+  sama_heads dout, dq, dk, dv;   /* of the gradients */
+} sama_attention;
+size_t sama_op_attention_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype);
+sama_status sama_op_attention(const sama_attention* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients: dq, dk, dv, all overwritten, from dout, the inputs, out and lse of the forward call (HOST struct, the same arguments).  A query that sees nothing has dq = 0 and its rows of
+ * q and dout reach nobody; keys that nobody sees have dk = dv = 0.  Key heads shared by several heads get the sum, in a fixed order.  bf16: probabilities and the scores' gradients
+ * are rounded to bf16 before the products they enter. */
+size_t sama_op_attention_grad_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype);
+sama_status sama_op_attention_grad(const sama_attention* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Spans of T packed tokens: document n is the tokens offsets[n] <= t < offsets[n + 1] (DEVICE int32 [documents + 1], not decreasing; clipped to [0, T)), and a token sees its
+ * document; causal = 1: of it only what is not behind the token, and the first prefix[n] tokens (DEVICE int32 [documents], or NULL: none).  Tokens outside every document see nothing. */
+sama_status sama_op_attention_spans(const int32_t* offsets, int64_t documents, const int32_t* prefix, int32_t causal, int64_t T, int32_t* spans, void* hip_stream);
+
+/* Distillation from a teacher's top logits, the loss of each token and its gradient.  Token i has student logits z [V] and up to K entries (ids[i][k], teacher[i][k]):
+ *     p = softmax over its entries of teacher / temperature,  q = softmax over the vocabulary of z / temperature
+ *     loss_i = temperature^2 sum_k p_k (log p_k - log q_{ids k}),   dz_ij = dloss_i temperature (q_j - sum over the k with ids k = j of p_k)
+ * Entries with an id outside [0, V) or a logit of minus infinity are none, whatever else they hold; a token without entries has loss 0, gradient 0, and its logits are not read.  An id may be listed more than once.  With K = 1 and
+ * temperature 1 this is the cross-entropy of a label.  logits [T][V] in dtype with row stride ldz, any alignment; ids int32, teacher fp32 [T][K], dense; K 1 to 256; loss fp32 [T]; saved fp32 [T][2], for the gradient; temperature
+ * 1e-4 to 1e4; T up to 2^22, 0 does nothing.  dlogits [T][V] in dtype, with stride lddz, may be logits themselves with the same stride; dloss fp32 [T]. */
+sama_status sama_op_distill(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,
+                            float* loss, float* saved, void* hip_stream);
+sama_status sama_op_distill_grad(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,
+                                 const float* dloss, const float* saved, void* dlogits, int64_t lddz, void* hip_stream);
 
 /* Diagnostic switches, process-wide, for tests and profiling.  They take effect from the next launch and are not
  * thread-safe.

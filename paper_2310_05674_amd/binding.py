@@ -3,6 +3,7 @@ supplies device memory and the current HIP stream, every step runs in the librar
 fallback: without libsama.so (or without a GPU) construction fails."""
 import ctypes as C
 import os
+import struct
 from array import array
 
 MODEL_MLP, MODEL_ENCODER = 0, 1
@@ -134,6 +135,14 @@ def load_library():
     L.sama_op_glu_ffn_grad.restype = C.c_int
     L.sama_op_glu_ffn_grad.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, sz, vp]
     L.sama_dev_glu_tile.restype = C.c_int; L.sama_dev_glu_tile.argtypes = [i32]
+    L.sama_op_rotary.restype = C.c_int; L.sama_op_rotary.argtypes = [vp, i64, i64, i64, i32, i32, i32, vp, i32, vp, C.c_double, i32, i32, vp, i64, i64, vp]
+    L.sama_op_attention_bytes.restype = sz; L.sama_op_attention_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    L.sama_op_attention_grad_bytes.restype = sz; L.sama_op_attention_grad_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    L.sama_op_attention.restype = C.c_int; L.sama_op_attention.argtypes = [vp, vp, sz, vp]
+    L.sama_op_attention_grad.restype = C.c_int; L.sama_op_attention_grad.argtypes = [vp, vp, sz, vp]
+    L.sama_op_attention_spans.restype = C.c_int; L.sama_op_attention_spans.argtypes = [vp, i64, vp, i32, i64, vp, vp]
+    L.sama_op_distill.restype = C.c_int; L.sama_op_distill.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, vp, vp]
+    L.sama_op_distill_grad.restype = C.c_int; L.sama_op_distill_grad.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp]
     _lib = L
     return L
 
@@ -587,3 +596,129 @@ def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, worksp
     _op(load_library().sama_op_glu_ffn_grad(_p(dy), _glu_rows(dy, T, d, t, "dy"), _p(x), _glu_rows(x, T, d, t, "x"), _p(w_in), _p(w_out), _p(hidden),
                                             _p(saved), T, d, F, ACT.get(act, -1), _glu_dtype(t), _p(dx), _glu_rows(dx, T, d, t, "dx"), _p(dw_in), _p(dw_out),
                                             _glu_dtype(dw_in.dtype), _p(workspace), _space(workspace), _raw_stream()), "sama_op_glu_ffn_grad")
+
+
+# ------------------------------------------------------------------------------------- operators of a token model's sequences
+def _heads(t, shape, dtype, what):
+    """A [tokens, heads, width] tensor of the current device whose width is dense -> its address and the strides between tokens and heads (of a single one: as
+    if it were dense, whatever the stride says)."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{what}: expected a {tuple(shape)} CUDA tensor of {dtype}, got {tuple(t.shape)}, {t.dtype}")
+    ld, hs, step = t.stride()
+    if step != 1 and shape[2] > 1:
+        raise ValueError(f"{what}: expected a dense last dimension, got strides {t.stride()}")
+    if shape[1] == 1:
+        hs = shape[2]
+    if shape[0] <= 1:
+        ld = max(hs, shape[2])
+    return t.data_ptr(), ld, hs
+
+
+def _words(t, shape, dtype, what):
+    """A contiguous tensor of 32-bit values -> its address."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {tuple(shape)} CUDA tensor of {dtype}, got {tuple(t.shape)}, {t.dtype}")
+    return t.data_ptr()
+
+
+def op_rotary(x, positions, out, *, sections=None, base=10000.0, neighbours=False, inverse=False):
+    """Rotary positions through sama_op_rotary.  x, out [T, H, D] (out may be x), fp32 or bf16, a dense last dimension; positions int32 [T] or [axes, T]; sections: how many
+    pairs turn by each axis (by default all D // 2 by one).  inverse: the other way round, which is the gradient."""
+    torch = _torch()
+    T, H, D = x.shape
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    if sections is None:
+        sections = (D // 2,)
+    if len(sections) != axes:
+        raise ValueError(f"sections: expected one for each of {axes} axes, got {tuple(sections)}")
+    at = _words(positions, (T,) if positions.dim() == 1 else (axes, T), torch.int32, "positions")
+    px, ldx, hsx = _heads(x, x.shape, x.dtype, "x")
+    po, ldo, hso = _heads(out, x.shape, x.dtype, "out")
+    counts = array("i", sections)
+    rc = load_library().sama_op_rotary(px, ldx, hsx, T, H, D, _DTYPES.get(x.dtype, -1), at, axes, counts.buffer_info()[0], base, 1 if neighbours else 0,
+                                       1 if inverse else 0, po, ldo, hso, _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_rotary")
+
+
+def op_attention_spans(offsets, spans, *, causal=False, prefix=None):
+    """spans [T, 2] int32: the keys [begin, end) that each of T packed tokens sees, through sama_op_attention_spans.  offsets: int32 [documents + 1], where documents begin, and the
+    end of the last; causal: only up to the token itself, and the first prefix[n] tokens (int32 [documents]) of its document."""
+    i32 = _torch().int32
+    n = offsets.numel() - 1
+    T = spans.shape[0]
+    rc = load_library().sama_op_attention_spans(_words(offsets, (n + 1,), i32, "offsets"), n, None if prefix is None else _words(prefix, (n,), i32, "prefix"),
+                                                1 if causal else 0, T, _words(spans, (T, 2), i32, "spans"), _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_attention_spans")
+
+
+def attention_bytes(Tq, Tk, Hq, Hk, D, dtype):
+    return load_library().sama_op_attention_bytes(Tq, Tk, Hq, Hk, D, _glu_dtype(dtype))
+
+
+def attention_grad_bytes(Tq, Tk, Hq, Hk, D, dtype):
+    return load_library().sama_op_attention_grad_bytes(Tq, Tk, Hq, Hk, D, _glu_dtype(dtype))
+
+
+_ATTENTION = struct.Struct("@12q4P2q4i2f12q")   # sama_attention
+_NO_HEADS = (0, 0, 0)
+
+
+def _attention_args(q, k, v, out, spans, scale, cap, slopes, at, lse, dout=None, dq=None, dk=None, dv=None):
+    torch = _torch()
+    Tq, Hq, D = q.shape
+    Tk, Hk = k.shape[:2]
+    t, shape, keys = q.dtype, q.shape, (Tk, Hk, D)
+    grads = _NO_HEADS * 4 if dout is None else (*_heads(dout, shape, t, "dout"), *_heads(dq, shape, t, "dq"), *_heads(dk, keys, t, "dk"), *_heads(dv, keys, t, "dv"))
+    return _ATTENTION.pack(*_heads(q, shape, t, "q"), *_heads(k, keys, t, "k"), *_heads(v, keys, t, "v"), *_heads(out, shape, t, "out"),
+                           _words(spans, (Tq, 2), torch.int32, "spans"), 0 if at is None else _words(at, (Tq,), torch.int32, "at"),
+                           0 if slopes is None else _words(slopes, (Hq,), torch.float32, "slopes"), 0 if lse is None else _words(lse, (Tq, Hq), torch.float32, "lse"),
+                           Tq, Tk, Hq, Hk, D, _DTYPES.get(t, -1), D ** -0.5 if scale is None else scale, cap, *grads)
+
+
+def op_attention(q, k, v, out, spans, workspace, *, scale=None, cap=0.0, slopes=None, at=None, lse=None):
+    """Attention of q [Tq, Hq, D] over the keys [begin, end) that spans (int32 [Tq, 2]) gives for each query of k, v [Tk, Hk, D], through sama_op_attention; out like q, all of
+    one type, fp32 or bf16, strided views with a dense last dimension.  scale: D ** -0.5 by default; cap: scores become cap tanh(score / cap); slopes: fp32 [Hq], scores lose
+    slope |at - key| (at: int32 [Tq], by default 0, 1, ...); lse: fp32 [Tq, Hq], for the gradients, or None.  workspace: uint8, attention_bytes(Tq, Tk, Hq, Hk, D, dtype)."""
+    args = _attention_args(q, k, v, out, spans, scale, cap, slopes, at, lse)
+    rc = load_library().sama_op_attention(args, workspace.data_ptr(), _space(workspace), _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_attention")
+
+
+def op_attention_grad(dout, q, k, v, out, lse, spans, dq, dk, dv, workspace, *, scale=None, cap=0.0, slopes=None, at=None):
+    """Gradients of op_attention through sama_op_attention_grad: dq like q, dk and dv like k, overwritten, from dout like out; out and lse are those of the forward
+    call.  workspace: uint8, attention_grad_bytes(Tq, Tk, Hq, Hk, D, dtype)."""
+    args = _attention_args(q, k, v, out, spans, scale, cap, slopes, at, lse, dout, dq, dk, dv)
+    rc = load_library().sama_op_attention_grad(args, workspace.data_ptr(), _space(workspace), _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_attention_grad")
+
+
+def op_distill(logits, ids, teacher, loss, saved, *, temperature=1.0):
+    """The loss of each token against its teacher's listed logits through sama_op_distill.  logits [T, V] fp32 or bf16 with contiguous rows; ids int32 and teacher fp32 [T, K], ids outside the
+    vocabulary (-1) for no entry; loss fp32 [T]; saved fp32 [T, 2], for the gradient."""
+    torch = _torch()
+    T, V = logits.shape
+    K = ids.shape[1]
+    f32 = torch.float32
+    rc = load_library().sama_op_distill(logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES.get(logits.dtype, -1), T, V, _words(ids, (T, K), torch.int32, "ids"),
+                                        _words(teacher, (T, K), f32, "teacher"), K, temperature, _words(loss, (T,), f32, "loss"), _words(saved, (T, 2), f32, "saved"), _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_distill")
+
+
+def op_distill_grad(logits, ids, teacher, dloss, saved, dlogits, *, temperature=1.0):
+    """The gradient of sum(dloss * loss) of op_distill in its logits through sama_op_distill_grad: dlogits like logits, or logits themselves; saved is that of the forward call."""
+    torch = _torch()
+    T, V = logits.shape
+    K = ids.shape[1]
+    f32 = torch.float32
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape:
+        raise ValueError(f"dlogits: expected {tuple(logits.shape)}, {logits.dtype}, got {tuple(dlogits.shape)}, {dlogits.dtype}")
+    rc = load_library().sama_op_distill_grad(logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES.get(logits.dtype, -1), T, V, _words(ids, (T, K), torch.int32, "ids"),
+                                             _words(teacher, (T, K), f32, "teacher"), K, temperature, _words(dloss, (T,), f32, "dloss"), _words(saved, (T, 2), f32, "saved"),
+                                             dlogits.data_ptr(), _rows(dlogits, V, "dlogits"), _raw_stream())
+    if rc != 0:
+        _op(rc, "sama_op_distill_grad")

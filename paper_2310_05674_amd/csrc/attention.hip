@@ -1,0 +1,302 @@
+// Attention of queries over the keys of their spans.  For query i, head h and the key head h' that it shares with G - 1 others:
+//   s_j = scale q_i . k_j, capped: cap tanh(s_j / cap), biased: - slope_h |at_i - j|,   p = softmax of s over begin_i <= j < end_i,   o_i = sum_j p_j v_j.
+// One pass over the keys with the running maximum and sum of the softmax: 4 D operations a pair, nothing of the scores leaves the registers.
+//
+// The G heads of a key head are rows of the same tiles (row = query G + head), so K and V are read once for all of them.  A workgroup has 32 WM rows and walks the
+// tiles of keys between its rows' first and last; tiles that no row sees are left out.  Where rows are few its four waves share 32 rows and take different keys of a
+// tile (KG groups), and where workgroups are few the keys are split between several, joined by k_attention_join.
+#include <algorithm>
+#include <cmath>
+#include "attention_tiles.h"
+
+namespace sama {
+namespace {
+using namespace attn;
+
+template <typename E, int DP_, int WM_>
+struct Config {
+  static constexpr int DP = DP_, WM = WM_;
+  static constexpr int KG = WM > 1 ? 1 : sizeof(E) * DP > 256 ? 2 : 4;            // groups of waves with keys of their own
+  static constexpr int NS = WM > 1 && sizeof(E) * DP <= 256 ? 2 : 1;              // 32 keys each of a wave's part of a tile
+  static constexpr int WAVES = WM * KG, THREADS = WAVES * 64, BM = 32 * WM, BK = 32 * NS * KG;
+  static constexpr int KV = BK * DP * (int)sizeof(E), LDS = 4 * KV;               // K and V, two stages
+  static_assert(LDS <= LDS_MAX && KG * DP * 32 * 4 + KG * 256 <= LDS, "LDS");
+};
+
+struct Parts { float* o; float* lse; int count; };   // of split keys: [count][Hk][rows][D] and [count][Hk][rows]
+
+template <typename E, typename C, bool SHAPED>
+__global__ __launch_bounds__(C::THREADS) void k_attention(AttentionArgs a, Parts parts, int tiles) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  typedef Tile<E, C::DP> T;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int rw = wave / C::KG, kg = wave % C::KG;
+  const int G = a.Hq / a.Hk, rows = (int)a.Tq * G, D = a.D;
+  const int hk = blockIdx.x % a.Hk, tile = tiles - 1 - blockIdx.x / a.Hk;   // the last queries, which see the most of a causal text, first
+  const int row = tile * C::BM + rw * 32 + (lane & 31), query = min(row, rows - 1) / G, head = hk * G + min(row, rows - 1) % G;
+  const int2 span = span_of(a.spans, query, (int)a.Tk);
+  // spans of all of the workgroup's rows, two a lane
+  const int r0 = min(tile * C::BM + lane % C::BM, rows - 1), r1 = min(tile * C::BM + (lane + 64) % C::BM, rows - 1);
+  const int2 s0 = span_of(a.spans, r0 / G, (int)a.Tk), s1 = span_of(a.spans, r1 / G, (int)a.Tk);
+  const int lo = __builtin_amdgcn_readfirstlane(wave_min(min(s0.x < s0.y ? s0.x : 0x7fffffff, s1.x < s1.y ? s1.x : 0x7fffffff)));
+  const int hi = __builtin_amdgcn_readfirstlane(wave_max(max(s0.y, s1.y)));
+  int t = 0, end = hi > lo ? (hi - lo + C::BK - 1) / C::BK : 0;
+  if (parts.count > 1) {
+    const int64_t n = end;
+    t = (int)(n * blockIdx.y / parts.count); end = (int)(n * (blockIdx.y + 1) / parts.count);
+  }
+  auto seen_from = [&](int i) {
+    for (; i < end; ++i) {
+      const int k0 = lo + i * C::BK;
+      if (__any((s0.x < k0 + C::BK && s0.y > k0) || (s1.x < k0 + C::BK && s1.y > k0))) break;
+    }
+    return i;
+  };
+
+  Loads<E, C::DP, C::BK, C::WAVES> lk, lv;
+  lk.init(a.k.ld, 0, 1, D, wave, lane);
+  lv.init(a.v.ld, 0, 1, D, wave, lane);
+  const E* const kp = static_cast<const E*>(a.k.p) + hk * a.k.hs;
+  const E* const vp = static_cast<const E*>(a.v.p) + hk * a.v.hs;
+  const uint32_t lds = lds_address(smem);
+  auto issue = [&](int i, int stage) {
+    const int64_t k0 = lo + (int64_t)i * C::BK;
+    const u32x4 dk = descriptor(kp + k0 * a.k.ld, ((a.Tk - 1 - k0) * a.k.ld + D) * (int64_t)sizeof(E));
+    const u32x4 dv = descriptor(vp + k0 * a.v.ld, ((a.Tk - 1 - k0) * a.v.ld + D) * (int64_t)sizeof(E));
+    lk.issue(lds + stage * 2 * C::KV, dk, wave);
+    lv.issue(lds + stage * 2 * C::KV + C::KV, dv, wave);
+  };
+  t = seen_from(t);
+  if (t < end) issue(t, 0);
+
+  Frag<E> q[T::KS];
+  {
+    const E* const p = static_cast<const E*>(a.q.p) + query * a.q.ld + head * a.q.hs;
+#pragma unroll
+    for (int ks = 0; ks < T::KS; ++ks) q[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(p + 16 * ks + 8 * h) : zero_fragment<E>();
+  }
+  const Shape shape(a.scale, a.cap);
+  const float slope = SHAPED && a.slopes != nullptr ? a.slopes[head] * LOG2E : 0.f;
+  const int at = SHAPED && a.slopes != nullptr ? (a.at != nullptr ? a.at[query] : query) : 0;
+  const float c = SHAPED ? 1.f : a.scale * LOG2E;
+  f32x16 o[T::DF];
+#pragma unroll
+  for (int df = 0; df < T::DF; ++df) o[df] = zeros();
+  float m = -INF, l = 0.f;   // of the scores before the factor c; l: of the lane's own keys
+
+  for (int stage = 0; t < end; stage ^= 1) {
+    const int next = seen_from(t + 1);
+    wait_loads();
+    if (next < end) issue(next, stage ^ 1);
+    const unsigned char* const kt = smem + stage * 2 * C::KV;
+    const unsigned char* const vt = kt + C::KV;
+    const int k0 = lo + t * C::BK + kg * 32 * C::NS;   // the wave's first key
+    t = next;
+    if (!__any(span.x < k0 + 32 * C::NS && span.y > k0)) continue;
+    f32x16 s[C::NS];
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) {
+      s[n] = zeros();
+#pragma unroll
+      for (int ks = 0; ks < T::KS; ++ks) s[n] = mma(T::rows(kt, (kg * C::NS + n) * 32, ks, lane), q[ks], s[n]);
+    }
+    if (SHAPED) {
+      const int away = at - k0 - 4 * h;
+#pragma unroll
+      for (int n = 0; n < C::NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { float bend; s[n][r] = shape.score<E>(s[n][r], slope, fabsf((float)(away - 32 * n - 8 * (r >> 2) - (r & 3))), bend); }
+    }
+    const bool whole = __all(span.x <= k0 && span.y >= k0 + 32 * C::NS);
+    uint32_t seen[C::NS] = {};
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < C::NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + 32 * n + register_row(r, h);
+          const bool see = key >= span.x && key < span.y;
+          seen[n] |= (see ? 1u : 0u) << r;
+          s[n][r] = see ? s[n][r] : -INF;
+        }
+    }
+    float top = m;
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+    top = other_half_max(top);
+    if (__any(top > m)) {
+      const float shrink = m == -INF ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
+      l *= shrink;
+#pragma unroll
+      for (int df = 0; df < T::DF; ++df)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[df][r] *= shrink;
+      m = top;
+    }
+    const float base = m == -INF ? 0.f : m * c;
+    float sum = 0.f;
+    Frag<E> p[C::NS][2];
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, -base)); sum += s[n][r]; }
+      p[n][0] = fragment<E>(s[n], 0); p[n][1] = fragment<E>(s[n], 1);
+    }
+    l += sum;
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) {
+      if (whole) add_product<E, C::DP, 2>(o, vt, (kg * C::NS + n) * 32, p[n], lane);
+      else add_product_seen<E, C::DP, 2>(o, vt, (kg * C::NS + n) * 32, p[n], seen[n], lane);
+    }
+  }
+
+  l = other_half_sum(l);
+  if constexpr (C::KG > 1) {   // the groups' parts, each of its own maximum, through LDS; a wave then has 32 of the columns
+    __syncthreads();
+    float* const part = reinterpret_cast<float*>(smem);                     // [KG][DP][32]
+    float* const stat = part + C::KG * C::DP * 32;                          // [KG][2][32]
+#pragma unroll
+    for (int df = 0; df < T::DF; ++df)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) part[(kg * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)] = o[df][r];
+    if (h == 0) { stat[(kg * 2) * 32 + lane] = m; stat[(kg * 2 + 1) * 32 + lane] = l; }
+    __syncthreads();
+    float top = -INF, factor[C::KG];
+#pragma unroll
+    for (int g = 0; g < C::KG; ++g) top = fmaxf(top, stat[2 * g * 32 + (lane & 31)]);
+    l = 0.f;
+#pragma unroll
+    for (int g = 0; g < C::KG; ++g) {
+      const float mg = stat[2 * g * 32 + (lane & 31)];
+      factor[g] = mg == -INF ? 0.f : __builtin_amdgcn_exp2f((mg - top) * c);
+      l += stat[(2 * g + 1) * 32 + (lane & 31)] * factor[g];
+    }
+    m = top;
+#pragma unroll
+    for (int df = 0; df < T::DF; ++df) {
+      if (df % C::KG != kg) continue;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = 0.f;
+#pragma unroll
+        for (int g = 0; g < C::KG; ++g) x = fmaf(part[(g * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)], factor[g], x);
+        o[df][r] = x;
+      }
+    }
+  }
+  if (row >= rows) return;
+  const bool none = m == -INF && l == 0.f;   // no key, or scores of minus infinity alone
+  const float inv = none ? 0.f : 1.f / l, lse = none ? -INF : m * c + log2f(l);
+  const bool first = kg == 0 && h == 0;
+  if (parts.count > 1) {
+    const int64_t at_row = ((int64_t)blockIdx.y * a.Hk + hk) * rows + row;
+    if (first) parts.lse[at_row] = lse;
+#pragma unroll
+    for (int df = 0; df < T::DF; ++df) if (C::KG == 1 || df % C::KG == kg) store_columns<float>(parts.o + at_row * D, df, D, o[df], inv, h);
+  } else {
+    E* const p = const_cast<E*>(static_cast<const E*>(a.out.p)) + query * a.out.ld + head * a.out.hs;
+    if (first && a.lse != nullptr) a.lse[(int64_t)query * a.Hq + head] = lse * LN2;
+#pragma unroll
+    for (int df = 0; df < T::DF; ++df) if (C::KG == 1 || df % C::KG == kg) store_columns<E>(p, df, D, o[df], inv, h);
+  }
+}
+
+// The parts of split keys, weighted by what each holds of the row's sum: four columns a thread, a row's of neighbouring threads.
+template <typename E>
+__global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a, Parts parts) {
+  const int G = a.Hq / a.Hk, rows = (int)a.Tq * G, quads = a.D / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, of_row = i / quads;
+  const int d = (int)(i - of_row * quads) * 4;
+  if (of_row >= (int64_t)a.Hk * rows) return;
+  const int64_t step = (int64_t)a.Hk * rows;
+  float top = -INF, sum = 0.f;
+  for (int p = 0; p < parts.count; ++p) top = fmaxf(top, parts.lse[p * step + of_row]);
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts.count; ++p) {
+    const float lse = parts.lse[p * step + of_row];
+    if (lse == -INF) continue;
+    const float w = __builtin_amdgcn_exp2f(lse - top);
+    sum += w;
+    x += *reinterpret_cast<const f32x4*>(parts.o + (p * step + of_row) * a.D + d) * w;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int hk = (int)(of_row / rows), row = (int)(of_row - (int64_t)hk * rows), query = row / G, head = hk * G + row % G;
+  E* const o = const_cast<E*>(static_cast<const E*>(a.out.p)) + query * a.out.ld + head * a.out.hs + d;
+  if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+  else *reinterpret_cast<f32x4*>(o) = x * inv;
+  if (d == 0 && a.lse != nullptr) a.lse[(int64_t)query * a.Hq + head] = sum == 0.f ? -INF : (top + log2f(sum)) * LN2;
+}
+
+__global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets, int documents, const int32_t* prefix, int causal, int T, int2* spans) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= T) return;
+  int lo = -1, hi = documents;   // offsets[lo] <= t < offsets[hi]; offsets beyond the ends are as if they were far away
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (offsets[mid] <= t) lo = mid; else hi = mid;
+  }
+  int2 s = make_int2(0, 0);
+  if (lo >= 0 && t < offsets[lo + 1]) {
+    const int first = max(offsets[lo], 0);
+    s = make_int2(first, min(offsets[lo + 1], T));
+    if (causal) s.y = min(s.y, max(t + 1, prefix == nullptr ? 0 : first + min(max(prefix[lo], 0), T)));
+  }
+  spans[t] = s;
+}
+
+// What a call looks like: rows of a workgroup, and into how many parts the keys are cut.
+constexpr int64_t MANY = 256, FILLED = 512, LEAST_KEYS = 512, MOST_PARTS = 64;
+struct Plan { bool few; int tiles, parts; };
+Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk) {
+  const int64_t rows = Tq * (Hq / Hk), wide = (rows + 127) / 128 * Hk, narrow = (rows + 31) / 32 * Hk;
+  Plan p;
+  p.few = wide < MANY;
+  p.tiles = (int)((rows + (p.few ? 31 : 127)) / (p.few ? 32 : 128));
+  p.parts = !p.few || narrow >= MANY ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({FILLED / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
+  return p;
+}
+
+template <typename E, int DP, int WM, bool SHAPED>
+void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspace) {
+  typedef Config<E, DP, WM> C;
+  static const bool once = [] {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attention<E, C, SHAPED>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+    return true;
+  }();
+  (void)once;
+  const int64_t rows = a.Tq * (a.Hq / a.Hk);
+  Parts parts{static_cast<float*>(workspace), nullptr, p.parts};
+  parts.lse = parts.o + (size_t)p.parts * a.Hk * rows * a.D;
+  ProfScope ps(st, F_OTHER, 0.0);
+  launch_kernel(ps, k_attention<E, C, SHAPED>, dim3((unsigned)(p.tiles * (int64_t)a.Hk), p.parts), C::THREADS, C::LDS, st, a, parts, p.tiles);
+  if (p.parts > 1) {
+    const int64_t threads = rows * a.Hk * (a.D / 4);
+    launch_kernel(ps, k_attention_join<E>, dim3((unsigned)((threads + 255) / 256)), 256, 0, st, a, parts);
+  }
+}
+template <typename E, int DP>
+void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
+  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk);
+  const bool shaped = a.cap > 0.f || a.slopes != nullptr;
+  if (p.few) shaped ? launch<E, DP, 1, true>(st, a, p, workspace) : launch<E, DP, 1, false>(st, a, p, workspace);
+  else shaped ? launch<E, DP, 4, true>(st, a, p, workspace) : launch<E, DP, 4, false>(st, a, p, workspace);
+}
+}  // namespace
+
+void launch_attention_spans(hipStream_t st, const int32_t* offsets, int64_t documents, const int32_t* prefix, bool causal, int64_t T, int32_t* spans) {
+  ProfScope ps(st, F_OTHER, 8.0 * T);
+  launch_kernel(ps, k_attention_spans, dim3((unsigned)((T + 255) / 256)), 256, 0, st, offsets, (int)documents, prefix, causal ? 1 : 0, (int)T, reinterpret_cast<int2*>(spans));
+}
+
+size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D) {
+  const Plan p = plan(Tq, Tk, Hq, Hk);
+  return p.parts <= 1 ? 256 : (size_t)p.parts * Tq * Hq * (D + 1) * sizeof(float);
+}
+void launch_attention(hipStream_t st, const AttentionArgs& a, bool bf16, void* workspace) {
+  if (bf16) a.D <= 64 ? launch_width<bf16_t, 64>(st, a, workspace) : launch_width<bf16_t, 128>(st, a, workspace);
+  else a.D <= 64 ? launch_width<float, 64>(st, a, workspace) : launch_width<float, 128>(st, a, workspace);
+}
+
+}  // namespace sama

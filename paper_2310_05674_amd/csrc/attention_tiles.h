@@ -1,0 +1,254 @@
+// What the attention kernels (attention.hip, attention_grad.hip) have in common: fragments of 32 rows by 16 of the contraction, tiles of rows in LDS and their
+// loads, the scores' transformation, and products that keep what is not finite out of results that do not see it.
+//
+// All three products of a pass run on 32x32 matrix instructions, 32x32x16 in bf16 and eight of 32x32x2 in fp32, with a lane holding eight of a row's sixteen
+// contraction indices: lane l, row l % 32, h = l / 32, indices 8 h + t.  The result has column l % 32 and, in register r, row 8 (r / 4) + 4 h + r % 4.  Scores are
+// computed transposed (rows: the tile in LDS, columns: what a wave keeps in registers), so a lane holds scores of one row of its own, its softmax needs one exchange
+// between two lanes, and eight neighbouring registers are already a fragment of the second product, if its contraction is taken in the order
+// (h, t) -> 8 (t / 4) + 4 h + t % 4, which the other operand's transposed fetch follows.
+#pragma once
+#include <limits>
+#include <type_traits>
+#include "kernels.h"
+#include "sequence_ops.h"
+
+namespace sama {
+namespace attn {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void lds_void;
+constexpr int LDS_MAX = 160 * 1024;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float INF = std::numeric_limits<float>::infinity();
+
+template <typename E> using Frag = std::conditional_t<sizeof(E) == 2, bf16x8, f32x8>;
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
+  return c;
+}
+__device__ __forceinline__ f32x16 zeros() { return (f32x16){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}; }
+// registers 8 half .. of a result as a fragment; in bf16 this is where probabilities and score gradients are rounded, once, because the products run on bf16 operands
+template <typename E> __device__ __forceinline__ Frag<E> fragment(const f32x16& x, int half) {
+  if constexpr (sizeof(E) == 2) {
+    union { bf16x8 v; uint32_t w[4]; } u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.w[i] = pack_bf16x2(x[8 * half + 2 * i], x[8 * half + 2 * i + 1]);
+    return u.v;
+  } else {
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x[8 * half + i];
+    return v;
+  }
+}
+template <typename E> __device__ __forceinline__ Frag<E> zero_fragment() {
+  if constexpr (sizeof(E) == 2) return __builtin_bit_cast(bf16x8, (u32x4){0, 0, 0, 0});
+  else return (f32x8){0, 0, 0, 0, 0, 0, 0, 0};
+}
+// eight values of a row in global memory, 16-byte aligned
+template <typename E> __device__ __forceinline__ Frag<E> load_fragment(const E* p) {
+  if constexpr (sizeof(E) == 2) return *reinterpret_cast<const bf16x8*>(p);
+  else { const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4); return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+}
+__device__ __forceinline__ int register_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// Tiles in LDS: rows of DP values, their 16-byte pieces permuted within the row so that both fetches fill all banks: sixteen rows at the same piece, and four
+// neighbouring rows at 64 neighbouring bytes.
+template <typename E, int DP> struct Tile {
+  static constexpr int ROW = DP * sizeof(E), PIECES = ROW / 16, DF = DP / 32, KS = DP / 16;
+  static_assert(PIECES == 8 || PIECES % 16 == 0, "row");
+  static __device__ __forceinline__ int permuted(int r) {
+    if constexpr (PIECES == 8) return (((r >> 1) & 1) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+    else return ((r & 3) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+  }
+  // rows row0 + lane % 32, contraction 16 ks ..
+  static __device__ __forceinline__ Frag<E> rows(const unsigned char* tile, int row0, int ks, int lane) {
+    const int r = lane & 31, h = lane >> 5, sw = permuted(r);
+    const unsigned char* const at = tile + (row0 + r) * ROW;
+    if constexpr (sizeof(E) == 2) {
+      return *reinterpret_cast<const bf16x8*>(at + (((2 * ks + h) ^ sw) << 4));
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(at + (((4 * ks + 2 * h) ^ sw) << 4)), b = *reinterpret_cast<const f32x4*>(at + (((4 * ks + 2 * h + 1) ^ sw) << 4));
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  // transposed: column 32 df + lane % 32 of rows row0 .. row0 + 15, in the order above
+  static __device__ __forceinline__ Frag<E> columns(const unsigned char* tile, int row0, int df, int lane) {
+    const int h = lane >> 5;
+    if constexpr (sizeof(E) == 2) {
+      union { bf16x8 v; s16x4 q[2]; } u;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int r = 8 * t + 4 * h + ((lane & 15) >> 2), piece = 4 * df + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+        const unsigned char* const at = tile + (row0 + r) * ROW + ((piece ^ permuted(r)) << 4) + (lane & 1) * 8;
+        u.q[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      }
+      return u.v;
+    } else {
+      f32x8 v;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int r = 8 * (t >> 2) + 4 * h + (t & 3), piece = 8 * df + ((lane & 31) >> 2);
+        v[t] = *reinterpret_cast<const float*>(tile + (row0 + r) * ROW + ((piece ^ permuted(r)) << 4) + (lane & 3) * 4);
+      }
+      return v;
+    }
+  }
+};
+
+// Loads go from memory straight to LDS, 1 KB a wave and instruction, through buffer descriptors that begin at the tile's first row: what lies behind the last row
+// or the row's last value reads as zero, and offsets stay below 2^31.
+constexpr uint32_t NOWHERE = 0x80000000u, MOST = 0x7fffffffu;
+__device__ __forceinline__ u32x4 descriptor(const void* p, int64_t left) {
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  auto uniform = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+  return (u32x4){uniform((uint32_t)at), uniform((uint32_t)(at >> 32)), uniform(left <= 0 ? 0u : left > (int64_t)MOST ? MOST : (uint32_t)left), 0x00020000u};
+}
+__device__ __forceinline__ void load_to_lds(uint32_t to, uint32_t offset, u32x4 from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_void*)p); }
+
+// ROWS rows of a tensor by WAVES waves: neighbouring tokens', or with `heads` the packed rows of G heads a token, see GROUP.
+constexpr int GROUP = 64;   // packed rows: GROUP / G whole tokens, their heads one after the other, and what is left of 64 rows stays empty
+template <typename E, int DP, int ROWS, int WAVES> struct Loads {
+  typedef Tile<E, DP> T;
+  static constexpr int BYTES = ROWS * T::ROW, N = BYTES / 1024 / WAVES;
+  static_assert(BYTES % (1024 * WAVES) == 0, "loads");
+  uint32_t offset[N];
+  __device__ __forceinline__ void init(int64_t ld, int64_t hs, int G, int D, int wave, int lane) {
+    const int tokens = GROUP / G;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const int at = (q * WAVES + wave) * 1024 + lane * 16, r = at / T::ROW, piece = (at % T::ROW / 16) ^ T::permuted(r), in = r % GROUP;
+      const uint32_t row = (uint32_t)(G == 1 ? r : r / GROUP * tokens + in / G) * (uint32_t)ld + (uint32_t)(G == 1 ? 0 : in % G) * (uint32_t)hs;
+      offset[q] = (G == 1 || in < tokens * G) && piece * 16 < D * (int)sizeof(E) ? row * (uint32_t)sizeof(E) + piece * 16 : NOWHERE;
+    }
+  }
+  __device__ __forceinline__ void issue(uint32_t lds, u32x4 from, int wave) const {
+#pragma unroll
+    for (int q = 0; q < N; ++q) load_to_lds(lds + (q * WAVES + wave) * 1024, offset[q], from);
+  }
+};
+// everything a wave has asked for is in LDS, for all of them
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// Scores in units of log 2: with `shaped`, cap tanh(scale s / cap) - slope |at - key|, else the factor alone.
+struct Shape {
+  float scale, cap;          // cap 0: none
+  float in, out;             // bf16: s -> exp2 of 2 log2(e) scale / cap s; out = cap log2(e)
+  __device__ __forceinline__ Shape(float scale_, float cap_) : scale(scale_), cap(cap_) { in = cap > 0.f ? 2.f * LOG2E * scale / cap : 0.f; out = cap * LOG2E; }
+  // the score, and what its derivative is multiplied by.  tanh y = 1 - 2 / (1 + e^2y) is within 2^-23 of itself in all, which a bf16 score's own rounding passes by far
+  // for any cap; in fp32 small scores want the library's tanh, whose error is relative.
+  template <typename E> __device__ __forceinline__ float score(float s, float slope, float distance, float& bend) const {
+    float x;
+    bend = 1.f;
+    if (cap > 0.f) {
+      const float t = sizeof(E) == 2 ? 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * in)) : tanhf(s * scale / cap);
+      x = t * out;
+      bend = 1.f - t * t;
+    } else {
+      x = s * (scale * LOG2E);
+    }
+    return x - slope * distance;
+  }
+};
+
+// acc[df] += (columns 32 df .. of the tile's rows row0 ..)^T times the N fragments b.
+template <typename E, int DP, int N>
+__device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsigned char* tile, int row0, const Frag<E> (&b)[N], int lane) {
+#pragma unroll
+  for (int s = 0; s < N; ++s)
+#pragma unroll
+    for (int df = 0; df < DP / 32; ++df) acc[df] = mma(Tile<E, DP>::columns(tile, row0 + 16 * s, df, lane), b[s], acc[df]);
+}
+// The same where some of a lane's weights are zero because it does not see the row (bit 8 s + t of `seen` clear): zero times infinity or NaN is NaN, so a
+// row that is not finite would reach lanes that do not see it.  The tile's part is formed by itself; if it is not finite, once more with zeros for what is not, and
+// a second product counts for each lane what it sees of those: NaN for it where there is any.
+template <typename E> __device__ __forceinline__ void split_finite(const Frag<E>& x, Frag<E>& finite, Frag<E>& rest) {
+  if constexpr (sizeof(E) == 2) {
+    union { bf16x8 v; uint16_t w[8]; } a, f, r;
+    a.v = x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { const bool bad = (a.w[i] & 0x7f80) == 0x7f80; f.w[i] = bad ? 0 : a.w[i]; r.w[i] = bad ? 0x3f80 : 0; }
+    finite = f.v; rest = r.v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { const bool bad = (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u; finite[i] = bad ? 0.f : x[i]; rest[i] = bad ? 1.f : 0.f; }
+  }
+}
+template <typename E, int DP, int N>
+__device__ __forceinline__ void add_product_seen(f32x16 (&acc)[DP / 32], const unsigned char* tile, int row0, const Frag<E> (&b)[N], uint32_t seen, int lane) {
+#pragma unroll
+  for (int df = 0; df < DP / 32; ++df) {
+    f32x16 part = zeros();
+#pragma unroll
+    for (int s = 0; s < N; ++s) part = mma(Tile<E, DP>::columns(tile, row0 + 16 * s, df, lane), b[s], part);
+    float check = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) check = fmaf(part[r], 0.f, check);
+    if (__any(check != check)) {
+      f32x16 count = zeros();
+      part = zeros();
+#pragma unroll
+      for (int s = 0; s < N; ++s) {
+        Frag<E> finite, rest, sees;
+        split_finite<E>(Tile<E, DP>::columns(tile, row0 + 16 * s, df, lane), finite, rest);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) sees[t] = (seen >> (8 * s + t) & 1) ? 1.f : 0.f;
+        part = mma(finite, b[s], part);
+        count = mma(rest, sees, count);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) part[r] = count[r] > 0.f ? std::numeric_limits<float>::quiet_NaN() : part[r];
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[df][r] += part[r];
+  }
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) x = min(x, __shfl_xor(x, k));
+  return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) x = max(x, __shfl_xor(x, k));
+  return x;
+}
+__device__ __forceinline__ float other_half_max(float x) { return join32(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float other_half_sum(float x) { return join32(x, [](float a, float b) { return a + b; }); }
+
+// keys [first, end) of a query, none as [0, 0)
+__device__ __forceinline__ int2 span_of(const int32_t* spans, int64_t query, int keys) {
+  const int2 s = reinterpret_cast<const int2*>(spans)[query];
+  const int first = max(s.x, 0), end = min(s.y, keys);
+  return first < end ? make_int2(first, end) : make_int2(0, 0);
+}
+
+// 32 columns of a result, df, from lane's registers to its row
+template <typename E>
+__device__ __forceinline__ void store_columns(E* row, int df, int D, const f32x16& x, float factor, int h) {
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const int d = 32 * df + 8 * b + 4 * h;
+    if (d >= D) continue;
+    if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(row + d) = make_uint2(pack_bf16x2(x[4 * b] * factor, x[4 * b + 1] * factor), pack_bf16x2(x[4 * b + 2] * factor, x[4 * b + 3] * factor));
+    else *reinterpret_cast<f32x4*>(row + d) = (f32x4){x[4 * b] * factor, x[4 * b + 1] * factor, x[4 * b + 2] * factor, x[4 * b + 3] * factor};
+  }
+}
+
+}  // namespace attn
+}  // namespace sama

@@ -6,6 +6,7 @@
 #include <string>
 #include "../../include/sama_ops.h"
 #include "kernels.h"
+#include "sequence_ops.h"
 #include "token_ops.h"
 
 using namespace sama;
@@ -364,6 +365,169 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
   else launch_glu_ffn_grad_f32((hipStream_t)hip_stream, a, workspace);
   return launched(op);
 }
+// ---- sequences
+namespace {
+constexpr int64_t MOST_ROTARY_TOKENS = (int64_t)1 << 23, MOST_DISTILL_TOKENS = (int64_t)1 << 22, MOST_HEAD_ROWS = (int64_t)1 << 28;
+// [tokens][heads][width] of any alignment
+bool is_heads(const void* p, int32_t dtype, int64_t tokens, int64_t heads, int64_t width, int64_t ld, int64_t hs) {
+  return ld >= width && hs >= width && is_rows(p, dtype, tokens, ld) && is_rows(p, dtype, heads, hs);
+}
+const char* check_attention_sizes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype) {
+  if (!is_dtype(dtype)) return "the type must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16";
+  if (Hk < 1 || Hq < Hk || Hq % Hk != 0 || Hq / Hk > 64) return "Hq must be 1 to 64 times Hk";
+  if (D < 8 || D > 128 || D % 8 != 0) return "D must be a multiple of 8, up to 128";
+  if (Tq < 0 || Tk < 0 || Tq > MOST_HEAD_ROWS / Hq || Tk > MOST_HEAD_ROWS / Hk) return "Tq Hq and Tk Hk must be 0 to 2^28";
+  return nullptr;
+}
+bool is_attention_heads(const sama_heads& t, int64_t tokens, const sama_attention& a, bool packed) {
+  const int unit = a.dtype == SAMA_DTYPE_BF16 ? 8 : 4;
+  if (tokens == 0) return true;
+  if (t.p == nullptr || (uintptr_t)t.p % 16 != 0 || t.ld % unit != 0 || t.hs % unit != 0) return false;
+  if (t.ld < a.D || t.hs < a.D || t.ld > ((int64_t)1 << 21) || t.hs > ((int64_t)1 << 40)) return false;
+  return !packed || (a.Hq / a.Hk - 1) * t.hs * value_bytes(a.dtype) < ((int64_t)1 << 30);
+}
+const char* check_attention(const sama_attention& a, bool grad) {
+  if (const char* e = check_attention_sizes(a.Tq, a.Tk, a.Hq, a.Hk, a.D, a.dtype)) return e;
+  if (!(a.scale > 0.f) || !std::isfinite(a.scale)) return "scale must be positive and finite";
+  if (!(a.cap >= 0.f) || !std::isfinite(a.cap)) return "cap must be 0 (none) or positive and finite";
+  if (a.Tq > 0 && (a.spans == nullptr || (uintptr_t)a.spans % 8 != 0)) return "spans missing, or not aligned to 8 bytes";
+  if ((uintptr_t)a.at % 4 != 0 || (uintptr_t)a.slopes % 4 != 0 || (uintptr_t)a.lse % 4 != 0) return "at, slopes or lse is not aligned to its values";
+  if (a.slopes != nullptr && a.at == nullptr && a.Tq != a.Tk) return "slopes need the queries' places (at) where Tq is not Tk";
+  if (!is_attention_heads(a.q, a.Tq, a, grad) || !is_attention_heads(a.k, a.Tk, a, false) || !is_attention_heads(a.v, a.Tk, a, false) ||
+      !is_attention_heads(a.out, a.Tq, a, false))
+    return "q, k, v or out is missing, not aligned to 16 bytes, or has a stride that is too small, too large or not a multiple of 16 bytes";
+  if (!grad) return nullptr;
+  if (a.Tq > 0 && a.lse == nullptr) return "null lse";
+  if (!is_attention_heads(a.dout, a.Tq, a, true) || !is_attention_heads(a.dq, a.Tq, a, false) || !is_attention_heads(a.dk, a.Tk, a, false) ||
+      !is_attention_heads(a.dv, a.Tk, a, false))
+    return "dout, dq, dk or dv is missing, not aligned to 16 bytes, or has a stride that is too small, too large or not a multiple of 16 bytes";
+  return nullptr;
+}
+AttentionArgs attention_args(const sama_attention& s) {
+  auto heads = [](const sama_heads& h) { return Heads{h.p, h.ld, h.hs}; };
+  AttentionArgs a{};
+  a.q = heads(s.q); a.k = heads(s.k); a.v = heads(s.v); a.out = heads(s.out); a.dout = heads(s.dout); a.dq = heads(s.dq); a.dk = heads(s.dk); a.dv = heads(s.dv);
+  a.spans = s.spans; a.at = s.at; a.slopes = s.slopes; a.lse = s.lse; a.Tq = s.Tq; a.Tk = s.Tk; a.Hq = s.Hq; a.Hk = s.Hk; a.D = s.D; a.scale = s.scale; a.cap = s.cap;
+  return a;
+}
+const char* check_distill(const void* z, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float tau) {
+  if (!is_dtype(dtype)) return "the type must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16";
+  if (T < 0 || T > MOST_DISTILL_TOKENS) return "T must be 0 to 2^22";
+  if (V < 1 || K < 1 || K > DISTILL_MAX_ENTRIES) return "V must be positive and K 1 to 256";
+  if (!(tau >= 1e-4f && tau <= 1e4f)) return "temperature must be 1e-4 to 1e4";
+  if (T == 0) return nullptr;
+  if (!z || !ids || !teacher) return "null logits, ids or teacher";
+  if ((uintptr_t)ids % 4 != 0 || (uintptr_t)teacher % 4 != 0) return "ids or teacher is not aligned to its values";
+  if (ldz < V || !is_rows(z, dtype, T, ldz)) return "logits are not aligned to their values, or their stride is smaller than a row or too large";
+  return nullptr;
+}
+}  // namespace
+
+sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, int32_t H, int32_t D, int32_t dtype, const int32_t* positions, int32_t axes,
+                           const int32_t* sections, double base, int32_t neighbours, int32_t inverse, void* out, int64_t ldo, int64_t hso, void* hip_stream) {
+  static const char* const op = "sama_op_rotary";
+  g_ops_error.clear();
+  if (!is_dtype(dtype)) return refuse(op, "the type must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16");
+  if (T < 0 || T > MOST_ROTARY_TOKENS) return refuse(op, "T must be 0 to 2^23");
+  if (H < 1 || D < 2 || (int64_t)H * D > (1 << 20)) return refuse(op, "H must be positive, D at least 2 and H D up to 2^20");
+  if (axes < 1 || axes > ROTARY_MAX_AXES || sections == nullptr) return refuse(op, "axes must be 1 to 4, with a section each");
+  int64_t pairs = 0;
+  for (int k = 0; k < axes; ++k) {
+    if (sections[k] < 0 || sections[k] > ROTARY_MAX_PAIRS) return refuse(op, "a section must be 0 to 128 pairs");
+    pairs += sections[k];
+  }
+  if (pairs < 1 || pairs > ROTARY_MAX_PAIRS || 2 * pairs > D) return refuse(op, "the sections must be 1 to 128 pairs together, and fit in D");
+  if (!(base > 0.0) || !std::isfinite(base)) return refuse(op, "base must be positive and finite");
+  if ((neighbours != 0 && neighbours != 1) || (inverse != 0 && inverse != 1)) return refuse(op, "neighbours and inverse must be 0 or 1");
+  if (T == 0) return SAMA_OK;
+  if (!x || !out || !positions) return refuse(op, "null x, output or positions");
+  if ((uintptr_t)positions % 4 != 0) return refuse(op, "positions must be aligned to 4 bytes");
+  if (!is_heads(x, dtype, T, H, D, ldx, hsx) || !is_heads(out, dtype, T, H, D, ldo, hso)) return refuse(op, "a pointer is not aligned to its values, or a stride is smaller than a head or too large");
+  if (out == x && (ldx != ldo || hsx != hso)) return refuse(op, "in place the strides must be the same");
+  RotaryArgs a{};
+  a.x = Heads{x, ldx, hsx}; a.out = out; a.ldo = ldo; a.hso = hso; a.T = T; a.H = H; a.D = D; a.R = (int)(2 * pairs); a.axes = axes; a.positions = positions;
+  a.sections = sections; a.base = base; a.neighbours = neighbours != 0; a.inverse = inverse != 0; a.bf16 = dtype == SAMA_DTYPE_BF16;
+  (void)hipGetLastError();
+  launch_rotary((hipStream_t)hip_stream, a);
+  return launched(op);
+}
+
+size_t sama_op_attention_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype) {
+  return check_attention_sizes(Tq, Tk, Hq, Hk, D, dtype) != nullptr ? 0 : attention_bytes(Tq, Tk, Hq, Hk, D);
+}
+size_t sama_op_attention_grad_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype) {
+  return check_attention_sizes(Tq, Tk, Hq, Hk, D, dtype) != nullptr ? 0 : attention_grad_bytes(Tq, Tk, Hq, Hk, D);
+}
+sama_status sama_op_attention(const sama_attention* args, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  static const char* const op = "sama_op_attention";
+  g_ops_error.clear();
+  if (args == nullptr) return refuse(op, "null arguments");
+  if (const char* e = check_attention(*args, false)) return refuse(op, e);
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < attention_bytes(args->Tq, args->Tk, args->Hq, args->Hk, args->D)) {
+    (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_attention_bytes()");
+    return SAMA_EWORKSPACE;
+  }
+  if (args->Tq == 0) return SAMA_OK;
+  (void)hipGetLastError();
+  launch_attention((hipStream_t)hip_stream, attention_args(*args), args->dtype == SAMA_DTYPE_BF16, workspace);
+  return launched(op);
+}
+sama_status sama_op_attention_grad(const sama_attention* args, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  static const char* const op = "sama_op_attention_grad";
+  g_ops_error.clear();
+  if (args == nullptr) return refuse(op, "null arguments");
+  if (const char* e = check_attention(*args, true)) return refuse(op, e);
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < attention_grad_bytes(args->Tq, args->Tk, args->Hq, args->Hk, args->D)) {
+    (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_attention_grad_bytes()");
+    return SAMA_EWORKSPACE;
+  }
+  (void)hipGetLastError();
+  launch_attention_grad((hipStream_t)hip_stream, attention_args(*args), args->dtype == SAMA_DTYPE_BF16, workspace);
+  return launched(op);
+}
+sama_status sama_op_attention_spans(const int32_t* offsets, int64_t documents, const int32_t* prefix, int32_t causal, int64_t T, int32_t* spans, void* hip_stream) {
+  static const char* const op = "sama_op_attention_spans";
+  g_ops_error.clear();
+  if (documents < 0 || documents > ((int64_t)1 << 30) || T < 0 || T > MOST_HEAD_ROWS) return refuse(op, "documents must be 0 to 2^30 and T 0 to 2^28");
+  if (causal != 0 && causal != 1) return refuse(op, "causal must be 0 or 1");
+  if (T == 0) return SAMA_OK;
+  if (!offsets || !spans) return refuse(op, "null offsets or spans");
+  if ((uintptr_t)offsets % 4 != 0 || (uintptr_t)prefix % 4 != 0 || (uintptr_t)spans % 8 != 0) return refuse(op, "offsets or prefix is not aligned to its values, or spans not to 8 bytes");
+  (void)hipGetLastError();
+  launch_attention_spans((hipStream_t)hip_stream, offsets, documents, prefix, causal != 0, T, spans);
+  return launched(op);
+}
+
+sama_status sama_op_distill(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,
+                            float* loss, float* saved, void* hip_stream) {
+  static const char* const op = "sama_op_distill";
+  g_ops_error.clear();
+  if (const char* e = check_distill(logits, ldz, dtype, T, V, ids, teacher, K, temperature)) return refuse(op, e);
+  if (T == 0) return SAMA_OK;
+  if (!loss || !saved || (uintptr_t)loss % 4 != 0 || (uintptr_t)saved % 4 != 0) return refuse(op, "loss or saved is null or not aligned to its values");
+  DistillArgs a{};
+  a.z = logits; a.ldz = ldz; a.bf16 = dtype == SAMA_DTYPE_BF16; a.T = T; a.V = V; a.K = K; a.ids = ids; a.teacher = teacher; a.tau = temperature; a.loss = loss; a.saved = saved;
+  (void)hipGetLastError();
+  launch_distill((hipStream_t)hip_stream, a);
+  return launched(op);
+}
+sama_status sama_op_distill_grad(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,
+                                 const float* dloss, const float* saved, void* dlogits, int64_t lddz, void* hip_stream) {
+  static const char* const op = "sama_op_distill_grad";
+  g_ops_error.clear();
+  if (const char* e = check_distill(logits, ldz, dtype, T, V, ids, teacher, K, temperature)) return refuse(op, e);
+  if (T == 0) return SAMA_OK;
+  if (!dloss || !saved || (uintptr_t)dloss % 4 != 0 || (uintptr_t)saved % 4 != 0) return refuse(op, "dloss or saved is null or not aligned to its values");
+  if (!dlogits || lddz < V || !is_rows(dlogits, dtype, T, lddz)) return refuse(op, "dlogits are null or not aligned to their values, or their stride is smaller than a row or too large");
+  if (dlogits == logits && lddz != ldz) return refuse(op, "in place the strides must be the same");
+  DistillArgs a{};
+  a.z = logits; a.ldz = ldz; a.bf16 = dtype == SAMA_DTYPE_BF16; a.T = T; a.V = V; a.K = K; a.ids = ids; a.teacher = teacher; a.tau = temperature;
+  a.dloss = dloss; a.saved = const_cast<float*>(saved); a.dz = dlogits; a.lddz = lddz;
+  (void)hipGetLastError();
+  launch_distill_grad((hipStream_t)hip_stream, a);
+  return launched(op);
+}
+
 sama_status sama_dev_glu_tile(int32_t tile) { return glu_ffn_force_tile(tile) ? SAMA_OK : SAMA_EINVAL; }
 
 }  // extern "C"

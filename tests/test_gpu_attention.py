@@ -1,0 +1,278 @@
+"""Attention within spans of keys, its gradients and the spans of packed documents, against plain implementations in 64 bits.
+
+Tolerances are bounds, computed with the results, element by element.  u is 2^-24, r is what rounding to the type costs at most: 2^-8 in bf16, u in fp32 (there is none of
+the probabilities there).  With a = sum |q_d k_d| scale and S the largest sum |score| + a of a row:
+  a score is off by at most  e_s = (D + 8) u S  (D products in any order, the factor, the units of the exponential, the bias), capped by 2^-21 cap more in bf16, 8 u cap in fp32;
+  a probability by  e_p = 2 e_s + (n + 16) u  of itself (n keys are summed; the exponential and the logarithm within 4 u), formed again from lse: by u |lse| more;
+  out by  (e_p + [r in bf16]) sum p |v| + n u sum p |v| + r |out|;
+  dp by  e_dp = (D + 2) u sum |do v|,  delta by  e_d = sum |do| (out's error) + D u sum |do out|;
+  ds by  E = e_p' |ds| + p (e_dp + e_d) + [r |ds|] + 2^-20 p |dp - delta| where capped (1 - tanh^2),  dq by scale (sum E |k| + (n + 2) u sum |ds k|) + r |dq|, dk alike;
+  dv by  (e_p' + [r]) sum p |do| + (m + 2) u sum p |do| + r |dv|   (m queries)."""
+import math
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def ints(a):
+    return torch.as_tensor(np.ascontiguousarray(a), dtype=torch.int32, device=DEV)
+
+
+def normal(gen, *shape, dtype, std=1.0):
+    return (torch.randn(*shape, device=DEV, generator=gen) * std).to(dtype)
+
+
+def reference(q, k, v, spans, scale, cap, slopes, at, dout=None):
+    """{name: (value, bound)} in 64 bits, [tokens, heads, width]."""
+    f = torch.float64
+    t = q.dtype
+    r = 2.0 ** -8 if t == torch.bfloat16 else U
+    soft = r if t == torch.bfloat16 else 0.0
+    (Tq, Hq, D), (Tk, Hk) = q.shape, k.shape[:2]
+    j = torch.arange(Tk, device=DEV)[None]
+    b, e = spans[:, :1].long().clamp(min=0), spans[:, 1:].long().clamp(max=Tk)
+    see = (j >= b) & (j < e)
+    n = see.sum(1, keepdim=True).double()
+    names = ["out", "lse"] + (["dq", "dk", "dv"] if dout is not None else [])
+    shapes = dict(out=q.shape, lse=(Tq, Hq), dq=q.shape, dk=k.shape, dv=v.shape)
+    val, err = ({x: torch.zeros(shapes[x], device=DEV, dtype=f) for x in names} for _ in range(2))
+    zero = torch.zeros((), device=DEV, dtype=f)
+    for h in range(Hq):
+        g = h * Hk // Hq
+        qh, kh, vh = q[:, h].double(), k[:, g].double(), v[:, g].double()
+        # what is hidden takes no part, whatever it holds
+        kz, vz = torch.where(see.any(0)[:, None], kh, zero), torch.where(see.any(0)[:, None], vh, zero)
+        qz = torch.where(see.any(1)[:, None], qh, zero)
+        s = qz @ kz.t() * scale
+        size = qz.abs() @ kz.abs().t() * scale
+        bend = torch.ones_like(s)
+        if cap > 0:
+            bend = 1 - torch.tanh(s / cap) ** 2
+            s = cap * torch.tanh(s / cap)
+        if slopes is not None:
+            s = s - float(slopes[h]) * (at.long()[:, None] - j).abs()
+        S = torch.where(see, s.abs() + size, zero).amax(1, keepdim=True)
+        e_s = (D + 8) * U * S + (0.0 if cap == 0 else cap * (2.0 ** -21 if t == torch.bfloat16 else 8 * U))
+        s = torch.where(see, s, torch.full_like(s, -math.inf))
+        top = s.amax(1, keepdim=True)
+        top = torch.where(torch.isfinite(top), top, zero)
+        p = torch.exp(s - top)
+        total = p.sum(1, keepdim=True)
+        p = torch.where(total > 0, p / total, zero)
+        e_p = 2 * e_s + (n + 16) * U
+        o, o_abs = p @ vz, p @ vz.abs()
+        eo = (e_p + soft + n * U) * o_abs + r * o.abs()
+        val["out"][:, h], err["out"][:, h] = o, eo
+        lse = torch.where(total > 0, top + torch.log(total), torch.full_like(top, -math.inf))[:, 0]
+        val["lse"][:, h], err["lse"][:, h] = lse, torch.where(torch.isfinite(lse), e_p[:, 0] + 4 * U * (lse.abs() + 1), zero)
+        if dout is None:
+            continue
+        do = torch.where(see.any(1)[:, None], dout[:, h].double(), zero)
+        dp = torch.where(see, do @ vz.t(), zero)
+        delta = (do * o).sum(1, keepdim=True)
+        ds = p * (dp - delta) * bend
+        e_dp = (D + 2) * U * (do.abs() @ vz.abs().t())
+        e_d = (do.abs() * eo).sum(1, keepdim=True) + D * U * (do * o).abs().sum(1, keepdim=True)
+        e_pp = e_p + U * (torch.where(torch.isfinite(lse), lse, torch.zeros_like(lse)).abs()[:, None] + 1) * 4
+        E = torch.where(see, e_pp * ds.abs() + p * (e_dp + e_d) + soft * ds.abs() + (2.0 ** -20 * p * (dp - delta).abs() if cap > 0 else 0.0), zero)
+        val["dq"][:, h] = scale * (ds @ kz)
+        err["dq"][:, h] = scale * (E @ kz.abs() + (n + 2) * U * (ds.abs() @ kz.abs())) + r * val["dq"][:, h].abs()
+        m = see.sum(0)[:, None].double() * (Hq // Hk)
+        val["dk"][:, g] += scale * (ds.t() @ qz)
+        err["dk"][:, g] += scale * (E.t() @ qz.abs() + (m + 2) * U * (ds.abs().t() @ qz.abs()))
+        val["dv"][:, g] += p.t() @ do
+        err["dv"][:, g] += ((e_pp + soft) * p).t() @ do.abs() + (m + 2) * U * (p.t() @ do.abs())
+    for x in ("dk", "dv"):
+        if x in val:
+            err[x] += r * val[x].abs()
+    return {x: (val[x], err[x]) for x in names}
+
+
+def close(name, got, want):
+    value, bound = want
+    g = got.double()
+    same = (g == value) | ((g - value).abs() <= bound * (1 + 2.0 ** -10) + 1e-37)
+    assert bool(same.all()), (name, float(torch.where(same, torch.zeros_like(g), (g - value).abs() - bound).abs().max()), int((~same).sum()), same.numel())
+
+
+class Case:
+    def __init__(self, Tq, Tk, Hq, Hk, D, t, seed=0, layout="rows", cap=0.0, slopes=False, at=None, scale=None):
+        self.t, self.cap, self.scale = TYPES[t], cap, D ** -0.5 if scale is None else scale
+        gen = torch.Generator(device=DEV).manual_seed(1000 * Tq + 10 * Tk + D + seed)
+
+        def make(T, H):
+            if layout == "heads":      # [heads][tokens][width]
+                return normal(gen, H, T, D, dtype=self.t).transpose(0, 1)
+            if layout == "wide":       # rows with something behind each head and each token
+                return normal(gen, T, H + 1, D + 8, dtype=self.t)[:, :H, :D]
+            return normal(gen, T, H, D, dtype=self.t)
+        self.q, self.k, self.v, self.dout = make(Tq, Hq), make(Tk, Hk), make(Tk, Hk), make(Tq, Hq)
+        self.dout *= 0.1
+        self.make = lambda like: torch.full_like(like, 7.0)      # keeps the strides of dense layouts
+        if layout == "wide":
+            self.make = lambda like: torch.full((like.shape[0], like.shape[1] + 1, D + 8), 7.0, device=DEV, dtype=self.t)[:, :like.shape[1], :D]
+        self.slopes = torch.exp2(-8.0 * torch.arange(1, Hq + 1, device=DEV, dtype=torch.float32) / Hq) if slopes else None
+        self.at = at if at is not None else torch.arange(Tq, device=DEV, dtype=torch.int32)
+        self.sizes = (Tq, Tk, Hq, Hk, D, self.t)
+
+    def run(self, spans, grad=True):
+        from paper_2310_05674_amd import binding as B
+        Tq, Tk, Hq, Hk, D, t = self.sizes
+        ws = torch.empty(max(B.attention_bytes(*self.sizes), B.attention_grad_bytes(*self.sizes)), dtype=torch.uint8, device=DEV).fill_(255)
+        out, lse = self.make(self.q), torch.full((Tq, Hq), 7.0, device=DEV)
+        kw = dict(scale=self.scale, cap=self.cap, slopes=self.slopes, at=self.at)
+        B.op_attention(self.q, self.k, self.v, out, spans, ws, lse=lse, **kw)
+        got = {"out": out, "lse": lse}
+        if grad:
+            ws.fill_(255)
+            got.update(dq=self.make(self.q), dk=self.make(self.k), dv=self.make(self.v))
+            B.op_attention_grad(self.dout, self.q, self.k, self.v, out, lse, spans, got["dq"], got["dk"], got["dv"], ws, **kw)
+        return got
+
+    def check(self, spans, grad=True):
+        got = self.run(spans, grad)
+        torch.cuda.synchronize()
+        want = reference(self.q, self.k, self.v, spans, self.scale, self.cap, self.slopes, self.at, self.dout if grad else None)
+        for name in want:
+            close(name, got[name], want[name])
+        return got
+
+
+def documents(lengths, T, causal=False, prefix=None):
+    """What op_attention_spans is to give."""
+    spans = np.zeros((T, 2), np.int32)
+    first = 0
+    for n, size in enumerate(lengths):
+        for i in range(first, min(first + size, T)):
+            end = min(first + size, T)
+            spans[i] = first, min(end, max(i + 1, first + (prefix[n] if prefix is not None else 0))) if causal else end
+        first += size
+    return spans
+
+
+@pytest.mark.parametrize("lengths,T,causal,prefix", [([5], 5, False, None), ([1], 1, True, None), ([3, 0, 4], 9, True, None), ([3, 0, 4], 9, False, None), ([10, 300, 1, 77], 400, True, [3, 100, 5, 0]),
+                                                     ([10, 300, 1, 77], 350, True, [3, 1000, 5, 0]), ([], 4, True, None), ([600, 423], 1023, False, [1, 2])])
+def test_spans(lengths, T, causal, prefix):
+    from paper_2310_05674_amd import binding as B
+    offsets = ints(np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32))
+    spans = torch.full((T, 2), 9, dtype=torch.int32, device=DEV)
+    B.op_attention_spans(offsets, spans, causal=causal, prefix=None if prefix is None else ints(np.asarray(prefix, np.int32)))
+    want = documents(lengths, T, causal, prefix)
+    got = spans.cpu().numpy()
+    some = want[:, 0] < want[:, 1]
+    assert np.array_equal(got[some], want[some]) and np.all(got[~some] == 0)
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,Hq,Hk,D", [(1, 1, 1, 8), (2, 2, 1, 64), (31, 2, 2, 128), (32, 1, 1, 64), (33, 3, 1, 40), (65, 4, 2, 128), (129, 2, 1, 96), (300, 6, 2, 64), (700, 4, 4, 32), (1025, 2, 2, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_one_document(T, Hq, Hk, D, causal, t):
+    Case(T, T, Hq, Hk, D, t).check(ints(documents([T], T, causal)))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_workgroups(D, t):
+    """Enough rows and keys for workgroups of 128 of them, forward and backward."""
+    T = 2180
+    Case(T, T, 16, 16, D, t).check(ints(documents([1500, 37, 500], T, True)))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("cap,slopes", [(20.0, False), (0.0, True), (5.0, True)])
+@pytest.mark.parametrize("T,D", [(90, 64), (333, 128)])
+def test_capped_and_biased(T, D, cap, slopes, t):
+    Case(T, T, 4, 2, D, t, cap=cap, slopes=slopes).check(ints(documents([T // 3, T // 2], T, True, [T // 6, 5])))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("G", [3, 5, 7, 8, 64])
+def test_shared_key_heads(G, t):
+    Case(77, 77, 2 * G, 2, 64, t).check(ints(documents([50, 20], 77, True)))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", ["heads", "wide"])
+def test_layouts(layout, t):
+    c = Case(150, 150, 4, 2, 80, t, layout=layout)
+    got = c.check(ints(documents([100, 41], 150, True)))
+    if layout == "wide":                                   # nothing beside the rows
+        for x in ("out", "dq", "dk", "dv"):
+            whole = got[x]._base if got[x]._base is not None else got[x]
+            assert bool((whole[:, -1] == 7).all()) and bool((whole[:, :, 80:] == 7).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,Hk", [(300, 2), (2200, 16)])
+def test_spans_in_any_order(T, Hk, t):
+    """Spans that overlap, lie apart, are empty, single, turned round or reach over the ends, in no order."""
+    r = np.random.RandomState(3)
+    a, n = r.randint(-5, T, T), r.choice([0, 1, 1, 2, 31, 64, 100, T + 9], T)
+    spans = np.stack([a, a + n], 1)
+    spans[7], spans[11], spans[12] = (50, 20), (-2 ** 31, 2 ** 31 - 1), (T - 1, 2 ** 31 - 1)
+    Case(T, T, Hk, Hk, 64, t).check(ints(spans))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,lengths", [(1, [1]), (1, [5000]), (3, [700, 1, 2049]), (32, [97] * 32)])
+@pytest.mark.parametrize("D,G", [(128, 4), (64, 1), (40, 3)])
+def test_new_tokens_over_caches(n, lengths, D, G, t):
+    room = [x // 64 * 64 + 64 for x in lengths]
+    first = np.concatenate([[0], np.cumsum(room)])
+    spans = np.stack([first[:-1], first[:-1] + lengths], 1)
+    at = ints(spans[:, 1] - 1)
+    c = Case(n, int(first[-1]), 2 * G, 2, D, t, slopes=True, at=at)
+    for i in range(n):                                     # what a cache has no token for yet
+        c.k[int(spans[i, 1]):int(first[i + 1])] = float("nan")
+        c.v[int(spans[i, 1]):int(first[i + 1])] = float("inf")
+    c.check(ints(spans))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,H", [(100, 2), (2180, 16)])
+def test_what_is_hidden_may_hold_anything(T, H, t):
+    """Rows of padding between documents, of all inputs, hold NaN and infinity."""
+    c = Case(T, T, H, H, 64, t)
+    spans = np.zeros((T, 2), np.int32)
+    for a, b in ((3, 20), (24, 60), (61, T - 7)):
+        for i in range(a, b):
+            spans[i] = a, i + 1
+    empty = torch.as_tensor(spans[:, 0] == spans[:, 1], device=DEV)
+    for x, y in ((c.q, float("nan")), (c.k, float("inf")), (c.v, float("nan")), (c.dout, -float("inf"))):
+        x[empty] = y
+    got = c.check(ints(spans))
+    for x in ("out", "dq", "dk", "dv"):
+        assert bool((got[x][empty] == 0).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [96, 1100])
+def test_what_is_not_finite_reaches_whom_sees_it(T, t):
+    """A later token's NaN in k and v stays with the queries behind it, and its column of v with that column."""
+    c = Case(T, T, 1, 1, 64, t)
+    spans = ints(documents([T], T, True))
+    clean = c.run(spans)
+    at = T - 40
+    v0 = c.v.clone()
+    c.v[at, 0, 5] = float("inf")
+    got = c.run(spans)
+    assert torch.equal(got["out"][:at], clean["out"][:at]) and torch.equal(got["dq"][:at], clean["dq"][:at])
+    bad = ~torch.isfinite(got["out"][:, 0])
+    assert bool(bad[at:, 5].all()) and int(bad.sum()) == T - at
+    c.v.copy_(v0)
+    c.k[at, 0, 9] = float("nan")
+    got = c.run(spans)
+    assert torch.equal(got["out"][:at], clean["out"][:at]) and torch.equal(got["dq"][:at], clean["dq"][:at])
+    assert bool(torch.isnan(got["out"][at:]).all()) and bool(torch.isnan(got["dq"][at:]).all())
+    c.k.copy_(torch.nan_to_num(c.k))
+    c.k[at, 0, 9] = 0.5
+    clean = c.run(spans)
+    c.dout[3] = float("nan")                               # sees the first four keys
+    got = c.run(spans)
+    for x in ("dk", "dv"):
+        assert torch.equal(got[x][4:], clean[x][4:]) and bool(torch.isnan(got[x][:4]).all())
