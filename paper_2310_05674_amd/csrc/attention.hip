@@ -20,13 +20,14 @@ struct Config {
   static constexpr int NS = WM > 1 && sizeof(E) * DP <= 256 ? 2 : 1;              // 32 keys each of a wave's part of a tile
   static constexpr int WAVES = WM * KG, THREADS = WAVES * 64, BM = 32 * WM, BK = 32 * NS * KG;
   static constexpr int KV = BK * DP * (int)sizeof(E), LDS = 4 * KV;               // K and V, two stages
+  static constexpr int PER_EU = sizeof(E) * DP <= 256 ? 2 : 1;
   static_assert(LDS <= LDS_MAX && KG * DP * 32 * 4 + KG * 256 <= LDS, "LDS");
 };
 
 struct Parts { float* o; float* lse; int count; };   // of split keys: [count][Hk][rows][D] and [count][Hk][rows]
 
 template <typename E, typename C, bool SHAPED>
-__global__ __launch_bounds__(C::THREADS) void k_attention(AttentionArgs a, Parts parts, int tiles) {
+__global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionArgs a, Parts parts, int tiles) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(C::THREADS) void k_attention(AttentionArgs a, Parts
   lv.init(a.v.ld, 0, 1, D, wave, lane);
   const E* const kp = static_cast<const E*>(a.k.p) + hk * a.k.hs;
   const E* const vp = static_cast<const E*>(a.v.p) + hk * a.v.hs;
-  const uint32_t lds = lds_address(smem);
+  const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
   auto issue = [&](int i, int stage) {
     const int64_t k0 = lo + (int64_t)i * C::BK;
     const u32x4 dk = descriptor(kp + k0 * a.k.ld, ((a.Tk - 1 - k0) * a.k.ld + D) * (int64_t)sizeof(E));
@@ -88,18 +89,17 @@ __global__ __launch_bounds__(C::THREADS) void k_attention(AttentionArgs a, Parts
     const int next = seen_from(t + 1);
     wait_loads();
     if (next < end) issue(next, stage ^ 1);
-    const unsigned char* const kt = smem + stage * 2 * C::KV;
-    const unsigned char* const vt = kt + C::KV;
+    const uint32_t k_rows = lds + stage * 2 * C::KV + row_lane, v_rows = k_rows + C::KV, v_cols = lds + stage * 2 * C::KV + C::KV + column_lane;
     const int k0 = lo + t * C::BK + kg * 32 * C::NS;   // the wave's first key
     t = next;
     if (!__any(span.x < k0 + 32 * C::NS && span.y > k0)) continue;
     f32x16 s[C::NS];
 #pragma unroll
-    for (int n = 0; n < C::NS; ++n) {
-      s[n] = zeros();
-#pragma unroll
-      for (int ks = 0; ks < T::KS; ++ks) s[n] = mma(T::rows(kt, (kg * C::NS + n) * 32, ks, lane), q[ks], s[n]);
-    }
+    for (int n = 0; n < C::NS; ++n) s[n] = row_product<E, C::DP>(k_rows, (kg * C::NS + n) * 32, q);
+    interleave<C::NS * T::KS, 4, ROW_READS<E>, PRODUCTS<E>>();
+    constexpr int AHEAD = C::DP * sizeof(E) > 128 ? 1 : 2;   // sets of columns: 16 registers or 32 in bf16
+    Columns<E, C::DP, 2> columns[AHEAD];
+    columns[0].fetch(v_cols, kg * C::NS * 32);
     if (SHAPED) {
       const int away = at - k0 - 4 * h;
 #pragma unroll
@@ -111,14 +111,11 @@ __global__ __launch_bounds__(C::THREADS) void k_attention(AttentionArgs a, Parts
     uint32_t seen[C::NS] = {};
     if (!whole) {
 #pragma unroll
-      for (int n = 0; n < C::NS; ++n)
+      for (int n = 0; n < C::NS; ++n) {
+        seen[n] = seen_keys(span, k0 + 32 * n, h);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = k0 + 32 * n + register_row(r, h);
-          const bool see = key >= span.x && key < span.y;
-          seen[n] |= (see ? 1u : 0u) << r;
-          s[n][r] = see ? s[n][r] : -INF;
-        }
+        for (int r = 0; r < 16; ++r) s[n][r] = where_seen(seen[n], r, s[n][r], -INF);
+      }
     }
     float top = m;
 #pragma unroll
@@ -147,8 +144,11 @@ __global__ __launch_bounds__(C::THREADS) void k_attention(AttentionArgs a, Parts
     l += sum;
 #pragma unroll
     for (int n = 0; n < C::NS; ++n) {
-      if (whole) add_product<E, C::DP, 2>(o, vt, (kg * C::NS + n) * 32, p[n], lane);
-      else add_product_seen<E, C::DP, 2>(o, vt, (kg * C::NS + n) * 32, p[n], seen[n], lane);
+      const int row0 = (kg * C::NS + n) * 32;
+      if (AHEAD > 1 && n + 1 < C::NS) columns[(n + 1) % AHEAD].fetch(v_cols, row0 + 32);
+      const bool finite = whole || all_finite<E, C::DP>(v_rows, row0);
+      add_product<E, C::DP, 2>(o, columns[n % AHEAD], p[n], finite, seen[n], v_cols, row0);
+      if (AHEAD == 1 && n + 1 < C::NS) columns[0].fetch(v_cols, row0 + 32);
     }
   }
 

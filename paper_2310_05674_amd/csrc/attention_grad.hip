@@ -66,10 +66,11 @@ struct QConfig {
   static constexpr int NS = WM > 1 && sizeof(E) * DP <= 256 ? 2 : 1;
   static constexpr int WAVES = WM * KG, THREADS = WAVES * 64, BM = 32 * WM, BK = 32 * NS * KG;
   static constexpr int KV = BK * DP * (int)sizeof(E), LDS = 4 * KV;
+  static constexpr int PER_EU = sizeof(E) * DP <= 256 ? 2 : 1;
   static_assert(LDS <= LDS_MAX && KG * DP * 32 * 4 <= LDS, "LDS");
 };
 template <typename E, typename C, bool SHAPED>
-__global__ __launch_bounds__(C::THREADS) void k_attention_dq(AttentionArgs a, Rows recs, int tiles) {
+__global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(AttentionArgs a, Rows recs, int tiles) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(C::THREADS) void k_attention_dq(AttentionArgs a, Ro
   lv.init(a.v.ld, 0, 1, D, wave, lane);
   const E* const kp = static_cast<const E*>(a.k.p) + hk * a.k.hs;
   const E* const vp = static_cast<const E*>(a.v.p) + hk * a.v.hs;
-  const uint32_t lds = lds_address(smem);
+  const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
   auto issue = [&](int i, int stage) {
     const int64_t k0 = lo + (int64_t)i * C::BK;
     const u32x4 dk = descriptor(kp + k0 * a.k.ld, ((a.Tk - 1 - k0) * a.k.ld + D) * (int64_t)sizeof(E));
@@ -130,19 +131,17 @@ __global__ __launch_bounds__(C::THREADS) void k_attention_dq(AttentionArgs a, Ro
     const int next = seen_from(t + 1);
     wait_loads();
     if (next < end) issue(next, stage ^ 1);
-    const unsigned char* const kt = smem + stage * 2 * C::KV;
-    const unsigned char* const vt = kt + C::KV;
+    const uint32_t k_rows = lds + stage * 2 * C::KV + row_lane, v_rows = k_rows + C::KV, k_cols = lds + stage * 2 * C::KV + column_lane;
     const int first = lo + t * C::BK + kg * 32 * C::NS;
     t = next;
 #pragma unroll
     for (int n = 0; n < C::NS; ++n) {
       const int k0 = first + 32 * n, row0 = (kg * C::NS + n) * 32;
       if (!__any(span.x < k0 + 32 && span.y > k0)) continue;
-      f32x16 s = zeros(), dp = zeros();
-#pragma unroll
-      for (int ks = 0; ks < T::KS; ++ks) s = mma(T::rows(kt, row0, ks, lane), q[ks], s);
-#pragma unroll
-      for (int ks = 0; ks < T::KS; ++ks) dp = mma(T::rows(vt, row0, ks, lane), d[ks], dp);
+      f32x16 s = row_product<E, C::DP>(k_rows, row0, q), dp = row_product<E, C::DP>(v_rows, row0, d);
+      interleave<2 * T::KS, 4, ROW_READS<E>, PRODUCTS<E>>();
+      Columns<E, C::DP, 2> columns;
+      columns.fetch(k_cols, row0);
       const bool whole = __all(span.x <= k0 && span.y >= k0 + 32);
       const int away = at - k0 - 4 * h;
       uint32_t seen = 0;
@@ -154,17 +153,13 @@ __global__ __launch_bounds__(C::THREADS) void k_attention_dq(AttentionArgs a, Ro
         s[r] = SHAPED ? p * (dp[r] - delta) * bend : p * (dp[r] - delta);
       }
       if (!whole) {
+        seen = seen_keys(span, k0, h);
+        const uint32_t matters = span.y - span.x > 1 ? seen : 0;   // a single key has probability 1, whatever its score
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = k0 + register_row(r, h);
-          const bool see = key >= span.x && key < span.y;
-          seen |= (see ? 1u : 0u) << r;
-          s[r] = see && span.y - span.x > 1 ? s[r] : 0.f;   // a single key has probability 1, whatever its score
-        }
+        for (int r = 0; r < 16; ++r) s[r] = where_seen(matters, r, s[r], 0.f);
       }
-      const Frag<E> ds[2] = {fragment<E>(s, 0), fragment<E>(s, 1)};
-      if (whole) add_product<E, C::DP, 2>(dq, kt, row0, ds, lane);
-      else add_product_seen<E, C::DP, 2>(dq, kt, row0, ds, seen, lane);
+      Frag<E> ds[2] = {fragment<E>(s, 0), fragment<E>(s, 1)};
+      add_product<E, C::DP, 2>(dq, columns, ds, whole || all_finite<E, C::DP>(k_rows, row0), seen, k_cols, row0);
     }
   }
   if constexpr (C::KG > 1) {   // the groups' sums; a wave then has 32 of the columns
@@ -194,22 +189,24 @@ __global__ __launch_bounds__(C::THREADS) void k_attention_dq(AttentionArgs a, Ro
 }
 
 // ------------------------------------------------------------------------------------------------------ dk, dv
-template <typename E, int DP_, int WK_>
+// Waves work in pairs on the same 32 keys: the first has k in registers, forms the scores and p, and adds up dv; the second has v, forms dp and, with the first one's p
+// through LDS, ds, and adds up dk.  One wave for both needs 300 registers at a width of 128, which leaves one to a SIMD and nothing to do while it waits.
+template <typename E, int DP_, int WK_, int QG_, int NS_>
 struct KConfig {
-  static constexpr int DP = DP_, WK = WK_;
-  static constexpr int QG = WK > 1 ? 1 : sizeof(E) * DP > 256 ? 2 : 4;            // groups of waves with rows of their own
-  static constexpr int NS = WK > 1 ? 2 : 1;                                       // 32 rows each of a wave's part of a tile
-  static constexpr int WAVES = WK * QG, THREADS = WAVES * 64, KEYS = 32 * WK, BQ = 32 * NS * QG, GROUPS = BQ / GROUP;
-  static constexpr int QD = BQ * DP * (int)sizeof(E), REC = (GROUPS * RECORD + 1023) / 1024 * 1024, STAGE = 2 * QD + REC, LDS = 2 * STAGE;
+  static constexpr int DP = DP_, WK = WK_, QG = QG_, NS = NS_;                    // pairs side by side over keys, over rows; 32 rows each of a pair's part of a tile
+  static constexpr int PAIRS = WK * QG, WAVES = 2 * PAIRS, THREADS = WAVES * 64, KEYS = 32 * WK, BQ = 32 * NS * QG, GROUPS = BQ / GROUP;
+  static constexpr int QD = BQ * DP * (int)sizeof(E), REC = (GROUPS * RECORD + 1023) / 1024 * 1024, STAGE = 2 * QD + REC;
+  static constexpr int P = 2 * STAGE, LDS = P + PAIRS * NS * 4096;                // the pairs' p, fp32
   static constexpr int REC_LOADS = (REC / 1024 + WAVES - 1) / WAVES;
-  static_assert(BQ % GROUP == 0 && LDS <= LDS_MAX && QG * DP * 32 * 4 <= LDS, "LDS");
+  static_assert(BQ % GROUP == 0 && LDS <= LDS_MAX && 2 * QG * DP * 32 * 4 <= LDS, "LDS");
 };
 template <typename E, typename C, bool SHAPED>
-__global__ __launch_bounds__(C::THREADS) void k_attention_dkv(AttentionArgs a, Rows recs) {
+__global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a, Rows recs) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int kw = wave / C::QG, qg = wave % C::QG;
+  const int pair = wave % C::PAIRS, kw = pair / C::QG, qg = pair % C::QG;
+  const bool second = wave >= C::PAIRS;   // (waves four apart share a SIMD: one of either kind, which want its units at different times)
   const int G = a.Hq / a.Hk, D = a.D, tokens = GROUP / G;
   const int hk = blockIdx.x % a.Hk, k_first = blockIdx.x / a.Hk * C::KEYS;   // the first keys, which most rows of a causal text see, first
   const int key0 = k_first + kw * 32, key = key0 + (lane & 31);
@@ -236,7 +233,7 @@ __global__ __launch_bounds__(C::THREADS) void k_attention_dkv(AttentionArgs a, R
   Loads<E, C::DP, C::BQ, C::WAVES> lq, ld;
   lq.init(a.q.ld, a.q.hs, G, D, wave, lane);
   ld.init(a.dout.ld, a.dout.hs, G, D, wave, lane);
-  const uint32_t lds = lds_address(smem);
+  const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
   auto issue = [&](int step, int stage) {
     const int64_t group = (int64_t)step * C::GROUPS, q0 = group * tokens;
     const E* const q = static_cast<const E*>(a.q.p) + q0 * a.q.ld + (int64_t)hk * G * a.q.hs;
@@ -255,107 +252,160 @@ __global__ __launch_bounds__(C::THREADS) void k_attention_dkv(AttentionArgs a, R
   int step = next_step();
   if (step < steps) issue(step, 0);
 
-  Frag<E> k[T::KS], v[T::KS];
+  Frag<E> f[T::KS];   // the keys' k, or v
   {
-    const int64_t from = min((int64_t)key, a.Tk - 1);
-    const E* const kp = static_cast<const E*>(a.k.p) + from * a.k.ld + hk * a.k.hs;
-    const E* const vp = static_cast<const E*>(a.v.p) + from * a.v.ld + hk * a.v.hs;
+    const Heads& from = second ? a.v : a.k;
+    const E* const p = static_cast<const E*>(from.p) + min((int64_t)key, a.Tk - 1) * from.ld + hk * from.hs;
 #pragma unroll
-    for (int ks = 0; ks < T::KS; ++ks) {
-      k[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(kp + 16 * ks + 8 * h) : zero_fragment<E>();
-      v[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(vp + 16 * ks + 8 * h) : zero_fragment<E>();
-    }
+    for (int ks = 0; ks < T::KS; ++ks) f[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(p + 16 * ks + 8 * h) : zero_fragment<E>();
   }
   const Shape shape(a.scale, a.cap);
   const float c = a.scale * LOG2E;
-  f32x16 dk[T::DF], dv[T::DF];
+  float* const shared_p = reinterpret_cast<float*>(smem + C::P) + pair * C::NS * 1024 + lane * 4;
+  f32x16 sum[T::DF];   // dv, or dk
 #pragma unroll
-  for (int df = 0; df < T::DF; ++df) { dk[df] = zeros(); dv[df] = zeros(); }
+  for (int df = 0; df < T::DF; ++df) sum[df] = zeros();
 
   for (int stage = 0; step < steps; stage ^= 1) {
     const int next = next_step();
     wait_loads();
     if (next < steps) issue(next, stage ^ 1);
     step = next;
-    const unsigned char* const qt = smem + stage * C::STAGE;
-    const unsigned char* const dt = qt + C::QD;
+    const uint32_t q_tile = lds + stage * C::STAGE, d_tile = q_tile + C::QD;
+    const uint32_t rows = (second ? d_tile : q_tile) + row_lane, other_rows = (second ? q_tile : d_tile) + row_lane, columns_at = (second ? q_tile : d_tile) + column_lane;
+    const uint32_t* const recs_at = reinterpret_cast<const uint32_t*>(smem + stage * C::STAGE + 2 * C::QD);
+    f32x16 s[C::NS];
+    Frag<E> b[C::NS][2];
+    bool some[C::NS], whole[C::NS];
+    uint32_t seen[C::NS], matters[C::NS];
 #pragma unroll
     for (int n = 0; n < C::NS; ++n) {
       const int row0 = (qg * C::NS + n) * 32;
-      const uint32_t* const rec = reinterpret_cast<const uint32_t*>(dt + C::QD) + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
+      const uint32_t* const rec = recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
       const int first = (int)rec[FIRST * GROUP + (lane & 31)], end = (int)rec[END * GROUP + (lane & 31)];
-      if (!__any(first < key0 + 32 && end > key0)) continue;
-      f32x16 s = zeros(), dp = zeros();
+      some[n] = __any(first < key0 + 32 && end > key0);
+      whole[n] = __all(first <= key0 && end >= key0 + 32);
+      seen[n] = matters[n] = 0;
+      if (some[n] && !whole[n]) {                // a single key has probability 1, whatever its score: its ds is zero
 #pragma unroll
-      for (int ks = 0; ks < T::KS; ++ks) s = mma(T::rows(qt, row0, ks, lane), k[ks], s);
-#pragma unroll
-      for (int ks = 0; ks < T::KS; ++ks) dp = mma(T::rows(dt, row0, ks, lane), v[ks], dp);
-      const bool whole = __all(first <= key0 && end >= key0 + 32);
-      uint32_t seen = 0;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int at = 8 * b + 4 * h;
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(rec + LSE * GROUP + at), delta = *reinterpret_cast<const f32x4*>(rec + DELTA * GROUP + at);
-        f32x4 slope = {}; u32x4 place = {};
-        if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(rec + SLOPE * GROUP + at); place = *reinterpret_cast<const u32x4*>(rec + AT * GROUP + at); }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * b + i;
-          float bend = 1.f, x = s[r] * c;
-          if (SHAPED) x = shape.score<E>(s[r], slope[i], fabsf((float)((int)place[i] - key)), bend);
-          s[r] = __builtin_amdgcn_exp2f(x - lse[i]);
-          dp[r] = SHAPED ? s[r] * (dp[r] - delta[i]) * bend : s[r] * (dp[r] - delta[i]);
-        }
-        if (!whole) {
+        for (int q = 0; q < 4; ++q) {
+          const int at = 8 * q + 4 * h;
           const u32x4 from = *reinterpret_cast<const u32x4*>(rec + FIRST * GROUP + at), to = *reinterpret_cast<const u32x4*>(rec + END * GROUP + at);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int r = 4 * b + i;
-            const bool see = key >= (int)from[i] && key < (int)to[i];
-            seen |= (see ? 1u : 0u) << r;
-            s[r] = see ? s[r] : 0.f;
-            dp[r] = see && to[i] - from[i] > 1 ? dp[r] : 0.f;
+            const uint32_t bit = key >= (int)from[i] && key < (int)to[i] ? 1u << seen_bit(4 * q + i) : 0;
+            seen[n] |= bit;
+            matters[n] |= to[i] - from[i] > 1 ? bit : 0;
           }
         }
       }
-      const Frag<E> p[2] = {fragment<E>(s, 0), fragment<E>(s, 1)}, ds[2] = {fragment<E>(dp, 0), fragment<E>(dp, 1)};
-      if (whole) {
-        add_product<E, C::DP, 2>(dv, dt, row0, p, lane);
-        add_product<E, C::DP, 2>(dk, qt, row0, ds, lane);
-      } else {
-        add_product_seen<E, C::DP, 2>(dv, dt, row0, p, seen, lane);
-        add_product_seen<E, C::DP, 2>(dk, qt, row0, ds, seen, lane);
+    }
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) {
+      if (some[n]) {
+        s[n] = row_product<E, C::DP>(rows, (qg * C::NS + n) * 32, f);
+        interleave<T::KS, 4, ROW_READS<E>, PRODUCTS<E>>();
+      }
+    }
+    if (!second) {
+#pragma unroll
+      for (int n = 0; n < C::NS; ++n) {
+        if (!some[n]) continue;
+        const int row0 = (qg * C::NS + n) * 32;
+        const uint32_t* const rec = recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int at = 8 * q + 4 * h;
+          const f32x4 lse = *reinterpret_cast<const f32x4*>(rec + LSE * GROUP + at);
+          f32x4 slope = {}, bent; u32x4 place = {};
+          if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(rec + SLOPE * GROUP + at); place = *reinterpret_cast<const u32x4*>(rec + AT * GROUP + at); }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = 4 * q + i;
+            float bend = 1.f, x = s[n][r] * c;
+            if (SHAPED) x = shape.score<E>(s[n][r], slope[i], fabsf((float)((int)place[i] - key)), bend);
+            s[n][r] = __builtin_amdgcn_exp2f(x - lse[i]);
+            bent[i] = SHAPED ? s[n][r] * bend : s[n][r];
+          }
+          *reinterpret_cast<f32x4*>(shared_p + n * 1024 + q * 256) = bent;
+        }
+        if (!whole[n]) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] = where_seen(seen[n], r, s[n][r], 0.f);
+        }
+        b[n][0] = fragment<E>(s[n], 0); b[n][1] = fragment<E>(s[n], 1);
+      }
+    }
+    __syncthreads();
+    if (second) {
+#pragma unroll
+      for (int n = 0; n < C::NS; ++n) {
+        if (!some[n]) continue;
+        const int row0 = (qg * C::NS + n) * 32;
+        const uint32_t* const rec = recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 delta = *reinterpret_cast<const f32x4*>(rec + DELTA * GROUP + 8 * q + 4 * h), p = *reinterpret_cast<const f32x4*>(shared_p + n * 1024 + q * 256);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { const int r = 4 * q + i; s[n][r] = p[i] * (s[n][r] - delta[i]); }
+        }
+        if (!whole[n]) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] = where_seen(matters[n], r, s[n][r], 0.f);
+        }
+        b[n][0] = fragment<E>(s[n], 0); b[n][1] = fragment<E>(s[n], 1);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) {
+      if (!some[n]) continue;
+      const int row0 = (qg * C::NS + n) * 32;
+      const bool finite = whole[n] || all_finite<E, C::DP>(other_rows, row0);
+      constexpr int N = sizeof(E) * C::DP > 256 ? 1 : 2;   // fragments at a time: 64 registers of columns at most
+#pragma unroll
+      for (int half = 0; half < 2; half += N) {
+        Columns<E, C::DP, N> columns;
+        Frag<E> weights[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) weights[i] = b[n][half + i];
+        columns.fetch(columns_at, row0 + 16 * half);
+        add_product<E, C::DP, N>(sum, columns, weights, finite, seen[n] >> (16 * half), columns_at, row0 + 16 * half);
       }
     }
   }
-  auto finish = [&](f32x16 (&x)[T::DF], const Heads& out, float factor) {
-    if constexpr (C::QG > 1) {
-      float* const part = reinterpret_cast<float*>(smem);                     // [QG][DP][32]
+  if constexpr (C::QG > 1) {   // the row groups' sums; a wave then has some of the columns
+    float* const part = reinterpret_cast<float*>(smem) + (second ? C::QG * C::DP * 32 : 0);                     // [QG][DP][32]
+    __syncthreads();
+#pragma unroll
+    for (int kk = 0; kk < C::WK; ++kk) {
+      if (kk == kw) {
+#pragma unroll
+        for (int df = 0; df < T::DF; ++df)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) part[(qg * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)] = sum[df][r];
+      }
       __syncthreads();
+      if (kk == kw) {
 #pragma unroll
-      for (int df = 0; df < T::DF; ++df)
+        for (int df = 0; df < T::DF; ++df) {
+          if (df % C::QG != qg) continue;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) part[(qg * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)] = x[df][r];
-      __syncthreads();
+          for (int r = 0; r < 16; ++r) {
+            float x = 0.f;
 #pragma unroll
-      for (int df = 0; df < T::DF; ++df) {
-        if (df % C::QG != qg) continue;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float sum = 0.f;
-#pragma unroll
-          for (int g = 0; g < C::QG; ++g) sum += part[(g * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)];
-          x[df][r] = sum;
+            for (int g = 0; g < C::QG; ++g) x += part[(g * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)];
+            sum[df][r] = x;
+          }
         }
       }
+      __syncthreads();
     }
-    if (key >= a.Tk) return;
-    E* const to = const_cast<E*>(static_cast<const E*>(out.p)) + (int64_t)key * out.ld + hk * out.hs;
+  }
+  if (key >= a.Tk) return;
+  const Heads& out = second ? a.dk : a.dv;
+  E* const to = const_cast<E*>(static_cast<const E*>(out.p)) + (int64_t)key * out.ld + hk * out.hs;
 #pragma unroll
-    for (int df = 0; df < T::DF; ++df) if (C::QG == 1 || df % C::QG == qg) store_columns<E>(to, df, D, x[df], factor, h);
-  };
-  finish(dk, a.dk, a.scale);
-  finish(dv, a.dv, 1.f);
+  for (int df = 0; df < T::DF; ++df) if (C::QG == 1 || df % C::QG == qg) store_columns<E>(to, df, D, sum[df], second ? a.scale : 1.f, h);
 }
 
 constexpr int64_t MANY = 256;
@@ -383,12 +433,17 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
     launch<&k_attention_dq<E, C, SHAPED>, C>(ps, (count + 31) / 32 * a.Hk, st, a, rows, (int)((count + 31) / 32));
   }
   if (a.Tk == 0) return;
-  if ((a.Tk + 127) / 128 * a.Hk >= MANY) {
-    typedef KConfig<E, DP, 4> C;
-    launch<&k_attention_dkv<E, C, SHAPED>, C>(ps, (a.Tk + 127) / 128 * a.Hk, st, a, rows);
+  auto dkv = [&](auto config) {
+    typedef decltype(config) C;
+    launch<&k_attention_dkv<E, C, SHAPED>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
+  };
+  if constexpr (sizeof(E) * DP > 256) {
+    if ((a.Tk + 63) / 64 * a.Hk >= MANY) dkv(KConfig<E, DP, 2, 2, 1>{});
+    else dkv(KConfig<E, DP, 1, 2, 1>{});
   } else {
-    typedef KConfig<E, DP, 1> C;
-    launch<&k_attention_dkv<E, C, SHAPED>, C>(ps, (a.Tk + 31) / 32 * a.Hk, st, a, rows);
+    if ((a.Tk + 127) / 128 * a.Hk >= 2 * MANY) dkv(KConfig<E, DP, 4, 1, 2>{});
+    else if ((a.Tk + 63) / 64 * a.Hk >= MANY) dkv(KConfig<E, DP, 2, 2, 1>{});
+    else dkv(KConfig<E, DP, 1, 4, 1>{});
   }
 }
 template <typename E, int DP>

@@ -22,6 +22,9 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef const __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef const __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef const __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int LDS_MAX = 160 * 1024;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
@@ -69,36 +72,39 @@ template <typename E, int DP> struct Tile {
     if constexpr (PIECES == 8) return (((r >> 1) & 1) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
     else return ((r & 3) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
   }
-  // rows row0 + lane % 32, contraction 16 ks ..
-  static __device__ __forceinline__ Frag<E> rows(const unsigned char* tile, int row0, int ks, int lane) {
-    const int r = lane & 31, h = lane >> 5, sw = permuted(r);
-    const unsigned char* const at = tile + (row0 + r) * ROW;
+  // A lane's place in a tile for either fetch, to be added to where the tile is (a multiple of ROW); which piece of a row is meant is then one exclusive or.
+  static __device__ __forceinline__ uint32_t row_lane(int lane) {
+    return (lane & 31) * ROW + ((permuted(lane & 31) ^ (lane >> 5) * (int)(sizeof(E) / 2)) << 4);
+  }
+  static __device__ __forceinline__ uint32_t column_lane(int lane) {
+    const int h = lane >> 5;
     if constexpr (sizeof(E) == 2) {
-      return *reinterpret_cast<const bf16x8*>(at + (((2 * ks + h) ^ sw) << 4));
+      const int r = 4 * h + ((lane & 15) >> 2), piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      return r * ROW + ((piece ^ permuted(r)) << 4) + (lane & 1) * 8;
     } else {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(at + (((4 * ks + 2 * h) ^ sw) << 4)), b = *reinterpret_cast<const f32x4*>(at + (((4 * ks + 2 * h + 1) ^ sw) << 4));
+      return 4 * h * ROW + ((((lane & 31) >> 2) ^ permuted(4 * h)) << 4) + (lane & 3) * 4;
+    }
+  }
+  // rows row0 + lane % 32, contraction 16 ks ..
+  static __device__ __forceinline__ Frag<E> rows(uint32_t at, int row0, int ks) {
+    if constexpr (sizeof(E) == 2) {
+      return *(lds_bf16x8*)(uintptr_t)((at ^ (uint32_t)(ks << 5)) + row0 * ROW);
+    } else {
+      const f32x4 a = *(lds_f32x4*)(uintptr_t)((at ^ (uint32_t)(ks << 6)) + row0 * ROW), b = *(lds_f32x4*)(uintptr_t)((at ^ (uint32_t)(ks << 6 | 16)) + row0 * ROW);
       return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
   // transposed: column 32 df + lane % 32 of rows row0 .. row0 + 15, in the order above
-  static __device__ __forceinline__ Frag<E> columns(const unsigned char* tile, int row0, int df, int lane) {
-    const int h = lane >> 5;
+  static __device__ __forceinline__ Frag<E> columns(uint32_t at, int row0, int df) {
     if constexpr (sizeof(E) == 2) {
       union { bf16x8 v; s16x4 q[2]; } u;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int r = 8 * t + 4 * h + ((lane & 15) >> 2), piece = 4 * df + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-        const unsigned char* const at = tile + (row0 + r) * ROW + ((piece ^ permuted(r)) << 4) + (lane & 1) * 8;
-        u.q[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-      }
+      for (int t = 0; t < 2; ++t) u.q[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ (uint32_t)(df << 6 | t << 4)) + (row0 + 8 * t) * ROW));
       return u.v;
     } else {
       f32x8 v;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int r = 8 * (t >> 2) + 4 * h + (t & 3), piece = 8 * df + ((lane & 31) >> 2);
-        v[t] = *reinterpret_cast<const float*>(tile + (row0 + r) * ROW + ((piece ^ permuted(r)) << 4) + (lane & 3) * 4);
-      }
+      for (int t = 0; t < 8; ++t) v[t] = *(lds_float*)(uintptr_t)((at ^ (uint32_t)((df << 7) ^ ((t & 3) << 6) ^ ((t >> 2) << 4))) + (row0 + 8 * (t >> 2) + (t & 3)) * ROW);
       return v;
     }
   }
@@ -165,56 +171,114 @@ struct Shape {
   }
 };
 
-// acc[df] += (columns 32 df .. of the tile's rows row0 ..)^T times the N fragments b.
-template <typename E, int DP, int N>
-__device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], const unsigned char* tile, int row0, const Frag<E> (&b)[N], int lane) {
+// The order of a block of `FRAGMENTS` fetches and products, left to itself the compiler waits for each fragment right after asking for it: AHEAD fragments first, then a
+// product for each further one.  READS and PRODUCTS: instructions of a fragment.
+template <int FRAGMENTS, int AHEAD, int READS, int PRODUCTS>
+__device__ __forceinline__ void interleave() {
+  constexpr int FIRST = AHEAD < FRAGMENTS ? AHEAD : FRAGMENTS;
+  __builtin_amdgcn_sched_group_barrier(0x100, FIRST * READS, 0);
 #pragma unroll
-  for (int s = 0; s < N; ++s)
-#pragma unroll
-    for (int df = 0; df < DP / 32; ++df) acc[df] = mma(Tile<E, DP>::columns(tile, row0 + 16 * s, df, lane), b[s], acc[df]);
+  for (int i = 0; i < FRAGMENTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS, 0);
+    if (i + FIRST < FRAGMENTS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
 }
-// The same where some of a lane's weights are zero because it does not see the row (bit 8 s + t of `seen` clear): zero times infinity or NaN is NaN, so a
-// row that is not finite would reach lanes that do not see it.  The tile's part is formed by itself; if it is not finite, once more with zeros for what is not, and
-// a second product counts for each lane what it sees of those: NaN for it where there is any.
-template <typename E> __device__ __forceinline__ void split_finite(const Frag<E>& x, Frag<E>& finite, Frag<E>& rest) {
+template <typename E> constexpr int ROW_READS = sizeof(E) == 2 ? 1 : 2;
+template <typename E> constexpr int PRODUCTS = sizeof(E) == 2 ? 1 : 8;
+
+// The keys of a subtile of 32 that a lane sees, as bits, for its registers: bit 8 (r / 4) + r % 4 is register r's.
+__device__ __forceinline__ uint32_t seen_keys(int2 span, int k0, int h) {
+  const int lo = min(max(span.x - k0, 0), 32), hi = min(max(span.y - k0, 0), 32);
+  const uint32_t below_hi = hi >= 32 ? 0xffffffffu : (1u << hi) - 1u, below_lo = lo >= 32 ? 0xffffffffu : (1u << lo) - 1u;
+  return (below_hi & ~below_lo) >> (4 * h);
+}
+__device__ __forceinline__ int seen_bit(int r) { return 8 * (r >> 2) + (r & 3); }
+// x where the bit is set, else `other`
+__device__ __forceinline__ float where_seen(uint32_t seen, int r, float x, float other) {
+  const uint32_t m = (uint32_t)((int32_t)(seen << (31 - seen_bit(r))) >> 31);
+  return __uint_as_float((__float_as_uint(x) & m) | (__float_as_uint(other) & ~m));
+}
+
+// the products of a tile's rows row0 .. with the fragments b of a row each
+template <typename E, int DP>
+__device__ __forceinline__ f32x16 row_product(uint32_t tile, int row0, const Frag<E> (&b)[DP / 16]) {
+  f32x16 x = zeros();
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) x = mma(Tile<E, DP>::rows(tile, row0, ks), b[ks], x);
+  return x;
+}
+// acc[df] += (columns 32 df .. of 16 N of a tile's rows)^T times the N fragments b.  The columns are fetched ahead of the arithmetic that makes b.
+//
+// Where some of a lane's weights are zero because it does not see the row (its bit of `seen` clear): zero times infinity or NaN is NaN, so a row that is not finite
+// would reach lanes that do not see it.  The rows are looked through first, and if one is not finite, the product runs twice: with zeros for what is not, and with
+// what is beyond every number where a lane sees such a value and nothing elsewhere.  One loop for both, because sums that leave a branch in two versions are copied.
+template <typename E, int DP, int N> struct Columns {
+  Frag<E> a[N][DP / 32];
+  __device__ __forceinline__ void fetch(uint32_t tile, int row0) {   // tile: of a lane, see column_lane
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+      for (int df = 0; df < DP / 32; ++df) a[s][df] = Tile<E, DP>::columns(tile, row0 + 16 * s, df);
+  }
+};
+template <typename E> __device__ __forceinline__ float add_unless_finite(const Frag<E>& x, float check) {   // check + 0 x
+  if constexpr (sizeof(E) == 2) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 zero = {(__bf16)0.f, (__bf16)0.f};
+    const union { bf16x8 v; bf16x2 w[4]; } u = {x};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) check = __builtin_amdgcn_fdot2_f32_bf16(u.w[i], zero, check, false);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) check = fmaf(x[i], 0.f, check);
+  }
+  return check;
+}
+template <typename E, int DP>
+__device__ __forceinline__ bool all_finite(uint32_t tile, int row0) {   // tile: of a lane, see row_lane
+  float check = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) check = add_unless_finite<E>(Tile<E, DP>::rows(tile, row0, ks), check);
+  return !__any(check != check);
+}
+template <typename E> __device__ __forceinline__ void split_finite(const Frag<E> x, Frag<E>& finite, Frag<E>& rest) {
   if constexpr (sizeof(E) == 2) {
     union { bf16x8 v; uint16_t w[8]; } a, f, r;
     a.v = x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const bool bad = (a.w[i] & 0x7f80) == 0x7f80; f.w[i] = bad ? 0 : a.w[i]; r.w[i] = bad ? 0x3f80 : 0; }
+    for (int i = 0; i < 8; ++i) { const bool bad = (a.w[i] & 0x7f80) == 0x7f80; f.w[i] = bad ? 0 : a.w[i]; r.w[i] = bad ? 0x7f7f : 0; }
     finite = f.v; rest = r.v;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const bool bad = (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u; finite[i] = bad ? 0.f : x[i]; rest[i] = bad ? 1.f : 0.f; }
+    for (int i = 0; i < 8; ++i) {
+      const bool bad = (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u;
+      finite[i] = bad ? 0.f : x[i]; rest[i] = bad ? std::numeric_limits<float>::max() : 0.f;
+    }
   }
 }
 template <typename E, int DP, int N>
-__device__ __forceinline__ void add_product_seen(f32x16 (&acc)[DP / 32], const unsigned char* tile, int row0, const Frag<E> (&b)[N], uint32_t seen, int lane) {
+__device__ __forceinline__ void add_product(f32x16 (&acc)[DP / 32], Columns<E, DP, N>& x, Frag<E> (&b)[N], bool finite, uint32_t seen, uint32_t tile, int row0) {
+  if (!finite) {
 #pragma unroll
-  for (int df = 0; df < DP / 32; ++df) {
-    f32x16 part = zeros();
+    for (int s = 0; s < N; ++s)
 #pragma unroll
-    for (int s = 0; s < N; ++s) part = mma(Tile<E, DP>::columns(tile, row0 + 16 * s, df, lane), b[s], part);
-    float check = 0.f;
+      for (int df = 0; df < DP / 32; ++df) { Frag<E> rest; split_finite<E>(x.a[s][df], x.a[s][df], rest); }
+  }
+  for (int turn = 0;; ++turn) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) check = fmaf(part[r], 0.f, check);
-    if (__any(check != check)) {
-      f32x16 count = zeros();
-      part = zeros();
+    for (int s = 0; s < N; ++s)
 #pragma unroll
-      for (int s = 0; s < N; ++s) {
-        Frag<E> finite, rest, sees;
-        split_finite<E>(Tile<E, DP>::columns(tile, row0 + 16 * s, df, lane), finite, rest);
+      for (int df = 0; df < DP / 32; ++df) acc[df] = mma(x.a[s][df], b[s], acc[df]);
+    if (finite || turn == 1) break;
+    asm volatile("" : "+v"(seen));   // here and not before, where it would be for nothing
+    x.fetch(tile, row0);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) sees[t] = (seen >> (8 * s + t) & 1) ? 1.f : 0.f;
-        part = mma(finite, b[s], part);
-        count = mma(rest, sees, count);
-      }
+    for (int s = 0; s < N; ++s) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) part[r] = count[r] > 0.f ? std::numeric_limits<float>::quiet_NaN() : part[r];
+      for (int df = 0; df < DP / 32; ++df) { Frag<E> rest; split_finite<E>(x.a[s][df], rest, x.a[s][df]); }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) b[s][t] = (seen >> seen_bit(8 * s + t) & 1) ? 3e38f : 0.f;
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[df][r] += part[r];
   }
 }
 
