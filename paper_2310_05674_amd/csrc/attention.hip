@@ -13,15 +13,13 @@ namespace sama {
 namespace {
 using namespace attn;
 
-template <typename E, int DP_, int WM_>
+template <typename E, int DP_, int WM_, int KG_, int NS_>
 struct Config {
-  static constexpr int DP = DP_, WM = WM_;
-  static constexpr int KG = WM > 1 ? 1 : sizeof(E) * DP > 256 ? 2 : 4;            // groups of waves with keys of their own
-  static constexpr int NS = WM > 1 && sizeof(E) * DP <= 256 ? 2 : 1;              // 32 keys each of a wave's part of a tile
+  static constexpr int DP = DP_, WM = WM_, KG = KG_, NS = NS_;                    // waves side by side over rows, over keys; 32 keys each of a wave's part of a tile
   static constexpr int WAVES = WM * KG, THREADS = WAVES * 64, BM = 32 * WM, BK = 32 * NS * KG;
   static constexpr int KV = BK * DP * (int)sizeof(E), LDS = 4 * KV;               // K and V, two stages
   static constexpr int PER_EU = sizeof(E) * DP <= 256 ? 2 : 1;
-  static_assert(LDS <= LDS_MAX && KG * DP * 32 * 4 + KG * 256 <= LDS, "LDS");
+  static_assert(LDS <= LDS_MAX && (KG == 1 || WAVES * (DP * 32 * 4 + 256) <= LDS), "LDS");
 };
 
 struct Parts { float* o; float* lse; int count; };   // of split keys: [count][Hk][rows][D] and [count][Hk][rows]
@@ -60,15 +58,10 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
   const E* const kp = static_cast<const E*>(a.k.p) + hk * a.k.hs;
   const E* const vp = static_cast<const E*>(a.v.p) + hk * a.v.hs;
   const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
-  auto issue = [&](int i, int stage) {
-    const int64_t k0 = lo + (int64_t)i * C::BK;
-    const u32x4 dk = descriptor(kp + k0 * a.k.ld, ((a.Tk - 1 - k0) * a.k.ld + D) * (int64_t)sizeof(E));
-    const u32x4 dv = descriptor(vp + k0 * a.v.ld, ((a.Tk - 1 - k0) * a.v.ld + D) * (int64_t)sizeof(E));
-    lk.issue(lds + stage * 2 * C::KV, dk, wave);
-    lv.issue(lds + stage * 2 * C::KV + C::KV, dv, wave);
-  };
+  const Source ks(kp + (int64_t)lo * a.k.ld, ((a.Tk - 1 - lo) * a.k.ld + D) * (int64_t)sizeof(E), C::BK * a.k.ld * (int64_t)sizeof(E));
+  const Source vs(vp + (int64_t)lo * a.v.ld, ((a.Tk - 1 - lo) * a.v.ld + D) * (int64_t)sizeof(E), C::BK * a.v.ld * (int64_t)sizeof(E));
   t = seen_from(t);
-  if (t < end) issue(t, 0);
+  if (t < end) { lk.issue(lds, ks.tile(t), wave); lv.issue(lds + C::KV, vs.tile(t), wave); }
 
   Frag<E> q[T::KS];
   {
@@ -76,6 +69,7 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
 #pragma unroll
     for (int ks = 0; ks < T::KS; ++ks) q[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(p + 16 * ks + 8 * h) : zero_fragment<E>();
   }
+  arrived(q);
   const Shape shape(a.scale, a.cap);
   const float slope = SHAPED && a.slopes != nullptr ? a.slopes[head] * LOG2E : 0.f;
   const int at = SHAPED && a.slopes != nullptr ? (a.at != nullptr ? a.at[query] : query) : 0;
@@ -88,15 +82,21 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
   for (int stage = 0; t < end; stage ^= 1) {
     const int next = seen_from(t + 1);
     wait_loads();
-    if (next < end) issue(next, stage ^ 1);
+    const u32x4 next_k = next < end ? ks.tile(next) : Source::nothing(), next_v = next < end ? vs.tile(next) : Source::nothing();
+    const uint32_t next_at = lds + (stage ^ 1) * 2 * C::KV;
+    constexpr int LOADS = lk.N + lv.N;
+    auto load = [&](int i) { if (i < lk.N) lk.issue_one(i, next_at, next_k, wave); else lv.issue_one(i - lk.N, next_at + C::KV, next_v, wave); };
     const uint32_t k_rows = lds + stage * 2 * C::KV + row_lane, v_rows = k_rows + C::KV, v_cols = lds + stage * 2 * C::KV + C::KV + column_lane;
     const int k0 = lo + t * C::BK + kg * 32 * C::NS;   // the wave's first key
     t = next;
-    if (!__any(span.x < k0 + 32 * C::NS && span.y > k0)) continue;
     f32x16 s[C::NS];
+    constexpr int STEPS = C::NS * T::KS;
+    pipeline<STEPS, ROWS_AHEAD<E>, Frag<E>>([&](int i) { return T::rows(k_rows, (kg * C::NS + i / T::KS) * 32, i % T::KS); }, [&](int i, const Frag<E>& x) {
+      s[i / T::KS] = mma(x, q[i % T::KS], i % T::KS == 0 ? zeros() : s[i / T::KS]);
 #pragma unroll
-    for (int n = 0; n < C::NS; ++n) s[n] = row_product<E, C::DP>(k_rows, (kg * C::NS + n) * 32, q);
-    interleave<C::NS * T::KS, 4, ROW_READS<E>, PRODUCTS<E>>();
+      for (int j = i * LOADS / STEPS; j < (i + 1) * LOADS / STEPS; ++j) load(j);
+    });
+    if (!__any(span.x < k0 + 32 * C::NS && span.y > k0)) continue;   // (not sooner: the loads are every wave's)
     constexpr int AHEAD = C::DP * sizeof(E) > 128 ? 1 : 2;   // sets of columns: 16 registers or 32 in bf16
     Columns<E, C::DP, 2> columns[AHEAD];
     columns[0].fetch(v_cols, kg * C::NS * 32);
@@ -152,11 +152,12 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
     }
   }
 
+  drain_loads();
   l = other_half_sum(l);
   if constexpr (C::KG > 1) {   // the groups' parts, each of its own maximum, through LDS; a wave then has 32 of the columns
     __syncthreads();
-    float* const part = reinterpret_cast<float*>(smem);                     // [KG][DP][32]
-    float* const stat = part + C::KG * C::DP * 32;                          // [KG][2][32]
+    float* const part = reinterpret_cast<float*>(smem) + rw * C::KG * (C::DP * 32 + 64);   // [KG][DP][32]
+    float* const stat = part + C::KG * C::DP * 32;                                           // [KG][2][32]
 #pragma unroll
     for (int df = 0; df < T::DF; ++df)
 #pragma unroll
@@ -203,30 +204,43 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
   }
 }
 
-// The parts of split keys, weighted by what each holds of the row's sum: four columns a thread, a row's of neighbouring threads.
+// The parts of split keys, weighted by what each holds of the row's sum.  A workgroup takes a row: four columns a thread, and eight threads to those, each with every eighth part: the
+// parts' loads are then on their way together (48 rows of 64 parts take 5 us, and 41 with one thread for all parts of its columns).
+constexpr int MOST_PARTS = 64;
 template <typename E>
 __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a, Parts parts) {
-  const int G = a.Hq / a.Hk, rows = (int)a.Tq * G, quads = a.D / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, of_row = i / quads;
-  const int d = (int)(i - of_row * quads) * 4;
-  if (of_row >= (int64_t)a.Hk * rows) return;
-  const int64_t step = (int64_t)a.Hk * rows;
-  float top = -INF, sum = 0.f;
-  for (int p = 0; p < parts.count; ++p) top = fmaxf(top, parts.lse[p * step + of_row]);
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts.count; ++p) {
-    const float lse = parts.lse[p * step + of_row];
-    if (lse == -INF) continue;
-    const float w = __builtin_amdgcn_exp2f(lse - top);
-    sum += w;
-    x += *reinterpret_cast<const f32x4*>(parts.o + (p * step + of_row) * a.D + d) * w;
+  __shared__ float s_weight[MOST_PARTS], s_total[2];
+  __shared__ f32x4 s_part[8][32];
+  const int G = a.Hq / a.Hk, rows = (int)a.Tq * G, quad = threadIdx.x & 31, share = threadIdx.x >> 5;
+  const int64_t of_row = blockIdx.x, step = (int64_t)a.Hk * rows;
+  if (threadIdx.x < 64) {
+    const float lse = (int)threadIdx.x < parts.count ? parts.lse[threadIdx.x * step + of_row] : -INF;
+    const float top = join_wave(lse, [](float x, float y) { return fmaxf(x, y); });
+    const float w = lse == -INF ? 0.f : __builtin_amdgcn_exp2f(lse - top), sum = wave_sum(w);
+    s_weight[threadIdx.x] = w;
+    if (threadIdx.x == 0) { s_total[0] = top; s_total[1] = sum; }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  __syncthreads();
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (4 * quad < a.D) {
+#pragma unroll 8
+    for (int p = share; p < parts.count; p += 8) {
+      const f32x4 o = *reinterpret_cast<const f32x4*>(parts.o + (p * step + of_row) * a.D + 4 * quad);
+      const float w = s_weight[p];
+      if (w != 0.f) x += o * w;   // a part without keys holds nothing
+    }
+  }
+  s_part[share][quad] = x;
+  __syncthreads();
+  if (share != 0 || 4 * quad >= a.D) return;
+#pragma unroll
+  for (int g = 1; g < 8; ++g) x += s_part[g][quad];
+  const float sum = s_total[1], inv = sum == 0.f ? 0.f : 1.f / sum;
   const int hk = (int)(of_row / rows), row = (int)(of_row - (int64_t)hk * rows), query = row / G, head = hk * G + row % G;
-  E* const o = const_cast<E*>(static_cast<const E*>(a.out.p)) + query * a.out.ld + head * a.out.hs + d;
+  E* const o = const_cast<E*>(static_cast<const E*>(a.out.p)) + query * a.out.ld + head * a.out.hs + 4 * quad;
   if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
   else *reinterpret_cast<f32x4*>(o) = x * inv;
-  if (d == 0 && a.lse != nullptr) a.lse[(int64_t)query * a.Hq + head] = sum == 0.f ? -INF : (top + log2f(sum)) * LN2;
+  if (quad == 0 && a.lse != nullptr) a.lse[(int64_t)query * a.Hq + head] = sum == 0.f ? -INF : (s_total[0] + log2f(sum)) * LN2;
 }
 
 __global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets, int documents, const int32_t* prefix, int causal, int T, int2* spans) {
@@ -247,20 +261,21 @@ __global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets,
 }
 
 // What a call looks like: rows of a workgroup, and into how many parts the keys are cut.
-constexpr int64_t MANY = 256, FILLED = 512, LEAST_KEYS = 512, MOST_PARTS = 64;
+// Two workgroups of 128 rows fit a CU; where there are fewer than that, workgroups of 32 rows with four groups of keys take over (4096 queries of 12 heads in four texts, capped: 70 us for 133;
+// 8111 of 16 heads on 4 key heads in 23 texts, which are enough: 50, and 70 with 32).  Where even those leave CUs without one the keys are split.
+constexpr int64_t FILLED = 512, LEAST_KEYS = 512;
 struct Plan { bool few; int tiles, parts; };
 Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk) {
   const int64_t rows = Tq * (Hq / Hk), wide = (rows + 127) / 128 * Hk, narrow = (rows + 31) / 32 * Hk;
   Plan p;
-  p.few = wide < MANY;
+  p.few = wide < FILLED;
   p.tiles = (int)((rows + (p.few ? 31 : 127)) / (p.few ? 32 : 128));
-  p.parts = !p.few || narrow >= MANY ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({FILLED / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
+  p.parts = !p.few || narrow > FILLED / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({FILLED / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
   return p;
 }
 
-template <typename E, int DP, int WM, bool SHAPED>
+template <typename E, typename C, bool SHAPED>
 void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspace) {
-  typedef Config<E, DP, WM> C;
   static const bool once = [] {
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attention<E, C, SHAPED>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
     return true;
@@ -271,17 +286,19 @@ void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspa
   parts.lse = parts.o + (size_t)p.parts * a.Hk * rows * a.D;
   ProfScope ps(st, F_OTHER, 0.0);
   launch_kernel(ps, k_attention<E, C, SHAPED>, dim3((unsigned)(p.tiles * (int64_t)a.Hk), p.parts), C::THREADS, C::LDS, st, a, parts, p.tiles);
-  if (p.parts > 1) {
-    const int64_t threads = rows * a.Hk * (a.D / 4);
-    launch_kernel(ps, k_attention_join<E>, dim3((unsigned)((threads + 255) / 256)), 256, 0, st, a, parts);
-  }
+  if (p.parts > 1) launch_kernel(ps, k_attention_join<E>, dim3((unsigned)(rows * a.Hk)), 256, 0, st, a, parts);
 }
 template <typename E, int DP>
 void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
   const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk);
   const bool shaped = a.cap > 0.f || a.slopes != nullptr;
-  if (p.few) shaped ? launch<E, DP, 1, true>(st, a, p, workspace) : launch<E, DP, 1, false>(st, a, p, workspace);
-  else shaped ? launch<E, DP, 4, true>(st, a, p, workspace) : launch<E, DP, 4, false>(st, a, p, workspace);
+  auto run = [&](auto config) {
+    typedef decltype(config) C;
+    shaped ? launch<E, C, true>(st, a, p, workspace) : launch<E, C, false>(st, a, p, workspace);
+  };
+  constexpr bool WIDE_ROWS = sizeof(E) * DP > 256;
+  if (p.few) run(Config<E, DP, 1, WIDE_ROWS ? 2 : 4, 1>{});
+  else run(Config<E, DP, 4, 1, WIDE_ROWS ? 1 : 2>{});
 }
 }  // namespace
 

@@ -97,15 +97,10 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
   const E* const kp = static_cast<const E*>(a.k.p) + hk * a.k.hs;
   const E* const vp = static_cast<const E*>(a.v.p) + hk * a.v.hs;
   const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
-  auto issue = [&](int i, int stage) {
-    const int64_t k0 = lo + (int64_t)i * C::BK;
-    const u32x4 dk = descriptor(kp + k0 * a.k.ld, ((a.Tk - 1 - k0) * a.k.ld + D) * (int64_t)sizeof(E));
-    const u32x4 dv = descriptor(vp + k0 * a.v.ld, ((a.Tk - 1 - k0) * a.v.ld + D) * (int64_t)sizeof(E));
-    lk.issue(lds + stage * 2 * C::KV, dk, wave);
-    lv.issue(lds + stage * 2 * C::KV + C::KV, dv, wave);
-  };
+  const Source ks(kp + (int64_t)lo * a.k.ld, ((a.Tk - 1 - lo) * a.k.ld + D) * (int64_t)sizeof(E), C::BK * a.k.ld * (int64_t)sizeof(E));
+  const Source vs(vp + (int64_t)lo * a.v.ld, ((a.Tk - 1 - lo) * a.v.ld + D) * (int64_t)sizeof(E), C::BK * a.v.ld * (int64_t)sizeof(E));
   int t = seen_from(0);
-  if (t < end) issue(t, 0);
+  if (t < end) { lk.issue(lds, ks.tile(t), wave); lv.issue(lds + C::KV, vs.tile(t), wave); }
 
   Frag<E> q[T::KS], d[T::KS];
   {
@@ -121,6 +116,7 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
   const float lse = __uint_as_float(rec[LSE * GROUP]), delta = __uint_as_float(rec[DELTA * GROUP]);
   const float slope = SHAPED ? __uint_as_float(rec[SLOPE * GROUP]) : 0.f;
   const int at = SHAPED ? (int)rec[AT * GROUP] : 0;
+  arrived(q); arrived(d);
   const Shape shape(a.scale, a.cap);
   const float c = a.scale * LOG2E;
   f32x16 dq[T::DF];
@@ -130,16 +126,24 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
   for (int stage = 0; t < end; stage ^= 1) {
     const int next = seen_from(t + 1);
     wait_loads();
-    if (next < end) issue(next, stage ^ 1);
+    const u32x4 next_k = next < end ? ks.tile(next) : Source::nothing(), next_v = next < end ? vs.tile(next) : Source::nothing();
+    const uint32_t next_at = lds + (stage ^ 1) * 2 * C::KV;
+    constexpr int LOADS = (lk.N + lv.N) / C::NS;   // in each subtile
+    auto load = [&](int i) { if (i < lk.N) lk.issue_one(i, next_at, next_k, wave); else lv.issue_one(i - lk.N, next_at + C::KV, next_v, wave); };
     const uint32_t k_rows = lds + stage * 2 * C::KV + row_lane, v_rows = k_rows + C::KV, k_cols = lds + stage * 2 * C::KV + column_lane;
     const int first = lo + t * C::BK + kg * 32 * C::NS;
     t = next;
 #pragma unroll
     for (int n = 0; n < C::NS; ++n) {
       const int k0 = first + 32 * n, row0 = (kg * C::NS + n) * 32;
-      if (!__any(span.x < k0 + 32 && span.y > k0)) continue;
-      f32x16 s = row_product<E, C::DP>(k_rows, row0, q), dp = row_product<E, C::DP>(v_rows, row0, d);
-      interleave<2 * T::KS, 4, ROW_READS<E>, PRODUCTS<E>>();
+      f32x16 s, dp;
+      pipeline<2 * T::KS, ROWS_AHEAD<E>, Frag<E>>([&](int i) { return T::rows(i < T::KS ? k_rows : v_rows, row0, i % T::KS); }, [&](int i, const Frag<E>& x) {
+        if (i < T::KS) s = mma(x, q[i], i == 0 ? zeros() : s);
+        else dp = mma(x, d[i - T::KS], i == T::KS ? zeros() : dp);
+#pragma unroll
+        for (int j = i * LOADS / (2 * T::KS); j < (i + 1) * LOADS / (2 * T::KS); ++j) load(n * LOADS + j);
+      });
+      if (!__any(span.x < k0 + 32 && span.y > k0)) continue;   // (not sooner: the loads are every wave's)
       Columns<E, C::DP, 2> columns;
       columns.fetch(k_cols, row0);
       const bool whole = __all(span.x <= k0 && span.y >= k0 + 32);
@@ -162,6 +166,7 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
       add_product<E, C::DP, 2>(dq, columns, ds, whole || all_finite<E, C::DP>(k_rows, row0), seen, k_cols, row0);
     }
   }
+  drain_loads();
   if constexpr (C::KG > 1) {   // the groups' sums; a wave then has 32 of the columns
     __syncthreads();
     float* const part = reinterpret_cast<float*>(smem);                     // [KG][DP][32]
@@ -189,6 +194,57 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
 }
 
 // ------------------------------------------------------------------------------------------------------ dk, dv
+// Tiles of GROUPS groups of rows, one after the other, that have rows which see one of the keys [first, end): their numbers, then -1.
+template <int GROUPS> struct Steps {
+  const int2* range; int groups, first, end, at = 0;
+  uint64_t ahead = 0;                                // which of the 64 tiles before `at` are still to come
+  __device__ __forceinline__ Steps(const Rows& r, int first_, int end_) : range(r.range), groups(r.groups), first(first_), end(end_) {}
+  __device__ __forceinline__ int next(int lane) {
+    while (ahead == 0) {
+      if (at * GROUPS >= groups) return -1;
+      bool any = false;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int group = (at + lane) * GROUPS + g;
+        if (group < groups) { const int2 s = range[group]; any |= s.x < end && s.y > first; }
+      }
+      ahead = __ballot(any);
+      at += 64;
+    }
+    const int bit = __builtin_ctzll(ahead);
+    ahead &= ahead - 1;
+    return at - 64 + bit;
+  }
+};
+template <typename E> __device__ __forceinline__ Source rows_source(const Heads& x, const AttentionArgs& a, int hk, int groups) {
+  const int G = a.Hq / a.Hk;
+  return Source(static_cast<const E*>(x.p) + (int64_t)hk * G * x.hs, ((a.Tq - 1) * x.ld + (G - 1) * x.hs + a.D) * (int64_t)sizeof(E), groups * (GROUP / G) * x.ld * (int64_t)sizeof(E));
+}
+template <typename C> __device__ __forceinline__ void load_records(u32x4 from, uint32_t stage_at, int wave, int lane) {
+#pragma unroll
+  for (int i = 0; i < C::REC_LOADS; ++i) {
+    const uint32_t at = (i * C::WAVES + wave) * 1024;
+    if (at < C::REC) load_to_lds(stage_at + 2 * C::QD + at, at + lane * 16 < C::GROUPS * RECORD ? at + lane * 16 : NOWHERE, from);
+  }
+}
+// Of a subtile's rows, as bits for a lane's registers: those that see the key, and of them those that see another one too: a single key has probability 1, whatever its score,
+// so its ds is zero.
+__device__ __forceinline__ uint2 seen_rows(const uint32_t* rec, int key, int h) {
+  uint2 bits = make_uint2(0, 0);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int at = 8 * q + 4 * h;
+    const u32x4 from = *reinterpret_cast<const u32x4*>(rec + FIRST * GROUP + at), to = *reinterpret_cast<const u32x4*>(rec + END * GROUP + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t bit = key >= (int)from[i] && key < (int)to[i] ? 1u << seen_bit(4 * q + i) : 0;
+      bits.x |= bit;
+      bits.y |= to[i] - from[i] > 1 ? bit : 0;
+    }
+  }
+  return bits;
+}
+
 // Waves work in pairs on the same 32 keys: the first has k in registers, forms the scores and p, and adds up dv; the second has v, forms dp and, with the first one's p
 // through LDS, ds, and adds up dk.  One wave for both needs 300 registers at a width of 128, which leaves one to a SIMD and nothing to do while it waits.
 template <typename E, int DP_, int WK_, int QG_, int NS_>
@@ -210,47 +266,15 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
   const int G = a.Hq / a.Hk, D = a.D, tokens = GROUP / G;
   const int hk = blockIdx.x % a.Hk, k_first = blockIdx.x / a.Hk * C::KEYS;   // the first keys, which most rows of a causal text see, first
   const int key0 = k_first + kw * 32, key = key0 + (lane & 31);
-  // steps of GROUPS groups; which of the next 64 have rows that see one of the workgroup's keys
-  const int steps = (recs.groups + C::GROUPS - 1) / C::GROUPS;
-  int at_step = 0;
-  uint64_t ahead = 0;
-  auto next_step = [&]() {   // the next step, or `steps`
-    while (ahead == 0) {
-      if (at_step >= steps) return steps;
-      bool any = false;
-#pragma unroll
-      for (int g = 0; g < C::GROUPS; ++g) {
-        const int group = (at_step + lane) * C::GROUPS + g;
-        if (group < recs.groups) { const int2 s = recs.range[group]; any |= s.x < k_first + C::KEYS && s.y > k_first; }
-      }
-      ahead = __ballot(any);
-      at_step += 64;
-    }
-    const int bit = __builtin_ctzll(ahead);
-    ahead &= ahead - 1;
-    return at_step - 64 + bit;
-  };
+  Steps<C::GROUPS> step_list(recs, k_first, k_first + C::KEYS);
   Loads<E, C::DP, C::BQ, C::WAVES> lq, ld;
   lq.init(a.q.ld, a.q.hs, G, D, wave, lane);
   ld.init(a.dout.ld, a.dout.hs, G, D, wave, lane);
   const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
-  auto issue = [&](int step, int stage) {
-    const int64_t group = (int64_t)step * C::GROUPS, q0 = group * tokens;
-    const E* const q = static_cast<const E*>(a.q.p) + q0 * a.q.ld + (int64_t)hk * G * a.q.hs;
-    const E* const d = static_cast<const E*>(a.dout.p) + q0 * a.dout.ld + (int64_t)hk * G * a.dout.hs;
-    const u32x4 dq = descriptor(q, ((a.Tq - 1 - q0) * a.q.ld + (G - 1) * a.q.hs + D) * (int64_t)sizeof(E));
-    const u32x4 dd = descriptor(d, ((a.Tq - 1 - q0) * a.dout.ld + (G - 1) * a.dout.hs + D) * (int64_t)sizeof(E));
-    const u32x4 dr = descriptor(recs.record + ((int64_t)hk * recs.groups + group) * (PLANES * GROUP), (recs.groups - group) * RECORD);
-    lq.issue(lds + stage * C::STAGE, dq, wave);
-    ld.issue(lds + stage * C::STAGE + C::QD, dd, wave);
-#pragma unroll
-    for (int i = 0; i < C::REC_LOADS; ++i) {
-      const uint32_t at = (i * C::WAVES + wave) * 1024;
-      if (at < C::REC) load_to_lds(lds + stage * C::STAGE + 2 * C::QD + at, at + lane * 16 < C::GROUPS * RECORD ? at + lane * 16 : NOWHERE, dr);
-    }
-  };
-  int step = next_step();
-  if (step < steps) issue(step, 0);
+  const Source qs = rows_source<E>(a.q, a, hk, C::GROUPS), ds = rows_source<E>(a.dout, a, hk, C::GROUPS);
+  const Source rs(recs.record + (int64_t)hk * recs.groups * (PLANES * GROUP), (int64_t)recs.groups * RECORD, C::GROUPS * RECORD);
+  int step = step_list.next(lane);
+  if (step >= 0) { load_records<C>(rs.tile(step), lds, wave, lane); lq.issue(lds, qs.tile(step), wave); ld.issue(lds + C::QD, ds.tile(step), wave); }
 
   Frag<E> f[T::KS];   // the keys' k, or v
   {
@@ -259,6 +283,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
 #pragma unroll
     for (int ks = 0; ks < T::KS; ++ks) f[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(p + 16 * ks + 8 * h) : zero_fragment<E>();
   }
+  arrived(f);
   const Shape shape(a.scale, a.cap);
   const float c = a.scale * LOG2E;
   float* const shared_p = reinterpret_cast<float*>(smem + C::P) + pair * C::NS * 1024 + lane * 4;
@@ -266,93 +291,82 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
 #pragma unroll
   for (int df = 0; df < T::DF; ++df) sum[df] = zeros();
 
-  for (int stage = 0; step < steps; stage ^= 1) {
-    const int next = next_step();
+  for (int stage = 0; step >= 0; stage ^= 1) {
+    const int next = step_list.next(lane);
     wait_loads();
-    if (next < steps) issue(next, stage ^ 1);
+    const bool more = next >= 0;
+    const u32x4 next_q = more ? qs.tile(next) : Source::nothing(), next_d = more ? ds.tile(next) : Source::nothing();
+    const uint32_t next_at = lds + (stage ^ 1) * C::STAGE;
+    if (more) load_records<C>(rs.tile(next), next_at, wave, lane);
     step = next;
     const uint32_t q_tile = lds + stage * C::STAGE, d_tile = q_tile + C::QD;
     const uint32_t rows = (second ? d_tile : q_tile) + row_lane, other_rows = (second ? q_tile : d_tile) + row_lane, columns_at = (second ? q_tile : d_tile) + column_lane;
     const uint32_t* const recs_at = reinterpret_cast<const uint32_t*>(smem + stage * C::STAGE + 2 * C::QD);
+    auto record = [&](int n) { const int row0 = (qg * C::NS + n) * 32; return recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP; };
     f32x16 s[C::NS];
+    f32x4 stat[C::NS][4];                        // lse, or delta, of the rows that a lane's registers are of
     Frag<E> b[C::NS][2];
+    int first[C::NS], end[C::NS];
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) { first[n] = (int)record(n)[FIRST * GROUP + (lane & 31)]; end[n] = (int)record(n)[END * GROUP + (lane & 31)]; }
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) stat[n][q] = *reinterpret_cast<const f32x4*>(record(n) + (second ? DELTA : LSE) * GROUP + 8 * q + 4 * h);
+    constexpr int STEPS = C::NS * T::KS, LOADS = lq.N + ld.N;
+    pipeline<STEPS, ROWS_AHEAD<E>, Frag<E>>([&](int i) { return T::rows(rows, (qg * C::NS + i / T::KS) * 32, i % T::KS); }, [&](int i, const Frag<E>& x) {
+      s[i / T::KS] = mma(x, f[i % T::KS], i % T::KS == 0 ? zeros() : s[i / T::KS]);
+#pragma unroll
+      for (int j = i * LOADS / STEPS; j < (i + 1) * LOADS / STEPS; ++j) { if (j < lq.N) lq.issue_one(j, next_at, next_q, wave); else ld.issue_one(j - lq.N, next_at + C::QD, next_d, wave); }
+    });
     bool some[C::NS], whole[C::NS];
-    uint32_t seen[C::NS], matters[C::NS];
+    uint32_t seen[C::NS];
 #pragma unroll
     for (int n = 0; n < C::NS; ++n) {
-      const int row0 = (qg * C::NS + n) * 32;
-      const uint32_t* const rec = recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
-      const int first = (int)rec[FIRST * GROUP + (lane & 31)], end = (int)rec[END * GROUP + (lane & 31)];
-      some[n] = __any(first < key0 + 32 && end > key0);
-      whole[n] = __all(first <= key0 && end >= key0 + 32);
-      seen[n] = matters[n] = 0;
-      if (some[n] && !whole[n]) {                // a single key has probability 1, whatever its score: its ds is zero
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int at = 8 * q + 4 * h;
-          const u32x4 from = *reinterpret_cast<const u32x4*>(rec + FIRST * GROUP + at), to = *reinterpret_cast<const u32x4*>(rec + END * GROUP + at);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t bit = key >= (int)from[i] && key < (int)to[i] ? 1u << seen_bit(4 * q + i) : 0;
-            seen[n] |= bit;
-            matters[n] |= to[i] - from[i] > 1 ? bit : 0;
-          }
-        }
-      }
+      some[n] = __any(first[n] < key0 + 32 && end[n] > key0);
+      whole[n] = __all(first[n] <= key0 && end[n] >= key0 + 32);
+      seen[n] = 0;
     }
+    auto mask = [&](int n) {
+      const uint2 bits = seen_rows(record(n), key, h);
+      seen[n] = bits.x;
 #pragma unroll
-    for (int n = 0; n < C::NS; ++n) {
-      if (some[n]) {
-        s[n] = row_product<E, C::DP>(rows, (qg * C::NS + n) * 32, f);
-        interleave<T::KS, 4, ROW_READS<E>, PRODUCTS<E>>();
-      }
-    }
+      for (int r = 0; r < 16; ++r) s[n][r] = where_seen(second ? bits.y : bits.x, r, s[n][r], 0.f);
+    };
     if (!second) {
 #pragma unroll
       for (int n = 0; n < C::NS; ++n) {
-        if (!some[n]) continue;
-        const int row0 = (qg * C::NS + n) * 32;
-        const uint32_t* const rec = recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int at = 8 * q + 4 * h;
-          const f32x4 lse = *reinterpret_cast<const f32x4*>(rec + LSE * GROUP + at);
           f32x4 slope = {}, bent; u32x4 place = {};
-          if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(rec + SLOPE * GROUP + at); place = *reinterpret_cast<const u32x4*>(rec + AT * GROUP + at); }
+          if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(record(n) + SLOPE * GROUP + 8 * q + 4 * h); place = *reinterpret_cast<const u32x4*>(record(n) + AT * GROUP + 8 * q + 4 * h); }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int r = 4 * q + i;
             float bend = 1.f, x = s[n][r] * c;
             if (SHAPED) x = shape.score<E>(s[n][r], slope[i], fabsf((float)((int)place[i] - key)), bend);
-            s[n][r] = __builtin_amdgcn_exp2f(x - lse[i]);
+            s[n][r] = __builtin_amdgcn_exp2f(x - stat[n][q][i]);
             bent[i] = SHAPED ? s[n][r] * bend : s[n][r];
           }
           *reinterpret_cast<f32x4*>(shared_p + n * 1024 + q * 256) = bent;
         }
-        if (!whole[n]) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[n][r] = where_seen(seen[n], r, s[n][r], 0.f);
-        }
+        if (!whole[n]) mask(n);
         b[n][0] = fragment<E>(s[n], 0); b[n][1] = fragment<E>(s[n], 1);
       }
     }
     __syncthreads();
     if (second) {
+      f32x4 p[C::NS][4];
+#pragma unroll
+      for (int n = 0; n < C::NS; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p[n][q] = *reinterpret_cast<const f32x4*>(shared_p + n * 1024 + q * 256);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4 * C::NS, 0);   // all of them are on their way before the first is waited for
 #pragma unroll
       for (int n = 0; n < C::NS; ++n) {
-        if (!some[n]) continue;
-        const int row0 = (qg * C::NS + n) * 32;
-        const uint32_t* const rec = recs_at + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 delta = *reinterpret_cast<const f32x4*>(rec + DELTA * GROUP + 8 * q + 4 * h), p = *reinterpret_cast<const f32x4*>(shared_p + n * 1024 + q * 256);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { const int r = 4 * q + i; s[n][r] = p[i] * (s[n][r] - delta[i]); }
-        }
-        if (!whole[n]) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[n][r] = where_seen(matters[n], r, s[n][r], 0.f);
-        }
+        for (int r = 0; r < 16; ++r) s[n][r] = p[n][r >> 2][r & 3] * (s[n][r] - stat[n][r >> 2][r & 3]);
+        if (!whole[n]) mask(n);
         b[n][0] = fragment<E>(s[n], 0); b[n][1] = fragment<E>(s[n], 1);
       }
     }
@@ -373,6 +387,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
       }
     }
   }
+  drain_loads();
   if constexpr (C::QG > 1) {   // the row groups' sums; a wave then has some of the columns
     float* const part = reinterpret_cast<float*>(smem) + (second ? C::QG * C::DP * 32 : 0);                     // [QG][DP][32]
     __syncthreads();
@@ -408,7 +423,140 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
   for (int df = 0; df < T::DF; ++df) if (C::QG == 1 || df % C::QG == qg) store_columns<E>(to, df, D, sum[df], second ? a.scale : 1.f, h);
 }
 
-constexpr int64_t MANY = 256;
+// The same with one wave for both, where its registers are enough for two waves to a SIMD (bf16, widths up to 64): one barrier a tile instead of two, and nothing to hand over.
+template <typename E, int DP_, int WK_, int QG_, int NS_>
+struct OneConfig {
+  static constexpr int DP = DP_, WK = WK_, QG = QG_, NS = NS_;
+  static constexpr int WAVES = WK * QG, THREADS = WAVES * 64, KEYS = 32 * WK, BQ = 32 * NS * QG, GROUPS = BQ / GROUP;
+  static constexpr int QD = BQ * DP * (int)sizeof(E), REC = (GROUPS * RECORD + 1023) / 1024 * 1024, STAGE = 2 * QD + REC, LDS = 2 * STAGE;
+  static constexpr int REC_LOADS = (REC / 1024 + WAVES - 1) / WAVES;
+  static_assert(BQ % GROUP == 0 && LDS <= LDS_MAX && WK * QG * DP * 32 * 4 <= LDS, "LDS");
+};
+template <typename E, typename C, bool SHAPED>
+__global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionArgs a, Rows recs) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  typedef Tile<E, C::DP> T;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int kw = wave / C::QG, qg = wave % C::QG;
+  const int G = a.Hq / a.Hk, D = a.D, tokens = GROUP / G;
+  const int hk = blockIdx.x % a.Hk, k_first = blockIdx.x / a.Hk * C::KEYS;
+  const int key0 = k_first + kw * 32, key = key0 + (lane & 31);
+  Steps<C::GROUPS> step_list(recs, k_first, k_first + C::KEYS);
+  Loads<E, C::DP, C::BQ, C::WAVES> lq, ld;
+  lq.init(a.q.ld, a.q.hs, G, D, wave, lane);
+  ld.init(a.dout.ld, a.dout.hs, G, D, wave, lane);
+  const uint32_t lds = lds_address(smem), row_lane = T::row_lane(lane), column_lane = T::column_lane(lane);
+  const Source qs = rows_source<E>(a.q, a, hk, C::GROUPS), ds = rows_source<E>(a.dout, a, hk, C::GROUPS);
+  const Source rs(recs.record + (int64_t)hk * recs.groups * (PLANES * GROUP), (int64_t)recs.groups * RECORD, C::GROUPS * RECORD);
+  int step = step_list.next(lane);
+  if (step >= 0) { load_records<C>(rs.tile(step), lds, wave, lane); lq.issue(lds, qs.tile(step), wave); ld.issue(lds + C::QD, ds.tile(step), wave); }
+
+  Frag<E> k[T::KS], v[T::KS];
+  {
+    const int64_t from = min((int64_t)key, a.Tk - 1);
+    const E* const kp = static_cast<const E*>(a.k.p) + from * a.k.ld + hk * a.k.hs;
+    const E* const vp = static_cast<const E*>(a.v.p) + from * a.v.ld + hk * a.v.hs;
+#pragma unroll
+    for (int ks = 0; ks < T::KS; ++ks) {
+      k[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(kp + 16 * ks + 8 * h) : zero_fragment<E>();
+      v[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(vp + 16 * ks + 8 * h) : zero_fragment<E>();
+    }
+  }
+  arrived(k); arrived(v);
+  const Shape shape(a.scale, a.cap);
+  const float c = a.scale * LOG2E;
+  f32x16 dk[T::DF], dv[T::DF];
+#pragma unroll
+  for (int df = 0; df < T::DF; ++df) { dk[df] = zeros(); dv[df] = zeros(); }
+
+  for (int stage = 0; step >= 0; stage ^= 1) {
+    const int next = step_list.next(lane);
+    wait_loads();
+    const bool more = next >= 0;
+    const u32x4 next_q = more ? qs.tile(next) : Source::nothing(), next_d = more ? ds.tile(next) : Source::nothing();
+    const uint32_t next_at = lds + (stage ^ 1) * C::STAGE;
+    if (more) load_records<C>(rs.tile(next), next_at, wave, lane);
+    step = next;
+    const uint32_t q_rows = lds + stage * C::STAGE + row_lane, q_cols = lds + stage * C::STAGE + column_lane, d_rows = q_rows + C::QD, d_cols = q_cols + C::QD;
+    constexpr int LOADS = (lq.N + ld.N) / C::NS;   // in each subtile
+    auto load = [&](int j) { if (j < lq.N) lq.issue_one(j, next_at, next_q, wave); else ld.issue_one(j - lq.N, next_at + C::QD, next_d, wave); };
+#pragma unroll
+    for (int n = 0; n < C::NS; ++n) {
+      const int row0 = (qg * C::NS + n) * 32;
+      const uint32_t* const rec = reinterpret_cast<const uint32_t*>(smem + stage * C::STAGE + 2 * C::QD) + row0 / GROUP * (PLANES * GROUP) + row0 % GROUP;
+      const int first = (int)rec[FIRST * GROUP + (lane & 31)], end = (int)rec[END * GROUP + (lane & 31)];
+      f32x16 s, dp;
+      pipeline<2 * T::KS, ROWS_AHEAD<E>, Frag<E>>([&](int i) { return T::rows(i < T::KS ? q_rows : d_rows, row0, i % T::KS); }, [&](int i, const Frag<E>& x) {
+        if (i < T::KS) s = mma(x, k[i], i == 0 ? zeros() : s);
+        else dp = mma(x, v[i - T::KS], i == T::KS ? zeros() : dp);
+#pragma unroll
+        for (int j = i * LOADS / (2 * T::KS); j < (i + 1) * LOADS / (2 * T::KS); ++j) load(n * LOADS + j);
+      });
+      if (!__any(first < key0 + 32 && end > key0)) continue;   // (not sooner: the loads are every wave's)
+      const bool whole = __all(first <= key0 && end >= key0 + 32);
+      Columns<E, C::DP, 2> columns;
+      columns.fetch(d_cols, row0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = 8 * q + 4 * h;
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(rec + LSE * GROUP + at), delta = *reinterpret_cast<const f32x4*>(rec + DELTA * GROUP + at);
+        f32x4 slope = {}; u32x4 place = {};
+        if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(rec + SLOPE * GROUP + at); place = *reinterpret_cast<const u32x4*>(rec + AT * GROUP + at); }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * q + i;
+          float bend = 1.f, x = s[r] * c;
+          if (SHAPED) x = shape.score<E>(s[r], slope[i], fabsf((float)((int)place[i] - key)), bend);
+          s[r] = __builtin_amdgcn_exp2f(x - lse[i]);
+          dp[r] = SHAPED ? s[r] * (dp[r] - delta[i]) * bend : s[r] * (dp[r] - delta[i]);
+        }
+      }
+      uint32_t seen = 0;
+      if (!whole) {
+        const uint2 bits = seen_rows(rec, key, h);
+        seen = bits.x;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) { s[r] = where_seen(bits.x, r, s[r], 0.f); dp[r] = where_seen(bits.y, r, dp[r], 0.f); }
+      }
+      Frag<E> p[2] = {fragment<E>(s, 0), fragment<E>(s, 1)}, w[2] = {fragment<E>(dp, 0), fragment<E>(dp, 1)};
+      Columns<E, C::DP, 2> q_columns;
+      q_columns.fetch(q_cols, row0);
+      add_product<E, C::DP, 2>(dv, columns, p, whole || all_finite<E, C::DP>(d_rows, row0), seen, d_cols, row0);
+      add_product<E, C::DP, 2>(dk, q_columns, w, whole || all_finite<E, C::DP>(q_rows, row0), seen, q_cols, row0);
+    }
+  }
+  drain_loads();
+  auto finish = [&](f32x16 (&x)[T::DF], const Heads& out, float factor) {
+    if constexpr (C::QG > 1) {   // the row groups' sums; a wave then has some of the columns
+      float* const part = reinterpret_cast<float*>(smem) + kw * C::QG * C::DP * 32;                     // [QG][DP][32]
+      __syncthreads();
+#pragma unroll
+      for (int df = 0; df < T::DF; ++df)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[(qg * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)] = x[df][r];
+      __syncthreads();
+#pragma unroll
+      for (int df = 0; df < T::DF; ++df) {
+        if (df % C::QG != qg) continue;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float sum = 0.f;
+#pragma unroll
+          for (int g = 0; g < C::QG; ++g) sum += part[(g * C::DP + 32 * df + register_row(r, h)) * 32 + (lane & 31)];
+          x[df][r] = sum;
+        }
+      }
+    }
+    if (key >= a.Tk) return;
+    E* const to = const_cast<E*>(static_cast<const E*>(out.p)) + (int64_t)key * out.ld + hk * out.hs;
+#pragma unroll
+    for (int df = 0; df < T::DF; ++df) if (C::QG == 1 || df % C::QG == qg) store_columns<E>(to, df, D, x[df], factor, h);
+  };
+  finish(dk, a.dk, a.scale);
+  finish(dv, a.dv, 1.f);
+}
+
+constexpr int64_t FILLED = 512;   // see attention.hip
 
 template <auto KERNEL, typename C, typename... A>
 void launch(ProfScope& ps, int64_t blocks, hipStream_t st, A... a) {
@@ -425,7 +573,7 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
   const int64_t count = a.Tq * (a.Hq / a.Hk);
   if (a.Tq > 0) launch_kernel(ps, k_attention_delta<E>, dim3((unsigned)((int64_t)rows.groups * a.Hk)), 256, 0, st, a, rows);
   if (a.Tq == 0) {
-  } else if ((count + 127) / 128 * a.Hk >= MANY) {
+  } else if ((count + 127) / 128 * a.Hk >= FILLED) {
     typedef QConfig<E, DP, 4> C;
     launch<&k_attention_dq<E, C, SHAPED>, C>(ps, (count + 127) / 128 * a.Hk, st, a, rows, (int)((count + 127) / 128));
   } else {
@@ -433,17 +581,25 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
     launch<&k_attention_dq<E, C, SHAPED>, C>(ps, (count + 31) / 32 * a.Hk, st, a, rows, (int)((count + 31) / 32));
   }
   if (a.Tk == 0) return;
-  auto dkv = [&](auto config) {
+  auto pairs = [&](auto config) {
     typedef decltype(config) C;
     launch<&k_attention_dkv<E, C, SHAPED>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
   };
-  if constexpr (sizeof(E) * DP > 256) {
-    if ((a.Tk + 63) / 64 * a.Hk >= MANY) dkv(KConfig<E, DP, 2, 2, 1>{});
-    else dkv(KConfig<E, DP, 1, 2, 1>{});
+  auto ones = [&](auto config) {
+    typedef decltype(config) C;
+    launch<&k_attention_dkv_one<E, C, SHAPED>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
+  };
+  const int64_t blocks = (a.Tk + 127) / 128 * a.Hk;   // of 128 keys
+  if constexpr (sizeof(E) * DP <= 128) {
+    if (blocks >= 1024) ones(OneConfig<E, DP, 4, 1, 2>{});
+    else ones(OneConfig<E, DP, 1, 4, 1>{});
+  } else if constexpr (sizeof(E) * DP <= 256) {
+    if (blocks >= 512) pairs(KConfig<E, DP, 4, 1, 2>{});
+    else if (2 * blocks >= 256) pairs(KConfig<E, DP, 2, 2, 1>{});
+    else pairs(KConfig<E, DP, 1, 4, 1>{});
   } else {
-    if ((a.Tk + 127) / 128 * a.Hk >= 2 * MANY) dkv(KConfig<E, DP, 4, 1, 2>{});
-    else if ((a.Tk + 63) / 64 * a.Hk >= MANY) dkv(KConfig<E, DP, 2, 2, 1>{});
-    else dkv(KConfig<E, DP, 1, 4, 1>{});
+    if (2 * blocks >= 256) pairs(KConfig<E, DP, 2, 2, 1>{});
+    else pairs(KConfig<E, DP, 1, 2, 1>{});
   }
 }
 template <typename E, int DP>

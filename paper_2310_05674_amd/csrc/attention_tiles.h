@@ -61,6 +61,11 @@ template <typename E> __device__ __forceinline__ Frag<E> load_fragment(const E* 
   if constexpr (sizeof(E) == 2) return *reinterpret_cast<const bf16x8*>(p);
   else { const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4); return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 }
+// Waits here for fragments from global memory.  Left to the compiler the wait is where they are first used, inside the loop, and there it would be for the loads of the next tile as well.
+template <typename F, int N> __device__ __forceinline__ void arrived(F (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
 __device__ __forceinline__ int register_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
 // Tiles in LDS: rows of DP values, their 16-byte pieces permuted within the row so that both fetches fill all banks: sixteen rows at the same piece, and four
@@ -113,11 +118,15 @@ template <typename E, int DP> struct Tile {
 // Loads go from memory straight to LDS, 1 KB a wave and instruction, through buffer descriptors that begin at the tile's first row: what lies behind the last row
 // or the row's last value reads as zero, and offsets stay below 2^31.
 constexpr uint32_t NOWHERE = 0x80000000u, MOST = 0x7fffffffu;
-__device__ __forceinline__ u32x4 descriptor(const void* p, int64_t left) {
-  const uint64_t at = (uint64_t)(uintptr_t)p;
-  auto uniform = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-  return (u32x4){uniform((uint32_t)at), uniform((uint32_t)(at >> 32)), uniform(left <= 0 ? 0u : left > (int64_t)MOST ? MOST : (uint32_t)left), 0x00020000u};
-}
+struct Source {   // tiles of `step` bytes each, from `at` on
+  uint64_t at, left; uint32_t step;
+  __device__ __forceinline__ Source(const void* p, int64_t bytes, int64_t step_) : at((uint64_t)(uintptr_t)p), left((uint64_t)bytes), step((uint32_t)step_) {}
+  __device__ __forceinline__ u32x4 tile(uint32_t t) const {
+    const uint64_t off = (uint64_t)t * step, from = at + off, rest = left - off;
+    return (u32x4){(uint32_t)from, (uint32_t)(from >> 32), rest > MOST ? MOST : (uint32_t)rest, 0x00020000u};
+  }
+  static __device__ __forceinline__ u32x4 nothing() { return (u32x4){0, 0, 0, 0x00020000u}; }   // reads as zero
+};
 __device__ __forceinline__ void load_to_lds(uint32_t to, uint32_t offset, u32x4 from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "memory", "m0");
 }
@@ -139,11 +148,14 @@ template <typename E, int DP, int ROWS, int WAVES> struct Loads {
       offset[q] = (G == 1 || in < tokens * G) && piece * 16 < D * (int)sizeof(E) ? row * (uint32_t)sizeof(E) + piece * 16 : NOWHERE;
     }
   }
+  __device__ __forceinline__ void issue_one(int q, uint32_t lds, u32x4 from, int wave) const { load_to_lds(lds + (q * WAVES + wave) * 1024, offset[q], from); }
   __device__ __forceinline__ void issue(uint32_t lds, u32x4 from, int wave) const {
 #pragma unroll
-    for (int q = 0; q < N; ++q) load_to_lds(lds + (q * WAVES + wave) * 1024, offset[q], from);
+    for (int q = 0; q < N; ++q) issue_one(q, lds, from, wave);
   }
 };
+// nothing is on its way to LDS any more: before a wave ends, or uses LDS for something else
+__device__ __forceinline__ void drain_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // everything a wave has asked for is in LDS, for all of them
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -171,20 +183,21 @@ struct Shape {
   }
 };
 
-// The order of a block of `FRAGMENTS` fetches and products, left to itself the compiler waits for each fragment right after asking for it: AHEAD fragments first, then a
-// product for each further one.  READS and PRODUCTS: instructions of a fragment.
-template <int FRAGMENTS, int AHEAD, int READS, int PRODUCTS>
-__device__ __forceinline__ void interleave() {
-  constexpr int FIRST = AHEAD < FRAGMENTS ? AHEAD : FRAGMENTS;
-  __builtin_amdgcn_sched_group_barrier(0x100, FIRST * READS, 0);
+// A run of TOTAL fetches, each used by use(i, fragment) AHEAD steps later.  Left to itself the compiler waits for each fragment right after asking for it.  What else a step does, such
+// as a load of the next tile, which takes 90 clocks when several are issued at once, is spread over the run by use().
+template <int TOTAL, int AHEAD_, typename F, typename Fetch, typename Use>
+__device__ __forceinline__ void pipeline(Fetch fetch, Use use) {
+  constexpr int AHEAD = AHEAD_ < TOTAL ? AHEAD_ : TOTAL;
+  F x[AHEAD];
 #pragma unroll
-  for (int i = 0; i < FRAGMENTS; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS, 0);
-    if (i + FIRST < FRAGMENTS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  for (int i = 0; i < AHEAD; ++i) x[i] = fetch(i);
+#pragma unroll
+  for (int i = 0; i < TOTAL; ++i) {
+    use(i, x[i % AHEAD]);
+    if (i + AHEAD < TOTAL) x[i % AHEAD] = fetch(i + AHEAD);
   }
 }
-template <typename E> constexpr int ROW_READS = sizeof(E) == 2 ? 1 : 2;
-template <typename E> constexpr int PRODUCTS = sizeof(E) == 2 ? 1 : 8;
+template <typename E> constexpr int ROWS_AHEAD = sizeof(E) == 2 ? 4 : 2;
 
 // The keys of a subtile of 32 that a lane sees, as bits, for its registers: bit 8 (r / 4) + r % 4 is register r's.
 __device__ __forceinline__ uint32_t seen_keys(int2 span, int k0, int h) {
@@ -199,14 +212,6 @@ __device__ __forceinline__ float where_seen(uint32_t seen, int r, float x, float
   return __uint_as_float((__float_as_uint(x) & m) | (__float_as_uint(other) & ~m));
 }
 
-// the products of a tile's rows row0 .. with the fragments b of a row each
-template <typename E, int DP>
-__device__ __forceinline__ f32x16 row_product(uint32_t tile, int row0, const Frag<E> (&b)[DP / 16]) {
-  f32x16 x = zeros();
-#pragma unroll
-  for (int ks = 0; ks < DP / 16; ++ks) x = mma(Tile<E, DP>::rows(tile, row0, ks), b[ks], x);
-  return x;
-}
 // acc[df] += (columns 32 df .. of 16 N of a tile's rows)^T times the N fragments b.  The columns are fetched ahead of the arithmetic that makes b.
 //
 // Where some of a lane's weights are zero because it does not see the row (its bit of `seen` clear): zero times infinity or NaN is NaN, so a row that is not finite
