@@ -24,7 +24,7 @@ struct Config {
 
 struct Parts { float* o; float* lse; int count; };   // of split keys: [count][Hk][rows][D] and [count][Hk][rows]
 
-template <typename E, typename C, bool SHAPED>
+template <typename E, typename C, int SHAPE>
 __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionArgs a, Parts parts, int tiles) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
@@ -70,10 +70,10 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
     for (int ks = 0; ks < T::KS; ++ks) q[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(p + 16 * ks + 8 * h) : zero_fragment<E>();
   }
   arrived(q);
-  const Shape shape(a.scale, a.cap);
-  const float slope = SHAPED && a.slopes != nullptr ? a.slopes[head] * LOG2E : 0.f;
-  const int at = SHAPED && a.slopes != nullptr ? (a.at != nullptr ? a.at[query] : query) : 0;
-  const float c = SHAPED ? 1.f : a.scale * LOG2E;
+  const Scores<E, SHAPE> score(a.scale, a.cap);
+  const float slope = SHAPE & BIASED ? a.slopes[head] * LOG2E : 0.f;
+  const int at = SHAPE & BIASED ? (a.at != nullptr ? a.at[query] : query) : 0;
+  const float c = SHAPE != PLAIN ? 1.f : a.scale * LOG2E;
   f32x16 o[T::DF];
 #pragma unroll
   for (int df = 0; df < T::DF; ++df) o[df] = zeros();
@@ -100,12 +100,12 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
     constexpr int AHEAD = C::DP * sizeof(E) > 128 ? 1 : 2;   // sets of columns: 16 registers or 32 in bf16
     Columns<E, C::DP, 2> columns[AHEAD];
     columns[0].fetch(v_cols, kg * C::NS * 32);
-    if (SHAPED) {
-      const int away = at - k0 - 4 * h;
+    if (SHAPE != PLAIN) {
+      const float away = (float)(at - k0 - 4 * h);
 #pragma unroll
       for (int n = 0; n < C::NS; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) { float bend; s[n][r] = shape.score<E>(s[n][r], slope, fabsf((float)(away - 32 * n - 8 * (r >> 2) - (r & 3))), bend); }
+        for (int r = 0; r < 16; ++r) { float bend; s[n][r] = score(s[n][r], slope, away - (float)(32 * n + 8 * (r >> 2) + (r & 3)), bend); }
     }
     const bool whole = __all(span.x <= k0 && span.y >= k0 + 32 * C::NS);
     uint32_t seen[C::NS] = {};
@@ -274,10 +274,10 @@ Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk) {
   return p;
 }
 
-template <typename E, typename C, bool SHAPED>
+template <typename E, typename C, int SHAPE>
 void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspace) {
   static const bool once = [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attention<E, C, SHAPED>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attention<E, C, SHAPE>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
     return true;
   }();
   (void)once;
@@ -285,16 +285,20 @@ void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspa
   Parts parts{static_cast<float*>(workspace), nullptr, p.parts};
   parts.lse = parts.o + (size_t)p.parts * a.Hk * rows * a.D;
   ProfScope ps(st, F_OTHER, 0.0);
-  launch_kernel(ps, k_attention<E, C, SHAPED>, dim3((unsigned)(p.tiles * (int64_t)a.Hk), p.parts), C::THREADS, C::LDS, st, a, parts, p.tiles);
+  launch_kernel(ps, k_attention<E, C, SHAPE>, dim3((unsigned)(p.tiles * (int64_t)a.Hk), p.parts), C::THREADS, C::LDS, st, a, parts, p.tiles);
   if (p.parts > 1) launch_kernel(ps, k_attention_join<E>, dim3((unsigned)(rows * a.Hk)), 256, 0, st, a, parts);
 }
 template <typename E, int DP>
 void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
   const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk);
-  const bool shaped = a.cap > 0.f || a.slopes != nullptr;
   auto run = [&](auto config) {
     typedef decltype(config) C;
-    shaped ? launch<E, C, true>(st, a, p, workspace) : launch<E, C, false>(st, a, p, workspace);
+    switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes != nullptr ? BIASED : 0)) {
+      case PLAIN: return launch<E, C, PLAIN>(st, a, p, workspace);
+      case CAPPED: return launch<E, C, CAPPED>(st, a, p, workspace);
+      case BIASED: return launch<E, C, BIASED>(st, a, p, workspace);
+      default: return launch<E, C, CAPPED | BIASED>(st, a, p, workspace);
+    }
   };
   constexpr bool WIDE_ROWS = sizeof(E) * DP > 256;
   if (p.few) run(Config<E, DP, 1, WIDE_ROWS ? 2 : 4, 1>{});

@@ -69,7 +69,7 @@ struct QConfig {
   static constexpr int PER_EU = sizeof(E) * DP <= 256 ? 2 : 1;
   static_assert(LDS <= LDS_MAX && KG * DP * 32 * 4 <= LDS, "LDS");
 };
-template <typename E, typename C, bool SHAPED>
+template <typename E, typename C, int SHAPE>
 __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(AttentionArgs a, Rows recs, int tiles) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
@@ -114,11 +114,10 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
   }
   const uint32_t* const rec = recs.record + ((int64_t)hk * recs.groups + query / tokens) * (PLANES * GROUP) + query % tokens * G + in;
   const float lse = __uint_as_float(rec[LSE * GROUP]), delta = __uint_as_float(rec[DELTA * GROUP]);
-  const float slope = SHAPED ? __uint_as_float(rec[SLOPE * GROUP]) : 0.f;
-  const int at = SHAPED ? (int)rec[AT * GROUP] : 0;
+  const float slope = SHAPE & BIASED ? __uint_as_float(rec[SLOPE * GROUP]) : 0.f;
+  const int at = SHAPE & BIASED ? (int)rec[AT * GROUP] : 0;
   arrived(q); arrived(d);
-  const Shape shape(a.scale, a.cap);
-  const float c = a.scale * LOG2E;
+  const Scores<E, SHAPE> score(a.scale, a.cap);
   f32x16 dq[T::DF];
 #pragma unroll
   for (int df = 0; df < T::DF; ++df) dq[df] = zeros();
@@ -147,14 +146,14 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
       Columns<E, C::DP, 2> columns;
       columns.fetch(k_cols, row0);
       const bool whole = __all(span.x <= k0 && span.y >= k0 + 32);
-      const int away = at - k0 - 4 * h;
+      const float away = (float)(at - k0 - 4 * h);
       uint32_t seen = 0;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        float bend = 1.f, x = s[r] * c;
-        if (SHAPED) x = shape.score<E>(s[r], slope, fabsf((float)(away - 8 * (r >> 2) - (r & 3))), bend);
+        float bend = 1.f;
+        const float x = score(s[r], slope, away - (float)(8 * (r >> 2) + (r & 3)), bend);
         const float p = __builtin_amdgcn_exp2f(x - lse);
-        s[r] = SHAPED ? p * (dp[r] - delta) * bend : p * (dp[r] - delta);
+        s[r] = SHAPE & CAPPED ? p * (dp[r] - delta) * bend : p * (dp[r] - delta);
       }
       if (!whole) {
         seen = seen_keys(span, k0, h);
@@ -256,7 +255,7 @@ struct KConfig {
   static constexpr int REC_LOADS = (REC / 1024 + WAVES - 1) / WAVES;
   static_assert(BQ % GROUP == 0 && LDS <= LDS_MAX && 2 * QG * DP * 32 * 4 <= LDS, "LDS");
 };
-template <typename E, typename C, bool SHAPED>
+template <typename E, typename C, int SHAPE>
 __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a, Rows recs) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
@@ -284,8 +283,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
     for (int ks = 0; ks < T::KS; ++ks) f[ks] = 16 * ks + 8 * h < D ? load_fragment<E>(p + 16 * ks + 8 * h) : zero_fragment<E>();
   }
   arrived(f);
-  const Shape shape(a.scale, a.cap);
-  const float c = a.scale * LOG2E;
+  const Scores<E, SHAPE> score(a.scale, a.cap);
   float* const shared_p = reinterpret_cast<float*>(smem + C::P) + pair * C::NS * 1024 + lane * 4;
   f32x16 sum[T::DF];   // dv, or dk
 #pragma unroll
@@ -339,14 +337,14 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv(AttentionArgs a
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           f32x4 slope = {}, bent; u32x4 place = {};
-          if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(record(n) + SLOPE * GROUP + 8 * q + 4 * h); place = *reinterpret_cast<const u32x4*>(record(n) + AT * GROUP + 8 * q + 4 * h); }
+          if (SHAPE & BIASED) { slope = *reinterpret_cast<const f32x4*>(record(n) + SLOPE * GROUP + 8 * q + 4 * h); place = *reinterpret_cast<const u32x4*>(record(n) + AT * GROUP + 8 * q + 4 * h); }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int r = 4 * q + i;
-            float bend = 1.f, x = s[n][r] * c;
-            if (SHAPED) x = shape.score<E>(s[n][r], slope[i], fabsf((float)((int)place[i] - key)), bend);
+            float bend = 1.f;
+            const float x = score(s[n][r], slope[i], (float)((int)place[i] - key), bend);
             s[n][r] = __builtin_amdgcn_exp2f(x - stat[n][q][i]);
-            bent[i] = SHAPED ? s[n][r] * bend : s[n][r];
+            bent[i] = SHAPE & CAPPED ? s[n][r] * bend : s[n][r];
           }
           *reinterpret_cast<f32x4*>(shared_p + n * 1024 + q * 256) = bent;
         }
@@ -432,7 +430,7 @@ struct OneConfig {
   static constexpr int REC_LOADS = (REC / 1024 + WAVES - 1) / WAVES;
   static_assert(BQ % GROUP == 0 && LDS <= LDS_MAX && WK * QG * DP * 32 * 4 <= LDS, "LDS");
 };
-template <typename E, typename C, bool SHAPED>
+template <typename E, typename C, int SHAPE>
 __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionArgs a, Rows recs) {
   extern __shared__ __align__(1024) unsigned char smem[];
   typedef Tile<E, C::DP> T;
@@ -463,8 +461,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionAr
     }
   }
   arrived(k); arrived(v);
-  const Shape shape(a.scale, a.cap);
-  const float c = a.scale * LOG2E;
+  const Scores<E, SHAPE> score(a.scale, a.cap);
   f32x16 dk[T::DF], dv[T::DF];
 #pragma unroll
   for (int df = 0; df < T::DF; ++df) { dk[df] = zeros(); dv[df] = zeros(); }
@@ -501,14 +498,14 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionAr
         const int at = 8 * q + 4 * h;
         const f32x4 lse = *reinterpret_cast<const f32x4*>(rec + LSE * GROUP + at), delta = *reinterpret_cast<const f32x4*>(rec + DELTA * GROUP + at);
         f32x4 slope = {}; u32x4 place = {};
-        if (SHAPED) { slope = *reinterpret_cast<const f32x4*>(rec + SLOPE * GROUP + at); place = *reinterpret_cast<const u32x4*>(rec + AT * GROUP + at); }
+        if (SHAPE & BIASED) { slope = *reinterpret_cast<const f32x4*>(rec + SLOPE * GROUP + at); place = *reinterpret_cast<const u32x4*>(rec + AT * GROUP + at); }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * q + i;
-          float bend = 1.f, x = s[r] * c;
-          if (SHAPED) x = shape.score<E>(s[r], slope[i], fabsf((float)((int)place[i] - key)), bend);
+          float bend = 1.f;
+          const float x = score(s[r], slope[i], (float)((int)place[i] - key), bend);
           s[r] = __builtin_amdgcn_exp2f(x - lse[i]);
-          dp[r] = SHAPED ? s[r] * (dp[r] - delta[i]) * bend : s[r] * (dp[r] - delta[i]);
+          dp[r] = SHAPE & CAPPED ? s[r] * (dp[r] - delta[i]) * bend : s[r] * (dp[r] - delta[i]);
         }
       }
       uint32_t seen = 0;
@@ -567,7 +564,7 @@ void launch(ProfScope& ps, int64_t blocks, hipStream_t st, A... a) {
   (void)once;
   launch_kernel(ps, KERNEL, dim3((unsigned)blocks), C::THREADS, C::LDS, st, a...);
 }
-template <typename E, int DP, bool SHAPED>
+template <typename E, int DP, int SHAPE>
 void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
   ProfScope ps(st, F_OTHER, 0.0);
   const int64_t count = a.Tq * (a.Hq / a.Hk);
@@ -575,19 +572,19 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
   if (a.Tq == 0) {
   } else if ((count + 127) / 128 * a.Hk >= FILLED) {
     typedef QConfig<E, DP, 4> C;
-    launch<&k_attention_dq<E, C, SHAPED>, C>(ps, (count + 127) / 128 * a.Hk, st, a, rows, (int)((count + 127) / 128));
+    launch<&k_attention_dq<E, C, SHAPE>, C>(ps, (count + 127) / 128 * a.Hk, st, a, rows, (int)((count + 127) / 128));
   } else {
     typedef QConfig<E, DP, 1> C;
-    launch<&k_attention_dq<E, C, SHAPED>, C>(ps, (count + 31) / 32 * a.Hk, st, a, rows, (int)((count + 31) / 32));
+    launch<&k_attention_dq<E, C, SHAPE>, C>(ps, (count + 31) / 32 * a.Hk, st, a, rows, (int)((count + 31) / 32));
   }
   if (a.Tk == 0) return;
   auto pairs = [&](auto config) {
     typedef decltype(config) C;
-    launch<&k_attention_dkv<E, C, SHAPED>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
+    launch<&k_attention_dkv<E, C, SHAPE>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
   };
   auto ones = [&](auto config) {
     typedef decltype(config) C;
-    launch<&k_attention_dkv_one<E, C, SHAPED>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
+    launch<&k_attention_dkv_one<E, C, SHAPE>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
   };
   const int64_t blocks = (a.Tk + 127) / 128 * a.Hk;   // of 128 keys
   if constexpr (sizeof(E) * DP <= 128) {
@@ -604,8 +601,12 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
 }
 template <typename E, int DP>
 void launch_width(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
-  if (a.cap > 0.f || a.slopes != nullptr) launch_all<E, DP, true>(st, a, rows);
-  else launch_all<E, DP, false>(st, a, rows);
+  switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes != nullptr ? BIASED : 0)) {
+    case PLAIN: return launch_all<E, DP, PLAIN>(st, a, rows);
+    case CAPPED: return launch_all<E, DP, CAPPED>(st, a, rows);
+    case BIASED: return launch_all<E, DP, BIASED>(st, a, rows);
+    default: return launch_all<E, DP, CAPPED | BIASED>(st, a, rows);
+  }
 }
 int64_t groups_of(int64_t Tq, int G) { const int64_t tokens = GROUP / G; return (Tq + tokens - 1) / tokens; }
 }  // namespace

@@ -162,24 +162,28 @@ __device__ __forceinline__ void wait_loads() {
   __syncthreads();
 }
 
-// Scores in units of log 2: with `shaped`, cap tanh(scale s / cap) - slope |at - key|, else the factor alone.
-struct Shape {
-  float scale, cap;          // cap 0: none
-  float in, out;             // bf16: s -> exp2 of 2 log2(e) scale / cap s; out = cap log2(e)
-  __device__ __forceinline__ Shape(float scale_, float cap_) : scale(scale_), cap(cap_) { in = cap > 0.f ? 2.f * LOG2E * scale / cap : 0.f; out = cap * LOG2E; }
-  // the score, and what its derivative is multiplied by.  tanh y = 1 - 2 / (1 + e^2y) is within 2^-23 of itself in all, which a bf16 score's own rounding passes by far
-  // for any cap; in fp32 small scores want the library's tanh, whose error is relative.
-  template <typename E> __device__ __forceinline__ float score(float s, float slope, float distance, float& bend) const {
+// Scores in units of log 2: scale s, or cap tanh(scale s / cap), less slope |distance|.
+enum { PLAIN = 0, CAPPED = 1, BIASED = 2 };
+template <typename E, int SHAPE> struct Scores {
+  float factor, in, out;     // s -> the exponent of e^2y for y = scale s / cap; cap log2(e)
+  __device__ __forceinline__ Scores(float scale, float cap) : factor(scale * LOG2E), in(SHAPE & CAPPED ? (sizeof(E) == 2 ? 2.f * LOG2E : 1.f) * scale / cap : 0.f), out(cap * LOG2E) {}
+  // The score, and what its derivative is multiplied by.  tanh y = 1 - 2 r, 1 - tanh^2 y = 4 r (1 - r) for r = 1 / (1 + e^2y): within 2^-22 of cap in all, which a bf16 score's own
+  // rounding passes by far; in fp32 small scores want the library's tanh, whose error is relative.
+  __device__ __forceinline__ float operator()(float s, float slope, float distance, float& bend) const {
     float x;
-    bend = 1.f;
-    if (cap > 0.f) {
-      const float t = sizeof(E) == 2 ? 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * in)) : tanhf(s * scale / cap);
-      x = t * out;
-      bend = 1.f - t * t;
+    if constexpr ((SHAPE & CAPPED) == 0) {
+      x = s * factor;
+    } else if constexpr (sizeof(E) == 2) {
+      const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * in)), four = 4.f * r;
+      x = fmaf(-2.f * out, r, out);
+      bend = fmaf(-four, r, four);
     } else {
-      x = s * (scale * LOG2E);
+      const float t = tanhf(s * in);
+      x = t * out;
+      bend = fmaf(-t, t, 1.f);
     }
-    return x - slope * distance;
+    if constexpr ((SHAPE & BIASED) != 0) x = fmaf(-slope, fabsf(distance), x);
+    return x;
   }
 };
 
