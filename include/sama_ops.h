@@ -170,8 +170,9 @@ sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, i
  * windows or any other interval of keys for each query can be given as well, in any order.  Keys and values that a query does not see do not reach it, whatever they hold; a value that is not finite
  * reaches those that see it as one that is not finite, if not the same.
  * q, out [Tq][Hq][D], k, v [Tk][Hk][D]; Hq a multiple of Hk, at most 64 times it; D a multiple of 8 up to 128; strides multiples of 16 bytes, ld at most 2^21, (Hq/Hk - 1) hs of q and dout
- * below 2^30 bytes; pointers 16-byte aligned; Tq Hq and Tk Hk up to 2^28.  at: DEVICE int32 [Tq], the place of each query among the keys, or NULL: query i is beside key i (Tq = Tk).
- * slopes: DEVICE fp32 [Hq], or NULL; constants, they get no gradient.  lse: DEVICE fp32 [Tq][Hq], natural logarithm, or NULL.  scale > 0; cap 0: none.
+ * below 2^30 bytes; pointers 16-byte aligned; Tq Hq and Tk Hk up to 2^28.  at: DEVICE int32 [Tq], the place of each query among the keys, up to 2^30 to either
+ * side of 0, or NULL: query i is beside key i (Tq = Tk).
+ * slopes: DEVICE fp32 [Hq], or NULL; constants, they get no gradient.  lse: DEVICE fp32 [Tq][Hq], natural logarithm, or NULL.  scale > 0; cap 0: none, or 1e-3 to 4096.
  * bf16: probabilities are rounded to bf16 before their product with v, sums are fp32; fp32: nothing is rounded.  workspace: sama_op_attention_bytes(), for these very sizes (0 for sizes that are refused). */
 typedef struct { void* p; int64_t ld, hs; } sama_heads;
 typedef struct {
@@ -189,7 +190,7 @@ sama_status sama_op_attention(const sama_attention* args, void* workspace, size_
 
 /* Its gradients: dq, dk, dv, all overwritten, from dout, the inputs, out and lse of the forward call (HOST struct, the same arguments).  A query that sees nothing has dq = 0 and its rows of
  * q and dout reach nobody; keys that nobody sees have dk = dv = 0.  Key heads shared by several heads get the sum, in a fixed order.  bf16: probabilities and the scores' gradients
- * are rounded to bf16 before the products they enter. */
+ * are rounded to bf16 before the products they enter, and sum_j p_j dp_j of a query that sees more than 8 keys is taken from out as it was rounded. */
 size_t sama_op_attention_grad_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype);
 sama_status sama_op_attention_grad(const sama_attention* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 

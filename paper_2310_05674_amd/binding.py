@@ -599,11 +599,19 @@ def op_glu_ffn_grad(dy, x, w_in, w_out, hidden, saved, dx, dw_in, dw_out, worksp
 
 
 # ------------------------------------------------------------------------------------- operators of a token model's sequences
-def _heads(t, shape, dtype, what):
-    """A [tokens, heads, width] tensor of the current device whose width is dense -> its address and the strides between tokens and heads (of a single one: as
-    if it were dense, whatever the stride says)."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError(f"{what}: expected a {tuple(shape)} CUDA tensor of {dtype}, got {tuple(t.shape)}, {t.dtype}")
+def _here(t, what):
+    """The number of the GPU that t is on, which has to be the current one: its stream is what the call is enqueued on."""
+    dev = t.get_device()
+    if dev < 0 or dev != _torch()._C._cuda_getDevice():
+        raise ValueError(f"{what}: expected a tensor on the current GPU, got one on {t.device}")
+    return dev
+
+
+def _heads(t, shape, dtype, dev, what):
+    """A [tokens, heads, width] tensor of GPU dev whose width is dense -> its address and the strides between tokens and heads (of a single one: as if it were
+    dense, whatever the stride says)."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what}: expected a {tuple(shape)} tensor of {dtype} on GPU {dev}, got {tuple(t.shape)}, {t.dtype}, {t.device}")
     ld, hs, step = t.stride()
     if step != 1 and shape[2] > 1:
         raise ValueError(f"{what}: expected a dense last dimension, got strides {t.stride()}")
@@ -614,26 +622,34 @@ def _heads(t, shape, dtype, what):
     return t.data_ptr(), ld, hs
 
 
-def _words(t, shape, dtype, what):
-    """A contiguous tensor of 32-bit values -> its address."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous {tuple(shape)} CUDA tensor of {dtype}, got {tuple(t.shape)}, {t.dtype}")
+def _words(t, shape, dtype, dev, what):
+    """A contiguous tensor of 32-bit values of GPU dev -> its address."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {tuple(shape)} tensor of {dtype} on GPU {dev}, got {tuple(t.shape)}, {t.dtype}, {t.device}")
     return t.data_ptr()
+
+
+def _workspace(t, dev):
+    """A workspace on GPU dev -> its address and bytes."""
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"workspace: expected contiguous memory on GPU {dev}")
+    return t.data_ptr(), t.nbytes
 
 
 def op_rotary(x, positions, out, *, sections=None, base=10000.0, neighbours=False, inverse=False):
     """Rotary positions through sama_op_rotary.  x, out [T, H, D] (out may be x), fp32 or bf16, a dense last dimension; positions int32 [T] or [axes, T]; sections: how many
     pairs turn by each axis (by default all D // 2 by one).  inverse: the other way round, which is the gradient."""
     torch = _torch()
+    dev = _here(x, "x")
     T, H, D = x.shape
     axes = 1 if positions.dim() == 1 else positions.shape[0]
     if sections is None:
         sections = (D // 2,)
     if len(sections) != axes:
         raise ValueError(f"sections: expected one for each of {axes} axes, got {tuple(sections)}")
-    at = _words(positions, (T,) if positions.dim() == 1 else (axes, T), torch.int32, "positions")
-    px, ldx, hsx = _heads(x, x.shape, x.dtype, "x")
-    po, ldo, hso = _heads(out, x.shape, x.dtype, "out")
+    at = _words(positions, (T,) if positions.dim() == 1 else (axes, T), torch.int32, dev, "positions")
+    px, ldx, hsx = _heads(x, x.shape, x.dtype, dev, "x")
+    po, ldo, hso = (px, ldx, hsx) if out is x else _heads(out, x.shape, x.dtype, dev, "out")
     counts = array("i", sections)
     rc = load_library().sama_op_rotary(px, ldx, hsx, T, H, D, _DTYPES.get(x.dtype, -1), at, axes, counts.buffer_info()[0], base, 1 if neighbours else 0,
                                        1 if inverse else 0, po, ldo, hso, _raw_stream())
@@ -644,11 +660,11 @@ def op_rotary(x, positions, out, *, sections=None, base=10000.0, neighbours=Fals
 def op_attention_spans(offsets, spans, *, causal=False, prefix=None):
     """spans [T, 2] int32: the keys [begin, end) that each of T packed tokens sees, through sama_op_attention_spans.  offsets: int32 [documents + 1], where documents begin, and the
     end of the last; causal: only up to the token itself, and the first prefix[n] tokens (int32 [documents]) of its document."""
-    i32 = _torch().int32
+    i32, dev = _torch().int32, _here(spans, "spans")
     n = offsets.numel() - 1
     T = spans.shape[0]
-    rc = load_library().sama_op_attention_spans(_words(offsets, (n + 1,), i32, "offsets"), n, None if prefix is None else _words(prefix, (n,), i32, "prefix"),
-                                                1 if causal else 0, T, _words(spans, (T, 2), i32, "spans"), _raw_stream())
+    rc = load_library().sama_op_attention_spans(_words(offsets, (n + 1,), i32, dev, "offsets"), n, None if prefix is None else _words(prefix, (n,), i32, dev, "prefix"),
+                                                1 if causal else 0, T, _words(spans, (T, 2), i32, dev, "spans"), _raw_stream())
     if rc != 0:
         _op(rc, "sama_op_attention_spans")
 
@@ -665,15 +681,15 @@ _ATTENTION = struct.Struct("@12q4P2q4i2f12q")   # sama_attention
 _NO_HEADS = (0, 0, 0)
 
 
-def _attention_args(q, k, v, out, spans, scale, cap, slopes, at, lse, dout=None, dq=None, dk=None, dv=None):
+def _attention_args(dev, q, k, v, out, spans, scale, cap, slopes, at, lse, dout=None, dq=None, dk=None, dv=None):
     torch = _torch()
     Tq, Hq, D = q.shape
     Tk, Hk = k.shape[:2]
     t, shape, keys = q.dtype, q.shape, (Tk, Hk, D)
-    grads = _NO_HEADS * 4 if dout is None else (*_heads(dout, shape, t, "dout"), *_heads(dq, shape, t, "dq"), *_heads(dk, keys, t, "dk"), *_heads(dv, keys, t, "dv"))
-    return _ATTENTION.pack(*_heads(q, shape, t, "q"), *_heads(k, keys, t, "k"), *_heads(v, keys, t, "v"), *_heads(out, shape, t, "out"),
-                           _words(spans, (Tq, 2), torch.int32, "spans"), 0 if at is None else _words(at, (Tq,), torch.int32, "at"),
-                           0 if slopes is None else _words(slopes, (Hq,), torch.float32, "slopes"), 0 if lse is None else _words(lse, (Tq, Hq), torch.float32, "lse"),
+    grads = _NO_HEADS * 4 if dout is None else (*_heads(dout, shape, t, dev, "dout"), *_heads(dq, shape, t, dev, "dq"), *_heads(dk, keys, t, dev, "dk"), *_heads(dv, keys, t, dev, "dv"))
+    return _ATTENTION.pack(*_heads(q, shape, t, dev, "q"), *_heads(k, keys, t, dev, "k"), *_heads(v, keys, t, dev, "v"), *_heads(out, shape, t, dev, "out"),
+                           _words(spans, (Tq, 2), torch.int32, dev, "spans"), 0 if at is None else _words(at, (Tq,), torch.int32, dev, "at"),
+                           0 if slopes is None else _words(slopes, (Hq,), torch.float32, dev, "slopes"), 0 if lse is None else _words(lse, (Tq, Hq), torch.float32, dev, "lse"),
                            Tq, Tk, Hq, Hk, D, _DTYPES.get(t, -1), D ** -0.5 if scale is None else scale, cap, *grads)
 
 
@@ -681,8 +697,9 @@ def op_attention(q, k, v, out, spans, workspace, *, scale=None, cap=0.0, slopes=
     """Attention of q [Tq, Hq, D] over the keys [begin, end) that spans (int32 [Tq, 2]) gives for each query of k, v [Tk, Hk, D], through sama_op_attention; out like q, all of
     one type, fp32 or bf16, strided views with a dense last dimension.  scale: D ** -0.5 by default; cap: scores become cap tanh(score / cap); slopes: fp32 [Hq], scores lose
     slope |at - key| (at: int32 [Tq], by default 0, 1, ...); lse: fp32 [Tq, Hq], for the gradients, or None.  workspace: uint8, attention_bytes(Tq, Tk, Hq, Hk, D, dtype)."""
-    args = _attention_args(q, k, v, out, spans, scale, cap, slopes, at, lse)
-    rc = load_library().sama_op_attention(args, workspace.data_ptr(), _space(workspace), _raw_stream())
+    dev = _here(q, "q")
+    args = _attention_args(dev, q, k, v, out, spans, scale, cap, slopes, at, lse)
+    rc = load_library().sama_op_attention(args, *_workspace(workspace, dev), _raw_stream())
     if rc != 0:
         _op(rc, "sama_op_attention")
 
@@ -690,8 +707,9 @@ def op_attention(q, k, v, out, spans, workspace, *, scale=None, cap=0.0, slopes=
 def op_attention_grad(dout, q, k, v, out, lse, spans, dq, dk, dv, workspace, *, scale=None, cap=0.0, slopes=None, at=None):
     """Gradients of op_attention through sama_op_attention_grad: dq like q, dk and dv like k, overwritten, from dout like out; out and lse are those of the forward
     call.  workspace: uint8, attention_grad_bytes(Tq, Tk, Hq, Hk, D, dtype)."""
-    args = _attention_args(q, k, v, out, spans, scale, cap, slopes, at, lse, dout, dq, dk, dv)
-    rc = load_library().sama_op_attention_grad(args, workspace.data_ptr(), _space(workspace), _raw_stream())
+    dev = _here(q, "q")
+    args = _attention_args(dev, q, k, v, out, spans, scale, cap, slopes, at, lse, dout, dq, dk, dv)
+    rc = load_library().sama_op_attention_grad(args, *_workspace(workspace, dev), _raw_stream())
     if rc != 0:
         _op(rc, "sama_op_attention_grad")
 
@@ -699,26 +717,26 @@ def op_attention_grad(dout, q, k, v, out, lse, spans, dq, dk, dv, workspace, *, 
 def op_distill(logits, ids, teacher, loss, saved, *, temperature=1.0):
     """The loss of each token against its teacher's listed logits through sama_op_distill.  logits [T, V] fp32 or bf16 with contiguous rows; ids int32 and teacher fp32 [T, K], ids outside the
     vocabulary (-1) for no entry; loss fp32 [T]; saved fp32 [T, 2], for the gradient."""
-    torch = _torch()
+    torch, dev = _torch(), _here(logits, "logits")
     T, V = logits.shape
     K = ids.shape[1]
     f32 = torch.float32
-    rc = load_library().sama_op_distill(logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES.get(logits.dtype, -1), T, V, _words(ids, (T, K), torch.int32, "ids"),
-                                        _words(teacher, (T, K), f32, "teacher"), K, temperature, _words(loss, (T,), f32, "loss"), _words(saved, (T, 2), f32, "saved"), _raw_stream())
+    rc = load_library().sama_op_distill(logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES.get(logits.dtype, -1), T, V, _words(ids, (T, K), torch.int32, dev, "ids"),
+                                        _words(teacher, (T, K), f32, dev, "teacher"), K, temperature, _words(loss, (T,), f32, dev, "loss"), _words(saved, (T, 2), f32, dev, "saved"), _raw_stream())
     if rc != 0:
         _op(rc, "sama_op_distill")
 
 
 def op_distill_grad(logits, ids, teacher, dloss, saved, dlogits, *, temperature=1.0):
     """The gradient of sum(dloss * loss) of op_distill in its logits through sama_op_distill_grad: dlogits like logits, or logits themselves; saved is that of the forward call."""
-    torch = _torch()
+    torch, dev = _torch(), _here(logits, "logits")
     T, V = logits.shape
     K = ids.shape[1]
     f32 = torch.float32
-    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape:
-        raise ValueError(f"dlogits: expected {tuple(logits.shape)}, {logits.dtype}, got {tuple(dlogits.shape)}, {dlogits.dtype}")
-    rc = load_library().sama_op_distill_grad(logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES.get(logits.dtype, -1), T, V, _words(ids, (T, K), torch.int32, "ids"),
-                                             _words(teacher, (T, K), f32, "teacher"), K, temperature, _words(dloss, (T,), f32, "dloss"), _words(saved, (T, 2), f32, "saved"),
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or dlogits.get_device() != dev:
+        raise ValueError(f"dlogits: expected {tuple(logits.shape)}, {logits.dtype} on GPU {dev}, got {tuple(dlogits.shape)}, {dlogits.dtype}, {dlogits.device}")
+    rc = load_library().sama_op_distill_grad(logits.data_ptr(), _rows(logits, V, "logits"), _DTYPES.get(logits.dtype, -1), T, V, _words(ids, (T, K), torch.int32, dev, "ids"),
+                                             _words(teacher, (T, K), f32, dev, "teacher"), K, temperature, _words(dloss, (T,), f32, dev, "dloss"), _words(saved, (T, 2), f32, dev, "saved"),
                                              dlogits.data_ptr(), _rows(dlogits, V, "dlogits"), _raw_stream())
     if rc != 0:
         _op(rc, "sama_op_distill_grad")

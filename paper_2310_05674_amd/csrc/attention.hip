@@ -270,7 +270,7 @@ Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk) {
   Plan p;
   p.few = wide < FILLED;
   p.tiles = (int)((rows + (p.few ? 31 : 127)) / (p.few ? 32 : 128));
-  p.parts = !p.few || narrow > FILLED / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({FILLED / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
+  p.parts = rows == 0 || narrow > FILLED / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({FILLED / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
   return p;
 }
 

@@ -389,7 +389,7 @@ bool is_attention_heads(const sama_heads& t, int64_t tokens, const sama_attentio
 const char* check_attention(const sama_attention& a, bool grad) {
   if (const char* e = check_attention_sizes(a.Tq, a.Tk, a.Hq, a.Hk, a.D, a.dtype)) return e;
   if (!(a.scale > 0.f) || !std::isfinite(a.scale)) return "scale must be positive and finite";
-  if (!(a.cap >= 0.f) || !std::isfinite(a.cap)) return "cap must be 0 (none) or positive and finite";
+  if (a.cap != 0.f && !(a.cap >= 1e-3f && a.cap <= 4096.f)) return "cap must be 0 (none), or 1e-3 to 4096";
   if (a.Tq > 0 && (a.spans == nullptr || (uintptr_t)a.spans % 8 != 0)) return "spans missing, or not aligned to 8 bytes";
   if ((uintptr_t)a.at % 4 != 0 || (uintptr_t)a.slopes % 4 != 0 || (uintptr_t)a.lse % 4 != 0) return "at, slopes or lse is not aligned to its values";
   if (a.slopes != nullptr && a.at == nullptr && a.Tq != a.Tk) return "slopes need the queries' places (at) where Tq is not Tk";
@@ -481,6 +481,7 @@ sama_status sama_op_attention_grad(const sama_attention* args, void* workspace, 
     (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_attention_grad_bytes()");
     return SAMA_EWORKSPACE;
   }
+  if (args->Tq == 0 && args->Tk == 0) return SAMA_OK;
   (void)hipGetLastError();
   launch_attention_grad((hipStream_t)hip_stream, attention_args(*args), args->dtype == SAMA_DTYPE_BF16, workspace);
   return launched(op);

@@ -5,7 +5,7 @@ the probabilities there).  With a = sum |q_d k_d| scale and S the largest sum |s
   a score is off by at most  e_s = (D + 8) u S  (D products in any order, the factor, the units of the exponential, the bias), capped by 2^-21 cap more in bf16, 8 u cap in fp32;
   a probability by  e_p = 2 e_s + (n + 16) u  of itself (n keys are summed; the exponential and the logarithm within 4 u), formed again from lse: by u |lse| more;
   out by  (e_p + [r in bf16]) sum p |v| + n u sum p |v| + r |out|;
-  dp by  e_dp = (D + 2) u sum |do v|,  delta by  e_d = sum |do| (out's error) + D u sum |do out|;
+  dp by  e_dp = (D + 2) u sum |do v|,  delta by  e_d = sum |do| (out's error) + D u sum |do out|, in bf16 rows of up to 8 keys by  sum (e_p' + n u) p |dp| + p e_dp;
   ds by  E = e_p' |ds| + p (e_dp + e_d) + [r |ds|] + 2^-20 p |dp - delta| where capped (1 - tanh^2),  dq by scale (sum E |k| + (n + 2) u sum |ds k|) + r |dq|, dk alike;
   dv by  (e_p' + [r]) sum p |do| + (m + 2) u sum p |do| + r |dv|   (m queries)."""
 import math
@@ -79,6 +79,8 @@ def reference(q, k, v, spans, scale, cap, slopes, at, dout=None):
         e_dp = (D + 2) * U * (do.abs() @ vz.abs().t())
         e_d = (do.abs() * eo).sum(1, keepdim=True) + D * U * (do * o).abs().sum(1, keepdim=True)
         e_pp = e_p + U * (torch.where(torch.isfinite(lse), lse, torch.zeros_like(lse)).abs()[:, None] + 1) * 4
+        if t == torch.bfloat16:
+            e_d = torch.where(n <= 8, ((e_pp + n * U) * p * dp.abs() + p * e_dp).sum(1, keepdim=True), e_d)
         E = torch.where(see, e_pp * ds.abs() + p * (e_dp + e_d) + soft * ds.abs() + (2.0 ** -20 * p * (dp - delta).abs() if cap > 0 else 0.0), zero)
         val["dq"][:, h] = scale * (ds @ kz)
         err["dq"][:, h] = scale * (E @ kz.abs() + (n + 2) * U * (ds.abs() @ kz.abs())) + r * val["dq"][:, h].abs()
@@ -176,11 +178,17 @@ def test_one_document(T, Hq, Hk, D, causal, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
-@pytest.mark.parametrize("D", [64, 128])
-def test_many_workgroups(D, t):
-    """Enough rows and keys for workgroups of 128 of them, forward and backward."""
-    T = 2180
-    Case(T, T, 16, 16, D, t).check(ints(documents([1500, 37, 500], T, True)))
+@pytest.mark.parametrize("T,D", [(2180, 64), (2180, 128), (4100, 64), (4100, 128), (8200, 64)])
+def test_many_workgroups(T, D, t):
+    """Rows and keys for workgroups of 64 and of 128 of them, forward and backward."""
+    Case(T, T, 16, 16, D, t).check(ints(documents([T * 2 // 3, 37, T // 4], T, True)))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("cap,slopes", [(20.0, False), (0.0, True), (5.0, True)])
+@pytest.mark.parametrize("T,D", [(4100, 64), (4100, 128)])
+def test_many_workgroups_capped_and_biased(T, D, cap, slopes, t):
+    Case(T, T, 16, 16, D, t, cap=cap, slopes=slopes).check(ints(documents([T * 2 // 3, 37, T // 4], T, True, [700, 20, 1])))
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
@@ -208,7 +216,7 @@ def test_layouts(layout, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,Hk", [(300, 2), (2200, 16)])
+@pytest.mark.parametrize("T,Hk", [(300, 2), (2200, 16), (4230, 16)])
 def test_spans_in_any_order(T, Hk, t):
     """Spans that overlap, lie apart, are empty, single, turned round or reach over the ends, in no order."""
     r = np.random.RandomState(3)
@@ -234,7 +242,7 @@ def test_new_tokens_over_caches(n, lengths, D, G, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,H", [(100, 2), (2180, 16)])
+@pytest.mark.parametrize("T,H", [(100, 2), (2180, 16), (4100, 16)])
 def test_what_is_hidden_may_hold_anything(T, H, t):
     """Rows of padding between documents, of all inputs, hold NaN and infinity."""
     c = Case(T, T, H, H, 64, t)
@@ -276,3 +284,93 @@ def test_what_is_not_finite_reaches_whom_sees_it(T, t):
     got = c.run(spans)
     for x in ("dk", "dv"):
         assert torch.equal(got[x][4:], clean[x][4:]) and not bool(torch.isfinite(got[x][:4]).any())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (5.0, True)])
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 9])
+def test_few_keys(n, cap, slopes, t):
+    """Rows of a few keys, beside each other in a group."""
+    T = 100
+    first = np.arange(T) // n * n
+    Case(T, T, 6, 2, 80, t, cap=cap, slopes=slopes).check(ints(np.stack([first, np.minimum(first + n, T)], 1)))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+def test_far_rows(t):
+    """Keys and values, their gradients and the queries in rows 2^17 values apart: offsets pass 2^31 values, and 2^33 bytes in fp32."""
+    Tq, Tk, D, ld = 40, 20011, 64, 2 ** 17
+    c = Case(Tq, Tk, 2, 1, D, t, at=torch.arange(Tq, device=DEV, dtype=torch.int32) + (Tk - Tq), slopes=True)
+    room = torch.empty(Tk, ld, dtype=c.t, device=DEV)
+    places = [room[:, 64 * i:64 * i + 64].view(Tk, 1, D) for i in range(4)]
+    far = torch.empty(Tq, 2, 2 ** 21 // 2, dtype=c.t, device=DEV)[:, :, :D]
+    for i, x in enumerate(("k", "v")):
+        places[i].copy_(getattr(c, x))
+        setattr(c, x, places[i])
+    c.q = far.copy_(c.q)
+    plain, used = c.make, []
+
+    def make(like):
+        if like.shape[0] == Tq:
+            return plain(like)
+        used.append(places[2 + len(used)].fill_(7.0))
+        return used[-1]
+    c.make = make
+    b = np.array([0, 5, 19000, 20010] * 10)
+    c.check(ints(np.stack([b, np.minimum(b + [20011, 1, 900, 1] * 10, Tk)], 1)))
+    assert len(used) == 2
+
+
+def test_no_queries_and_no_keys():
+    from paper_2310_05674_amd import binding as B
+    new = lambda *s, dtype=torch.bfloat16: torch.full(s, 7, dtype=dtype, device=DEV)
+    ws = new(4096, dtype=torch.uint8)
+    q, out, lse, spans = new(5, 4, 64), new(5, 4, 64), new(5, 4, dtype=torch.float32), ints(np.array([[0, 9]] * 5))
+    none = new(0, 2, 64)
+    B.op_attention(q, none, none, out, spans, ws, lse=lse)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    dq = new(5, 4, 64)
+    B.op_attention_grad(q, q, none, none, out, lse, spans, dq, none, none, ws)
+    assert bool((dq == 0).all())
+    k, dk, dv = new(300, 2, 64), new(300, 2, 64), new(300, 2, 64)
+    q = new(0, 4, 64)
+    B.op_attention(q, k, k, q, spans[:0], ws, lse=lse[:0])
+    B.op_attention_grad(q, q, k, k, q, lse[:0], spans[:0], q, dk, dv, ws)
+    assert bool((dk == 0).all()) and bool((dv == 0).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("Tq,Tk,Hq,Hk,D", [(700, 700, 4, 2, 64), (2200, 2200, 8, 8, 128), (4200, 4200, 16, 16, 64), (2, 9000, 8, 2, 128)])
+def test_the_same_call_gives_the_same_bits(Tq, Tk, Hq, Hk, D, t):
+    c = Case(Tq, Tk, Hq, Hk, D, t, slopes=True)
+    spans = ints(np.stack([np.arange(Tq) // 500 * 500, np.arange(Tq) + (Tk - Tq) + 1], 1))
+    first = c.run(spans)
+    for _ in range(3):
+        got = c.run(spans)
+        for x in first:
+            assert torch.equal(got[x], first[x]), x
+
+
+def test_gradients_against_differences():
+    """Gradients along a direction of q, k and v against central differences of sum(dout out), formed in 64 bits by reference() at steps h and 2 h: truncation is
+    a third of what the two differ by; the sums, of 10^4 values up to 1, round by less than 1e-10.  The formula's gradients keep within that, the kernel's within their bounds
+    more, added up along the direction."""
+    T, Hq, Hk, D, cap = 70, 4, 2, 40, 8.0
+    c = Case(T, T, Hq, Hk, D, "fp32", cap=cap, slopes=True)
+    spans = ints(documents([33, 30], T, True, [9, 0]))
+    got = c.run(spans)
+    want = reference(c.q, c.k, c.v, spans, c.scale, cap, c.slopes, c.at, c.dout)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    for x in ("q", "k", "v"):
+        way = torch.randn(getattr(c, x).shape, device=DEV, generator=gen, dtype=torch.float64)
+
+        def loss(h):
+            moved = {y: getattr(c, y).double() for y in ("q", "k", "v")}
+            moved[x] = moved[x] + h * way
+            return float((reference(moved["q"], moved["k"], moved["v"], spans, c.scale, cap, c.slopes, c.at)["out"][0] * c.dout.double()).sum())
+        h = 2.0 ** -12
+        one, two = ((loss(s) - loss(-s)) / (2 * s) for s in (h, 2 * h))
+        tolerance = abs(one - two) + 1e-10 / h
+        value, bound = want["d" + x]
+        assert abs(float((value * way).sum()) - one) <= tolerance < 1e-4
+        assert abs(float((got["d" + x].double() * way).sum()) - one) <= tolerance + float((bound * way.abs()).sum())
