@@ -2,8 +2,8 @@
 //   p = softmax over its entries of t / tau,  q = softmax over the vocabulary of z / tau,
 //   loss = tau^2 sum_k p_k (log p_k - log q_{id_k}),  dz_j = g tau (q_j - sum over the k with id_k = j of p_k)  for dloss = g.
 // Bound by memory: the loss reads z once (the running maximum and sum of a softmax), the gradient reads z and writes dz once, with the row's maximum and sum
-// that the loss kept.  A workgroup takes a token; what concerns its entries is done by as many threads, in 64 bits (fewer than 256 of V values), because
-// the loss is a small difference where student and teacher agree.
+// that the loss kept.  A workgroup takes a token; what concerns its entries is done by as many threads, in 64 bits (256 of them at most), because the loss is a
+// small difference where student and teacher agree.
 // Entries outside the vocabulary, or of a logit of minus infinity, are none; a token without entries has loss and gradient zero, and its logits are not read.
 #include <algorithm>
 #include <cmath>
@@ -52,24 +52,29 @@ __device__ __forceinline__ T block_join(T x, T* red, F op) {
   return x;
 }
 
-// A thread's entry, if it has one, and its probability.
+// A thread's entry, if it has one, and its probability.  Up to 64 entries are the first wave's: every wave looks whether there are any, and nobody waits for the first one's
+// exponentials before the row's loads.
 struct Entry { int id; bool there; double p, logp; float z; };
 template <typename E, int THREADS>
 __device__ __forceinline__ bool entries(const DistillArgs& a, int64_t row, Entry& e, double* red) {
-  const int k = threadIdx.x;
+  const bool one_wave = a.K <= 64;
+  const int k = one_wave ? threadIdx.x & 63 : threadIdx.x;
   e = Entry{-1, false, 0.0, 0.0, 0.f};
   float t = 0.f;
   if (k < a.K) {
     e.id = a.ids[row * a.K + k];
     t = a.teacher[row * a.K + k];
     e.there = e.id >= 0 && e.id < a.V && t != -std::numeric_limits<float>::infinity();
-    if (e.there) e.z = value<E>(static_cast<const E*>(a.z)[row * a.ldz + e.id]);
   }
-  if (!__syncthreads_or(e.there)) return false;
+  if (!(one_wave ? __any(e.there) : __syncthreads_or(e.there))) return false;
+  if (one_wave && threadIdx.x >= 64) { e.id = -1; e.there = false; return true; }
+  if (e.there) e.z = value<E>(static_cast<const E*>(a.z)[row * a.ldz + e.id]);
   const double low = -std::numeric_limits<double>::infinity(), tau = a.tau;
-  const double top = block_join<THREADS>(e.there ? (double)t : low, red, [](double x, double y) { return fmax(x, y); });
+  auto larger = [](double x, double y) { return fmax(x, y); };
+  auto add = [](double x, double y) { return x + y; };
+  const double mine = e.there ? (double)t : low, top = one_wave ? join_wave(mine, larger) : block_join<THREADS>(mine, red, larger);
   const double x = ((double)t - top) / tau, w = e.there ? exp(x) : 0.0;
-  const double sum = block_join<THREADS>(w, red, [](double x, double y) { return x + y; });
+  const double sum = one_wave ? join_wave(w, add) : block_join<THREADS>(w, red, add);
   e.p = w / sum; e.logp = x - log(sum);
   return true;
 }
@@ -84,7 +89,7 @@ template <typename E> __device__ __forceinline__ void split_row(const E* row, in
 template <typename E, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a) {
   __shared__ double red64[THREADS / 64];
-  __shared__ float red[THREADS / 64];
+  __shared__ float2 red[THREADS / 64];
   const int64_t row = blockIdx.x;
   Entry e;
   if (!entries<E, THREADS>(a, row, e, red64)) {
@@ -122,10 +127,21 @@ __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a) {
     }
   }
   if (tail + (int)threadIdx.x < a.V) one(value<E>(z[tail + threadIdx.x]));
-  const float top = block_join<THREADS>(m, red, [](float x, float y) { return fmaxf(x, y); });
-  const float sum = block_join<THREADS>(s * __builtin_amdgcn_exp2f((m - top) * c), red, [](float x, float y) { return x + y; });
-  const double logq = ((double)e.z - (double)top) / (double)a.tau - log((double)sum);
-  const double loss = block_join<THREADS>(e.p == 0.0 ? 0.0 : e.p * (e.logp - logq), red64, [](double x, double y) { return x + y; });
+  // each wave's maximum and sum, then all of them
+  const float top_w = join_wave(m, [](float x, float y) { return fmaxf(x, y); });
+  const float sum_w = join_wave(s * __builtin_amdgcn_exp2f((m - top_w) * c), [](float x, float y) { return x + y; });
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(top_w, sum_w);
+  __syncthreads();
+  const bool one_wave = a.K <= 64;
+  if (one_wave && threadIdx.x >= 64) return;
+  float top = red[0].x, sum = 0.f;
+#pragma unroll
+  for (int i = 1; i < THREADS / 64; ++i) top = fmaxf(top, red[i].x);
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) sum += red[i].y * __builtin_amdgcn_exp2f((red[i].x - top) * c);
+  const double logq = ((double)e.z - (double)top) / (double)a.tau - log((double)sum), part = e.p == 0.0 ? 0.0 : e.p * (e.logp - logq);
+  auto add = [](double x, double y) { return x + y; };
+  const double loss = one_wave ? join_wave(part, add) : block_join<THREADS>(part, red64, add);
   if (threadIdx.x == 0) {
     a.loss[row] = (float)((double)a.tau * (double)a.tau * loss);
     a.saved[2 * row] = top; a.saved[2 * row + 1] = sum;
@@ -190,18 +206,17 @@ __global__ __launch_bounds__(THREADS) void k_distill_grad(DistillArgs a) {
   dz[e.id] = rounded<E>((__builtin_amdgcn_exp2f((zk - top) * c) * inv - p) * g);
 }
 
-// Few rows: more waves to each, one row's pieces being all there is to load.
-template <typename E, int THREADS>
+// Waves of a row, us at 256 / 512 / 1024 threads (T x V, loss and gradient): 37 x 8192 fp32: 4.3 / 3.9 / 4.1 and 5.0 / 4.7 / 4.7; 4096 x 8192 fp32: 22.7 / 22.0 / 30.2 and
+// 44.2 / 43.2 / 43.0; 4096 x 30522 bf16: 41.4 / 39.6 / 44.5 and 105 / 97.2 / 97.2; 37 x 50304 fp32: 9.3 / 6.5 / 6.4 and 10.7 / 8.3 / 8.1; 4096 x 50304 fp32: 139 / 136 / 132 and
+// 329 / 321 / 310.  The last are 6.2 and 5.3 TB/s (a copy: 5.0).
+constexpr int LOSS_THREADS = 512, GRAD_THREADS = 1024;
+template <typename E>
 void launch(hipStream_t st, const DistillArgs& a, bool grad) {
   ProfScope ps(st, F_OTHER, (double)a.T * a.V * sizeof(E) * (grad ? 2 : 1));
-  if (grad) launch_kernel(ps, k_distill_grad<E, THREADS>, dim3((unsigned)a.T), THREADS, 0, st, a);
-  else launch_kernel(ps, k_distill<E, THREADS>, dim3((unsigned)a.T), THREADS, 0, st, a);
+  if (grad) launch_kernel(ps, k_distill_grad<E, GRAD_THREADS>, dim3((unsigned)a.T), GRAD_THREADS, 0, st, a);
+  else launch_kernel(ps, k_distill<E, LOSS_THREADS>, dim3((unsigned)a.T), LOSS_THREADS, 0, st, a);
 }
-void launch_either(hipStream_t st, const DistillArgs& a, bool grad) {
-  const bool few = a.T <= 512;
-  if (a.bf16) few ? launch<bf16_t, 1024>(st, a, grad) : launch<bf16_t, 256>(st, a, grad);
-  else few ? launch<float, 1024>(st, a, grad) : launch<float, 256>(st, a, grad);
-}
+void launch_either(hipStream_t st, const DistillArgs& a, bool grad) { a.bf16 ? launch<bf16_t>(st, a, grad) : launch<float>(st, a, grad); }
 }  // namespace
 
 void launch_distill(hipStream_t st, const DistillArgs& a) { launch_either(st, a, false); }
