@@ -261,16 +261,21 @@ __global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets,
 }
 
 // What a call looks like: rows of a workgroup, and into how many parts the keys are cut.
-// Two workgroups of 128 rows fit a CU; where there are fewer than that, workgroups of 32 rows with four groups of keys take over (4096 queries of 12 heads in four texts, capped: 70 us for 133;
-// 8111 of 16 heads on 4 key heads in 23 texts, which are enough: 50, and 70 with 32).  Where even those leave CUs without one the keys are split.
-constexpr int64_t FILLED = 512, LEAST_KEYS = 512;
+// Two workgroups of 128 rows fit a CU; where there are fewer than that, workgroups of 32 rows with four groups of keys take over (4096 queries of 12 heads in four texts, capped: 70 us for
+// 133; 8111 of 16 heads on 4 key heads in 23 texts, which are enough: 50, and 70 with 32).  Rows of 512 bytes leave LDS for one workgroup a CU, and with 32 rows for two groups of keys, half of
+// the matrix units: there 128 rows are ahead sooner (a training step in fp32, width 128, one causal text: 8 heads of 2000, 128 workgroups, 717 us with 32 and 995 with 128; of 3500, 224
+// workgroups, 1742 and 1697; 12 heads of 4096 in four texts, 384 workgroups, 1714 and 1487).  Where even those of 32 rows leave CUs without one the keys are split, into as many parts as
+// there is room for at once (fp32, width 128, 10 tokens over 5908 keys each, 5 heads: 180 us in 64 parts, of which the CUs hold 51 at a time, and 117 in 51).
+constexpr int64_t LEAST_KEYS = 512;
+constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }
+constexpr int64_t resident_workgroups(int row_bytes) { return row_bytes > 256 ? 256 : 512; }
 struct Plan { bool few; int tiles, parts; };
-Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk) {
+Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk, int row_bytes) {
   const int64_t rows = Tq * (Hq / Hk), wide = (rows + 127) / 128 * Hk, narrow = (rows + 31) / 32 * Hk;
   Plan p;
-  p.few = wide < FILLED;
+  p.few = wide < enough_workgroups(row_bytes);
   p.tiles = (int)((rows + (p.few ? 31 : 127)) / (p.few ? 32 : 128));
-  p.parts = rows == 0 || narrow > FILLED / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({FILLED / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
+  p.parts = rows == 0 || narrow > 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({resident_workgroups(row_bytes) / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
   return p;
 }
 
@@ -290,7 +295,7 @@ void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspa
 }
 template <typename E, int DP>
 void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
-  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk);
+  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk, DP * (int)sizeof(E));
   auto run = [&](auto config) {
     typedef decltype(config) C;
     switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes != nullptr ? BIASED : 0)) {
@@ -311,8 +316,8 @@ void launch_attention_spans(hipStream_t st, const int32_t* offsets, int64_t docu
   launch_kernel(ps, k_attention_spans, dim3((unsigned)((T + 255) / 256)), 256, 0, st, offsets, (int)documents, prefix, causal ? 1 : 0, (int)T, reinterpret_cast<int2*>(spans));
 }
 
-size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D) {
-  const Plan p = plan(Tq, Tk, Hq, Hk);
+size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D, bool bf16) {
+  const Plan p = plan(Tq, Tk, Hq, Hk, (D <= 64 ? 64 : 128) * (bf16 ? 2 : 4));
   return p.parts <= 1 ? 256 : (size_t)p.parts * Tq * Hq * (D + 1) * sizeof(float);
 }
 void launch_attention(hipStream_t st, const AttentionArgs& a, bool bf16, void* workspace) {

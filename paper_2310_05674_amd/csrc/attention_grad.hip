@@ -38,7 +38,23 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows r
   float sum = 0.f;
   const float lse = some ? a.lse[query * a.Hq + head] * LOG2E : 0.f, slope = some && a.slopes != nullptr ? a.slopes[head] * LOG2E : 0.f;
   const int at = some ? (a.at != nullptr ? a.at[query] : (int)query) : 0;
+  if (some) {
+    const E* const o = static_cast<const E*>(a.out.p) + query * a.out.ld + head * a.out.hs;
+    const E* const d = static_cast<const E*>(a.dout.p) + query * a.dout.ld + head * a.dout.hs;
+    Frag<E> x[4], y[4];   // all on their way together
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = 8 * part + 32 * u;
+      x[u] = i < a.D ? load_fragment<E>(o + i) : zero_fragment<E>(); y[u] = i < a.D ? load_fragment<E>(d + i) : zero_fragment<E>();
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)x[u][e], (float)y[u][e], sum);
+  }
+  sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2);
   if (some && sizeof(E) == 2 && span.y - span.x <= FEW) {
+    sum = 0.f;
     const E* const q = static_cast<const E*>(a.q.p) + query * a.q.ld + head * a.q.hs;
     const E* const d = static_cast<const E*>(a.dout.p) + query * a.dout.ld + head * a.dout.hs;
     const E* const k = static_cast<const E*>(a.k.p) + hk * a.k.hs;
@@ -64,16 +80,8 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows r
         if (j0 + n < span.y) sum = fmaf(__builtin_amdgcn_exp2f(x - lse), dp[n], sum);
       }
     }
-  } else if (some) {
-    const E* const o = static_cast<const E*>(a.out.p) + query * a.out.ld + head * a.out.hs;
-    const E* const d = static_cast<const E*>(a.dout.p) + query * a.dout.ld + head * a.dout.hs;
-    for (int i = 8 * part; i < a.D; i += 32) {
-      const Frag<E> x = load_fragment<E>(o + i), y = load_fragment<E>(d + i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], (float)y[e], sum);
-    }
+    sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2);
   }
-  sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2);
   if (part == 0) {
     uint32_t* const to = rows.record + ((int64_t)hk * rows.groups + group) * (PLANES * GROUP) + r;
     to[LSE * GROUP] = __float_as_uint(lse);
@@ -586,7 +594,7 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionAr
   finish(dv, a.dv, 1.f);
 }
 
-constexpr int64_t FILLED = 512;   // see attention.hip
+constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }   // of 128 rows: see attention.hip, which measures both passes
 
 template <auto KERNEL, typename C, typename... A>
 void launch(ProfScope& ps, int64_t blocks, hipStream_t st, A... a) {
@@ -603,7 +611,7 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
   const int64_t count = a.Tq * (a.Hq / a.Hk);
   if (a.Tq > 0) launch_kernel(ps, k_attention_delta<E, SHAPE>, dim3((unsigned)((int64_t)rows.groups * a.Hk)), 256, 0, st, a, rows);
   if (a.Tq == 0) {
-  } else if ((count + 127) / 128 * a.Hk >= FILLED) {
+  } else if ((count + 127) / 128 * a.Hk >= enough_workgroups(DP * (int)sizeof(E))) {
     typedef QConfig<E, DP, 4> C;
     launch<&k_attention_dq<E, C, SHAPE>, C>(ps, (count + 127) / 128 * a.Hk, st, a, rows, (int)((count + 127) / 128));
   } else {

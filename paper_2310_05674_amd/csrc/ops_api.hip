@@ -453,7 +453,7 @@ sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, i
 }
 
 size_t sama_op_attention_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype) {
-  return check_attention_sizes(Tq, Tk, Hq, Hk, D, dtype) != nullptr ? 0 : attention_bytes(Tq, Tk, Hq, Hk, D);
+  return check_attention_sizes(Tq, Tk, Hq, Hk, D, dtype) != nullptr ? 0 : attention_bytes(Tq, Tk, Hq, Hk, D, dtype == SAMA_DTYPE_BF16);
 }
 size_t sama_op_attention_grad_bytes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype) {
   return check_attention_sizes(Tq, Tk, Hq, Hk, D, dtype) != nullptr ? 0 : attention_grad_bytes(Tq, Tk, Hq, Hk, D);
@@ -463,7 +463,7 @@ sama_status sama_op_attention(const sama_attention* args, void* workspace, size_
   g_ops_error.clear();
   if (args == nullptr) return refuse(op, "null arguments");
   if (const char* e = check_attention(*args, false)) return refuse(op, e);
-  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < attention_bytes(args->Tq, args->Tk, args->Hq, args->Hk, args->D)) {
+  if (!workspace || (uintptr_t)workspace % 256 != 0 || workspace_bytes < attention_bytes(args->Tq, args->Tk, args->Hq, args->Hk, args->D, args->dtype == SAMA_DTYPE_BF16)) {
     (void)refuse(op, "workspace missing, not aligned to 256 bytes or smaller than sama_op_attention_bytes()");
     return SAMA_EWORKSPACE;
   }

@@ -40,7 +40,7 @@ struct AttentionArgs {
   float scale, cap;
 };
 void launch_attention_spans(hipStream_t, const int32_t* offsets, int64_t documents, const int32_t* prefix, bool causal, int64_t T, int32_t* spans);
-size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D);
+size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D, bool bf16);
 size_t attention_grad_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D);
 void launch_attention(hipStream_t, const AttentionArgs&, bool bf16, void* workspace);
 void launch_attention_grad(hipStream_t, const AttentionArgs&, bool bf16, void* workspace);
