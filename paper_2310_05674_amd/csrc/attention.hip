@@ -17,9 +17,10 @@ template <typename E, int DP_, int WM_, int KG_, int NS_>
 struct Config {
   static constexpr int DP = DP_, WM = WM_, KG = KG_, NS = NS_;                    // waves side by side over rows, over keys; 32 keys each of a wave's part of a tile
   static constexpr int WAVES = WM * KG, THREADS = WAVES * 64, BM = 32 * WM, BK = 32 * NS * KG;
-  static constexpr int KV = BK * DP * (int)sizeof(E), LDS = 4 * KV;               // K and V, two stages
+  static constexpr int KV = BK * DP * (int)sizeof(E), JOIN = KG == 1 ? 0 : WAVES * (DP * 32 * 4 + 256);
+  static constexpr int LDS = 4 * KV > JOIN ? 4 * KV : JOIN;                       // K and V, two stages; the groups' parts
   static constexpr int PER_EU = sizeof(E) * DP <= 256 ? 2 : 1;
-  static_assert(LDS <= LDS_MAX && (KG == 1 || WAVES * (DP * 32 * 4 + 256) <= LDS), "LDS");
+  static_assert(LDS <= LDS_MAX, "LDS");
 };
 
 struct Parts { float* o; float* lse; int count; };   // of split keys: [count][Hk][rows][D] and [count][Hk][rows]
@@ -266,15 +267,19 @@ __global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets,
 // the matrix units: there 128 rows are ahead sooner (a training step in fp32, width 128, one causal text: 8 heads of 2000, 128 workgroups, 717 us with 32 and 995 with 128; of 3500, 224
 // workgroups, 1742 and 1697; 12 heads of 4096 in four texts, 384 workgroups, 1714 and 1487).  Where even those of 32 rows leave CUs without one the keys are split, into as many parts as
 // there is room for at once (fp32, width 128, 10 tokens over 5908 keys each, 5 heads: 180 us in 64 parts, of which the CUs hold 51 at a time, and 117 in 51).
+// In between, with rows of 256 bytes, workgroups of 32 rows leave LDS for one a CU, and those of 64 rows and two groups of keys for two (forward, causal, 12 heads of 4096 in 4 or 41 texts,
+// 768 of them: bf16 of width 128 103 -> 73 and 53 -> 30 us, fp32 of width 64 173 -> 164 and 63 -> 47; 8 heads of 3500 in ten, 440: 39 -> 31, but 56 -> 69; of 2000 in two, 256: 30 -> 43 and
+// 50 -> 80).  Rows of 128 bytes, of which two workgroups fit either way, take 44 -> 51 and 23 -> 15 us in the first two, rows of 512 the same time.
 constexpr int64_t LEAST_KEYS = 512;
+constexpr int64_t middle_workgroups(bool bf16) { return bf16 ? 384 : 640; }
 constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }
 constexpr int64_t resident_workgroups(int row_bytes) { return row_bytes > 256 ? 256 : 512; }
-struct Plan { bool few; int tiles, parts; };
-Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk, int row_bytes) {
+struct Plan { int rows, tiles, parts; };
+Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk, int row_bytes, bool bf16) {
   const int64_t rows = Tq * (Hq / Hk), wide = (rows + 127) / 128 * Hk, narrow = (rows + 31) / 32 * Hk;
   Plan p;
-  p.few = wide < enough_workgroups(row_bytes);
-  p.tiles = (int)((rows + (p.few ? 31 : 127)) / (p.few ? 32 : 128));
+  p.rows = wide >= enough_workgroups(row_bytes) ? 128 : row_bytes == 256 && (rows + 63) / 64 * Hk >= middle_workgroups(bf16) ? 64 : 32;
+  p.tiles = (int)((rows + p.rows - 1) / p.rows);
   p.parts = rows == 0 || narrow > 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({resident_workgroups(row_bytes) / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
   return p;
 }
@@ -295,7 +300,7 @@ void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspa
 }
 template <typename E, int DP>
 void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
-  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk, DP * (int)sizeof(E));
+  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk, DP * (int)sizeof(E), sizeof(E) == 2);
   auto run = [&](auto config) {
     typedef decltype(config) C;
     switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes != nullptr ? BIASED : 0)) {
@@ -305,9 +310,10 @@ void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
       default: return launch<E, C, CAPPED | BIASED>(st, a, p, workspace);
     }
   };
-  constexpr bool WIDE_ROWS = sizeof(E) * DP > 256;
-  if (p.few) run(Config<E, DP, 1, WIDE_ROWS ? 2 : 4, 1>{});
-  else run(Config<E, DP, 4, 1, WIDE_ROWS ? 1 : 2>{});
+  constexpr bool LONG = sizeof(E) * DP > 256;
+  if (p.rows == 128) return run(Config<E, DP, 4, 1, LONG ? 1 : 2>{});
+  if constexpr (sizeof(E) * DP == 256) if (p.rows == 64) return run(Config<E, DP, 2, 2, 1>{});
+  run(Config<E, DP, 1, LONG ? 2 : 4, 1>{});
 }
 }  // namespace
 
@@ -317,7 +323,7 @@ void launch_attention_spans(hipStream_t st, const int32_t* offsets, int64_t docu
 }
 
 size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D, bool bf16) {
-  const Plan p = plan(Tq, Tk, Hq, Hk, (D <= 64 ? 64 : 128) * (bf16 ? 2 : 4));
+  const Plan p = plan(Tq, Tk, Hq, Hk, (D <= 64 ? 64 : 128) * (bf16 ? 2 : 4), bf16);
   return p.parts <= 1 ? 256 : (size_t)p.parts * Tq * Hq * (D + 1) * sizeof(float);
 }
 void launch_attention(hipStream_t st, const AttentionArgs& a, bool bf16, void* workspace) {

@@ -24,7 +24,7 @@ struct Rows {
 // o was rounded to the gradients' type, and delta with it: off by 2^-9 |do| |o| or so.  A row of many keys, whose o is a mean, hardly shows that, three keys do: dq off by 0.0046 of
 // its norm.  So a 16-bit row of at most FEW keys has delta = sum_j p_ij dp_ij from its keys themselves.  60 drawn cases from one token to 3000: at most 0.0046 without, 0.0027 with FEW
 // = 8 or 16; 8111 packed tokens, 16 heads of 64: 208.7 us a step without, 213.9 with 8, 218.3 with 16.
-constexpr int FEW = 8;
+constexpr int FEW = 8;   // two a lane
 
 template <typename E, int SHAPE>
 __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows rows) {
@@ -36,8 +36,6 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows r
   if (r < tokens * G && query < a.Tq) span = span_of(a.spans, query, (int)a.Tk);
   const bool some = span.x < span.y;
   float sum = 0.f;
-  const float lse = some ? a.lse[query * a.Hq + head] * LOG2E : 0.f, slope = some && a.slopes != nullptr ? a.slopes[head] * LOG2E : 0.f;
-  const int at = some ? (a.at != nullptr ? a.at[query] : (int)query) : 0;
   if (some) {
     const E* const o = static_cast<const E*>(a.out.p) + query * a.out.ld + head * a.out.hs;
     const E* const d = static_cast<const E*>(a.dout.p) + query * a.dout.ld + head * a.dout.hs;
@@ -52,6 +50,8 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows r
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum = fmaf((float)x[u][e], (float)y[u][e], sum);
   }
+  const float lse = some ? a.lse[query * a.Hq + head] * LOG2E : 0.f, slope = some && a.slopes != nullptr ? a.slopes[head] * LOG2E : 0.f;
+  const int at = some ? (a.at != nullptr ? a.at[query] : (int)query) : 0;
   sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2);
   if (some && sizeof(E) == 2 && span.y - span.x <= FEW) {
     sum = 0.f;
@@ -60,26 +60,32 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows r
     const E* const k = static_cast<const E*>(a.k.p) + hk * a.k.hs;
     const E* const v = static_cast<const E*>(a.v.p) + hk * a.v.hs;
     const Scores<E, SHAPE> score(a.scale, a.cap);
-    for (int j0 = span.x; j0 < span.y; j0 += 4) {   // four keys' loads together
-      float s[4] = {}, dp[4] = {};
-      for (int i = 8 * part; i < a.D; i += 32) {
-        const Frag<E> x = load_fragment<E>(q + i), y = load_fragment<E>(d + i);
+    // two keys a lane, with as many loads on their way as there are registers for: one after the other, the keys of one such row are all that the launch waits for
+    const int j0 = span.x + part, j1 = j0 + 4;
+    const int64_t in0 = min(j0, span.y - 1), in1 = min(j1, span.y - 1);
+    const E *const k0 = k + in0 * a.k.ld, *const k1 = k + in1 * a.k.ld, *const v0 = v + in0 * a.v.ld, *const v1 = v + in1 * a.v.ld;
+    float s0 = 0.f, s1 = 0.f, dp0 = 0.f, dp1 = 0.f;
+    for (int i = 0; i < a.D; i += 32) {
+      Frag<E> x[4], y[4], xk0[4], xk1[4], xv0[4], xv1[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const int64_t j = min(j0 + n, span.y - 1);
-          const Frag<E> xk = load_fragment<E>(k + j * a.k.ld + i), xv = load_fragment<E>(v + j * a.v.ld + i);
+      for (int u = 0; u < 4; ++u) {
+        const int c = min(i + 8 * u, a.D - 8);
+        x[u] = load_fragment<E>(q + c); y[u] = load_fragment<E>(d + c);
+        xk0[u] = load_fragment<E>(k0 + c); xk1[u] = load_fragment<E>(k1 + c); xv0[u] = load_fragment<E>(v0 + c); xv1[u] = load_fragment<E>(v1 + c);
+      }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) { s[n] = fmaf((float)x[e], (float)xk[e], s[n]); dp[n] = fmaf((float)y[e], (float)xv[e], dp[n]); }
+      for (int u = 0; u < 4; ++u) {
+        if (i + 8 * u >= a.D) break;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s0 = fmaf((float)x[u][e], (float)xk0[u][e], s0); s1 = fmaf((float)x[u][e], (float)xk1[u][e], s1);
+          dp0 = fmaf((float)y[u][e], (float)xv0[u][e], dp0); dp1 = fmaf((float)y[u][e], (float)xv1[u][e], dp1);
         }
       }
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        s[n] += __shfl_xor(s[n], 1); s[n] += __shfl_xor(s[n], 2);
-        float bend;
-        const float x = score(s[n], slope, (float)(at - (j0 + n)), bend);
-        if (j0 + n < span.y) sum = fmaf(__builtin_amdgcn_exp2f(x - lse), dp[n], sum);
-      }
     }
+    float bend;
+    if (j0 < span.y) sum = __builtin_amdgcn_exp2f(score(s0, slope, (float)(at - j0), bend) - lse) * dp0;
+    if (j1 < span.y) sum = fmaf(__builtin_amdgcn_exp2f(score(s1, slope, (float)(at - j1), bend) - lse), dp1, sum);
     sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2);
   }
   if (part == 0) {
@@ -103,12 +109,12 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Rows r
 template <typename E, int DP_, int WM_>
 struct QConfig {
   static constexpr int DP = DP_, WM = WM_;
-  static constexpr int KG = WM > 1 ? 1 : sizeof(E) * DP > 256 ? 2 : 4;
-  static constexpr int NS = WM > 1 && sizeof(E) * DP <= 256 ? 2 : 1;
+  static constexpr int KG = WM > 2 ? 1 : WM > 1 || sizeof(E) * DP > 256 ? 2 : 4;
+  static constexpr int NS = WM > 2 && sizeof(E) * DP <= 256 ? 2 : 1;
   static constexpr int WAVES = WM * KG, THREADS = WAVES * 64, BM = 32 * WM, BK = 32 * NS * KG;
-  static constexpr int KV = BK * DP * (int)sizeof(E), LDS = 4 * KV;
+  static constexpr int KV = BK * DP * (int)sizeof(E), JOIN = KG == 1 ? 0 : WAVES * DP * 32 * 4, LDS = 4 * KV > JOIN ? 4 * KV : JOIN;
   static constexpr int PER_EU = sizeof(E) * DP <= 256 ? 2 : 1;
-  static_assert(LDS <= LDS_MAX && KG * DP * 32 * 4 <= LDS, "LDS");
+  static_assert(LDS <= LDS_MAX, "LDS");
 };
 template <typename E, typename C, int SHAPE>
 __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(AttentionArgs a, Rows recs, int tiles) {
@@ -209,7 +215,7 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention_dq(Attentio
   drain_loads();
   if constexpr (C::KG > 1) {   // the groups' sums; a wave then has 32 of the columns
     __syncthreads();
-    float* const part = reinterpret_cast<float*>(smem);                     // [KG][DP][32]
+    float* const part = reinterpret_cast<float*>(smem) + rw * C::KG * C::DP * 32;   // [KG][DP][32]
 #pragma unroll
     for (int df = 0; df < T::DF; ++df)
 #pragma unroll
@@ -594,7 +600,9 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionAr
   finish(dv, a.dv, 1.f);
 }
 
-constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }   // of 128 rows: see attention.hip, which measures both passes
+// of 128 rows and of 64: see attention.hip; both passes change sides at about the same sizes (768 workgroups of 64: 111 -> 80 and 56 -> 34 us in bf16, 220 -> 215 and 75 -> 60 in fp32)
+constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }
+constexpr int64_t middle_workgroups(bool bf16) { return bf16 ? 384 : 640; }
 
 template <auto KERNEL, typename C, typename... A>
 void launch(ProfScope& ps, int64_t blocks, hipStream_t st, A... a) {
@@ -610,14 +618,17 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
   ProfScope ps(st, F_OTHER, 0.0);
   const int64_t count = a.Tq * (a.Hq / a.Hk);
   if (a.Tq > 0) launch_kernel(ps, k_attention_delta<E, SHAPE>, dim3((unsigned)((int64_t)rows.groups * a.Hk)), 256, 0, st, a, rows);
-  if (a.Tq == 0) {
-  } else if ((count + 127) / 128 * a.Hk >= enough_workgroups(DP * (int)sizeof(E))) {
-    typedef QConfig<E, DP, 4> C;
-    launch<&k_attention_dq<E, C, SHAPE>, C>(ps, (count + 127) / 128 * a.Hk, st, a, rows, (int)((count + 127) / 128));
-  } else {
-    typedef QConfig<E, DP, 1> C;
-    launch<&k_attention_dq<E, C, SHAPE>, C>(ps, (count + 31) / 32 * a.Hk, st, a, rows, (int)((count + 31) / 32));
-  }
+  auto rows_of = [&](auto config) {
+    typedef decltype(config) C;
+    const int64_t n = (count + C::BM - 1) / C::BM;
+    launch<&k_attention_dq<E, C, SHAPE>, C>(ps, n * a.Hk, st, a, rows, (int)n);
+  };
+  auto by_rows = [&] {
+    if ((count + 127) / 128 * a.Hk >= enough_workgroups(DP * (int)sizeof(E))) return rows_of(QConfig<E, DP, 4>{});
+    if constexpr (sizeof(E) * DP == 256) if ((count + 63) / 64 * a.Hk >= middle_workgroups(sizeof(E) == 2)) return rows_of(QConfig<E, DP, 2>{});
+    rows_of(QConfig<E, DP, 1>{});
+  };
+  if (a.Tq > 0) by_rows();
   if (a.Tk == 0) return;
   auto pairs = [&](auto config) {
     typedef decltype(config) C;

@@ -178,15 +178,15 @@ def test_one_document(T, Hq, Hk, D, causal, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,D", [(2180, 64), (2180, 128), (4100, 64), (4100, 128), (8200, 64)])
+@pytest.mark.parametrize("T,D", [(2180, 64), (2180, 128), (2700, 64), (4100, 64), (4100, 128), (8200, 64)])
 def test_many_workgroups(T, D, t):
-    """Rows and keys for workgroups of 64 and of 128 of them, forward and backward."""
+    """Rows and keys for workgroups of 32, 64 and 128 of them, forward and backward."""
     Case(T, T, 16, 16, D, t).check(ints(documents([T * 2 // 3, 37, T // 4], T, True)))
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
 @pytest.mark.parametrize("cap,slopes", [(20.0, False), (0.0, True), (5.0, True)])
-@pytest.mark.parametrize("T,D", [(4100, 64), (4100, 128)])
+@pytest.mark.parametrize("T,D", [(2700, 64), (2700, 128), (4100, 64), (4100, 128)])
 def test_many_workgroups_capped_and_biased(T, D, cap, slopes, t):
     Case(T, T, 16, 16, D, t, cap=cap, slopes=slopes).check(ints(documents([T * 2 // 3, 37, T // 4], T, True, [700, 20, 1])))
 
@@ -216,7 +216,7 @@ def test_layouts(layout, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,Hk", [(300, 2), (2200, 16), (4230, 16)])
+@pytest.mark.parametrize("T,Hk", [(300, 2), (2200, 16), (2700, 16), (4230, 16)])
 def test_spans_in_any_order(T, Hk, t):
     """Spans that overlap, lie apart, are empty, single, turned round or reach over the ends, in no order."""
     r = np.random.RandomState(3)
@@ -242,7 +242,7 @@ def test_new_tokens_over_caches(n, lengths, D, G, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,H", [(100, 2), (2180, 16), (4100, 16)])
+@pytest.mark.parametrize("T,H", [(100, 2), (2180, 16), (2700, 16), (4100, 16)])
 def test_what_is_hidden_may_hold_anything(T, H, t):
     """Rows of padding between documents, of all inputs, hold NaN and infinity."""
     c = Case(T, T, H, H, 64, t)
