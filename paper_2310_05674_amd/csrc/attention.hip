@@ -261,26 +261,17 @@ __global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets,
   spans[t] = s;
 }
 
-// What a call looks like: rows of a workgroup, and into how many parts the keys are cut.
-// Two workgroups of 128 rows fit a CU; where there are fewer than that, workgroups of 32 rows with four groups of keys take over (4096 queries of 12 heads in four texts, capped: 70 us for
-// 133; 8111 of 16 heads on 4 key heads in 23 texts, which are enough: 50, and 70 with 32).  Rows of 512 bytes leave LDS for one workgroup a CU, and with 32 rows for two groups of keys, half of
-// the matrix units: there 128 rows are ahead sooner (a training step in fp32, width 128, one causal text: 8 heads of 2000, 128 workgroups, 717 us with 32 and 995 with 128; of 3500, 224
-// workgroups, 1742 and 1697; 12 heads of 4096 in four texts, 384 workgroups, 1714 and 1487).  Where even those of 32 rows leave CUs without one the keys are split, into as many parts as
-// there is room for at once (fp32, width 128, 10 tokens over 5908 keys each, 5 heads: 180 us in 64 parts, of which the CUs hold 51 at a time, and 117 in 51).
-// In between, with rows of 256 bytes, workgroups of 32 rows leave LDS for one a CU, and those of 64 rows and two groups of keys for two (forward, causal, 12 heads of 4096 in 4 or 41 texts,
-// 768 of them: bf16 of width 128 103 -> 73 and 53 -> 30 us, fp32 of width 64 173 -> 164 and 63 -> 47; 8 heads of 3500 in ten, 440: 39 -> 31, but 56 -> 69; of 2000 in two, 256: 30 -> 43 and
-// 50 -> 80).  Rows of 128 bytes, of which two workgroups fit either way, take 44 -> 51 and 23 -> 15 us in the first two, rows of 512 the same time.
+// What a call looks like: rows of a workgroup, and into how many parts the keys are cut.  Where even workgroups of 32 rows leave CUs without one the keys are split, into as many parts as
+// there is room for at once: two workgroups a CU, or one with rows of 512 bytes (fp32, width 128, 10 tokens over 5908 keys each, 5 heads: 180 us in 64 parts, of which the CUs hold 51 at a
+// time, and 117 in 51).
 constexpr int64_t LEAST_KEYS = 512;
-constexpr int64_t middle_workgroups(bool bf16) { return bf16 ? 384 : 640; }
-constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }
-constexpr int64_t resident_workgroups(int row_bytes) { return row_bytes > 256 ? 256 : 512; }
 struct Plan { int rows, tiles, parts; };
-Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk, int row_bytes, bool bf16) {
-  const int64_t rows = Tq * (Hq / Hk), wide = (rows + 127) / 128 * Hk, narrow = (rows + 31) / 32 * Hk;
+Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk, int width, bool bf16) {
+  const int64_t rows = Tq * (Hq / Hk), narrow = (rows + 31) / 32 * Hk, resident = width > 64 && !bf16 ? 256 : 512;
   Plan p;
-  p.rows = wide >= enough_workgroups(row_bytes) ? 128 : row_bytes == 256 && (rows + 63) / 64 * Hk >= middle_workgroups(bf16) ? 64 : 32;
+  p.rows = rows_of_workgroup(rows, Hk, width, bf16);
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
-  p.parts = rows == 0 || narrow > 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({resident_workgroups(row_bytes) / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
+  p.parts = rows == 0 || narrow > 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({resident / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
   return p;
 }
 
@@ -300,7 +291,7 @@ void launch(hipStream_t st, const AttentionArgs& a, const Plan& p, void* workspa
 }
 template <typename E, int DP>
 void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
-  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk, DP * (int)sizeof(E), sizeof(E) == 2);
+  const Plan p = plan(a.Tq, a.Tk, a.Hq, a.Hk, DP, sizeof(E) == 2);
   auto run = [&](auto config) {
     typedef decltype(config) C;
     switch ((a.cap > 0.f ? CAPPED : 0) | (a.slopes != nullptr ? BIASED : 0)) {
@@ -311,8 +302,8 @@ void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
     }
   };
   constexpr bool LONG = sizeof(E) * DP > 256;
-  if (p.rows == 128) return run(Config<E, DP, 4, 1, LONG ? 1 : 2>{});
-  if constexpr (sizeof(E) * DP == 256) if (p.rows == 64) return run(Config<E, DP, 2, 2, 1>{});
+  if constexpr (DP > 64) if (p.rows == 128) return run(Config<E, DP, 4, 1, LONG ? 1 : 2>{});
+  if constexpr (!LONG) if (p.rows == 64) return run(Config<E, DP, 2, 2, 1>{});
   run(Config<E, DP, 1, LONG ? 2 : 4, 1>{});
 }
 }  // namespace
@@ -323,7 +314,7 @@ void launch_attention_spans(hipStream_t st, const int32_t* offsets, int64_t docu
 }
 
 size_t attention_bytes(int64_t Tq, int64_t Tk, int Hq, int Hk, int D, bool bf16) {
-  const Plan p = plan(Tq, Tk, Hq, Hk, (D <= 64 ? 64 : 128) * (bf16 ? 2 : 4), bf16);
+  const Plan p = plan(Tq, Tk, Hq, Hk, D <= 64 ? 64 : 128, bf16);
   return p.parts <= 1 ? 256 : (size_t)p.parts * Tq * Hq * (D + 1) * sizeof(float);
 }
 void launch_attention(hipStream_t st, const AttentionArgs& a, bool bf16, void* workspace) {

@@ -600,10 +600,6 @@ __global__ __launch_bounds__(C::THREADS, 2) void k_attention_dkv_one(AttentionAr
   finish(dv, a.dv, 1.f);
 }
 
-// of 128 rows and of 64: see attention.hip; both passes change sides at about the same sizes (768 workgroups of 64: 111 -> 80 and 56 -> 34 us in bf16, 220 -> 215 and 75 -> 60 in fp32)
-constexpr int64_t enough_workgroups(int row_bytes) { return row_bytes > 256 ? 192 : 512; }
-constexpr int64_t middle_workgroups(bool bf16) { return bf16 ? 384 : 640; }
-
 template <auto KERNEL, typename C, typename... A>
 void launch(ProfScope& ps, int64_t blocks, hipStream_t st, A... a) {
   static const bool once = [] {
@@ -624,8 +620,9 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
     launch<&k_attention_dq<E, C, SHAPE>, C>(ps, n * a.Hk, st, a, rows, (int)n);
   };
   auto by_rows = [&] {
-    if ((count + 127) / 128 * a.Hk >= enough_workgroups(DP * (int)sizeof(E))) return rows_of(QConfig<E, DP, 4>{});
-    if constexpr (sizeof(E) * DP == 256) if ((count + 63) / 64 * a.Hk >= middle_workgroups(sizeof(E) == 2)) return rows_of(QConfig<E, DP, 2>{});
+    const int n = rows_of_workgroup(count, a.Hk, DP, sizeof(E) == 2);
+    if constexpr (DP > 64) if (n == 128) return rows_of(QConfig<E, DP, 4>{});
+    if constexpr (sizeof(E) * DP <= 256) if (n == 64) return rows_of(QConfig<E, DP, 2>{});
     rows_of(QConfig<E, DP, 1>{});
   };
   if (a.Tq > 0) by_rows();

@@ -323,5 +323,21 @@ __device__ __forceinline__ void store_columns(E* row, int df, int D, const f32x1
   }
 }
 
+// Rows of a workgroup that walks the keys: 128 (four waves side by side), 64 (two, and two groups of keys) or 32 (four groups of keys, two where rows have 512 bytes).  What decides is how many
+// workgroups there are, how many fit a CU, and how much of a tile the rows of a workgroup see.  us of the forward pass and of dq, causal; workgroups of 64 in brackets:
+//   bf16, width 64: never 128.  16 heads of 8192 in one text (2048): 240 and 271 with 128, 216 and 264 with 64; 16 on 4 of 8111 in 23 texts (2028): 50 and 59, 42 and 48.  64 or 32, 12 heads of
+//     4096 in 4 texts (768): 51 and 55, 44 and 48; in 41: 15 and 18, 23 and 26; 8 heads of 2000 in two (256): 32 and 33, 20 and 22.
+//   fp32, width 64: never 128.  12 heads of 6000 in two texts (1128): 358 and 504 with 128, 311 and 418 with 64.  64 or 32, 12 heads of 4096 in 4 texts (768): 164 and 215, 173 and 220; in 41:
+//     47 and 60, 63 and 75; 8 heads of 3500 in ten (440): 69 and 92, 56 and 70.
+//   bf16, width 128: 16 heads on 8 of 8192 in one text (2048): 345 and 404 with 128, 414 and 478 with 64; 16 of 6000 in 20 texts (1504): 60 and 72, 59 and 66.  64 or 32, 12 heads of 4096 in
+//     4 texts (768): 73 and 80, 103 and 111; 8 of 3500 in ten (440): 31 and 34, 39 and 42; of 2000 in two (256): 43 and 45, 30 and 32.
+//   fp32, width 128: 64 takes the time of 32.  128 or 32, a training step of 12 heads of 4096 in 4 texts (768): 1487, 1714; of 8 heads of 3500 in one (440): 1697, 1742; of 2000 (250): 995, 717.
+inline int rows_of_workgroup(int64_t rows, int Hk, int width, bool bf16) {
+  const int64_t of_128 = (rows + 127) / 128 * Hk, of_64 = (rows + 63) / 64 * Hk;
+  if (width > 64 && of_128 >= (bf16 ? 512 : 192)) return 128;
+  if (width > 64 && !bf16) return 32;
+  return of_64 >= (width > 64 ? 384 : bf16 ? 1024 : 640) ? 64 : 32;
+}
+
 }  // namespace attn
 }  // namespace sama
