@@ -635,16 +635,26 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
     typedef decltype(config) C;
     launch<&k_attention_dkv_one<E, C, SHAPE>, C>(ps, (a.Tk + C::KEYS - 1) / C::KEYS * a.Hk, st, a, rows);
   };
-  const int64_t blocks = (a.Tk + 127) / 128 * a.Hk;   // of 128 keys
-  if constexpr (sizeof(E) * DP <= 128) {
+  // How many waves a workgroup has side by side over keys, how many groups over rows: the more workgroups of 128 keys there are, the fewer groups.  us of dk and dv, causal, at that many (-: not measured):
+  //   bf16, width 64: 16 heads of 8192 in one text (1024) 368 with 128 keys, 445 with 32 and four groups of rows; of 6000 in five (752) 32 keys 186; 16 on 4 of 8111 in 23 texts (256) 303, 174
+  //     with 64 keys, 101 with 32
+  //   bf16, width 128, pairs of waves over 128, 64, 32 keys: 16 of 8192 on 8 in one text (512) 688, 1008, 1491; 12 of 4096 in 4 texts (384) 172, 155, 194, in 41 60, 65, 100; 8 of 3200 in 4 texts
+  //     (200) 134, 100, 87, in 30 44, 37, 58; 8 of 4096 on 4 in 4 texts (128) -, 236, 144
+  //   fp32, width 64: 12 of 6000 in two texts (564) 574, 552, 579; of 4096 in 4 (384) -, 255, 269; 8 of 3200 in 4 (200) 325, 176, 134, in 30 97, 57, 65
+  //   fp32, width 128, 64 keys or 32, two groups of rows: 16 of 6000 in 3 texts (752) 1132, 1244; 12 of 4096 in 41 (384) 156, 159; 8 of 4096 in 4 (256) 393, 361; of 1500 in 4 (96) 159, 103
+  const int64_t blocks = (a.Tk + 127) / 128 * a.Hk;
+  if constexpr (sizeof(E) == 2 && DP == 64) {
     if (blocks >= 1024) ones(OneConfig<E, DP, 4, 1, 2>{});
     else ones(OneConfig<E, DP, 1, 4, 1>{});
-  } else if constexpr (sizeof(E) * DP <= 256) {
+  } else if constexpr (sizeof(E) == 2) {
     if (blocks >= 512) pairs(KConfig<E, DP, 4, 1, 2>{});
-    else if (2 * blocks >= 256) pairs(KConfig<E, DP, 2, 2, 1>{});
+    else if (blocks >= 192) pairs(KConfig<E, DP, 2, 2, 1>{});
+    else pairs(KConfig<E, DP, 1, 4, 1>{});
+  } else if constexpr (DP == 64) {
+    if (blocks >= 256) pairs(KConfig<E, DP, 2, 2, 1>{});
     else pairs(KConfig<E, DP, 1, 4, 1>{});
   } else {
-    if (2 * blocks >= 256) pairs(KConfig<E, DP, 2, 2, 1>{});
+    if (blocks >= 384) pairs(KConfig<E, DP, 2, 2, 1>{});
     else pairs(KConfig<E, DP, 1, 2, 1>{});
   }
 }
