@@ -3,8 +3,8 @@
 // One pass over the keys with the running maximum and sum of the softmax: 4 D operations a pair, nothing of the scores leaves the registers.
 //
 // The G heads of a key head are rows of the same tiles (row = query G + head), so K and V are read once for all of them.  A workgroup has 32 WM rows and walks the
-// tiles of keys between its rows' first and last; tiles that no row sees are left out.  Where rows are few its four waves share 32 rows and take different keys of a
-// tile (KG groups), and where workgroups are few the keys are split between several, joined by k_attention_join.
+// tiles of keys between its rows' first and last; tiles that no row sees are left out.  Its four waves have 32 rows each, or share 64 or 32 with different keys of a tile for each half or quarter of
+// them (KG groups; see rows_of_workgroup), and where workgroups are few the keys are split between several, joined by k_attention_join.
 #include <algorithm>
 #include <cmath>
 #include "attention_tiles.h"
