@@ -230,8 +230,7 @@ __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a, Parts p
 #pragma unroll 8
     for (int p = share; p < parts.count; p += 8) {
       const f32x4 o = *reinterpret_cast<const f32x4*>(parts.o + (p * step + of_row) * a.D + 4 * quad);
-      const float w = s_weight[p];
-      if (w != 0.f) x += o * w;   // a part without keys holds nothing
+      x += o * s_weight[p];   // a weight of zero too: what is not finite in a part far below the others stays so, and a part without keys holds zeros
     }
   }
   s_part[share][quad] = x;

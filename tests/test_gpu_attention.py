@@ -374,3 +374,33 @@ def test_gradients_against_differences():
         value, bound = want["d" + x]
         assert abs(float((value * way).sum()) - one) <= tolerance < 1e-4
         assert abs(float((got["d" + x].double() * way).sum()) - one) <= tolerance + float((bound * way.abs()).sum())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("Tk,H", [(1000, 2), (12000, 2), (40000, 1), (12000, 60)])   # keys in one part, and split
+def test_what_is_not_finite_reaches_a_query_far_away(Tk, H, t):
+    """Values of keys so far behind that their probability is zero in 32 bits: zero times what is not finite is not finite, in whichever part of the keys it lies."""
+    from paper_2310_05674_amd import binding as B
+    D = 64
+    gen = torch.Generator(device=DEV).manual_seed(Tk + H)
+    q, k, v = (normal(gen, n, H, D, dtype=TYPES[t]) for n in (2, Tk, Tk))
+    spans, at = ints(np.array([[0, Tk], [Tk // 2, Tk]])), ints([Tk - 1, Tk - 1])
+    slopes = torch.ones(H, device=DEV)
+    ws = torch.empty(B.attention_bytes(2, Tk, H, H, D, TYPES[t]), dtype=torch.uint8, device=DEV)
+
+    def run():
+        out, lse = torch.full_like(q, 7.0), torch.full((2, H), 7.0, device=DEV)
+        ws.fill_(255)
+        B.op_attention(q, k, v, out, spans, ws, slopes=slopes, at=at, lse=lse)
+        return out, lse
+    clean, clean_lse = run()
+    assert bool(torch.isfinite(clean).all())
+    for value in (float("nan"), math.inf, -math.inf):
+        kept = v[3, :, 9].clone()
+        v[3, :, 9] = value                                    # only the first query sees it
+        out, lse = run()
+        v[3, :, 9] = kept
+        assert torch.equal(out[1], clean[1]) and torch.equal(lse, clean_lse)
+        assert not bool(torch.isfinite(out[0, :, 9]).any())
+        rest = torch.arange(D, device=DEV) != 9
+        assert torch.equal(out[0][:, rest], clean[0][:, rest])
