@@ -166,7 +166,8 @@ sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, i
 /* Attention.  Query i of head h sees the keys begin <= j < end of its span (spans: DEVICE int32 [Tq][2], clipped to [0, Tk)) of key head h Hk / Hq:
  *     s_j = scale q_i . k_j;  with cap > 0: s_j = cap tanh(s_j / cap);  with slopes: s_j -= slopes[h] |at_i - j|
  *     p = softmax of s over those j,  out_i = sum_j p_j v_j,  lse_i = log sum_j exp(s_j)
- * A query that sees nothing has out = 0 and lse = minus infinity.  Spans of packed documents come from sama_op_attention_spans; a cache per text, rows of padding,
+ * A query that sees nothing has out = 0 and lse = minus infinity; one whose scores are all minus infinity has the same lse, but out is NaN, and its
+ * gradients are not finite either.  Spans of packed documents come from sama_op_attention_spans; a cache per text, rows of padding,
  * windows or any other interval of keys for each query can be given as well, in any order.  Keys and values that a query does not see do not reach it, whatever they hold; a value that is not finite
  * reaches those that see it as one that is not finite, if not the same.
  * q, out [Tq][Hq][D], k, v [Tk][Hk][D]; Hq a multiple of Hk, at most 64 times it; D a multiple of 8 up to 128; strides multiples of 16 bytes, ld at most 2^21, (Hq/Hk - 1) hs of q and dout

@@ -192,7 +192,8 @@ __global__ __launch_bounds__(C::THREADS, C::PER_EU) void k_attention(AttentionAr
     }
   }
   if (row >= rows) return;
-  const bool none = m == -INF && l == 0.f;   // no key, or scores of minus infinity alone
+  // Without a key: nothing.  Scores of minus infinity alone have no softmax, so the row's sum of zero makes out NaN; a part of the row that has no others leaves that to the join.
+  const bool none = parts.count > 1 ? m == -INF && l == 0.f : span.x >= span.y;
   const float inv = none ? 0.f : 1.f / l, lse = none ? -INF : m * c + log2f(l);
   const bool first = kg == 0 && h == 0;
   if (parts.count > 1) {
@@ -238,8 +239,10 @@ __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a, Parts p
   if (share != 0 || 4 * quad >= a.D) return;
 #pragma unroll
   for (int g = 1; g < 8; ++g) x += s_part[g][quad];
-  const float sum = s_total[1], inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float sum = s_total[1];
   const int hk = (int)(of_row / rows), row = (int)(of_row - (int64_t)hk * rows), query = row / G, head = hk * G + row % G;
+  float inv = 1.f / sum;
+  if (sum == 0.f) { const int2 span = span_of(a.spans, query, (int)a.Tk); if (span.x >= span.y) inv = 0.f; }   // else scores of minus infinity alone: out is NaN
   E* const o = const_cast<E*>(static_cast<const E*>(a.out.p)) + query * a.out.ld + head * a.out.hs + 4 * quad;
   if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
   else *reinterpret_cast<f32x4*>(o) = x * inv;

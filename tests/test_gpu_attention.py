@@ -404,3 +404,44 @@ def test_what_is_not_finite_reaches_a_query_far_away(Tk, H, t):
         assert not bool(torch.isfinite(out[0, :, 9]).any())
         rest = torch.arange(D, device=DEV) != 9
         assert torch.equal(out[0][:, rest], clean[0][:, rest])
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,H", [(100, 2), (2180, 16), (4100, 16)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_of_minus_infinity_alone(T, H, D, t):
+    """The softmax of scores that are all minus infinity is no number: neither is out, nor what the query's gradients reach.  One score that is finite is enough for out, and who sees
+    nothing of it keeps his bits."""
+    c = Case(T, T, H, H, D, t)
+    third = T // 3
+    spans = documents([third, third, third], T, True)
+    c.q[:, :, 0], c.k[:, :, 0] = 1.0, 0.5
+    clean = c.run(ints(spans))
+    c.k[:third, :, 0] = -math.inf                             # of the first document all, of the second all but its first
+    c.k[third + 1:2 * third, :, 0] = -math.inf
+    got = c.run(ints(spans))
+    assert bool(torch.isnan(got["out"][:third]).all()) and bool((got["lse"][:third] == -math.inf).all())
+    for x in ("dq", "dk", "dv"):
+        assert not bool(torch.isfinite(got[x][:third]).all(-1).any()), x
+    first = c.v[third].double()                               # probability 1, within 64 u for a score of up to 40
+    assert bool(((got["out"][third:2 * third].double() - first).abs() <= ((2.0 ** -8 if t == "bf16" else U) + 64 * U) * first.abs()).all()) and bool(torch.isfinite(got["lse"][third:2 * third]).all())
+    for x in clean:
+        assert torch.equal(got[x][2 * third:], clean[x][2 * third:]), x
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_of_minus_infinity_in_split_keys(D, t):
+    """The same for few queries over keys that are split: all scores minus infinity, all of some parts, no key, no key in some parts."""
+    Tk = 9000
+    c = Case(4, Tk, 2, 2, D, t, at=ints([Tk - 1] * 4))
+    c.q[:, :, 0], c.k[:, :, 0] = 1.0, 0.5
+    spans = np.array([[0, 5000], [0, Tk], [17, 17], [5000, Tk]])
+    c.k[:5000, :, 0] = -math.inf
+    got = c.run(ints(spans), grad=False)
+    assert bool(torch.isnan(got["out"][0]).all()) and bool((got["lse"][0] == -math.inf).all())
+    assert bool((got["out"][2] == 0).all()) and bool((got["lse"][2] == -math.inf).all())
+    c.k[:5000, :, 0] = 0.5
+    want = reference(c.q, c.k, c.v, ints(spans[3:].repeat(4, 0)), c.scale, 0.0, None, c.at)
+    for x in ("out", "lse"):
+        close(x, got[x][1::2], (want[x][0][1::2], want[x][1][1::2]))
