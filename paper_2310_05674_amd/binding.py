@@ -608,8 +608,8 @@ def _here(t, what):
 
 
 def _heads(t, shape, dtype, dev, what):
-    """A [tokens, heads, width] tensor of GPU dev whose width is dense -> its address and the strides between tokens and heads (of a single one: as if it were
-    dense, whatever the stride says)."""
+    """A [tokens, heads, width] tensor of GPU dev whose width is dense -> its address and the strides between tokens and heads (of a single one: the width, whatever
+    the stride says)."""
     if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
         raise ValueError(f"{what}: expected a {tuple(shape)} tensor of {dtype} on GPU {dev}, got {tuple(t.shape)}, {t.dtype}, {t.device}")
     ld, hs, step = t.stride()
@@ -618,7 +618,7 @@ def _heads(t, shape, dtype, dev, what):
     if shape[1] == 1:
         hs = shape[2]
     if shape[0] <= 1:
-        ld = max(hs, shape[2])
+        ld = shape[2]
     return t.data_ptr(), ld, hs
 
 

@@ -445,3 +445,20 @@ def test_scores_of_minus_infinity_in_split_keys(D, t):
     want = reference(c.q, c.k, c.v, ints(spans[3:].repeat(4, 0)), c.scale, 0.0, None, c.at)
     for x in ("out", "lse"):
         close(x, got[x][1::2], (want[x][0][1::2], want[x][1][1::2]))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("Tk", [700, 16640])
+def test_one_query_out_of_a_long_text(Tk, t):
+    """[heads][tokens][width] memory: a query's heads lie a whole text apart, and it is the only token of its call."""
+    D, i = 128, Tk - 100
+    c = Case(Tk, Tk, 2, 2, D, t, layout="heads")
+    new, c.at = c.q, ints([i])
+    c.q, c.dout, c.sizes = new[i:i + 1], c.dout[i:i + 1], (1, Tk, 2, 2, D, c.t)
+    whole = [torch.full((2, Tk, D), 7.0, dtype=c.t, device=DEV) for _ in range(2)]
+    places = [w.transpose(0, 1)[i:i + 1] for w in whole]
+    plain = c.make
+    c.make = lambda like: places.pop() if like.shape[0] == 1 else plain(like)
+    c.check(ints(np.array([[3, i + 1]])))
+    for w in whole:                                        # nothing beside the token
+        assert bool((w[:, :i] == 7).all()) and bool((w[:, i + 1:] == 7).all()) and not bool((w[:, i] == 7).all())

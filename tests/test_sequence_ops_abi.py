@@ -144,3 +144,21 @@ def test_binding_wants_tensors_of_the_gpu(lib):
                  lambda: B.op_distill_grad(z, ids, teacher, loss, saved, z)):
         with pytest.raises(ValueError, match="current GPU"):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_single_token_has_no_stride_between_tokens(lib, dtype):
+    """One token of [heads][tokens][width] memory of a long text: what lies between its heads is no stride between tokens, which has a limit."""
+    from paper_2310_05674_amd import binding as B
+    H, D = 2, 128
+    whole = torch.empty(H, 16640, D, dtype=dtype).transpose(0, 1)
+    code, between = {torch.float32: F32, torch.bfloat16: BF16}[dtype], 16640 * D
+    for view in (whole[100:101], whole[:0]):
+        p, ld, hs = B._heads(view, view.shape, dtype, -1, "q")
+        assert (ld, hs) == (D, between)
+    assert B._heads(whole[100:102], (2, H, D), dtype, -1, "q")[1:] == (D, between) and B._heads(whole[5:6, 1:], (1, 1, D), dtype, -1, "q")[1:] == (D, D)
+    # every stride of such a token is one that the call takes: what it refuses is the workspace alone
+    one = (P, *B._heads(whole[100:101], (1, H, D), dtype, -1, "q")[1:])
+    for name in ("sama_op_attention", "sama_op_attention_grad"):
+        good = dict(good_attention(lib, code, 0), D=D, Hq=H, Hk=H, Tq=1, Tk=1, **{x: one for x in HEADS})
+        refused(lib, name, attention(lib, name), good, [dict(ws=None)], code=3)
