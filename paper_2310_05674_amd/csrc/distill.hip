@@ -86,11 +86,15 @@ template <typename E> __device__ __forceinline__ void split_row(const E* row, in
   tail = head + pieces * VALUES<E>;
 }
 
+// Tokens are workgroups along x, and where that would be more work items than one dimension of a launch holds (2^32 - 1), half of them along y.
+__device__ __forceinline__ int64_t token_of_workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 template <typename E, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_distill(DistillArgs a) {
   __shared__ double red64[THREADS / 64];
   __shared__ float2 red[THREADS / 64];
-  const int64_t row = blockIdx.x;
+  const int64_t row = token_of_workgroup();
+  if (row >= a.T) return;
   Entry e;
   if (!entries<E, THREADS>(a, row, e, red64)) {
     if (threadIdx.x == 0) { a.loss[row] = 0.f; a.saved[2 * row] = 0.f; a.saved[2 * row + 1] = 1.f; }
@@ -153,7 +157,8 @@ __global__ __launch_bounds__(THREADS) void k_distill_grad(DistillArgs a) {
   __shared__ double red64[THREADS / 64];
   __shared__ int s_id[DISTILL_MAX_ENTRIES];
   __shared__ float s_p[DISTILL_MAX_ENTRIES];
-  const int64_t row = a.T - 1 - blockIdx.x;   // from the end, which the loss read last: the last-level cache may still have it
+  const int64_t row = a.T - 1 - token_of_workgroup();   // from the end, which the loss read last: the last-level cache may still have it
+  if (row < 0) return;
   const E* const z = static_cast<const E*>(a.z) + row * a.ldz;
   E* const dz = static_cast<E*>(a.dz) + row * a.lddz;
   int head, pieces, tail;
@@ -213,8 +218,10 @@ constexpr int LOSS_THREADS = 512, GRAD_THREADS = 1024;
 template <typename E>
 void launch(hipStream_t st, const DistillArgs& a, bool grad) {
   ProfScope ps(st, F_OTHER, (double)a.T * a.V * sizeof(E) * (grad ? 2 : 1));
-  if (grad) launch_kernel(ps, k_distill_grad<E, GRAD_THREADS>, dim3((unsigned)a.T), GRAD_THREADS, 0, st, a);
-  else launch_kernel(ps, k_distill<E, LOSS_THREADS>, dim3((unsigned)a.T), LOSS_THREADS, 0, st, a);
+  const int64_t most = ((int64_t)1 << 32) / (grad ? GRAD_THREADS : LOSS_THREADS) - 1;
+  const dim3 grid = a.T <= most ? dim3((unsigned)a.T) : dim3((unsigned)((a.T + 1) / 2), 2);
+  if (grad) launch_kernel(ps, k_distill_grad<E, GRAD_THREADS>, grid, GRAD_THREADS, 0, st, a);
+  else launch_kernel(ps, k_distill<E, LOSS_THREADS>, grid, LOSS_THREADS, 0, st, a);
 }
 void launch_either(hipStream_t st, const DistillArgs& a, bool grad) { a.bf16 ? launch<bf16_t>(st, a, grad) : launch<float>(st, a, grad); }
 }  // namespace

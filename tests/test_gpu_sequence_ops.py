@@ -345,3 +345,14 @@ def test_a_run_in_a_graph_and_on_another_stream(t):
     for r, w in zip(runs, want):
         for b, x in zip([b for i, b in enumerate(r[-1]) if i != 3], w):
             assert torch.equal(b, x)
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [2 ** 22 - 1, 2 ** 22])
+def test_distill_of_the_most_tokens(T, t):
+    """As many tokens as there may be: a workgroup each, more work items than one dimension of a launch holds."""
+    V, K = 3, 2
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    z = torch.randn(T, V, device=DEV, generator=gen).to(TYPES[t])
+    ids = torch.randint(-1, V, (T, K), device=DEV, generator=gen, dtype=torch.int32)
+    check_distill(z, ids, torch.randn(T, K, device=DEV, generator=gen), 1.5)
