@@ -170,7 +170,7 @@ sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, i
  * gradients are not finite either.  Spans of packed documents come from sama_op_attention_spans; a cache per text, rows of padding,
  * windows or any other interval of keys for each query can be given as well, in any order.  Keys and values that a query does not see do not reach it, whatever they hold; a value that is not finite
  * reaches those that see it as one that is not finite, if not the same.
- * q, out [Tq][Hq][D], k, v [Tk][Hk][D]; Hq a multiple of Hk, at most 64 times it; D a multiple of 8 up to 128; strides multiples of 16 bytes, ld at most 2^21, (Hq/Hk - 1) hs of q and dout
+ * q, out [Tq][Hq][D], k, v [Tk][Hk][D]; Hk up to 2^20, Hq a multiple of it, at most 64 times; D a multiple of 8 up to 128; strides multiples of 16 bytes, ld at most 2^21, (Hq/Hk - 1) hs of q and dout
  * below 2^30 bytes; pointers 16-byte aligned; Tq Hq and Tk Hk up to 2^28.  at: DEVICE int32 [Tq], the place of each query among the keys, up to 2^30 to either
  * side of 0, or NULL: query i is beside key i (Tq = Tk).
  * slopes: DEVICE fp32 [Hq], or NULL; constants, they get no gradient.  lse: DEVICE fp32 [Tq][Hq], natural logarithm, or NULL.  scale > 0; cap 0: none, or 1e-3 to 4096.

@@ -368,6 +368,7 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
 // ---- sequences
 namespace {
 constexpr int64_t MOST_ROTARY_TOKENS = (int64_t)1 << 23, MOST_DISTILL_TOKENS = (int64_t)1 << 22, MOST_HEAD_ROWS = (int64_t)1 << 28;
+constexpr int32_t MOST_KEY_HEADS = 1 << 20;
 // [tokens][heads][width] of any alignment
 bool is_heads(const void* p, int32_t dtype, int64_t tokens, int64_t heads, int64_t width, int64_t ld, int64_t hs) {
   return ld >= width && hs >= width && is_rows(p, dtype, tokens, ld) && is_rows(p, dtype, heads, hs);
@@ -375,6 +376,8 @@ bool is_heads(const void* p, int32_t dtype, int64_t tokens, int64_t heads, int64
 const char* check_attention_sizes(int64_t Tq, int64_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t dtype) {
   if (!is_dtype(dtype)) return "the type must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16";
   if (Hk < 1 || Hq < Hk || Hq % Hk != 0 || Hq / Hk > 64) return "Hq must be 1 to 64 times Hk";
+  // workgroups of up to 512 threads for each key head and each 32 rows or more: 0.63 of the 2^32 work items of a launch at most
+  if (Hk > MOST_KEY_HEADS) return "Hk must be up to 2^20";
   if (D < 8 || D > 128 || D % 8 != 0) return "D must be a multiple of 8, up to 128";
   if (Tq < 0 || Tk < 0 || Tq > MOST_HEAD_ROWS / Hq || Tk > MOST_HEAD_ROWS / Hk) return "Tq Hq and Tk Hk must be 0 to 2^28";
   return nullptr;

@@ -462,3 +462,20 @@ def test_one_query_out_of_a_long_text(Tk, t):
     c.check(ints(np.array([[3, i + 1]])))
     for w in whole:                                        # nothing beside the token
         assert bool((w[:, :i] == 7).all()) and bool((w[:, i + 1:] == 7).all()) and not bool((w[:, i] == 7).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [8, 72])
+def test_as_many_key_heads_as_there_may_be(D, t):
+    """2^20 key heads of one token, the most workgroups for a few rows.  A single key has probability 1, within 2 e_s + 17 u (e_s above, S at most 2 sum |q k| scale) where it is formed from
+    the logarithm again: out = v, dv = dout, dq = dk = 0."""
+    H = 2 ** 20
+    c = Case(1, 1, H, H, D, t)
+    got = c.run(ints(np.array([[0, 1]])))
+    size = (c.q.float().abs() * c.k.float().abs()).sum(-1, keepdim=True) * c.scale
+    for name, want in (("out", c.v), ("dv", c.dout)):
+        off = 2 * (D + 8) * U * 2 * size + (17 + 8) * U + (2.0 ** -8 + 2.0 ** -8 if t == "bf16" else U)
+        assert bool(((got[name].float() - want.float()).abs() <= off * want.float().abs()).all()), name
+    s = (c.q.double() * c.k.double()).sum(-1) * c.scale
+    assert bool(((got["lse"].double() - s).abs() <= (2 * (D + 8) * U * 2 * size[..., 0] + 21 * U * (s.abs() + 1))).all())
+    assert bool((got["dq"] == 0).all()) and bool((got["dk"] == 0).all())

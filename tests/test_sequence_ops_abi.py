@@ -162,3 +162,15 @@ def test_a_single_token_has_no_stride_between_tokens(lib, dtype):
     for name in ("sama_op_attention", "sama_op_attention_grad"):
         good = dict(good_attention(lib, code, 0), D=D, Hq=H, Hk=H, Tq=1, Tk=1, **{x: one for x in HEADS})
         refused(lib, name, attention(lib, name), good, [dict(ws=None)], code=3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_refuses_more_key_heads_than_a_launch_has_workgroups(lib, dtype):
+    """One token of 2^20 + 1 key heads and more is within Tq Hq <= 2^28, but their workgroups may be more work items than a launch holds."""
+    for name in ("sama_op_attention", "sama_op_attention_grad"):
+        size = getattr(lib, name + "_bytes")
+        assert size(1, 1, 2 ** 20, 2 ** 20, 64, dtype) > 0
+        good = dict(good_attention(lib, dtype, 2 ** 40), Tq=1, Tk=1)
+        bad = [dict(Hq=h, Hk=h) for h in (2 ** 20 + 1, 2 ** 24, 2 ** 28)]
+        refused(lib, name, attention(lib, name), good, bad)
+        assert all(size(1, 1, b["Hq"], b["Hk"], 64, dtype) == 0 for b in bad)
