@@ -204,7 +204,7 @@ sama_status sama_op_attention_spans(const int32_t* offsets, int64_t documents, c
  *     loss_i = temperature^2 sum_k p_k (log p_k - log q_{ids k}),   dz_ij = dloss_i temperature (q_j - sum over the k with ids k = j of p_k)
  * Entries with an id outside [0, V) or a logit of minus infinity are none, whatever else they hold; a token without entries has loss 0, gradient 0, and its logits are not read.  An id may be listed more than once.  With K = 1 and
  * temperature 1 this is the cross-entropy of a label.  logits [T][V] in dtype with row stride ldz, any alignment; ids int32, teacher fp32 [T][K], dense; K 1 to 256; loss fp32 [T]; saved fp32 [T][2], for the gradient; temperature
- * 1e-4 to 1e4; T up to 2^22, 0 does nothing.  dlogits [T][V] in dtype, with stride lddz, may be logits themselves with the same stride; dloss fp32 [T]. */
+ * 1e-4 to 1e4; V up to 2^30, T up to 2^22, 0 does nothing.  dlogits [T][V] in dtype, with stride lddz, may be logits themselves with the same stride; dloss fp32 [T]. */
 sama_status sama_op_distill(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,
                             float* loss, float* saved, void* hip_stream);
 sama_status sama_op_distill_grad(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,

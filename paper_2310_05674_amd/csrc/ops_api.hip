@@ -416,7 +416,8 @@ AttentionArgs attention_args(const sama_attention& s) {
 const char* check_distill(const void* z, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float tau) {
   if (!is_dtype(dtype)) return "the type must be SAMA_DTYPE_FP32 or SAMA_DTYPE_BF16";
   if (T < 0 || T > MOST_DISTILL_TOKENS) return "T must be 0 to 2^22";
-  if (V < 1 || K < 1 || K > DISTILL_MAX_ENTRIES) return "V must be positive and K 1 to 256";
+  if (V < 1 || V > (1 << 30)) return "V must be 1 to 2^30";   // places in a row are 32 bits, behind its end too
+  if (K < 1 || K > DISTILL_MAX_ENTRIES) return "K must be 1 to 256";
   if (!(tau >= 1e-4f && tau <= 1e4f)) return "temperature must be 1e-4 to 1e4";
   if (T == 0) return nullptr;
   if (!z || !ids || !teacher) return "null logits, ids or teacher";

@@ -174,3 +174,13 @@ def test_attention_refuses_more_key_heads_than_a_launch_has_workgroups(lib, dtyp
         bad = [dict(Hq=h, Hk=h) for h in (2 ** 20 + 1, 2 ** 24, 2 ** 28)]
         refused(lib, name, attention(lib, name), good, bad)
         assert all(size(1, 1, b["Hq"], b["Hk"], 64, dtype) == 0 for b in bad)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_distill_refuses_rows_whose_last_pieces_pass_32_bits(lib, dtype):
+    """A thread's place in a row is a 32-bit number, and the last one's is up to 4 x 1024 pieces behind the row's end."""
+    good = dict(z=P, ldz=2 ** 31, dtype=dtype, T=1, V=100, ids=P, teacher=P, K=8, tau=2.0, loss=P, saved=P, st=None)
+    bad = [dict(V=v) for v in (2 ** 30 + 1, 2 ** 31 - 1024, 2 ** 31 - 1)]
+    refused(lib, "sama_op_distill", ordered(lib, "sama_op_distill"), good, bad)
+    good = dict(z=P, ldz=2 ** 31, dtype=dtype, T=1, V=100, ids=P, teacher=P, K=8, tau=2.0, dloss=P, saved=P, dz=P + 0x10000, lddz=2 ** 31, st=None)
+    refused(lib, "sama_op_distill_grad", ordered(lib, "sama_op_distill_grad"), good, bad)
