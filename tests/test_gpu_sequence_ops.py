@@ -356,3 +356,44 @@ def test_distill_of_the_most_tokens(T, t):
     z = torch.randn(T, V, device=DEV, generator=gen).to(TYPES[t])
     ids = torch.randint(-1, V, (T, K), device=DEV, generator=gen, dtype=torch.int32)
     check_distill(z, ids, torch.randn(T, K, device=DEV, generator=gen), 1.5)
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+def test_distill_beyond_2_to_31_values(t):
+    """The first row, the rows about value 2^31 and the last, of 33000 x 65537 logits in place, rows at every alignment."""
+    from paper_2310_05674_amd import binding as B
+    T, V, K = 33000, 65537, 5
+    z = torch.empty(T, V, device=DEV, dtype=TYPES[t])
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    for part in z.split(4096):
+        part.copy_(torch.randn(part.shape, device=DEV, generator=gen))
+    ids, teacher = entries(T, V, K, 3)
+    at = torch.tensor([0, 2 ** 31 // V - 1, 2 ** 31 // V, 2 ** 31 // V + 1, T - 1], device=DEV)
+    kept = z[at]
+    g, loss, saved = torch.rand(T, device=DEV) + 0.1, torch.full((T,), 7.0, device=DEV), torch.full((T, 2), 7.0, device=DEV)
+    B.op_distill(z, ids, teacher, loss, saved, temperature=2.0)
+    B.op_distill_grad(z, ids, teacher, g, saved, z, temperature=2.0)
+    want, tol, grad, gtol = distilled(kept, ids[at], teacher[at], 2.0, g[at])
+    assert bool(((loss[at].double() - want).abs() <= tol).all())
+    assert bool(((z[at].double() - grad).abs() <= gtol * (1 + 2.0 ** -10) + 1e-37).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_rotary_beyond_2_to_31_values(neighbours, t):
+    """33000 tokens of 512 heads of 128, in place and out of place: the first token, those about value 2^31 and the last."""
+    from paper_2310_05674_amd import binding as B
+    T, H, D = 33000, 512, 128
+    x = torch.empty(T, H, D, device=DEV, dtype=TYPES[t])
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    for part in x.split(4096):
+        part.copy_(torch.randn(part.shape, device=DEV, generator=gen))
+    positions = torch.arange(T, device=DEV, dtype=torch.int32)
+    at = torch.tensor([0, 2 ** 15 - 1, 2 ** 15, 2 ** 15 + 1, T - 1], device=DEV)
+    kept = x[at]
+    out = torch.empty_like(x)
+    B.op_rotary(x, positions, out, neighbours=neighbours)
+    B.op_rotary(x, positions, x, neighbours=neighbours)
+    want, size = rotated(kept, positions[at], (D // 2,), 10000.0, neighbours, False)
+    for got in (out[at], x[at]):
+        assert bool(((got.double() - want).abs() <= 6 * U * size + T * 2.0 ** -50 * size + step(x.dtype) * want.abs() * (1 + 2.0 ** -10) + 1e-40).all())
