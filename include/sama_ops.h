@@ -159,7 +159,7 @@ sama_status sama_op_glu_ffn_grad(const void* dy, int64_t lddy, const void* x, in
  *     (x, y) -> (x cos phi - y sin phi, x sin phi + y cos phi);  inverse = 1: by -phi, which is also the gradient.
  * neighbours = 0: pair i is values i and i + R/2; 1: values 2 i and 2 i + 1.  sections: HOST array [axes] of numbers of pairs: the first sections[0] turn by axis a = 0, the next
  * sections[1] by axis 1 and so on (time, height and width of a video; text has one axis).  positions: DEVICE int32 [axes][T], any value.  The other D - R values are copied.  Angles are
- * formed in 64 bits.  x and out [T][H][D] in dtype; out may be x itself, with the same strides.  axes 1 to 4, R 2 to 256, H D up to 2^20, T up to 2^23. */
+ * formed in 64 bits, off by 2^-46 of themselves or so; base is at least 1e-6 (below 1 an angle is up to |position| / base).  x and out [T][H][D] in dtype; out may be x itself, with the same strides.  axes 1 to 4, R 2 to 256, H D up to 2^20, T up to 2^23. */
 sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, int32_t H, int32_t D, int32_t dtype, const int32_t* positions, int32_t axes,
                            const int32_t* sections, double base, int32_t neighbours, int32_t inverse, void* out, int64_t ldo, int64_t hso, void* hip_stream);
 

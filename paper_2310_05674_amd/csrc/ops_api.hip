@@ -441,7 +441,7 @@ sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, i
     pairs += sections[k];
   }
   if (pairs < 1 || pairs > ROTARY_MAX_PAIRS || 2 * pairs > D) return refuse(op, "the sections must be 1 to 128 pairs together, and fit in D");
-  if (!(base > 0.0) || !std::isfinite(base)) return refuse(op, "base must be positive and finite");
+  if (!(base >= 1e-6) || !std::isfinite(base)) return refuse(op, "base must be finite, and at least 1e-6");   // below it turns of far positions have no fraction left in 64 bits
   if ((neighbours != 0 && neighbours != 1) || (inverse != 0 && inverse != 1)) return refuse(op, "neighbours and inverse must be 0 or 1");
   if (T == 0) return SAMA_OK;
   if (!x || !out || !positions) return refuse(op, "null x, output or positions");

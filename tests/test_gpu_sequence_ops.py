@@ -397,3 +397,22 @@ def test_rotary_beyond_2_to_31_values(neighbours, t):
     want, size = rotated(kept, positions[at], (D // 2,), 10000.0, neighbours, False)
     for got in (out[at], x[at]):
         assert bool(((got.double() - want).abs() <= 6 * U * size + T * 2.0 ** -50 * size + step(x.dtype) * want.abs() * (1 + 2.0 ** -10) + 1e-40).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("base,positions", [(0.5, [0, 1, 1000003, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31]), (1.0, [5, 2 ** 31 - 1, -2 ** 31]), (1e-6, [0, 1, -3, 999]), (1e300, [7, 2 ** 31 - 1])])
+def test_rotary_bases(base, positions, t):
+    """Bases whose rates grow with the pair, or vanish.  With v = 2^-53 the kernel's rate is off by (5 ln rate + 4) v of itself (a logarithm, its share of the pair, an exponential, 1 / 2 pi), the
+    reference's by (ln rate + 4) v, and each product with the position by v: angles differ by (6 |ln rate| + 10) v of themselves, where turns have a fraction at all."""
+    from paper_2310_05674_amd import binding as B
+    D = 64
+    x = torch.randn(len(positions), 2, D, device=DEV).to(TYPES[t])
+    pos, out = torch.tensor(positions, dtype=torch.int32, device=DEV), torch.empty_like(x)
+    for neighbours in (False, True):
+        B.op_rotary(x, pos, out, base=base, neighbours=neighbours)
+        want, size = rotated(x, pos, (D // 2,), base, neighbours, False)
+        ln_rate = torch.arange(D // 2, device=DEV, dtype=torch.float64) * (-2.0 * math.log(base) / D)
+        far = pos.double().abs()[:, None] * torch.exp(ln_rate) * (6 * ln_rate.abs() + 10) * 2.0 ** -53
+        far = (far.repeat_interleave(2, 1) if neighbours else torch.cat([far, far], 1))[:, None]
+        assert float(far.max()) < 2.0 ** -12                  # it says something
+        assert bool(((out.double() - want).abs() <= (6 * U + far) * size + step(x.dtype) * want.abs() * (1 + 2.0 ** -10) + 1e-40).all())

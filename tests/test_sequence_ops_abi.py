@@ -184,3 +184,17 @@ def test_distill_refuses_rows_whose_last_pieces_pass_32_bits(lib, dtype):
     refused(lib, "sama_op_distill", ordered(lib, "sama_op_distill"), good, bad)
     good = dict(z=P, ldz=2 ** 31, dtype=dtype, T=1, V=100, ids=P, teacher=P, K=8, tau=2.0, dloss=P, saved=P, dz=P + 0x10000, lddz=2 ** 31, st=None)
     refused(lib, "sama_op_distill_grad", ordered(lib, "sama_op_distill_grad"), good, bad)
+
+
+def test_rotary_refuses_bases_whose_angles_have_no_fraction(lib):
+    """Rates grow with the pair where the base is below 1: at 1e-6 the last position's 2^48 turns have 4 bits behind the point, far below that an angle is infinite and its sine no number."""
+    def call(a):
+        a = dict(a)
+        a["sections"] = (C.c_int32 * len(a["sections"]))(*a["sections"])
+        return lib.sama_op_rotary(*a.values())
+
+    assert 2.0 ** 31 * 1e-6 ** (-126 / 128) / 6.28 < 2.0 ** 49 and 5e-324 == 2.0 ** -1074 and 1074 * 126 / 128 > 1024
+    good = dict(x=P, ldx=512, hsx=128, T=5, H=4, D=128, dtype=F32, positions=P, axes=1, sections=(64,), base=1e4, neighbours=0, inverse=0, out=P + 0x8000, ldo=512, hso=128, st=None)
+    refused(lib, "sama_op_rotary", call, good, [dict(base=b) for b in (9.9e-7, 1e-100, 1e-300, 5e-324)])
+    for base in (1e-6, 0.5, 1.0, 1.7e308):
+        assert call(dict(good, T=0, base=base)) == 0
