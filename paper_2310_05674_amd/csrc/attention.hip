@@ -267,16 +267,26 @@ __global__ __launch_bounds__(256) void k_attention_spans(const int32_t* offsets,
 }
 
 // What a call looks like: rows of a workgroup, and into how many parts the keys are cut.  Where even workgroups of 32 rows leave CUs without one the keys are split, into as many parts as
-// there is room for at once: two workgroups a CU, or one with rows of 512 bytes (fp32, width 128, 10 tokens over 5908 keys each, 5 heads: 180 us in 64 parts, of which the CUs hold 51 at a
-// time, and 117 in 51).
-constexpr int64_t LEAST_KEYS = 512;
+// there is room for at once: workgroups of 128 KB of LDS have a CU each, those of 64 KB (bf16, widths up to 64) share it in twos.  us of two new tokens over caches of 24000 keys each, by the
+// workgroups before the split and the parts:
+//   bf16, width 128: 5 in 51 parts 29, in 64 38; 10 in 25 45, in 51 50; 33 in 7 142, in 15 145.  fp32, width 64: 5 in 51 37, in 64 51; 10 in 25 56, in 51 64; 33 in 7 179, in 15 174
+//   fp32, width 128: 5 in 51 95, in 64 149; 10 in 25 176, in 51 185
+// Two rounds, where that is one part more than twice as many and parts are few but long enough: bf16, width 128, 100 in 5 443, in 2 482; 130 in 3 602, in 1 763 (of 2048 keys each: 57, 61, but 100 in 5
+// 45, in 2 42); fp32, width 64, 100 in 5 521, in 2 629; 130 in 3 782, in 1 1139; fp32, width 128, 130 in 3 2698, in 1 4002; bf16, width 64, 200 in 5 472, in 2 526 (of 2048 keys: 43, 40).
+constexpr int64_t LEAST_KEYS = 512, CUS = 256;
+constexpr int narrow_groups(int row_bytes) { return row_bytes > 256 ? 2 : 4; }                        // KG of workgroups of 32 rows
+constexpr int narrow_lds(int row_bytes) { return 4 * 32 * narrow_groups(row_bytes) * row_bytes; }
 struct Plan { int rows, tiles, parts; };
 Plan plan(int64_t Tq, int64_t Tk, int Hq, int Hk, int width, bool bf16) {
-  const int64_t rows = Tq * (Hq / Hk), narrow = (rows + 31) / 32 * Hk, resident = width > 64 && !bf16 ? 256 : 512;
+  const int64_t rows = Tq * (Hq / Hk), narrow = (rows + 31) / 32 * Hk, places = CUS * (LDS_MAX / narrow_lds(width * (bf16 ? 2 : 4)));
   Plan p;
   p.rows = rows_of_workgroup(rows, Hk, width, bf16);
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
-  p.parts = rows == 0 || narrow > 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({resident / narrow, Tk / LEAST_KEYS, MOST_PARTS}));
+  p.parts = 1;
+  if (rows > 0 && narrow <= CUS) {
+    const int64_t one = places / narrow, two = 2 * places / narrow, parts = one <= 2 && two > 2 * one && Tk >= 2 * LEAST_KEYS * two ? two : one;
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({parts, Tk / LEAST_KEYS, MOST_PARTS}));
+  }
   return p;
 }
 
@@ -309,7 +319,9 @@ void launch_width(hipStream_t st, const AttentionArgs& a, void* workspace) {
   constexpr bool LONG = sizeof(E) * DP > 256;
   if constexpr (DP > 64) if (p.rows == 128) return run(Config<E, DP, 4, 1, LONG ? 1 : 2>{});
   if constexpr (!LONG) if (p.rows == 64) return run(Config<E, DP, 2, 2, 1>{});
-  run(Config<E, DP, 1, LONG ? 2 : 4, 1>{});
+  typedef Config<E, DP, 1, narrow_groups(DP * sizeof(E)), 1> Narrow;
+  static_assert(Narrow::LDS == narrow_lds(DP * sizeof(E)), "what plan() counts with");
+  run(Narrow{});
 }
 }  // namespace
 

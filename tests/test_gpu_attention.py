@@ -479,3 +479,12 @@ def test_as_many_key_heads_as_there_may_be(D, t):
     s = (c.q.double() * c.k.double()).sum(-1) * c.scale
     assert bool(((got["lse"].double() - s).abs() <= (2 * (D + 8) * U * 2 * size[..., 0] + 21 * U * (s.abs() + 1))).all())
     assert bool((got["dq"] == 0).all()) and bool((got["dk"] == 0).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hk,G", [(1, 1), (2, 33), (5, 8), (33, 1), (100, 2), (130, 1), (200, 1), (256, 1)])
+def test_keys_in_one_round_of_parts_and_in_two(Hk, G, D, t):
+    """Two new tokens over caches, with as many key heads as make parts of every number, and one that sees keys of a few parts alone."""
+    Tk = 8001
+    Case(3, Tk, G * Hk, Hk, D, t, at=ints([2999, Tk - 1, 7000])).check(ints([[0, 3000], [3000, Tk], [6990, 7001]]), grad=False)

@@ -198,3 +198,22 @@ def test_rotary_refuses_bases_whose_angles_have_no_fraction(lib):
     refused(lib, "sama_op_rotary", call, good, [dict(base=b) for b in (9.9e-7, 1e-100, 1e-300, 5e-324)])
     for base in (1e-6, 0.5, 1.0, 1.7e308):
         assert call(dict(good, T=0, base=base)) == 0
+
+
+@pytest.mark.parametrize("dtype,D,places", [(BF16, 128, 256), (F32, 64, 256), (F32, 128, 256), (BF16, 64, 512), (BF16, 32, 512), (BF16, 72, 256)])
+def test_split_keys_fill_the_chip_once_or_twice(lib, dtype, D, places):
+    """The parts of split keys, from the workspace's size: as many workgroups as fit the chip at once, of 128 KB each or (bf16, widths up to 64) 64 KB, where two rounds of them would not do
+    with much shorter parts."""
+    def parts(heads, Tk):
+        size = lib.sama_op_attention_bytes(1, Tk, heads, heads, D, dtype)
+        each = heads * (D + 1) * 4
+        assert size == 256 or size % each == 0
+        return 1 if size == 256 else size // each
+
+    for heads in range(1, 257):
+        one, two = places // heads, 2 * places // heads
+        for Tk in (1, 511, 1023, 1024, 5000, 100000):
+            n, most = parts(heads, Tk), max(1, min(64, Tk // 512))
+            twice = one <= 2 and two > 2 * one and Tk >= 1024 * two
+            assert n == max(1, min(most, two if twice else one)), (heads, Tk, n)
+    assert parts(257, 100000) == 1
