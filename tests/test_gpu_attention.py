@@ -488,3 +488,30 @@ def test_keys_in_one_round_of_parts_and_in_two(Hk, G, D, t):
     """Two new tokens over caches, with as many key heads as make parts of every number, and one that sees keys of a few parts alone."""
     Tk = 8001
     Case(3, Tk, G * Hk, Hk, D, t, at=ints([2999, Tk - 1, 7000])).check(ints([[0, 3000], [3000, Tk], [6990, 7001]]), grad=False)
+
+
+class ProductCase(Case):
+    """Queries, keys and values, and their gradients, as parts of one product's rows."""
+    def __init__(self, T, Hq, Hk, D, t, **kw):
+        super().__init__(T, T, Hq, Hk, D, t, **kw)
+        rows, self.grads = torch.cat([self.q, self.k, self.v], 1), torch.full((T, Hq + 2 * Hk, D), 7.0, device=DEV, dtype=self.t)
+        self.q, self.k, self.v = rows.split([Hq, Hk, Hk], 1)
+        plain, made = self.make, []
+
+        def make(like):      # out, then dq, dk, dv
+            made.append(like)
+            return plain(like) if len(made) == 1 else self.grads.split([Hq, Hk, Hk], 1)[len(made) - 2]
+        self.make = make
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,Hk,G,D", [(2180, 4, 4, 72), (4100, 8, 3, 80), (8200, 8, 2, 96), (6200, 8, 5, 128), (8200, 16, 2, 64), (4100, 8, 7, 40)])
+def test_many_workgroups_of_shared_key_heads(T, Hk, G, D, t):
+    """Shared key heads, and widths that leave pieces of a tile empty, in workgroups of every size, with documents of every kind and tokens outside them."""
+    ProductCase(T, G * Hk, Hk, D, t).check(ints(documents([T * 2 // 3, 0, 37, T // 4, 1], T, True, [300, 0, 20, 1, 0])))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,Hk,G,D", [(4100, 8, 3, 80), (8200, 8, 2, 96), (8200, 16, 2, 48)])
+def test_many_workgroups_of_shared_key_heads_capped_and_biased(T, Hk, G, D, t):
+    ProductCase(T, G * Hk, Hk, D, t, cap=5.0, slopes=True).check(ints(documents([T // 2, 500, T // 4], T, True)))
