@@ -496,11 +496,11 @@ class ProductCase(Case):
         super().__init__(T, T, Hq, Hk, D, t, **kw)
         rows, self.grads = torch.cat([self.q, self.k, self.v], 1), torch.full((T, Hq + 2 * Hk, D), 7.0, device=DEV, dtype=self.t)
         self.q, self.k, self.v = rows.split([Hq, Hk, Hk], 1)
-        plain, made = self.make, []
+        plain, self.made = self.make, 0
 
         def make(like):      # out, then dq, dk, dv
-            made.append(like)
-            return plain(like) if len(made) == 1 else self.grads.split([Hq, Hk, Hk], 1)[len(made) - 2]
+            self.made += 1
+            return plain(like) if self.made % 4 == 1 else self.grads.split([Hq, Hk, Hk], 1)[(self.made - 2) % 4]
         self.make = make
 
 
@@ -515,3 +515,46 @@ def test_many_workgroups_of_shared_key_heads(T, Hk, G, D, t):
 @pytest.mark.parametrize("T,Hk,G,D", [(4100, 8, 3, 80), (8200, 8, 2, 96), (8200, 16, 2, 48)])
 def test_many_workgroups_of_shared_key_heads_capped_and_biased(T, Hk, G, D, t):
     ProductCase(T, G * Hk, Hk, D, t, cap=5.0, slopes=True).check(ints(documents([T // 2, 500, T // 4], T, True)))
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,Hk,G,D", [(300, 2, 3, 128), (2180, 8, 2, 128), (4100, 8, 2, 96), (8200, 8, 2, 128), (8200, 16, 2, 64)])
+def test_what_is_hidden_and_what_is_seen_in_workgroups_of_every_size(T, Hk, G, D, t):
+    """Padding that holds NaN and infinity changes no bit; a key, value or gradient that is not finite changes whom it reaches and nobody else."""
+    c = ProductCase(T, G * Hk, Hk, D, t)
+    spans = documents([T // 2 + 3], T, True)
+    tail = slice(T // 2 + 11, T - 5)
+    spans[tail] = [[T // 2 + 11, i + 1] for i in range(tail.start, tail.stop)]
+    empty = torch.as_tensor(spans[:, 0] == spans[:, 1], device=DEV)
+    spans = ints(spans)
+
+    def run():
+        c.grads.fill_(7.0)
+        return {x: v.clone() for x, v in c.run(spans).items()}
+    clean = run()
+    for x, y in ((c.q, float("nan")), (c.k, math.inf), (c.v, float("nan")), (c.dout, -math.inf)):
+        x[empty] = y
+    got = run()
+    for x in ("out", "dq", "dk", "dv"):
+        assert torch.equal(got[x][~empty], clean[x][~empty]) and bool((got[x][empty] == 0).all()), x
+    at = T // 4                                            # a token of the first document, seen from itself on
+    kept = c.v[at, 0, 5].clone()
+    c.v[at, 0, 5] = math.inf
+    got = run()
+    c.v[at, 0, 5] = kept
+    reached = slice(at, T // 2 + 3)
+    bad = ~torch.isfinite(got["out"])
+    assert bool(bad[reached, :G, 5].all()) and int(bad.sum()) == (reached.stop - at) * G
+    for x in ("out", "dq"):
+        assert torch.equal(got[x][:at], clean[x][:at]) and torch.equal(got[x][tail], clean[x][tail]) and torch.equal(got[x][:, G:], clean[x][:, G:]), x
+    for x in ("dk", "dv"):
+        assert torch.equal(got[x][:, 1:], clean[x][:, 1:]) and torch.equal(got[x][tail], clean[x][tail]), x
+    kept = c.dout[at, 0].clone()
+    c.dout[at, 0] = float("nan")                           # sees the keys up to its own
+    got = run()
+    c.dout[at, 0] = kept
+    for x in ("dk", "dv"):
+        assert not bool(torch.isfinite(got[x][:at + 1, 0]).any()) and torch.equal(got[x][at + 1:], clean[x][at + 1:]) and torch.equal(got[x][:, 1:], clean[x][:, 1:]), x
+    rest = torch.ones(T, G * Hk, dtype=torch.bool, device=DEV)
+    rest[at, 0] = False
+    assert not bool(torch.isfinite(got["dq"][at, 0]).any()) and torch.equal(got["dq"][rest], clean["dq"][rest])
