@@ -173,7 +173,7 @@ sama_status sama_op_rotary(const void* x, int64_t ldx, int64_t hsx, int64_t T, i
  * q, out [Tq][Hq][D], k, v [Tk][Hk][D]; Hk up to 2^20, Hq a multiple of it, at most 64 times; D a multiple of 8 up to 128; strides multiples of 16 bytes, ld at most 2^21, (Hq/Hk - 1) hs of q and dout
  * below 2^30 bytes; pointers 16-byte aligned; Tq Hq and Tk Hk up to 2^28.  at: DEVICE int32 [Tq], the place of each query among the keys, up to 2^30 to either
  * side of 0, or NULL: query i is beside key i (Tq = Tk).
- * slopes: DEVICE fp32 [Hq], or NULL; constants, they get no gradient.  lse: DEVICE fp32 [Tq][Hq], natural logarithm, or NULL.  scale > 0; cap 0: none, or 1e-3 to 4096.
+ * slopes: DEVICE fp32 [Hq], or NULL; constants, they get no gradient; the bias is formed in 32 bits, off by up to 2^-22 slopes[h] |at_i - j|.  lse: DEVICE fp32 [Tq][Hq], natural logarithm, or NULL.  scale > 0; cap 0: none, or 1e-3 to 4096.
  * bf16: probabilities are rounded to bf16 before their product with v, sums are fp32; fp32: nothing is rounded.  workspace: sama_op_attention_bytes(), for these very sizes (0 for sizes that are refused). */
 typedef struct { void* p; int64_t ld, hs; } sama_heads;
 typedef struct {
@@ -203,7 +203,7 @@ sama_status sama_op_attention_spans(const int32_t* offsets, int64_t documents, c
  *     p = softmax over its entries of teacher / temperature,  q = softmax over the vocabulary of z / temperature
  *     loss_i = temperature^2 sum_k p_k (log p_k - log q_{ids k}),   dz_ij = dloss_i temperature (q_j - sum over the k with ids k = j of p_k)
  * Entries with an id outside [0, V) or a logit of minus infinity are none, whatever else they hold; a token without entries has loss 0, gradient 0, and its logits are not read.  An id may be listed more than once.  With K = 1 and
- * temperature 1 this is the cross-entropy of a label.  logits [T][V] in dtype with row stride ldz, any alignment; ids int32, teacher fp32 [T][K], dense; K 1 to 256; loss fp32 [T]; saved fp32 [T][2], for the gradient; temperature
+ * temperature 1 this is the cross-entropy of a label.  q is formed in 32 bits: a loss is off by about temperature^2 2^-20, which at temperatures of hundreds may be all of a small one.  logits [T][V] in dtype with row stride ldz, any alignment; ids int32, teacher fp32 [T][K], dense; K 1 to 256; loss fp32 [T]; saved fp32 [T][2], for the gradient; temperature
  * 1e-4 to 1e4; V up to 2^30, T up to 2^22, 0 does nothing.  dlogits [T][V] in dtype, with stride lddz, may be logits themselves with the same stride; dloss fp32 [T]. */
 sama_status sama_op_distill(const void* logits, int64_t ldz, int32_t dtype, int64_t T, int32_t V, const int32_t* ids, const float* teacher, int32_t K, float temperature,
                             float* loss, float* saved, void* hip_stream);

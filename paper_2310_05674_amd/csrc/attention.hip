@@ -6,8 +6,8 @@
 // tiles of keys between its rows' first and last; tiles that no row sees are left out.  Its four waves have 32 rows each, or share 64 or 32 with different keys of a tile for each half or quarter of
 // them (KG groups; see rows_of_workgroup), and where workgroups are few the keys are split between several, joined by k_attention_join.
 //
-// Long texts are bound by products: 8192 causal tokens in bf16, 16 heads of 128 on 8 key heads, take 336 us, 820 TFLOP/s.  Short ones by each workgroup's chain of spans, first loads, tiles and
-// join: 8111 tokens in 23 texts, 16 heads of 64 on 4, 42 us, of which products alone would be 5.  New tokens by memory: 3 over 24001 keys each, 16 heads of 128 on 4, 28.4 us, 5.2 TB/s.
+// Long texts are bound by products: 8192 causal tokens in bf16, 16 heads of 128 on 8 key heads, take 330 us, 834 TFLOP/s.  Short ones by each workgroup's chain of spans, first loads, tiles and
+// join: 8111 tokens in 23 texts, 16 heads of 64 on 4, 43 us, of which products alone would be 8.5.  New tokens by memory: 3 over 24001 keys each, 16 heads of 128 on 4, 28.0 us, 5.3 TB/s.
 #include <algorithm>
 #include <cmath>
 #include "attention_tiles.h"

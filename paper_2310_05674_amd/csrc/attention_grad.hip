@@ -5,7 +5,7 @@
 // would do if one launch made both; but then one side would have to be added up in memory by workgroups as they come, in an order of their own.
 // k_attention_delta goes ahead: delta, and what else the second launch needs of each row, laid out in the order in which it is read.
 //
-// Bound by products where texts are long: 8192 causal tokens in bf16, 16 heads of 128 on 8 key heads, take 391 us for dq (6 D operations a pair, 1055 TFLOP/s) and 671 for dk and dv (8 D, 820).
+// Bound by products where texts are long: 8192 causal tokens in bf16, 16 heads of 128 on 8 key heads, take 383 us for dq (6 D operations a pair, 1077 TFLOP/s) and 652 for dk and dv (8 D, 843).
 // Short texts are bound by each workgroup's chain of spans, first loads, tiles and the join of its groups: 8111 tokens in 23 texts, 16 heads of 64 on 4, 48 and 100 us.
 #include <algorithm>
 #include <cmath>
@@ -641,7 +641,7 @@ void launch_all(hipStream_t st, const AttentionArgs& a, const Rows& rows) {
   // How many waves a workgroup has side by side over keys, how many groups over rows: the more workgroups of 128 keys there are, the fewer groups.  us of dk and dv, causal, at that many (-: not measured):
   //   bf16, width 64: 16 heads of 8192 in one text (1024) 368 with 128 keys, 445 with 32 and four groups of rows; of 6000 in five (752) 32 keys 186; 16 on 4 of 8111 in 23 texts (256) 303, 174
   //     with 64 keys, 101 with 32
-  //   bf16, width 128, pairs of waves over 128, 64, 32 keys: 16 of 8192 on 8 in one text (512) 688, 1008, 1491; 12 of 4096 in 4 texts (384) 172, 155, 194, in 41 60, 65, 100; 8 of 3200 in 4 texts
+  //   bf16, width 128, pairs of waves over 128, 64, 32 keys: 16 of 8192 on 8 in one text (512) 688, 1008, 1491; 12 of 4096 in 4 texts (384) 172, 155, 194, in 41 60, 65, 100 (64 keys for both); 8 of 3200 in 4 texts
   //     (200) 134, 100, 87, in 30 44, 37, 58; 8 of 4096 on 4 in 4 texts (128) -, 236, 144
   //   fp32, width 64: 12 of 6000 in two texts (564) 574, 552, 579; of 4096 in 4 (384) -, 255, 269; 8 of 3200 in 4 (200) 325, 176, 134, in 30 97, 57, 65
   //   fp32, width 128, 64 keys or 32, two groups of rows: 16 of 6000 in 3 texts (752) 1132, 1244; 12 of 4096 in 41 (384) 156, 159; 8 of 4096 in 4 (256) 393, 361; of 1500 in 4 (96) 159, 103

@@ -167,8 +167,8 @@ enum { PLAIN = 0, CAPPED = 1, BIASED = 2 };
 template <typename E, int SHAPE> struct Scores {
   float factor, in, out;     // s -> the exponent of e^2y for y = scale s / cap; cap log2(e)
   __device__ __forceinline__ Scores(float scale, float cap) : factor(scale * LOG2E), in(SHAPE & CAPPED ? (sizeof(E) == 2 ? 2.f * LOG2E : 1.f) * scale / cap : 0.f), out(cap * LOG2E) {}
-  // The score, and what its derivative is multiplied by.  tanh y = 1 - 2 r, 1 - tanh^2 y = 4 r (1 - r) for r = 1 / (1 + e^2y): within 2^-22 of cap in all, which a bf16 score's own
-  // rounding passes by far; in fp32 small scores want the library's tanh, whose error is relative.
+  // The score, and what its derivative is multiplied by.  tanh y = 1 - 2 r, 1 - tanh^2 y = 4 r (1 - r) for r = 1 / (1 + e^2y): within 2^-22 of cap in all, 2^-17 of
+  // a score for a cap of 30 and 2^-10 for the largest, where bf16 probabilities are rounded by 2^-9; in fp32 small scores want the library's tanh, whose error is relative.
   __device__ __forceinline__ float operator()(float s, float slope, float distance, float& bend) const {
     float x;
     if constexpr ((SHAPE & CAPPED) == 0) {
@@ -329,7 +329,7 @@ __device__ __forceinline__ void store_columns(E* row, int df, int D, const f32x1
 //     4096 in 4 texts (768): 51 and 55, 44 and 48; in 41: 15 and 18, 23 and 26; 8 heads of 2000 in two (256): 32 and 33, 20 and 22.
 //   fp32, width 64: never 128.  12 heads of 6000 in two texts (1128): 358 and 504 with 128, 311 and 418 with 64.  64 or 32, 12 heads of 4096 in 4 texts (768): 164 and 215, 173 and 220; in 41:
 //     47 and 60, 63 and 75; 8 heads of 3500 in ten (440): 69 and 92, 56 and 70.
-//   bf16, width 128: 16 heads on 8 of 8192 in one text (2048): 345 and 404 with 128, 414 and 478 with 64; 16 of 6000 in 20 texts (1504): 60 and 72, 59 and 66.  64 or 32, 12 heads of 4096 in
+//   bf16, width 128: 16 heads on 8 of 8192 in one text (2048): 345 and 404 with 128, 414 and 478 with 64; 16 of 6000 in 20 texts (1504): 60 and 72, 59 and 66 (the rule takes 128, for long texts' sake).  64 or 32, 12 heads of 4096 in
 //     4 texts (768): 73 and 80, 103 and 111; 8 of 3500 in ten (440): 31 and 34, 39 and 42; of 2000 in two (256): 43 and 45, 30 and 32.
 //   fp32, width 128: 64 takes the time of 32.  128 or 32, a training step of 12 heads of 4096 in 4 texts (768): 1487, 1714; of 8 heads of 3500 in one (440): 1697, 1742; of 2000 (250): 995, 717.
 inline int rows_of_workgroup(int64_t rows, int Hk, int width, bool bf16) {
